@@ -443,6 +443,95 @@ based_status based_prefill_static_scratch(const void* q, const void* k, const vo
 size_t based_static_scratch_bytes(void);
 
 /*
+ * Gated linear recurrence: a token mixer with one fp32 state per channel, for the place behind the gated short convolution.
+ * Per sequence and channel, t = 0 .. N-1, from state_in (NULL: zeros):
+ *
+ *   s = sigmoid(r_t),  a = exp(-rate s),  m = sqrt(1 - a^2),     h_t = a h_{t-1} + m sigmoid(g_t) x_t,     out_t = h_t
+ *
+ * x, r, g, out [B,N,C] in the io dtype; rate [C] fp32, >= 0 (not checked; a negative one gives NaN); state_in, state_out [B,C]
+ * fp32: the state before token 0 and behind token N-1 (NULL: not wanted), which may be the same array.  Arithmetic and state are
+ * fp32, out is rounded once.  A sigmoid below 2^-60 is taken as 2^-60.
+ * Supported: C a multiple of 8; io in {F32, BF16}; any N >= 1.  out and state_out must not alias an input (state_out may be
+ * state_in).
+ */
+based_status based_gated_recurrence_forward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                            void* out, float* state_out, int B, int N, int C, based_dtype io, void* cuda_stream);
+
+/* The same for one new token per sequence (generation): x, r, g, out [B,C]; state_in and state_out required. */
+based_status based_gated_recurrence_step(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                         void* out, float* state_out, int B, int C, based_dtype io, void* cuda_stream);
+
+/*
+ * Its backward pass.  out: what the forward call returned (h_{t-1} is read from it, as rounded there); dout: the gradient of
+ * out; dstate_out [B,C] fp32: that of state_out (NULL: zeros).  With i = sigmoid(g), from the last token to the first,
+ *
+ *   G_t = dout_t + E_{t+1},   E_t = a_t G_t,   E_N = dstate_out;    dx = G m i,   dg = G m x i (1 - i),
+ *   dlog a = a G h_{t-1} - (a^2 / m) G i x,   dr = -rate dlog a s (1 - s),   drate = -sum_{b,t} dlog a s,   dstate_in = E_0.
+ *
+ * dx, dr, dg [B,N,C] in the io dtype, drate [C] fp32, dstate_in [B,C] fp32 (NULL: not wanted; may be dstate_out).  drate is summed
+ * in a fixed order.  Where m = 0 (a rate of 0) the gradient with respect to the rate is infinite by the formula; a large finite
+ * number stands for 1 / m there.  workspace: based_gated_recurrence_backward_workspace_bytes.  No other output may alias an input.
+ */
+based_status based_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                             const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+                                             float* drate, float* dstate_in, int B, int N, int C, based_dtype io, void* workspace,
+                                             size_t workspace_bytes, void* cuda_stream);
+size_t based_gated_recurrence_backward_workspace_bytes(int B, int N, int C, based_dtype io);
+
+/*
+ * Norm of queries and keys for each head, with the position rotation, between a layer's projections and its attention.  For
+ * every token and head, over the head's d elements,
+ *
+ *   y = w x / sqrt(mean(x^2) + eps),     then pair j < n turns by t = position * freqs[j]:
+ *   (y_lo, y_hi) -> (y_lo cos t - y_hi sin t, y_hi cos t + y_lo sin t),
+ *
+ * where pair j is (y_j, y_{n+j}), or with BASED_ROTATE_PAIRS (y_2j, y_2j+1); elements from 2 n on stay as they are.
+ * q, k: as the projections leave them, token m = b L + t at q + m * q_token_stride (elements), its heads side by side,
+ * [H_q][d] and [H_k][d]: slices of one fused projection are taken as they lie.  out_q [B,H_q,L,d], out_k [B,H_k,L,d]: what the
+ * mixers take.  q_weight, k_weight [d] fp32 (NULL: ones).  freqs [n] fp64, radians per position (NULL with n = 0: no
+ * rotation).  positions: int32 on the device, one per sequence (positions_per_sequence = 1: token t is at positions[b] + t) or one
+ * per token (positions_per_sequence = L); NULL: token t is at start + t.  Angles are taken in fp64, sums in fp32; one
+ * rounding, of the result.
+ * A generation step is the call with L = 1.
+ * Supported: d a multiple of 16, 16 <= d <= 256; n a multiple of 8, 2 n <= d; token strides at least H d and multiples of 16
+ * bytes; eps >= 0; io in {F32, BF16}.  Outputs must not alias inputs.
+ */
+#define BASED_ROTATE_PAIRS 8
+based_status based_qk_norm_rotate(const void* q, const void* k, long long q_token_stride, long long k_token_stride,
+                                  const float* q_weight, const float* k_weight, const double* freqs, const int* positions,
+                                  int positions_per_sequence, int start, void* out_q, void* out_k, int B, int L, int H_q, int H_k,
+                                  int d, int n, float eps, based_dtype io, int flags, void* cuda_stream);
+
+/*
+ * Its backward pass: dout_q [B,H_q,L,d], dout_k [B,H_k,L,d] -> dq, dk, laid out like q, k with token strides of their own, and
+ * dq_weight, dk_weight [d] fp32 (both, or both NULL), summed over all rows in a fixed order.  With e the output gradient turned
+ * back and inv = 1 / sqrt(mean(x^2) + eps):  dw = sum e x inv,   dx = inv (w e - x inv^2 mean(w e x)).
+ * workspace: based_qk_norm_rotate_backward_workspace_bytes (none is needed where the weights' gradients are not wanted).
+ */
+based_status based_qk_norm_rotate_backward(const void* q, const void* k, long long q_token_stride, long long k_token_stride,
+                                           const float* q_weight, const float* k_weight, const double* freqs, const int* positions,
+                                           int positions_per_sequence, int start, const void* dout_q, const void* dout_k, void* dq,
+                                           void* dk, long long dq_token_stride, long long dk_token_stride, float* dq_weight,
+                                           float* dk_weight, int B, int L, int H_q, int H_k, int d, int n, float eps, based_dtype io,
+                                           int flags, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t based_qk_norm_rotate_backward_workspace_bytes(int B, int L, int H_q, int H_k, int d, based_dtype io);
+
+/*
+ * Backward pass of swa_forward: dout the gradient of its output, P the softmax weights, c the softmax scale,
+ *
+ *   dv_j = sum_i P_ij dout_i,   dS_ij = c P_ij (dout_i.v_j - sum_l P_il dout_i.v_l),   dq_i = sum_j dS_ij k_j,   dk_j = sum_i dS_ij q_i.
+ *
+ * All arrays [B,H,L,d] in the io dtype; the weights are computed again, so neither the output nor statistics of the forward
+ * call are needed.  bf16 io: P and dS are rounded to bf16 once as operands of the products, sums are fp32.  softmax_scale,
+ * supported set and limits as swa_forward.  Where a token's values are not finite, all gradients of the tokens within 255 tokens
+ * of it may not be either.  workspace: swa_backward_workspace_bytes (0 is possible).  Outputs must not alias inputs.
+ */
+based_status swa_backward(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, int B, int H,
+                          int L, int d, int window, float softmax_scale, based_dtype io, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream);
+size_t swa_backward_workspace_bytes(int B, int H, int L, int window, based_dtype io);
+
+/*
  * Synchronises the stream and returns the sticky device-side status: BASED_OK, or
  * BASED_ERR_DEVICE_TIMEOUT if a kernel abandoned a bounded wait (its outputs are then
  * undefined), or BASED_ERR_CUDA if the stream reported a CUDA error.  Clears the flag.

@@ -21,6 +21,7 @@ LIB_PATH = _PKG / "libbased.so"
 BASED_OK = 0
 BASED_F32, BASED_BF16 = 0, 1
 BASED_STATE_ZERO_INIT, BASED_STATE_CONTINUE, BASED_STATE_SYM, BASED_NUMERATOR_ONLY = 0, 1, 2, 4
+BASED_ROTATE_PAIRS = 8
 D_FEAT = 16
 D_EXPANDED = 1 + D_FEAT + D_FEAT * D_FEAT
 D_SYM = 1 + D_FEAT + D_FEAT * (D_FEAT + 1) // 2         # rows of the symmetric state format
@@ -34,7 +35,9 @@ EXPORTS = (
     "based_prefill_backward_workspace_bytes", "based_prefill_backward_with_out", "based_prefill_backward_block_tokens", "swa_decode_step_advance", "swa_decode_step_ragged", "based_generation_step",
     "based_prefill_state", "based_prefill_state_workspace_bytes", "based_generation_graph_create", "based_generation_graph_step",
     "based_generation_graph_destroy", "based_tokens_to_heads", "based_f32_parts_bytes", "based_prefill_backward_tokens_first", "based_prefill_f32_parts",
-    "based_prefill_backward_tokens_first_with_out",
+    "based_prefill_backward_tokens_first_with_out", "based_gated_recurrence_forward", "based_gated_recurrence_step",
+    "based_gated_recurrence_backward", "based_gated_recurrence_backward_workspace_bytes", "based_qk_norm_rotate",
+    "based_qk_norm_rotate_backward", "based_qk_norm_rotate_backward_workspace_bytes", "swa_backward", "swa_backward_workspace_bytes",
 )
 
 _lib = None
@@ -113,6 +116,26 @@ def lib() -> ctypes.CDLL:
         L.baseconv_gate_step.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, i, vp]
         L.based_tokens_to_heads.restype = i
         L.based_tokens_to_heads.argtypes = [vp, vp, i, i, i, i, vp]
+        ll = ctypes.c_longlong
+        L.based_gated_recurrence_forward.restype = i
+        L.based_gated_recurrence_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, vp]
+        L.based_gated_recurrence_step.restype = i
+        L.based_gated_recurrence_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, vp]
+        L.based_gated_recurrence_backward.restype = i
+        L.based_gated_recurrence_backward.argtypes = [vp] * 13 + [i, i, i, i, vp, sz, vp]
+        L.based_gated_recurrence_backward_workspace_bytes.restype = sz
+        L.based_gated_recurrence_backward_workspace_bytes.argtypes = [i, i, i, i]
+        L.based_qk_norm_rotate.restype = i
+        L.based_qk_norm_rotate.argtypes = [vp, vp, ll, ll, vp, vp, vp, vp, i, i, vp, vp, i, i, i, i, i, i, f, i, i, vp]
+        L.based_qk_norm_rotate_backward.restype = i
+        L.based_qk_norm_rotate_backward.argtypes = [vp, vp, ll, ll, vp, vp, vp, vp, i, i, vp, vp, vp, vp, ll, ll, vp, vp, i, i, i, i,
+                                                    i, i, f, i, i, vp, sz, vp]
+        L.based_qk_norm_rotate_backward_workspace_bytes.restype = sz
+        L.based_qk_norm_rotate_backward_workspace_bytes.argtypes = [i, i, i, i, i, i]
+        L.swa_backward.restype = i
+        L.swa_backward.argtypes = [vp] * 7 + [i, i, i, i, i, f, i, vp, sz, vp]
+        L.swa_backward_workspace_bytes.restype = sz
+        L.swa_backward_workspace_bytes.argtypes = [i, i, i, i, i]
         L.based_poll_error.restype = i
         L.based_poll_error.argtypes = [vp]
         L.based_status_string.restype = ctypes.c_char_p
@@ -372,6 +395,53 @@ def based_generation_step(q, k, v, kv_state, z_state, qw, kw, vw, k_cache, v_cac
     Returns (out, out_w)."""
     return (_native_module or native()).generation_step(q, k, v, kv_state, z_state, qw, kw, vw, k_cache, v_cache, pos_state, out,
                                                         out_w, int(flags), float(softmax_scale), _handle(stream))
+
+
+def based_gated_recurrence_forward(x, r, g, rate, state_in=None, out=None, state_out=None, stream=None):
+    """h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(g_t) x_t with a_t = exp(-rate sigmoid(r_t)): x, r, g [B,N,C], rate [C] fp32;
+    state_in, state_out [B,C] fp32 (the states before and behind the tokens; state_out is written).  Returns out [B,N,C]."""
+    if x.dim() != 3:
+        raise ValueError("x must have 3 dimensions")
+    return (_native_module or native()).recurrence(x, r, g, rate, state_in, out, state_out, _handle(stream))
+
+
+def based_gated_recurrence_step(x, r, g, rate, state, out=None, state_out=None, stream=None):
+    """The same for one token: x, r, g [B,C]; state [B,C] fp32 is updated in place, or left as it is and the new one written
+    to state_out."""
+    if x.dim() != 2:
+        raise ValueError("x must have 2 dimensions")
+    return (_native_module or native()).recurrence(x, r, g, rate, state, out, state if state_out is None else state_out,
+                                                   _handle(stream))
+
+
+def based_gated_recurrence_backward(x, r, g, rate, out, dout, state_in=None, dstate_out=None, workspace=None, stream=None):
+    """Gradients (dx, dr, dg, drate, dstate_in) of based_gated_recurrence_forward, whose output is out; dstate_out: the
+    gradient of its state_out.  dstate_in is None without state_in."""
+    return (_native_module or native()).recurrence_backward(x, r, g, rate, out, dout, state_in, dstate_out, workspace,
+                                                            _handle(stream))
+
+
+def based_qk_norm_rotate(q, k, q_weight=None, k_weight=None, freqs=None, positions=None, eps: float = 1e-6, flags: int = 0,
+                         start: int = 0, out_q=None, out_k=None, stream=None):
+    """Norm of every head's query and key over its d elements, weighted (fp32 [d]; None: ones), and the rotation of the first
+    2 len(freqs) of them by position * freqs (fp64, radians; None: no rotation), pairs (j, n + j), or (2j, 2j+1) with
+    BASED_ROTATE_PAIRS.  q [B,L,H_q,d], k [B,L,H_k,d] as projections leave them (slices of a fused one are taken as they lie)
+    -> [B,H_q,L,d], [B,H_k,L,d].  positions: int32 [B] (the first token's) or [B,L]; None: token t is at start + t."""
+    return (_native_module or native()).rotate(q, k, q_weight, k_weight, freqs, positions, float(eps), int(flags), int(start), out_q,
+                                               out_k, _handle(stream))
+
+
+def based_qk_norm_rotate_backward(q, k, dout_q, dout_k, q_weight=None, k_weight=None, freqs=None, positions=None, eps: float = 1e-6,
+                                  flags: int = 0, start: int = 0, dq=None, dk=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dq_weight, dk_weight) of based_qk_norm_rotate for dout_q [B,H_q,L,d], dout_k [B,H_k,L,d]; dq, dk
+    (allocated if None) are laid out like q, k and may be slices of one gradient.  A weight's gradient is None without it."""
+    return (_native_module or native()).rotate_backward(q, k, dout_q, dout_k, q_weight, k_weight, freqs, positions, float(eps),
+                                                        int(flags), int(start), dq, dk, workspace, _handle(stream))
+
+
+def swa_backward(q, k, v, dout, window: int = 64, softmax_scale: float = 0.0, workspace=None, stream=None):
+    """Gradients (dq, dk, dv) of swa_forward(q, k, v, window=window, softmax_scale=softmax_scale) for the output gradient dout."""
+    return (_native_module or native()).swa_grad(q, k, v, dout, int(window), float(softmax_scale), workspace, _handle(stream))
 
 
 def based_selftest_bounded_wait(limit_ms: int = 20, stream=None) -> None:

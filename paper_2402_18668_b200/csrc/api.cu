@@ -3,6 +3,7 @@
 #include <atomic>
 #include <mutex>
 #include <cstdio>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -523,6 +524,156 @@ based_status baseconv_gate_step(const void* a, const void* g, const float* h, co
     if (!aligned16(conv_state)) return BASED_ERR_ALIGNMENT;
     return launch_baseconv(a, g, h, b2, conv_state, out, B, 1, C, width, true, io,
                            static_cast<cudaStream_t>(cuda_stream));
+}
+
+static inline bool is_one_of(const void* p, std::initializer_list<const void*> of) {
+    for (const void* q : of)
+        if (p && p == q) return true;
+    return false;
+}
+static based_status recurrence_check(const void* x, const void* r, const void* g, const float* rate, int B, int N, int C, based_dtype io) {
+    if (!x || !r || !g || !rate || B <= 0 || N <= 0 || C <= 0) return BASED_ERR_INVALID_ARG;
+    if (io != BASED_F32 && io != BASED_BF16) return BASED_ERR_INVALID_ARG;
+    if (C % 8 != 0 || (long long)B * C > (1ll << 36) || gated_recurrence_blocks(B, N, C, io) > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    if (!aligned16(x) || !aligned16(r) || !aligned16(g) || !aligned16(rate)) return BASED_ERR_ALIGNMENT;
+    return BASED_OK;
+}
+
+based_status based_gated_recurrence_forward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                            void* out, float* state_out, int B, int N, int C, based_dtype io, void* cuda_stream) {
+    if (!out || is_one_of(out, {x, r, g, rate, state_in, state_out}) || is_one_of(state_out, {x, r, g, rate})) return BASED_ERR_INVALID_ARG;
+    const based_status st = recurrence_check(x, r, g, rate, B, N, C, io);
+    if (st != BASED_OK) return st;
+    if (!aligned16(out) || !aligned16(state_in) || !aligned16(state_out)) return BASED_ERR_ALIGNMENT;
+    return launch_gated_recurrence(x, r, g, rate, state_in, out, state_out, B, N, C, io, static_cast<cudaStream_t>(cuda_stream));
+}
+
+based_status based_gated_recurrence_step(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                         void* out, float* state_out, int B, int C, based_dtype io, void* cuda_stream) {
+    if (!state_in || !state_out) return BASED_ERR_INVALID_ARG;
+    return based_gated_recurrence_forward(x, r, g, rate, state_in, out, state_out, B, 1, C, io, cuda_stream);
+}
+
+size_t based_gated_recurrence_backward_workspace_bytes(int B, int N, int C, based_dtype io) {
+    if (B <= 0 || N <= 0 || C <= 0 || (io != BASED_F32 && io != BASED_BF16)) return 0;
+    return gated_recurrence_backward_bytes(B, N, C, io);
+}
+
+based_status based_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                             const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+                                             float* drate, float* dstate_in, int B, int N, int C, based_dtype io, void* workspace,
+                                             size_t workspace_bytes, void* cuda_stream) {
+    if (!out || !dout || !dx || !dr || !dg || !drate) return BASED_ERR_INVALID_ARG;
+    const void* outs[] = {dx, dr, dg, drate, dstate_in};
+    for (int i = 0; i < 5; ++i) {
+        if (is_one_of(outs[i], {x, r, g, rate, state_in, out, dout, workspace})) return BASED_ERR_INVALID_ARG;
+        if (i < 4 && is_one_of(outs[i], {dstate_out})) return BASED_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (is_one_of(outs[i], {outs[j]})) return BASED_ERR_INVALID_ARG;
+    }
+    const based_status st = recurrence_check(x, r, g, rate, B, N, C, io);
+    if (st != BASED_OK) return st;
+    for (const void* p : {(const void*)state_in, out, dout, (const void*)dstate_out, (const void*)dx, (const void*)dr, (const void*)dg,
+                          (const void*)drate, (const void*)dstate_in, (const void*)workspace})
+        if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < gated_recurrence_backward_bytes(B, N, C, io)) return BASED_ERR_WORKSPACE;
+    return launch_gated_recurrence_backward(x, r, g, rate, state_in, out, dout, dstate_out, dx, dr, dg, drate, dstate_in, B, N, C,
+                                            static_cast<float*>(workspace), io, static_cast<cudaStream_t>(cuda_stream));
+}
+
+static based_status norm_rotate_check(const NormRotate& a, int positions_per_sequence, based_dtype io, int flags) {
+    if (!a.q || !a.k || a.B <= 0 || a.L <= 0 || a.Hq <= 0 || a.Hk <= 0 || a.d <= 0 || a.n < 0 || !(a.eps >= 0.f)) return BASED_ERR_INVALID_ARG;
+    if (io != BASED_F32 && io != BASED_BF16) return BASED_ERR_INVALID_ARG;
+    if ((flags & ~BASED_ROTATE_PAIRS) || (a.n > 0) != (a.freqs != nullptr)) return BASED_ERR_INVALID_ARG;
+    if (a.positions && positions_per_sequence != 1 && positions_per_sequence != a.L) return BASED_ERR_INVALID_ARG;
+    const long long width_q = (long long)a.Hq * a.d, width_k = (long long)a.Hk * a.d, per16 = 16 / (long long)esize(io);
+    if (a.q_stride < width_q || a.k_stride < width_k) return BASED_ERR_INVALID_ARG;
+    if (a.d % 16 != 0 || a.d > 256 || a.n % 8 != 0 || 2 * a.n > a.d || a.q_stride % per16 != 0 || a.k_stride % per16 != 0 ||
+        width_q > 0x7fffffffLL || width_k > 0x7fffffffLL || (long long)a.B * a.L > 0x7fffffffLL)
+        return BASED_ERR_UNSUPPORTED;
+    if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.wq) || !aligned16(a.wk)) return BASED_ERR_ALIGNMENT;
+    if ((reinterpret_cast<uintptr_t>(a.freqs) & 7u) || (reinterpret_cast<uintptr_t>(a.positions) & 3u)) return BASED_ERR_ALIGNMENT;
+    return BASED_OK;
+}
+
+based_status based_qk_norm_rotate(const void* q, const void* k, long long q_token_stride, long long k_token_stride,
+                                  const float* q_weight, const float* k_weight, const double* freqs, const int* positions,
+                                  int positions_per_sequence, int start, void* out_q, void* out_k, int B, int L, int H_q, int H_k,
+                                  int d, int n, float eps, based_dtype io, int flags, void* cuda_stream) {
+    const NormRotate a{q, k, q_token_stride, k_token_stride, q_weight, k_weight, freqs, positions, positions_per_sequence != 1, start,
+                       (flags & BASED_ROTATE_PAIRS) != 0, B, L, H_q, H_k, d, n, eps};
+    if (!out_q || !out_k || out_q == out_k || is_one_of(out_q, {q, k, q_weight, k_weight, freqs, positions}) ||
+        is_one_of(out_k, {q, k, q_weight, k_weight, freqs, positions}))
+        return BASED_ERR_INVALID_ARG;
+    const based_status st = norm_rotate_check(a, positions_per_sequence, io, flags);
+    if (st != BASED_OK) return st;
+    if (!aligned16(out_q) || !aligned16(out_k)) return BASED_ERR_ALIGNMENT;
+    return launch_norm_rotate(a, out_q, out_k, io, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t based_qk_norm_rotate_backward_workspace_bytes(int B, int L, int H_q, int H_k, int d, based_dtype io) {
+    if (B <= 0 || L <= 0 || H_q <= 0 || H_k <= 0 || d <= 0 || d % 16 != 0 || d > 256 || (io != BASED_F32 && io != BASED_BF16)) return 0;
+    return norm_rotate_backward_bytes(B, L, d, io);
+}
+
+based_status based_qk_norm_rotate_backward(const void* q, const void* k, long long q_token_stride, long long k_token_stride,
+                                           const float* q_weight, const float* k_weight, const double* freqs, const int* positions,
+                                           int positions_per_sequence, int start, const void* dout_q, const void* dout_k, void* dq,
+                                           void* dk, long long dq_token_stride, long long dk_token_stride, float* dq_weight,
+                                           float* dk_weight, int B, int L, int H_q, int H_k, int d, int n, float eps, based_dtype io,
+                                           int flags, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    const NormRotate a{q, k, q_token_stride, k_token_stride, q_weight, k_weight, freqs, positions, positions_per_sequence != 1, start,
+                       (flags & BASED_ROTATE_PAIRS) != 0, B, L, H_q, H_k, d, n, eps};
+    if (!dout_q || !dout_k || !dq || !dk || dq == dk || !dq_weight != !dk_weight || (dq_weight && dq_weight == dk_weight))
+        return BASED_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)dq, (const void*)dk, (const void*)dq_weight, (const void*)dk_weight})
+        if (is_one_of(p, {q, k, q_weight, k_weight, freqs, positions, dout_q, dout_k, workspace})) return BASED_ERR_INVALID_ARG;
+    based_status st = norm_rotate_check(a, positions_per_sequence, io, flags);
+    if (st != BASED_OK) return st;
+    NormRotate to = a;                         // (the gradients' layout has the same rules)
+    to.q_stride = dq_token_stride;
+    to.k_stride = dk_token_stride;
+    st = norm_rotate_check(to, positions_per_sequence, io, flags);
+    if (st != BASED_OK) return st;
+    for (const void* p : {dout_q, dout_k, (const void*)dq, (const void*)dk, (const void*)dq_weight, (const void*)dk_weight, (const void*)workspace})
+        if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
+    if (dq_weight && (!workspace || workspace_bytes < norm_rotate_backward_bytes(B, L, d, io))) return BASED_ERR_WORKSPACE;
+    return launch_norm_rotate_backward(a, dout_q, dout_k, dq, dq_token_stride, dk, dk_token_stride, dq_weight, dk_weight,
+                                       static_cast<float*>(workspace), io, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t swa_backward_workspace_bytes(int B, int H, int L, int window, based_dtype io) {
+    if (B <= 0 || H <= 0 || L <= 0 || window <= 0 || window > 128 || (io != BASED_F32 && io != BASED_BF16)) return 0;
+    const long long BH = (long long)B * H < kHeadSlab ? (long long)B * H : kHeadSlab;       // the largest slab of heads
+    return (size_t)BH * L * 16;
+}
+
+based_status swa_backward(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, int B, int H,
+                          int L, int d, int window, float softmax_scale, based_dtype io, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream) {
+    if (!q || !k || !v || !dout || !dq || !dk || !dv || B <= 0 || H <= 0 || L <= 0 || window <= 0) return BASED_ERR_INVALID_ARG;
+    if (io != BASED_F32 && io != BASED_BF16) return BASED_ERR_INVALID_ARG;
+    if (dq == dk || dq == dv || dk == dv) return BASED_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)dq, (const void*)dk, (const void*)dv})
+        if (is_one_of(p, {q, k, v, dout, workspace})) return BASED_ERR_INVALID_ARG;
+    if (d != 64 || window > 128) return BASED_ERR_UNSUPPORTED;
+    const long long BH = (long long)B * H;
+    if (BH > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    for (const void* p : {q, k, v, dout, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)workspace})
+        if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
+    const size_t need = swa_backward_workspace_bytes(B, H, L, window, io);
+    if (need && (!workspace || workspace_bytes < need)) return BASED_ERR_WORKSPACE;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 0.125f;   // 1/sqrt(64)
+    const size_t hb = (size_t)L * d * esize(io);
+    for (long long h0 = 0; h0 < BH; h0 += kHeadSlab) {
+        const int n = (int)(BH - h0 < kHeadSlab ? BH - h0 : kHeadSlab);
+        const based_status st = launch_swa_backward_simt(off(q, h0 * hb), off(k, h0 * hb), off(v, h0 * hb), off(dout, h0 * hb),
+                                                         off(dq, h0 * hb), off(dk, h0 * hb), off(dv, h0 * hb),
+                                                         static_cast<float*>(workspace), n, L, window, scale, io,
+                                                         static_cast<cudaStream_t>(cuda_stream));
+        if (st != BASED_OK) return st;
+    }
+    return BASED_OK;
 }
 
 size_t based_prefill_backward_workspace_bytes(int B, int H, int L, int d_v, based_dtype io) {

@@ -228,6 +228,36 @@ based_status launch_quadratic_forward_tc(const void* q, const void* k, const voi
 // the same with two groups of row warps per CTA (quadratic_fwd_tc.cu)
 based_status launch_quadratic_groups_tc(const void* q, const void* k, const void* v, void* out, int BH, int L,
                                         int d_feat, int d_v, int numerator_only, bool overlapped, cudaStream_t stream);
+// sums of the columns of part [rows][cols], in a fixed order: columns 0 .. split - 1 to a, the others to b (column_sums.cu)
+based_status launch_column_sums(const float* part, long long rows, int cols, float* a, int split, float* b, cudaStream_t stream);
+// gated linear recurrence (gated_recurrence.cu); _blocks: CTAs of a launch (a grid has at most 2^31 - 1); part: _bytes of scratch
+long long gated_recurrence_blocks(int B, int N, int C, based_dtype io);
+size_t gated_recurrence_backward_bytes(int B, int N, int C, based_dtype io);
+based_status launch_gated_recurrence(const void* x, const void* r, const void* g, const float* rate, const float* state_in, void* out,
+                                     float* state_out, int B, int N, int C, based_dtype io, cudaStream_t stream);
+based_status launch_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+                                              const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+                                              float* drate, float* dstate_in, int B, int N, int C, float* part, based_dtype io,
+                                              cudaStream_t stream);
+// norm of queries and keys with the position rotation (norm_rotate.cu)
+struct NormRotate {
+    const void *q, *k;                          // [B x L] tokens of Hq, Hk heads side by side
+    long long q_stride, k_stride;               // elements from a token to the next
+    const float *wq, *wk;                       // [d] or null
+    const double* freqs;                        // [n] radians per position, or null (n 0)
+    const int* positions;                       // null, [B] (each sequence's first) or [B, L]
+    int per_token, start, pairs;
+    int B, L, Hq, Hk, d, n;
+    float eps;
+};
+based_status launch_norm_rotate(const NormRotate& a, void* out_q, void* out_k, based_dtype io, cudaStream_t stream);
+size_t norm_rotate_backward_bytes(int B, int L, int d, based_dtype io);
+// gq, gk [B,H,L,d] -> dq, dk as q, k lie, with token strides of their own; dwq, dwk [d], both or neither
+based_status launch_norm_rotate_backward(const NormRotate& a, const void* gq, const void* gk, void* dq, long long dq_stride, void* dk,
+                                         long long dk_stride, float* dwq, float* dwk, float* part, based_dtype io, cudaStream_t stream);
+// backward of the sliding window (swa_backward.cu: multiply-adds); stats: [BH, L] float4 scratch
+based_status launch_swa_backward_simt(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
+                                      float* stats, int BH, int L, int window, float scale, based_dtype io, cudaStream_t stream);
 // load the generation-step kernels into the current context
 based_status preload_decode();
 based_status preload_swa_decode();

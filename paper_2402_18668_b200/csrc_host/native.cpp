@@ -14,6 +14,7 @@
 #include <c10/cuda/CUDAStream.h>
 
 #include <algorithm>
+#include <optional>
 #include <stdexcept>
 #include <string>
 
@@ -481,6 +482,283 @@ PyObject* baseconv(PyObject* const* p) {
     return wrap(out);
 }
 
+// ---------------------------------------------------------------------------------------------- layers around the mixers
+// a dimension as the library takes it
+int dim(const Tensor& t, int i) {
+    const int64_t n = t.size(i);
+    if (n > 0x7fffffff) value_error("a dimension of 2^31 or more");
+    return static_cast<int>(n);
+}
+// Every tensor of a call lies on one device, and what it writes overlaps nothing else of the call.  An undefined tensor is
+// passed over.
+void check_places(std::initializer_list<const Tensor*> in, std::initializer_list<const Tensor*> out) {
+    const Tensor& first = **in.begin();
+    auto same = [&](const Tensor& t) {
+        if (t.defined() && t.device() != first.device()) value_error("the tensors of a call lie on different devices");
+    };
+    for (const Tensor* t : in) same(*t);
+    for (auto o = out.begin(); o != out.end(); ++o) {
+        if (!(*o)->defined()) continue;
+        same(**o);
+        for (const Tensor* t : in)
+            if (t->defined() && overlap(**o, *t)) value_error("an output overlaps an input");
+        for (auto p = out.begin(); p != o; ++p)
+            if ((*p)->defined() && overlap(**o, **p)) value_error("two outputs overlap");
+    }
+}
+// None: the current stream of the tensors' device
+void* stream_on(PyObject* o, const Tensor& t) {
+    return o == Py_None ? c10::cuda::getCurrentCUDAStream(t.get_device()).stream() : stream_of(o);
+}
+// runs f without the interpreter lock and on the device of t
+template <typename F> void away(const Tensor& t, F f) {
+    std::exception_ptr fault;
+    Py_BEGIN_ALLOW_THREADS
+    try {
+        const c10::cuda::CUDAGuard on(t.device());
+        f();
+    } catch (...) {
+        fault = std::current_exception();
+    }
+    Py_END_ALLOW_THREADS
+    if (fault) std::rethrow_exception(fault);
+}
+const float* f32(const Tensor& t) { return static_cast<const float*>(cptr(t)); }
+void check_f32(const Tensor& t, at::IntArrayRef shape, const char* name) {
+    if (!t.defined()) return;
+    if (t.scalar_type() != at::kFloat) throw TypeFault(std::string(name) + " is fp32");
+    if (!shape_is(t, shape)) value_error(std::string(name) + " must be " + text(shape) + ", got " + text(t.sizes()));
+}
+void check_like(const Tensor& t, const Tensor& like, const char* name, const char* whose) {
+    if (t.defined() && (t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type()))
+        value_error(std::string(name) + " must have the shape and dtype of " + whose);
+}
+void check_gates(const Tensor& x, const Tensor& r, const Tensor& g, const Tensor& rate) {
+    check_like(r, x, "r", "x");
+    check_like(g, x, "g", "x");
+    check_f32(rate, {x.size(-1)}, "rate");
+}
+Tensor recurrence_call(const Tensor& x, const Tensor& r, const Tensor& g, const Tensor& rate, const Tensor& in, Tensor out,
+                       const Tensor& last, void* stream) {
+    const bool step = x.dim() == 2;
+    if (!out.defined()) out = fresh(x);
+    const int B = dim(x, 0), C = dim(x, static_cast<int>(x.dim()) - 1);
+    const based_dtype io = dtype_code(x);
+    check(step ? based_gated_recurrence_step(cptr(x), cptr(r), cptr(g), f32(rate), f32(in), ptr(out), fptr(last), B, C, io, stream)
+               : based_gated_recurrence_forward(cptr(x), cptr(r), cptr(g), f32(rate), f32(in), ptr(out), fptr(last), B, dim(x, 1), C, io,
+                                                stream),
+          step ? "based_gated_recurrence_step" : "based_gated_recurrence_forward");
+    return out;
+}
+struct RecurrenceGradients { Tensor dx, dr, dg, drate, dstate; };
+RecurrenceGradients recurrence_backward_call(const Tensor& x, const Tensor& r, const Tensor& g, const Tensor& rate, const Tensor& in,
+                                             const Tensor& out, const Tensor& dout, const Tensor& dlast, const Tensor& workspace,
+                                             void* stream) {
+    const int B = dim(x, 0), N = dim(x, 1), C = dim(x, 2);
+    const based_dtype io = dtype_code(x);
+    const Workspace ws(workspace, based_gated_recurrence_backward_workspace_bytes(B, N, C, io), x, stream);
+    RecurrenceGradients d{fresh(x), fresh(x), fresh(x), fresh(rate), in.defined() ? fresh(in) : Tensor()};
+    check(based_gated_recurrence_backward(cptr(x), cptr(r), cptr(g), f32(rate), f32(in), cptr(out), cptr(dout), f32(dlast), ptr(d.dx),
+                                          ptr(d.dr), ptr(d.dg), fptr(d.drate), fptr(d.dstate), B, N, C, io, ws.data, ws.bytes, stream),
+          "based_gated_recurrence_backward");
+    return d;
+}
+// x, r, g, rate, state_in, out, state_out, stream; [B,N,C], or [B,C] for one token (whose states are required)
+PyObject* recurrence(PyObject* const* a) {
+    const Tensor &x = need(a[0], "x"), &r = need(a[1], "r"), &g = need(a[2], "g"), &rate = need(a[3], "rate"), &in = dev(a[4]),
+                 &out = dev(a[5]), &last = dev(a[6]);
+    check_gates(x, r, g, rate);
+    check_like(out, x, "out", "x");
+    check_f32(in, {x.size(0), x.size(-1)}, "state_in");
+    check_f32(last, {x.size(0), x.size(-1)}, "state_out");
+    const bool in_place = in.defined() && last.defined() && in.const_data_ptr() == last.const_data_ptr();
+    if (in_place) check_places({&x, &r, &g, &rate}, {&out, &last});
+    else check_places({&x, &r, &g, &rate, &in}, {&out, &last});
+    void* stream = stream_on(a[7], x);
+    Tensor y;
+    away(x, [&] { y = recurrence_call(x, r, g, rate, in, out, last, stream); });
+    return wrap(y);
+}
+// x, r, g, rate, out, dout, state_in, dstate_out, workspace, stream -> dx, dr, dg, drate, dstate_in (None without state_in)
+PyObject* recurrence_backward(PyObject* const* a) {
+    const Tensor &x = need(a[0], "x"), &r = need(a[1], "r"), &g = need(a[2], "g"), &rate = need(a[3], "rate"), &out = need(a[4], "out"),
+                 &dout = need(a[5], "dout"), &in = dev(a[6]), &dlast = dev(a[7]), &ws = dev(a[8]);
+    dims(x, 3, "x");
+    check_gates(x, r, g, rate);
+    check_like(out, x, "out", "x");
+    check_like(dout, x, "dout", "x");
+    check_f32(in, {x.size(0), x.size(2)}, "state_in");
+    check_f32(dlast, {x.size(0), x.size(2)}, "dstate_out");
+    check_places({&x, &r, &g, &rate, &out, &dout, &in, &dlast}, {&ws});
+    void* stream = stream_on(a[9], x);
+    RecurrenceGradients d;
+    away(x, [&] { d = recurrence_backward_call(x, r, g, rate, in, out, dout, dlast, ws, stream); });
+    return wrap({d.dx, d.dr, d.dg, d.drate, d.dstate});
+}
+
+// queries and keys as projections leave them: [B,L,H,d], the heads of a token side by side and the tokens evenly spaced
+bool evenly_spaced(const Tensor& t) {
+    if (t.dim() != 4) return false;
+    const int64_t B = t.size(0), L = t.size(1), H = t.size(2), d = t.size(3);
+    return (d == 1 || t.stride(3) == 1) && (H == 1 || t.stride(2) == d) && (L == 1 || B == 1 || t.stride(0) == L * t.stride(1));
+}
+int64_t token_stride(const Tensor& t) {
+    if (t.size(1) > 1) return t.stride(1);
+    if (t.size(0) > 1) return t.stride(0);
+    return t.size(2) * t.size(3);
+}
+const Tensor& rows(PyObject* o, const char* name) {
+    const Tensor& t = tensor(o);
+    if (!t.defined()) throw TypeFault(std::string(name) + " is required");
+    if (!t.is_cuda()) value_error("libbased takes CUDA tensors only (there is no CPU path)");
+    dims(t, 4, name);
+    if (!evenly_spaced(t)) value_error(std::string(name) + " must be [B,L,H,d] with the heads of a token side by side and evenly spaced tokens");
+    return t;
+}
+// overlap() for such rows, which reach beyond their number of bytes: the whole stretch from the first to the last
+bool stretches_overlap(const Tensor& a, const Tensor& b) {
+    auto end = [](const Tensor& t) {
+        int64_t last = 0;
+        for (int64_t i = 0; i < t.dim(); ++i) {
+            if (t.size(i) == 0) return static_cast<const char*>(t.const_data_ptr());
+            last += (t.size(i) - 1) * t.stride(i);
+        }
+        return static_cast<const char*>(t.const_data_ptr()) + (last + 1) * static_cast<int64_t>(t.element_size());
+    };
+    return static_cast<const char*>(a.const_data_ptr()) < end(b) && static_cast<const char*>(b.const_data_ptr()) < end(a);
+}
+struct Rotation {
+    Tensor q, k, wq, wk, freqs, positions;
+    float eps;
+    int flags, start;
+    int B = 0, L = 0, Hq = 0, Hk = 0, d = 0, n = 0, per = 0;
+    based_dtype io = BASED_F32;
+    Rotation(Tensor q_, Tensor k_, Tensor wq_, Tensor wk_, Tensor f_, Tensor p_, float eps_, int flags_, int start_)
+        : q(std::move(q_)), k(std::move(k_)), wq(std::move(wq_)), wk(std::move(wk_)), freqs(std::move(f_)), positions(std::move(p_)),
+          eps(eps_), flags(flags_), start(start_) {
+        B = dim(q, 0); L = dim(q, 1); Hq = dim(q, 2); Hk = dim(k, 2); d = dim(q, 3);
+        if (k.size(0) != B || k.size(1) != L || k.size(3) != d || k.scalar_type() != q.scalar_type())
+            value_error("q, k shapes/dtypes disagree");
+        check_f32(wq, {d}, "q_weight");
+        check_f32(wk, {d}, "k_weight");
+        if (freqs.defined()) {
+            if (freqs.scalar_type() != at::kDouble) throw TypeFault("freqs is fp64");
+            if (freqs.dim() != 1 || freqs.size(0) == 0) value_error("freqs must be [n], or None for no rotation");
+            n = dim(freqs, 0);
+        }
+        if (positions.defined()) {
+            if (positions.scalar_type() != at::kInt || !(shape_is(positions, {B}) || shape_is(positions, {B, L})))
+                value_error("positions is an int32 tensor with one entry per sequence, [B], or per token, [B,L]");
+            if (start) value_error("positions and start exclude each other");
+            per = positions.dim() == 2 ? L : 1;
+        }
+        io = dtype_code(q);
+        check_places({&q, &k, &wq, &wk, &freqs, &positions}, {});
+    }
+    const double* f() const { return static_cast<const double*>(cptr(freqs)); }
+    const int* p() const { return static_cast<const int*>(cptr(positions)); }
+    // an output of the caller's own: on the device, and apart from what the call reads
+    void own(const Tensor& t, std::initializer_list<const Tensor*> more) const {
+        if (!t.defined()) return;
+        if (t.device() != q.device()) value_error("the tensors of a call lie on different devices");
+        for (const Tensor* in : {&q, &k, &wq, &wk, &freqs, &positions})
+            if (in->defined() && stretches_overlap(t, *in)) value_error("an output overlaps an input");
+        for (const Tensor* in : more)
+            if (in->defined() && stretches_overlap(t, *in)) value_error("an output overlaps an input");
+    }
+    void forward(Tensor& oq, Tensor& ok, void* stream) const {
+        if (!oq.defined()) oq = at::empty({B, Hq, L, d}, q.options());
+        if (!ok.defined()) ok = at::empty({B, Hk, L, d}, k.options());
+        check(based_qk_norm_rotate(cptr(q), cptr(k), token_stride(q), token_stride(k), f32(wq), f32(wk), f(), p(), per, start, ptr(oq),
+                                   ptr(ok), B, L, Hq, Hk, d, n, eps, io, flags, stream),
+              "based_qk_norm_rotate");
+    }
+    void backward(const Tensor& gq, const Tensor& gk, Tensor& dq, Tensor& dk, bool weights, Tensor& dwq, Tensor& dwk,
+                  const Tensor& workspace, void* stream) const {
+        const Workspace ws(workspace, weights ? based_qk_norm_rotate_backward_workspace_bytes(B, L, Hq, Hk, d, io) : 0, q, stream);
+        if (!dq.defined()) dq = at::empty({B, L, Hq, d}, q.options());
+        if (!dk.defined()) dk = at::empty({B, L, Hk, d}, k.options());
+        if (weights) {
+            dwq = at::empty({d}, q.options().dtype(at::kFloat));
+            dwk = at::empty({d}, q.options().dtype(at::kFloat));
+        }
+        check(based_qk_norm_rotate_backward(cptr(q), cptr(k), token_stride(q), token_stride(k), f32(wq), f32(wk), f(), p(), per, start,
+                                            cptr(gq), cptr(gk), ptr(dq), ptr(dk), token_stride(dq), token_stride(dk), fptr(dwq),
+                                            fptr(dwk), B, L, Hq, Hk, d, n, eps, io, flags, ws.data, ws.bytes, stream),
+              "based_qk_norm_rotate_backward");
+    }
+};
+// q, k, q_weight, k_weight, freqs, positions, eps, flags, start, out_q, out_k, stream
+PyObject* rotate(PyObject* const* a) {
+    const Rotation o(rows(a[0], "q"), rows(a[1], "k"), dev(a[2]), dev(a[3]), dev(a[4]), dev(a[5]), number(a[6]), integer(a[7]), integer(a[8]));
+    Tensor oq = dev(a[9]), ok = dev(a[10]);
+    if (oq.defined() && (!shape_is(oq, {o.B, o.Hq, o.L, o.d}) || oq.scalar_type() != o.q.scalar_type()))
+        value_error("out_q must be [B,H_q,L,d] in the io dtype");
+    if (ok.defined() && (!shape_is(ok, {o.B, o.Hk, o.L, o.d}) || ok.scalar_type() != o.q.scalar_type()))
+        value_error("out_k must be [B,H_k,L,d] in the io dtype");
+    o.own(oq, {});
+    o.own(ok, {&oq});
+    void* stream = stream_on(a[11], o.q);
+    away(o.q, [&] { o.forward(oq, ok, stream); });
+    return wrap({oq, ok});
+}
+// q, k, dout_q, dout_k, q_weight, k_weight, freqs, positions, eps, flags, start, dq, dk, workspace, stream
+// -> dq, dk, dq_weight, dk_weight (None where there is no such weight)
+PyObject* rotate_backward(PyObject* const* a) {
+    const Rotation o(rows(a[0], "q"), rows(a[1], "k"), dev(a[4]), dev(a[5]), dev(a[6]), dev(a[7]), number(a[8]), integer(a[9]), integer(a[10]));
+    const Tensor &gq = need(a[2], "dout_q"), &gk = need(a[3], "dout_k"), &ws = dev(a[13]);
+    if (!shape_is(gq, {o.B, o.Hq, o.L, o.d}) || gq.scalar_type() != o.q.scalar_type())
+        value_error("dout_q must be [B,H_q,L,d] in the io dtype");
+    if (!shape_is(gk, {o.B, o.Hk, o.L, o.d}) || gk.scalar_type() != o.q.scalar_type())
+        value_error("dout_k must be [B,H_k,L,d] in the io dtype");
+    check_places({&o.q, &gq, &gk}, {});
+    Tensor dq = a[11] == Py_None ? Tensor() : rows(a[11], "dq"), dk = a[12] == Py_None ? Tensor() : rows(a[12], "dk");
+    check_like(dq, o.q, "dq", "q");
+    check_like(dk, o.k, "dk", "k");
+    o.own(ws, {&gq, &gk});
+    o.own(dq, {&gq, &gk, &ws});
+    o.own(dk, {&gq, &gk, &ws});
+    // slices of one gradient lie between each other: every token's rows apart
+    if (dq.defined() && dk.defined() && stretches_overlap(dq, dk)) {
+        const int64_t s = token_stride(dq) * dq.element_size(), row_q = static_cast<int64_t>(o.Hq) * o.d * dq.element_size(),
+                      row_k = static_cast<int64_t>(o.Hk) * o.d * dk.element_size();
+        const int64_t gap = static_cast<const char*>(dk.const_data_ptr()) - static_cast<const char*>(dq.const_data_ptr());
+        if (token_stride(dk) != token_stride(dq) || !(gap >= 0 ? gap >= row_q && gap + row_k <= s : -gap >= row_k && -gap + row_q <= s))
+            value_error("two outputs overlap");
+    }
+    void* stream = stream_on(a[14], o.q);
+    Tensor dwq, dwk;
+    away(o.q, [&] { o.backward(gq, gk, dq, dk, o.wq.defined() || o.wk.defined(), dwq, dwk, ws, stream); });
+    return wrap({dq, dk, o.wq.defined() ? dwq : Tensor(), o.wk.defined() ? dwk : Tensor()});
+}
+
+Gradients swa_backward_call(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& dout, const Tensor& workspace, int window,
+                            float scale, void* stream) {
+    const int B = dim(q, 0), H = dim(q, 1), L = dim(q, 2), d = dim(q, 3);
+    const based_dtype io = dtype_code(q);
+    const Workspace ws(workspace, swa_backward_workspace_bytes(B, H, L, window, io), q, stream);
+    Gradients g{fresh(q), fresh(k), fresh(v)};
+    check(swa_backward(cptr(q), cptr(k), cptr(v), cptr(dout), ptr(g.dq), ptr(g.dk), ptr(g.dv), B, H, L, d, window, scale, io, ws.data,
+                       ws.bytes, stream),
+          "swa_backward");
+    return g;
+}
+// q, k, v, dout, window, softmax_scale, workspace, stream
+PyObject* swa_grad(PyObject* const* a) {
+    const Tensor &q = need(a[0], "q"), &k = need(a[1], "k"), &v = need(a[2], "v"), &dout = need(a[3], "dout"), &ws = dev(a[6]);
+    dims(q, 4, "q");
+    check_qkv(q, k, v, kNone);
+    if (v.sizes() != q.sizes()) value_error("the sliding-window mixer takes q, k, v of one shape");
+    check_like(dout, q, "dout", "q");
+    check_places({&q, &k, &v, &dout}, {&ws});
+    const int window = integer(a[4]);
+    const float scale = number(a[5]);
+    void* stream = stream_on(a[7], q);
+    Gradients g;
+    away(q, [&] { g = swa_backward_call(q, k, v, dout, ws, window, scale, stream); });
+    return wrap({g.dq, g.dk, g.dv});
+}
+
 // Python's exception for a status of the library
 void set_status_error(const StatusFault& e) {
     PyObject* mod = PyImport_ImportModule("paper_2402_18668_b200.binding");
@@ -615,6 +893,159 @@ PyObject* linear_attention(PyObject* const* a) {
     return wrap(r);
 }
 
+// What the nodes of the layers share: the current stream of the tensors' device, and a status handed on as Python's exception.
+// Their gradients are kernels' results, with no graph of their own: a second derivative is refused rather than left out.
+template <typename F> torch::autograd::variable_list node_backward(const Tensor& on, F f) {
+    if (at::GradMode::is_enabled()) throw std::runtime_error("this operator's gradient cannot be differentiated again (create_graph)");
+    const c10::cuda::CUDAGuard device(on.device());
+    try {
+        return f(c10::cuda::getCurrentCUDAStream(on.get_device()).stream());
+    } catch (const StatusFault& e) {
+        pybind11::gil_scoped_acquire lock;
+        set_status_error(e);
+        python_error err;
+        err.persist();
+        throw err;
+    }
+}
+Tensor as_input(const Tensor& g, const Tensor& like) { return g.defined() ? g.contiguous().to(like.scalar_type()) : Tensor(); }
+void on_gpu(const Tensor& t) {
+    if (!t.is_cuda()) value_error("libbased takes CUDA tensors only (there is no CPU path)");
+}
+Tensor packed(const std::optional<Tensor>& t) { return t ? t->contiguous() : Tensor(); }
+std::optional<Tensor> maybe(const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; }
+struct GatedRecurrence : torch::autograd::Function<GatedRecurrence> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x_, const Tensor& r_,
+                                                  const Tensor& g_, const Tensor& rate_, const std::optional<Tensor>& in_) {
+        ctx->set_materialize_grads(false);
+        on_gpu(x_);
+        const Tensor x = x_.contiguous(), r = r_.contiguous(), g = g_.contiguous(), rate = rate_.contiguous(), in = packed(in_);
+        dims(x, 3, "x");
+        check_gates(x, r, g, rate);
+        check_f32(in, {x.size(0), x.size(2)}, "state");
+        check_places({&x, &r, &g, &rate, &in}, {});
+        const c10::cuda::CUDAGuard device(x.device());
+        const Tensor last = at::empty({x.size(0), x.size(2)}, x.options().dtype(at::kFloat));
+        const Tensor out = recurrence_call(x, r, g, rate, in, Tensor(), last, c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
+        ctx->save_for_backward({x, r, g, rate, in, out});
+        return {out, last};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        const auto saved = ctx->get_saved_variables();
+        const Tensor &x = saved[0], &in = saved[4];
+        if (!grads[0].defined() && !grads[1].defined()) return {Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        return node_backward(x, [&](void* stream) -> torch::autograd::variable_list {
+            const Tensor dout = grads[0].defined() ? as_input(grads[0], x) : at::zeros_like(x);
+            const RecurrenceGradients d = recurrence_backward_call(x, saved[1], saved[2], saved[3], in, saved[5], dout,
+                                                                   as_input(grads[1], saved[3]), kNone, stream);
+            return {d.dx, d.dr, d.dg, d.drate, d.dstate};
+        });
+    }
+};
+struct NormRotation : torch::autograd::Function<NormRotation> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& q_, const Tensor& k_,
+                                                  const std::optional<Tensor>& wq, const std::optional<Tensor>& wk,
+                                                  const std::optional<Tensor>& freqs, const std::optional<Tensor>& positions, double eps, int64_t flags, int64_t start) {
+        on_gpu(q_);
+        on_gpu(k_);
+        dims(q_, 4, "q");
+        dims(k_, 4, "k");
+        const Rotation o(evenly_spaced(q_) ? q_ : q_.contiguous(), evenly_spaced(k_) ? k_ : k_.contiguous(), packed(wq), packed(wk),
+                         packed(freqs), packed(positions), static_cast<float>(eps), static_cast<int>(flags), static_cast<int>(start));
+        const c10::cuda::CUDAGuard device(o.q.device());
+        Tensor oq, ok;
+        o.forward(oq, ok, c10::cuda::getCurrentCUDAStream(o.q.get_device()).stream());
+        ctx->save_for_backward({o.q, o.k, o.wq, o.wk, o.freqs, o.positions});
+        ctx->saved_data["eps"] = eps;
+        ctx->saved_data["flags"] = flags;
+        ctx->saved_data["start"] = start;
+        ctx->saved_data["weights"] = (wq && wq->requires_grad()) || (wk && wk->requires_grad());
+        return {oq, ok};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        const auto s = ctx->get_saved_variables();
+        const Rotation o(s[0], s[1], s[2], s[3], s[4], s[5], static_cast<float>(ctx->saved_data["eps"].toDouble()),
+                         static_cast<int>(ctx->saved_data["flags"].toInt()), static_cast<int>(ctx->saved_data["start"].toInt()));
+        return node_backward(o.q, [&](void* stream) -> torch::autograd::variable_list {
+            Tensor dq, dk, dwq, dwk;
+            o.backward(as_input(grads[0], o.q), as_input(grads[1], o.k), dq, dk, ctx->saved_data["weights"].toBool(), dwq, dwk, kNone, stream);
+            return {dq, dk, o.wq.defined() ? dwq : Tensor(), o.wk.defined() ? dwk : Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        });
+    }
+};
+struct SlidingWindow : torch::autograd::Function<SlidingWindow> {
+    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& q_, const Tensor& k_, const Tensor& v_, int64_t window,
+                          double scale) {
+        on_gpu(q_);
+        const Tensor q = q_.contiguous(), k = k_.contiguous(), v = v_.contiguous();
+        dims(q, 4, "q");
+        check_qkv(q, k, v, kNone);
+        if (v.sizes() != q.sizes()) value_error("the sliding-window mixer takes q, k, v of one shape");
+        check_places({&q, &k, &v}, {});
+        const c10::cuda::CUDAGuard device(q.device());
+        Tensor out = fresh(q);
+        check(swa_forward(cptr(q), cptr(k), cptr(v), ptr(out), dim(q, 0), dim(q, 1), dim(q, 2), dim(q, 3), static_cast<int>(window),
+                          static_cast<float>(scale), dtype_code(q), c10::cuda::getCurrentCUDAStream(q.get_device()).stream()),
+              "swa_forward");
+        ctx->save_for_backward({q, k, v});
+        ctx->saved_data["window"] = window;
+        ctx->saved_data["scale"] = scale;
+        return out;
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        const auto s = ctx->get_saved_variables();
+        return node_backward(s[0], [&](void* stream) -> torch::autograd::variable_list {
+            const Tensor dout = tokens_first(grads[0], s[0].scalar_type()) ? heads_first(grads[0], s[0].scalar_type(), stream)
+                                                                           : as_input(grads[0], s[0]);
+            const Gradients g = swa_backward_call(s[0], s[1], s[2], dout, kNone, static_cast<int>(ctx->saved_data["window"].toInt()),
+                                                  static_cast<float>(ctx->saved_data["scale"].toDouble()), stream);
+            return {g.dq, g.dk, g.dv, Tensor(), Tensor()};
+        });
+    }
+};
+// a call of a node, without the interpreter lock
+template <typename F> auto applied(F f) {
+    decltype(f()) r;
+    std::exception_ptr fault;
+    Py_BEGIN_ALLOW_THREADS
+    try {
+        r = f();
+    } catch (...) {
+        fault = std::current_exception();
+    }
+    Py_END_ALLOW_THREADS
+    if (fault) std::rethrow_exception(fault);
+    return r;
+}
+Tensor given(PyObject* o, const char* name) {
+    const Tensor& t = tensor(o);
+    if (!t.defined()) throw TypeFault(std::string(name) + " is required");
+    return t;
+}
+// x, r, g, rate, state
+PyObject* gated_recurrence(PyObject* const* a) {
+    const Tensor x = given(a[0], "x"), r = given(a[1], "r"), g = given(a[2], "g"), rate = given(a[3], "rate");
+    const auto in = maybe(tensor(a[4]));
+    const auto y = applied([&] { return GatedRecurrence::apply(x, r, g, rate, in); });
+    return wrap({y[0], y[1]});
+}
+// q, k, q_weight, k_weight, freqs, positions, eps, flags, start
+PyObject* qk_norm_rotate(PyObject* const* a) {
+    const Tensor q = given(a[0], "q"), k = given(a[1], "k");
+    const auto wq = maybe(tensor(a[2])), wk = maybe(tensor(a[3])), f = maybe(tensor(a[4])), p = maybe(tensor(a[5]));
+    const double eps = number(a[6]);
+    const int64_t flags = integer(a[7]), start = integer(a[8]);
+    const auto y = applied([&] { return NormRotation::apply(q, k, wq, wk, f, p, eps, flags, start); });
+    return wrap({y[0], y[1]});
+}
+// q, k, v, window, softmax_scale
+PyObject* sliding_window(PyObject* const* a) {
+    const Tensor q = given(a[0], "q"), k = given(a[1], "k"), v = given(a[2], "v");
+    const int64_t window = integer(a[3]);
+    const double scale = number(a[4]);
+    return wrap(applied([&] { return SlidingWindow::apply(q, k, v, window, scale); }));
+}
+
 // ---------------------------------------------------------------------------------------------- module
 // Everything but the faults of this file is torch's to translate: its own error types, and Python exceptions that passed
 // through C++ (python_error, from a saved-tensor hook for instance), which go on as they are.
@@ -647,7 +1078,11 @@ PyMethodDef methods[] = {method<prefill, 9>("prefill"), method<prefill_backward,
                          method<generation_step, 16>("generation_step"), method<baseconv, 8>("baseconv"),
                          method<generation_graph, 15>("generation_graph"), method<generation_graph_step, 7>("generation_graph_step"),
                          method<generation_graph_replay, 1>("generation_graph_replay"),
-                         method<linear_attention, 4>("linear_attention"), {nullptr, nullptr, 0, nullptr}};
+                         method<linear_attention, 4>("linear_attention"),
+                         method<recurrence, 8>("recurrence"), method<recurrence_backward, 10>("recurrence_backward"),
+                         method<rotate, 12>("rotate"), method<rotate_backward, 15>("rotate_backward"),
+                         method<swa_grad, 8>("swa_grad"), method<gated_recurrence, 5>("gated_recurrence"),
+                         method<qk_norm_rotate, 9>("qk_norm_rotate"), method<sliding_window, 5>("sliding_window"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 
