@@ -644,6 +644,7 @@ based_status based_qk_norm_rotate_backward(const void* q, const void* k, long lo
 
 size_t swa_backward_workspace_bytes(int B, int H, int L, int window, based_dtype io) {
     if (B <= 0 || H <= 0 || L <= 0 || window <= 0 || window > 128 || (io != BASED_F32 && io != BASED_BF16)) return 0;
+    if (io == BASED_BF16) return 0;
     const long long BH = (long long)B * H < kHeadSlab ? (long long)B * H : kHeadSlab;       // the largest slab of heads
     return (size_t)BH * L * 16;
 }
@@ -667,10 +668,13 @@ based_status swa_backward(const void* q, const void* k, const void* v, const voi
     const size_t hb = (size_t)L * d * esize(io);
     for (long long h0 = 0; h0 < BH; h0 += kHeadSlab) {
         const int n = (int)(BH - h0 < kHeadSlab ? BH - h0 : kHeadSlab);
-        const based_status st = launch_swa_backward_simt(off(q, h0 * hb), off(k, h0 * hb), off(v, h0 * hb), off(dout, h0 * hb),
-                                                         off(dq, h0 * hb), off(dk, h0 * hb), off(dv, h0 * hb),
-                                                         static_cast<float*>(workspace), n, L, window, scale, io,
-                                                         static_cast<cudaStream_t>(cuda_stream));
+        const size_t at = h0 * hb;
+        const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+        const based_status st =
+            io == BASED_BF16 ? launch_swa_backward_tc(off(q, at), off(k, at), off(v, at), off(dout, at), off(dq, at), off(dk, at), off(dv, at),
+                                                      n, L, window, scale, stream)
+                             : launch_swa_backward_f32(off(q, at), off(k, at), off(v, at), off(dout, at), off(dq, at), off(dk, at),
+                                                       off(dv, at), static_cast<float*>(workspace), n, L, window, scale, stream);
         if (st != BASED_OK) return st;
     }
     return BASED_OK;

@@ -255,9 +255,12 @@ size_t norm_rotate_backward_bytes(int B, int L, int d, based_dtype io);
 // gq, gk [B,H,L,d] -> dq, dk as q, k lie, with token strides of their own; dwq, dwk [d], both or neither
 based_status launch_norm_rotate_backward(const NormRotate& a, const void* gq, const void* gk, void* dq, long long dq_stride, void* dk,
                                          long long dk_stride, float* dwq, float* dwk, float* part, based_dtype io, cudaStream_t stream);
-// backward of the sliding window (swa_backward.cu: multiply-adds); stats: [BH, L] float4 scratch
-based_status launch_swa_backward_simt(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
-                                      float* stats, int BH, int L, int window, float scale, based_dtype io, cudaStream_t stream);
+// backward of the sliding window, fp32 io (swa_backward_f32.cu: multiply-adds); stats: [BH, L] float4 scratch
+based_status launch_swa_backward_f32(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
+                                     float* stats, int BH, int L, int window, float scale, cudaStream_t stream);
+// bf16 io, on tensor cores (swa_backward_tc.cu)
+based_status launch_swa_backward_tc(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, int BH,
+                                    int L, int window, float scale, cudaStream_t stream);
 // load the generation-step kernels into the current context
 based_status preload_decode();
 based_status preload_swa_decode();

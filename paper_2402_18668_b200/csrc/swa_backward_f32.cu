@@ -1,4 +1,4 @@
-// swa_backward on fp32 multiply-adds: gradients of the sliding-window softmax attention of swa_forward.  With c = scale,
+// swa_backward, fp32 io, on multiply-adds: gradients of the sliding-window softmax attention of swa_forward.  With c = scale,
 // row i over its keys j = max(0, i-w+1) .. i:
 //
 //   P_ij = exp(c (s_ij - m_i)) / l_i,  dP_ij = dout_i . v_j,  D_i = sum_j P_ij dP_ij,  dS_ij = c P_ij (dP_ij - D_i),
@@ -9,7 +9,6 @@
 // row statistics m, 1/l, D, then dS and dq.  The second takes 64 keys and recomputes P and dS of the queries that see them
 // from the statistics.  Neither adds into memory that another CTA writes, so results do not depend on any order.
 #include "common.cuh"
-#include "pairs.cuh"
 
 namespace based {
 
@@ -19,16 +18,12 @@ constexpr int kTile = kT * kStride;
 constexpr size_t kSmemQ = 5 * kTile * sizeof(float), kSmemK = 6 * kTile * sizeof(float) + kT * sizeof(float4);
 
 // rows r0 .. r0 + 63 of [L][64] into a padded tile, zeros outside [0, L)
-template <typename T> __device__ __forceinline__ void load_tile(float* dst, const T* src, int r0, int L) {
-    constexpr int V = pairs::Piece<T>::V, P2 = V / 2;
-    for (int i = threadIdx.x; i < kT * kHD / V; i += kThreads) {
-        const int row = i / (kHD / V), col = (i % (kHD / V)) * V;
-        pairs::pair x[P2];
-#pragma unroll
-        for (int e = 0; e < P2; ++e) x[e] = 0;
-        if (r0 + row >= 0 && r0 + row < L)
-            pairs::Piece<T>::unpack(*reinterpret_cast<const uint4*>(src + (size_t)(r0 + row) * kHD + col), x);
-        pairs::store_f32<P2>(dst + row * kStride + col, x);
+__device__ __forceinline__ void load_tile(float* dst, const float* src, int r0, int L) {
+    for (int i = threadIdx.x; i < kT * kHD / 4; i += kThreads) {
+        const int row = i / (kHD / 4), col = (i % (kHD / 4)) * 4;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r0 + row >= 0 && r0 + row < L) x = *reinterpret_cast<const float4*>(src + (size_t)(r0 + row) * kHD + col);
+        *reinterpret_cast<float4*>(dst + row * kStride + col) = x;
     }
 }
 __device__ __forceinline__ float4 lds(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -70,14 +65,12 @@ __device__ __forceinline__ void product(float (&acc)[4][4], const float* a, cons
         }
     }
 }
-template <typename T> __device__ __forceinline__ void store_rows(T* dst, const float (&acc)[4][4], int r0, int L, int ty, int tx) {
+__device__ __forceinline__ void store_rows(float* dst, const float (&acc)[4][4], int r0, int L, int ty, int tx) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = r0 + ty + 16 * i;
         if (row >= L) continue;
-        T* p = dst + (size_t)row * kHD + 4 * tx;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) p[j] = from_f32<T>(acc[i][j]);
+        *reinterpret_cast<float4*>(dst + (size_t)row * kHD + 4 * tx) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
     }
 }
 __device__ __forceinline__ float max16(float x) {
@@ -93,10 +86,10 @@ __device__ __forceinline__ float sum16(float x) {
 }  // namespace
 
 // 64 queries against TILES tiles of 64 keys (the last of them their own); stats: (m, 1 / l, D, 0) per row
-template <typename T, int TILES>
-__global__ void __launch_bounds__(kThreads) swa_backward_queries_kernel(const T* __restrict__ q, const T* __restrict__ k,
-                                                                        const T* __restrict__ v, const T* __restrict__ dout,
-                                                                        T* __restrict__ dq, float4* __restrict__ stats, int L, int window,
+template <int TILES>
+__global__ void __launch_bounds__(kThreads) swa_backward_queries_kernel(const float* __restrict__ q, const float* __restrict__ k,
+                                                                        const float* __restrict__ v, const float* __restrict__ dout,
+                                                                        float* __restrict__ dq, float4* __restrict__ stats, int L, int window,
                                                                         float scale) {
     extern __shared__ __align__(16) float smem[];
     float *sQ = smem, *sO = sQ + kTile, *sK = sO + kTile, *sV = sK + kTile, *sD = sV + kTile;
@@ -166,11 +159,11 @@ __global__ void __launch_bounds__(kThreads) swa_backward_queries_kernel(const T*
 }
 
 // 64 keys and the TILES tiles of queries that see them (the first of them their own)
-template <typename T, int TILES>
-__global__ void __launch_bounds__(kThreads) swa_backward_keys_kernel(const T* __restrict__ q, const T* __restrict__ k,
-                                                                     const T* __restrict__ v, const T* __restrict__ dout,
-                                                                     const float4* __restrict__ stats, T* __restrict__ dk,
-                                                                     T* __restrict__ dv, int L, int window, float scale) {
+template <int TILES>
+__global__ void __launch_bounds__(kThreads) swa_backward_keys_kernel(const float* __restrict__ q, const float* __restrict__ k,
+                                                                     const float* __restrict__ v, const float* __restrict__ dout,
+                                                                     const float4* __restrict__ stats, float* __restrict__ dk,
+                                                                     float* __restrict__ dv, int L, int window, float scale) {
     extern __shared__ __align__(16) float smem[];
     float *sK = smem, *sV = sK + kTile, *sQ = sV + kTile, *sO = sQ + kTile, *sP = sO + kTile, *sD = sP + kTile;
     float4* sS = reinterpret_cast<float4*>(sD + kTile);
@@ -214,37 +207,33 @@ __global__ void __launch_bounds__(kThreads) swa_backward_keys_kernel(const T* __
     store_rows(dv + head, av, j0, L, ty, tx);
 }
 
-template <typename T, int TILES>
+template <int TILES>
 static based_status launch_tiles(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, float* stats,
                                  int BH, int L, int window, float scale, cudaStream_t stream) {
-    auto kq = swa_backward_queries_kernel<T, TILES>;
-    auto kk = swa_backward_keys_kernel<T, TILES>;
+    auto kq = swa_backward_queries_kernel<TILES>;
+    auto kk = swa_backward_keys_kernel<TILES>;
     // per-device attributes; setting them on every call keeps multi-device processes correct
     if (cudaFuncSetAttribute(kq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemQ) != cudaSuccess ||
         cudaFuncSetAttribute(kk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemK) != cudaSuccess)
         return BASED_ERR_CUDA;
     const dim3 grid((L + kT - 1) / kT, BH);
-    auto in = [](const void* p) { return static_cast<const T*>(p); };
-    cudaError_t e = launch_ex(kq, grid, dim3(kThreads), kSmemQ, 1, true, stream, in(q), in(k), in(v), in(dout), static_cast<T*>(dq),
+    auto in = [](const void* p) { return static_cast<const float*>(p); };
+    cudaError_t e = launch_ex(kq, grid, dim3(kThreads), kSmemQ, 1, true, stream, in(q), in(k), in(v), in(dout), static_cast<float*>(dq),
                               reinterpret_cast<float4*>(stats), L, window, scale);
     if (e == cudaSuccess)
         e = launch_ex(kk, grid, dim3(kThreads), kSmemK, 1, true, stream, in(q), in(k), in(v), in(dout),
-                      reinterpret_cast<const float4*>(stats), static_cast<T*>(dk), static_cast<T*>(dv), L, window, scale);
+                      reinterpret_cast<const float4*>(stats), static_cast<float*>(dk), static_cast<float*>(dv), L, window, scale);
     note_launch();
     note_launch();
     const based_status st = check_launch("swa_backward_queries_kernel, swa_backward_keys_kernel");
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
 }
 
-based_status launch_swa_backward_simt(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
-                                      float* stats, int BH, int L, int window, float scale, based_dtype io, cudaStream_t stream) {
-    auto go = [&](auto zero) {
-        using T = decltype(zero);
-        // a query's first key lies window - 1 before it: one tile of 64 back, or two
-        return window <= kT + 1 ? launch_tiles<T, 2>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream)
-                                : launch_tiles<T, 3>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
-    };
-    return io == BASED_F32 ? go(0.f) : go(__nv_bfloat16{});
+based_status launch_swa_backward_f32(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
+                                     float* stats, int BH, int L, int window, float scale, cudaStream_t stream) {
+    // a query's first key lies window - 1 before it: one tile of 64 back, or two
+    return window <= kT + 1 ? launch_tiles<2>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream)
+                            : launch_tiles<3>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
 }
 
 }  // namespace based
