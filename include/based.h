@@ -443,22 +443,29 @@ based_status based_prefill_static_scratch(const void* q, const void* k, const vo
 size_t based_static_scratch_bytes(void);
 
 /*
+ * [B,N,C] values that need not lie contiguous: element (b, n, c) at data + b * batch_stride + n * token_stride + c.  Slices of a
+ * fused projection or of a longer batch are taken as they lie.  Strides in elements, multiples of 16 bytes, tokens and sequences not
+ * overlapping (a stride along a dimension of size 1 is not looked at).
+ */
+typedef struct { const void* data; long long batch_stride, token_stride; } based_tokens;
+
+/*
  * Gated linear recurrence: a token mixer with one fp32 state per channel, for the place behind the gated short convolution.
  * Per sequence and channel, t = 0 .. N-1, from state_in (NULL: zeros):
  *
  *   s = sigmoid(r_t),  a = exp(-rate s),  m = sqrt(1 - a^2),     h_t = a h_{t-1} + m sigmoid(g_t) x_t,     out_t = h_t
  *
- * x, r, g, out [B,N,C] in the io dtype; rate [C] fp32, >= 0 (not checked; a negative one gives NaN); state_in, state_out [B,C]
- * fp32: the state before token 0 and behind token N-1 (NULL: not wanted), which may be the same array.  Arithmetic and state are
- * fp32, out is rounded once.  A sigmoid below 2^-60 is taken as 2^-60.
- * Supported: C a multiple of 8; io in {F32, BF16}; any N >= 1.  out and state_out must not alias an input (state_out may be
- * state_in).
+ * x, r, g [B,N,C] in the io dtype; out [B,N,C] contiguous; rate [C] fp32, >= 0 (not checked; a negative one gives NaN); state_in,
+ * state_out [B,C] fp32: the state before token 0 and behind token N-1 (NULL: not wanted), which may be the same array.  Arithmetic
+ * and state are fp32, out is rounded once.  A sigmoid below 2^-59 is taken as 2^-59.
+ * Supported: C a multiple of 8; io in {F32, BF16}; 1 <= N <= 2^31 - 2^16.  out and state_out must not alias an input (state_out may
+ * be state_in).
  */
-based_status based_gated_recurrence_forward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+based_status based_gated_recurrence_forward(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
                                             void* out, float* state_out, int B, int N, int C, based_dtype io, void* cuda_stream);
 
 /* The same for one new token per sequence (generation): x, r, g, out [B,C]; state_in and state_out required. */
-based_status based_gated_recurrence_step(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+based_status based_gated_recurrence_step(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
                                          void* out, float* state_out, int B, int C, based_dtype io, void* cuda_stream);
 
 /*
@@ -468,12 +475,12 @@ based_status based_gated_recurrence_step(const void* x, const void* r, const voi
  *   G_t = dout_t + E_{t+1},   E_t = a_t G_t,   E_N = dstate_out;    dx = G m i,   dg = G m x i (1 - i),
  *   dlog a = a G h_{t-1} - (a^2 / m) G i x,   dr = -rate dlog a s (1 - s),   drate = -sum_{b,t} dlog a s,   dstate_in = E_0.
  *
- * dx, dr, dg [B,N,C] in the io dtype, drate [C] fp32, dstate_in [B,C] fp32 (NULL: not wanted; may be dstate_out).  drate is summed
+ * dx, dr, dg [B,N,C] in the io dtype, contiguous, drate [C] fp32, dstate_in [B,C] fp32 (NULL: not wanted; may be dstate_out).  drate is summed
  * in a fixed order.  Where m = 0 (a rate of 0) the gradient with respect to the rate is infinite by the formula; a large finite
  * number stands for 1 / m there.  workspace: based_gated_recurrence_backward_workspace_bytes.  No other output may alias an input.
  */
-based_status based_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
-                                             const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+based_status based_gated_recurrence_backward(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
+                                             based_tokens out, based_tokens dout, const float* dstate_out, void* dx, void* dr, void* dg,
                                              float* drate, float* dstate_in, int B, int N, int C, based_dtype io, void* workspace,
                                              size_t workspace_bytes, void* cuda_stream);
 size_t based_gated_recurrence_backward_workspace_bytes(int B, int N, int C, based_dtype io);

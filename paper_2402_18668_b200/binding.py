@@ -44,6 +44,11 @@ _lib = None
 _native_module = None
 
 
+class Tokens(ctypes.Structure):
+    """based_tokens: [B,N,C] values with strides, in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_longlong), ("token_stride", ctypes.c_longlong)]
+
+
 class BasedError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -118,11 +123,11 @@ def lib() -> ctypes.CDLL:
         L.based_tokens_to_heads.argtypes = [vp, vp, i, i, i, i, vp]
         ll = ctypes.c_longlong
         L.based_gated_recurrence_forward.restype = i
-        L.based_gated_recurrence_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, vp]
+        L.based_gated_recurrence_forward.argtypes = [Tokens, Tokens, Tokens, vp, vp, vp, vp, i, i, i, i, vp]
         L.based_gated_recurrence_step.restype = i
-        L.based_gated_recurrence_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, vp]
+        L.based_gated_recurrence_step.argtypes = [Tokens, Tokens, Tokens, vp, vp, vp, vp, i, i, i, vp]
         L.based_gated_recurrence_backward.restype = i
-        L.based_gated_recurrence_backward.argtypes = [vp] * 13 + [i, i, i, i, vp, sz, vp]
+        L.based_gated_recurrence_backward.argtypes = [Tokens, Tokens, Tokens, vp, vp, Tokens, Tokens] + [vp] * 6 + [i, i, i, i, vp, sz, vp]
         L.based_gated_recurrence_backward_workspace_bytes.restype = sz
         L.based_gated_recurrence_backward_workspace_bytes.argtypes = [i, i, i, i]
         L.based_qk_norm_rotate.restype = i
@@ -398,8 +403,8 @@ def based_generation_step(q, k, v, kv_state, z_state, qw, kw, vw, k_cache, v_cac
 
 
 def based_gated_recurrence_forward(x, r, g, rate, state_in=None, out=None, state_out=None, stream=None):
-    """h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(g_t) x_t with a_t = exp(-rate sigmoid(r_t)): x, r, g [B,N,C], rate [C] fp32;
-    state_in, state_out [B,C] fp32 (the states before and behind the tokens; state_out is written).  Returns out [B,N,C]."""
+    """h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(g_t) x_t with a_t = exp(-rate sigmoid(r_t)): x, r, g [B,N,C] (slices of a fused
+    projection or of a longer batch are taken as they lie), rate [C] fp32; state_in, state_out [B,C] fp32 (the states before and behind the tokens; state_out is written).  Returns out [B,N,C]."""
     if x.dim() != 3:
         raise ValueError("x must have 3 dimensions")
     return (_native_module or native()).recurrence(x, r, g, rate, state_in, out, state_out, _handle(stream))

@@ -531,24 +531,38 @@ static inline bool is_one_of(const void* p, std::initializer_list<const void*> o
         if (p && p == q) return true;
     return false;
 }
-static based_status recurrence_check(const void* x, const void* r, const void* g, const float* rate, int B, int N, int C, based_dtype io) {
-    if (!x || !r || !g || !rate || B <= 0 || N <= 0 || C <= 0) return BASED_ERR_INVALID_ARG;
+static based_status tokens_check(const based_tokens& t, int B, int N, int C, based_dtype io) {
+    const long long per16 = 16 / (long long)esize(io);
+    if (N > 1 && t.token_stride < C) return BASED_ERR_INVALID_ARG;
+    if (B > 1 && t.batch_stride < (N > 1 ? (N - 1) * t.token_stride : 0) + C) return BASED_ERR_INVALID_ARG;
+    // (the copies' tensor maps hold strides below 2^40 bytes)
+    if ((N > 1 && (t.token_stride % per16 != 0 || t.token_stride >= 1ll << 36)) || (B > 1 && (t.batch_stride % per16 != 0 || t.batch_stride >= 1ll << 37)))
+        return BASED_ERR_UNSUPPORTED;
+    return aligned16(t.data) ? BASED_OK : BASED_ERR_ALIGNMENT;
+}
+static based_status recurrence_check(const based_tokens& x, const based_tokens& r, const based_tokens& g, const float* rate, int B, int N, int C,
+                                     based_dtype io) {
+    if (!x.data || !r.data || !g.data || !rate || B <= 0 || N <= 0 || C <= 0) return BASED_ERR_INVALID_ARG;
     if (io != BASED_F32 && io != BASED_BF16) return BASED_ERR_INVALID_ARG;
-    if (C % 8 != 0 || (long long)B * C > (1ll << 36) || gated_recurrence_blocks(B, N, C, io) > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
-    if (!aligned16(x) || !aligned16(r) || !aligned16(g) || !aligned16(rate)) return BASED_ERR_ALIGNMENT;
-    return BASED_OK;
+    if (C % 8 != 0 || N > 0x7fff0000 || (long long)B * C > (1ll << 36) || gated_recurrence_blocks(B, N, C) > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    for (const based_tokens* t : {&x, &r, &g}) {
+        const based_status st = tokens_check(*t, B, N, C, io);
+        if (st != BASED_OK) return st;
+    }
+    return aligned16(rate) ? BASED_OK : BASED_ERR_ALIGNMENT;
 }
 
-based_status based_gated_recurrence_forward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+based_status based_gated_recurrence_forward(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
                                             void* out, float* state_out, int B, int N, int C, based_dtype io, void* cuda_stream) {
-    if (!out || is_one_of(out, {x, r, g, rate, state_in, state_out}) || is_one_of(state_out, {x, r, g, rate})) return BASED_ERR_INVALID_ARG;
+    if (!out || is_one_of(out, {x.data, r.data, g.data, rate, state_in, state_out}) || is_one_of(state_out, {x.data, r.data, g.data, rate}))
+        return BASED_ERR_INVALID_ARG;
     const based_status st = recurrence_check(x, r, g, rate, B, N, C, io);
     if (st != BASED_OK) return st;
     if (!aligned16(out) || !aligned16(state_in) || !aligned16(state_out)) return BASED_ERR_ALIGNMENT;
     return launch_gated_recurrence(x, r, g, rate, state_in, out, state_out, B, N, C, io, static_cast<cudaStream_t>(cuda_stream));
 }
 
-based_status based_gated_recurrence_step(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
+based_status based_gated_recurrence_step(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
                                          void* out, float* state_out, int B, int C, based_dtype io, void* cuda_stream) {
     if (!state_in || !state_out) return BASED_ERR_INVALID_ARG;
     return based_gated_recurrence_forward(x, r, g, rate, state_in, out, state_out, B, 1, C, io, cuda_stream);
@@ -556,27 +570,29 @@ based_status based_gated_recurrence_step(const void* x, const void* r, const voi
 
 size_t based_gated_recurrence_backward_workspace_bytes(int B, int N, int C, based_dtype io) {
     if (B <= 0 || N <= 0 || C <= 0 || (io != BASED_F32 && io != BASED_BF16)) return 0;
-    return gated_recurrence_backward_bytes(B, N, C, io);
+    return gated_recurrence_backward_bytes(B, N, C);
 }
 
-based_status based_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
-                                             const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+based_status based_gated_recurrence_backward(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
+                                             based_tokens out, based_tokens dout, const float* dstate_out, void* dx, void* dr, void* dg,
                                              float* drate, float* dstate_in, int B, int N, int C, based_dtype io, void* workspace,
                                              size_t workspace_bytes, void* cuda_stream) {
-    if (!out || !dout || !dx || !dr || !dg || !drate) return BASED_ERR_INVALID_ARG;
+    if (!out.data || !dout.data || !dx || !dr || !dg || !drate) return BASED_ERR_INVALID_ARG;
     const void* outs[] = {dx, dr, dg, drate, dstate_in};
     for (int i = 0; i < 5; ++i) {
-        if (is_one_of(outs[i], {x, r, g, rate, state_in, out, dout, workspace})) return BASED_ERR_INVALID_ARG;
+        if (is_one_of(outs[i], {x.data, r.data, g.data, rate, state_in, out.data, dout.data, workspace})) return BASED_ERR_INVALID_ARG;
         if (i < 4 && is_one_of(outs[i], {dstate_out})) return BASED_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
             if (is_one_of(outs[i], {outs[j]})) return BASED_ERR_INVALID_ARG;
     }
-    const based_status st = recurrence_check(x, r, g, rate, B, N, C, io);
+    based_status st = recurrence_check(x, r, g, rate, B, N, C, io);
+    if (st == BASED_OK) st = tokens_check(out, B, N, C, io);
+    if (st == BASED_OK) st = tokens_check(dout, B, N, C, io);
     if (st != BASED_OK) return st;
-    for (const void* p : {(const void*)state_in, out, dout, (const void*)dstate_out, (const void*)dx, (const void*)dr, (const void*)dg,
+    for (const void* p : {(const void*)state_in, (const void*)dstate_out, (const void*)dx, (const void*)dr, (const void*)dg,
                           (const void*)drate, (const void*)dstate_in, (const void*)workspace})
         if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
-    if (!workspace || workspace_bytes < gated_recurrence_backward_bytes(B, N, C, io)) return BASED_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < gated_recurrence_backward_bytes(B, N, C)) return BASED_ERR_WORKSPACE;
     return launch_gated_recurrence_backward(x, r, g, rate, state_in, out, dout, dstate_out, dx, dr, dg, drate, dstate_in, B, N, C,
                                             static_cast<float*>(workspace), io, static_cast<cudaStream_t>(cuda_stream));
 }

@@ -230,13 +230,15 @@ based_status launch_quadratic_groups_tc(const void* q, const void* k, const void
                                         int d_feat, int d_v, int numerator_only, bool overlapped, cudaStream_t stream);
 // sums of the columns of part [rows][cols], in a fixed order: columns 0 .. split - 1 to a, the others to b (column_sums.cu)
 based_status launch_column_sums(const float* part, long long rows, int cols, float* a, int split, float* b, cudaStream_t stream);
+// [B,N,C] values as the caller holds them: strides in elements (based_tokens)
+using Tokens = based_tokens;
 // gated linear recurrence (gated_recurrence.cu); _blocks: CTAs of a launch (a grid has at most 2^31 - 1); part: _bytes of scratch
-long long gated_recurrence_blocks(int B, int N, int C, based_dtype io);
-size_t gated_recurrence_backward_bytes(int B, int N, int C, based_dtype io);
-based_status launch_gated_recurrence(const void* x, const void* r, const void* g, const float* rate, const float* state_in, void* out,
+long long gated_recurrence_blocks(int B, int N, int C);
+size_t gated_recurrence_backward_bytes(int B, int N, int C);
+based_status launch_gated_recurrence(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, void* out,
                                      float* state_out, int B, int N, int C, based_dtype io, cudaStream_t stream);
-based_status launch_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
-                                              const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+based_status launch_gated_recurrence_backward(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in,
+                                              const Tokens& out, const Tokens& dout, const float* dstate_out, void* dx, void* dr, void* dg,
                                               float* drate, float* dstate_in, int B, int N, int C, float* part, based_dtype io,
                                               cudaStream_t stream);
 // norm of queries and keys with the position rotation (norm_rotate.cu)

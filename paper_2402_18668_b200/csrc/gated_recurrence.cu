@@ -4,28 +4,33 @@
 //   s = sigmoid(r),  a = exp(-rate s),  m = sqrt(1 - a^2),     h_t = a_t h_{t-1} + m_t sigmoid(g_t) x_t
 //
 // A run of tokens maps the state before it to the state behind it by h -> A h + H, and two runs in a row join to
-// (A2 A1, A2 H1 + H2).  A thread takes TOK consecutive tokens of one 16-byte piece of channels, the four token groups of a
-// warp join by shuffles, the warps of a CTA and the CTAs of a cluster through shared memory, and every thread then replays
-// its own tokens from the state that reaches it.  So the inputs are read once, whatever the sequence's length, and the loop
-// along the sequence carries nothing but the state.  The backward pass is the same scan from the last token to the first, of
+// (A2 A1, A2 H1 + H2).  A thread takes TOK consecutive tokens of 4 channels; the two token groups of a warp join by a shuffle, the
+// warps of a CTA and the CTAs of a cluster through shared memory, and every thread then replays its own tokens from the state that
+// reaches it.  So the inputs are read once, whatever the sequence's length, and the loop along the sequence carries nothing but the
+// state.  The backward pass is the same scan from the last token to the first, of
 //
 //   E_t = a_t (dout_t + E_{t+1}),     G_t = dout_t + E_{t+1} the gradient of h_t,
 //   dx = G m i,  dg = G m x i (1 - i),  dlog a = a G h_{t-1} - (a^2 / m) G i x,  dr = -rate dlog a s (1 - s),
 //   drate = -sum dlog a s  (i = sigmoid(g); h_{t-1} is read from the output that the caller kept).
 //
-// A thread's inputs come by asynchronous copies into a slot of shared memory that only it reads (no barrier), those of the
-// next step while this one is computed.
+// HBM bound by its bytes (4 values a token and channel forward, 8 backward), with little to spare: four special-function calls per
+// element forward take 60 us of the 82 us that the bytes of B8 N4096 C2048 bf16 take.  So one reciprocal serves both sigmoids, the
+// decay comes from a polynomial where the rates allow, everything else works on two channels per instruction, and tiles of
+// tokens x 64 channels come by TMA, which needs no address arithmetic and reads views with strides as they lie.
 #include <type_traits>
 
 #include "common.cuh"
 #include "pairs.cuh"
+#include "sm100.cuh"
 
 namespace based {
 using namespace pairs;
+using namespace sm100;
 
 namespace {
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kLanes = 8;                        // pieces of 16 bytes side by side: 128 bytes of a row
+constexpr int kV = 4, kP = kV / 2;               // channels of a thread, and pairs of them
+constexpr int kLanes = 16, kSlab = kLanes * kV;  // threads side by side, and their channels
 constexpr int kGroups = kThreads / kLanes;       // groups of TOK consecutive tokens
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -50,34 +55,75 @@ __device__ __forceinline__ float rroot(float x) {
     return y;
 }
 // (a NaN stays one)
-__device__ __forceinline__ float min_nan(float x, float y) {
-    float z;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
-    return z;
-}
 __device__ __forceinline__ float max_nan(float x, float y) {
     float z;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
     return z;
 }
 
-// 1 + exp(-x).  The exponent is held at 2^60, so that the product of two of them and its reciprocal stay finite: a
-// sigmoid below 2^-60 is taken as 2^-60
+// Four values of a row, as two pairs
+template <typename T> struct Four;
+// A gate is taken as -41 at least, so that exp(-x) stays below 2^60 and the product of two such sums and its reciprocal are finite: a
+// sigmoid below 2^-59 counts as 2^-59.  A NaN stays one.
+constexpr float kLeast = -41.f;
+template <> struct Four<float> {
+    using Raw = float4;
+    static __device__ __forceinline__ void values(const Raw& u, pair (&x)[kP]) {
+        x[0] = make(u.x, u.y);
+        x[1] = make(u.z, u.w);
+    }
+    static __device__ __forceinline__ Raw gate(const Raw& u) {
+        return make_float4(max_nan(u.x, kLeast), max_nan(u.y, kLeast), max_nan(u.z, kLeast), max_nan(u.w, kLeast));
+    }
+    static __device__ __forceinline__ Raw pack(const pair (&x)[kP]) {
+        const float2 a = split(x[0]), b = split(x[1]);
+        return make_float4(a.x, a.y, b.x, b.y);
+    }
+};
+template <> struct Four<__nv_bfloat16> {
+    using Raw = uint2;
+    static __device__ __forceinline__ void values(const Raw& u, pair (&x)[kP]) {
+        x[0] = make(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
+        x[1] = make(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+    }
+    static __device__ __forceinline__ Raw gate(Raw u) {
+        constexpr uint32_t least = 0xc224c224u;                      // -41 twice
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u.x) : "r"(least));
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u.y) : "r"(least));
+        return u;
+    }
+    static __device__ __forceinline__ Raw pack(const pair (&x)[kP]) {
+        const float2 a = split(x[0]), b = split(x[1]);
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x, a.y), hi = __floats2bfloat162_rn(b.x, b.y);
+        return make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    }
+};
+template <typename T> __device__ __forceinline__ void values4(const void* p, pair (&x)[kP]) {
+    Four<T>::values(*static_cast<const typename Four<T>::Raw*>(p), x);
+}
+template <typename T> __device__ __forceinline__ void gate4(const void* p, pair (&x)[kP]) {
+    Four<T>::values(Four<T>::gate(*static_cast<const typename Four<T>::Raw*>(p)), x);
+}
+template <typename T> __device__ __forceinline__ void write4(T* p, const pair (&x)[kP]) {
+    __stcs(reinterpret_cast<typename Four<T>::Raw*>(p), Four<T>::pack(x));
+}
+
+// 1 + exp(-x)
 __device__ __forceinline__ pair one_plus_exp_neg(pair x) {
     const float2 t = split(mul2(x, both(-kLog2e)));
-    return add2(make(ex2(min_nan(t.x, 60.f)), ex2(min_nan(t.y, 60.f))), both(1.f));
+    return add2(make(ex2(t.x), ex2(t.y)), both(1.f));
 }
 __device__ __forceinline__ pair rcp2(pair x) {
     const float2 t = split(x);
     return make(rcp(t.x), rcp(t.y));
 }
-// exp(la) - 1 for la <= 0.  Near 0 by its power series (to 2^-24 of la from -1/4 on: six terms), so that 1 - a^2 = -p (2 + p)
-// keeps its digits where the decay is slow.  SMALL: every la is in that range
+// exp(la) - 1 for la <= 0.  On [-1/4, 0] la times the polynomial of degree 4 that interpolates (exp(la) - 1) / la at the Chebyshev
+// points of the interval (off by 5e-9 relative at most, coefficients rounded to fp32), so that 1 - a^2 = -p (2 + p) keeps its digits
+// where the decay is slow.  SMALL: every la is in that range
 template <bool SMALL> __device__ __forceinline__ pair exp_less_one(pair la) {
-    pair y = fma2(la, both(1.f / 720.f), both(1.f / 120.f));
-    y = fma2(la, y, both(1.f / 24.f));
-    y = fma2(la, y, both(1.f / 6.f));
-    y = fma2(la, y, both(0.5f));
+    pair y = fma2(la, both(0.0075136062f), both(0.041490654f));
+    y = fma2(la, y, both(0.16665108f));
+    y = fma2(la, y, both(0.49999951f));
     y = fma2(la, y, both(1.f));
     y = mul2(la, y);
     if constexpr (!SMALL) {
@@ -87,7 +133,12 @@ template <bool SMALL> __device__ __forceinline__ pair exp_less_one(pair la) {
     return y;
 }
 // 1 - a^2 from p = a - 1
-__device__ __forceinline__ pair one_less_square(pair p) { return mul2(neg2(p), add2(p, both(2.f))); }
+__device__ __forceinline__ pair one_less_square(pair p) { return mul2(p, fma2(p, both(-1.f), both(-2.f))); }
+// whether the rates of a warp's threads keep -rate sigmoid above -1/4
+__device__ __forceinline__ bool all_small(const pair (&nrate)[kP]) {
+    const float2 a = split(nrate[0]), b = split(nrate[1]);
+    return __all_sync(0xffffffffu, a.x > -0.25f && a.y > -0.25f && b.x > -0.25f && b.y > -0.25f);
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -98,214 +149,205 @@ __device__ __forceinline__ void cluster_arrive_wait() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// 16 bytes into the same place of another CTA's shared memory
-__device__ __forceinline__ void store_remote(const void* own, uint32_t rank, ulonglong2 v) {
-    uint32_t addr;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(own))), "r"(rank));
-    asm volatile("st.shared::cluster.v2.b64 [%0], {%1, %2};" ::"r"(addr), "l"(v.x), "l"(v.y) : "memory");
+// 16 bytes into the same place of another CTA's shared memory, counted by its barrier
+__device__ __forceinline__ void store_remote(const void* own, uint64_t* own_bar, uint32_t rank, pair x, pair y) {
+    uint32_t addr, bar;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(own)), "r"(rank));
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(smem_u32(own_bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(addr), "l"(x), "l"(y), "r"(bar)
+                 : "memory");
 }
 
-// The joins of a step.  Shared memory holds two sets, used in turn: a set is written again two steps on, when every thread has
+// What a CTA shares.  The joins of a step use one of two sets in turn: a set is written again two steps on, when every thread has
 // passed the barrier of the step between and so has read it.
-template <int P2, int PARTS> struct Joins {                      // P2: pairs of channels per thread
-    ulonglong2 warp[2][kWarps][P2][kLanes];                      // A (P2 / 2 words), then H
-    ulonglong2 part[2][PARTS > 1 ? PARTS : 1][P2][kLanes];
+template <int PARTS> struct Shared {
+    ulonglong2 warp[2][kWarps][2][kLanes];                       // A, H of a warp's tokens
+    ulonglong2 part[2][PARTS > 1 ? PARTS : 1][2][kLanes];        // of a CTA's
+    pair sums[kWarps][kP][kLanes];
+    uint64_t full[3], arrived[2];                                // a stage's tiles; the parts of a set
+    uint32_t abort_flag;
 };
-// A, H: what the thread's tokens do to the state.  h: the state before this step, on return the one behind it.  Returns the
-// state that reaches the thread's first token in `first`.
-template <int P2, int PARTS>
-__device__ __forceinline__ void join(Joins<P2, PARTS>& sm, int turn, int rank, pair (&A)[P2], pair (&H)[P2], pair (&h)[P2],
-                                     pair (&first)[P2]) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane & (kLanes - 1);
-    // inclusive over the warp's four groups
+// A, H: what the thread's tokens do to the state.  h: the state before this step, on return the one behind it.  first: the state
+// that reaches the thread's first token.  after_barrier: run once every thread of the CTA has come this far.
+template <int PARTS, typename F>
+__device__ __forceinline__ bool join(Shared<PARTS>& sm, int step, int rank, const pair (&A0)[kP], const pair (&H0)[kP], pair (&h)[kP],
+                                     pair (&first)[kP], F after_barrier) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane & (kLanes - 1), turn = step & 1;
+    const bool upper = lane >= kLanes;
+    // the lower group's, for the upper one: in front of its own tokens, and joined to them the warp's
+    pair A[kP], H[kP];
 #pragma unroll
-    for (int d = kLanes; d < 32; d *= 2) {
-#pragma unroll
-        for (int e = 0; e < P2; ++e) {
-            const pair a = shfl_up2(A[e], d), b = shfl_up2(H[e], d);
-            if (lane >= d) {
-                H[e] = fma2(A[e], b, H[e]);
-                A[e] = mul2(A[e], a);
-            }
-        }
+    for (int e = 0; e < kP; ++e) {
+        A[e] = shfl_up2(A0[e], kLanes);
+        H[e] = shfl_up2(H0[e], kLanes);
     }
-    if (lane >= 32 - kLanes) {
-#pragma unroll
-        for (int w = 0; w < P2 / 2; ++w) {
-            sm.warp[turn][warp][w][col] = make_ulonglong2(A[2 * w], A[2 * w + 1]);
-            sm.warp[turn][warp][P2 / 2 + w][col] = make_ulonglong2(H[2 * w], H[2 * w + 1]);
-        }
-    }
-    // exclusive
-#pragma unroll
-    for (int e = 0; e < P2; ++e) {
-        A[e] = shfl_up2(A[e], kLanes);
-        H[e] = shfl_up2(H[e], kLanes);
-        if (lane < kLanes) {
-            A[e] = both(1.f);
-            H[e] = 0;
-        }
+    if (upper) {
+        sm.warp[turn][warp][0][col] = make_ulonglong2(mul2(A0[0], A[0]), mul2(A0[1], A[1]));
+        sm.warp[turn][warp][1][col] = make_ulonglong2(fma2(A0[0], H[0], H0[0]), fma2(A0[1], H[1], H0[1]));
     }
     __syncthreads();
+    after_barrier();
+    bool ok = true;
+    pair x[kP];                                                  // the state that reaches the warp
     if constexpr (PARTS > 1) {
-        // the CTA's total, and in front of the own warp's tokens the prefix of the warps before it
-        pair ta[P2], th[P2], pa[P2], ph[P2];
-#pragma unroll
-        for (int e = 0; e < P2; ++e) {
-            ta[e] = both(1.f);
-            th[e] = 0;
-        }
+        // the CTA's total, and of it what lies before the warp
+        pair ta[kP] = {both(1.f), both(1.f)}, th[kP] = {0, 0}, pa[kP], ph[kP];
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             if (w == warp) {
 #pragma unroll
-                for (int e = 0; e < P2; ++e) {
+                for (int e = 0; e < kP; ++e) {
                     pa[e] = ta[e];
                     ph[e] = th[e];
                 }
             }
-#pragma unroll
-            for (int u = 0; u < P2 / 2; ++u) {
-                const ulonglong2 a = sm.warp[turn][w][u][col], b = sm.warp[turn][w][P2 / 2 + u][col];
-                th[2 * u] = fma2(a.x, th[2 * u], b.x);
-                th[2 * u + 1] = fma2(a.y, th[2 * u + 1], b.y);
-                ta[2 * u] = mul2(a.x, ta[2 * u]);
-                ta[2 * u + 1] = mul2(a.y, ta[2 * u + 1]);
-            }
+            const ulonglong2 a = sm.warp[turn][w][0][col], b = sm.warp[turn][w][1][col];
+            th[0] = fma2(a.x, th[0], b.x);
+            th[1] = fma2(a.y, th[1], b.y);
+            ta[0] = mul2(a.x, ta[0]);
+            ta[1] = mul2(a.y, ta[1]);
         }
-        // the total goes to every CTA of the cluster, and the state runs through the totals of the CTAs before this one
-        if (lane < kLanes) {
+        // it goes to every CTA of the cluster
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&sm.arrived[turn], PARTS * 2 * kLanes * 16);
 #pragma unroll
-            for (int to = 0; to < PARTS; ++to) {
-                if ((to & (kWarps - 1)) != warp) continue;
-#pragma unroll
-                for (int u = 0; u < P2 / 2; ++u) {
-                    store_remote(&sm.part[turn][rank][u][col], to, make_ulonglong2(ta[2 * u], ta[2 * u + 1]));
-                    store_remote(&sm.part[turn][rank][P2 / 2 + u][col], to, make_ulonglong2(th[2 * u], th[2 * u + 1]));
-                }
-            }
+        for (int to = 0; to < PARTS; ++to) {
+            if ((to & (kWarps - 1)) != warp) continue;
+            if (upper) store_remote(&sm.part[turn][rank][1][col], &sm.arrived[turn], to, th[0], th[1]);
+            else store_remote(&sm.part[turn][rank][0][col], &sm.arrived[turn], to, ta[0], ta[1]);
         }
-        cluster_arrive_wait();
-        pair hs[P2];
+        ok = mbar_wait(&sm.arrived[turn], (step >> 1) & 1, &sm.abort_flag);
+        pair hs[kP];
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {
             if (q == rank) {
 #pragma unroll
-                for (int e = 0; e < P2; ++e) hs[e] = h[e];
+                for (int e = 0; e < kP; ++e) hs[e] = h[e];
             }
-#pragma unroll
-            for (int u = 0; u < P2 / 2; ++u) {
-                const ulonglong2 a = sm.part[turn][q][u][col], b = sm.part[turn][q][P2 / 2 + u][col];
-                h[2 * u] = fma2(a.x, h[2 * u], b.x);
-                h[2 * u + 1] = fma2(a.y, h[2 * u + 1], b.y);
-            }
+            const ulonglong2 a = sm.part[turn][q][0][col], b = sm.part[turn][q][1][col];
+            h[0] = fma2(a.x, h[0], b.x);
+            h[1] = fma2(a.y, h[1], b.y);
         }
 #pragma unroll
-        for (int e = 0; e < P2; ++e) first[e] = fma2(A[e], fma2(pa[e], hs[e], ph[e]), H[e]);
+        for (int e = 0; e < kP; ++e) x[e] = fma2(pa[e], hs[e], ph[e]);
     } else {
-        pair hs[P2];
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             if (w == warp) {
 #pragma unroll
-                for (int e = 0; e < P2; ++e) hs[e] = h[e];
+                for (int e = 0; e < kP; ++e) x[e] = h[e];
             }
-#pragma unroll
-            for (int u = 0; u < P2 / 2; ++u) {
-                const ulonglong2 a = sm.warp[turn][w][u][col], b = sm.warp[turn][w][P2 / 2 + u][col];
-                h[2 * u] = fma2(a.x, h[2 * u], b.x);
-                h[2 * u + 1] = fma2(a.y, h[2 * u + 1], b.y);
-            }
+            const ulonglong2 a = sm.warp[turn][w][0][col], b = sm.warp[turn][w][1][col];
+            h[0] = fma2(a.x, h[0], b.x);
+            h[1] = fma2(a.y, h[1], b.y);
         }
-#pragma unroll
-        for (int e = 0; e < P2; ++e) first[e] = fma2(A[e], hs[e], H[e]);
     }
+#pragma unroll
+    for (int e = 0; e < kP; ++e) first[e] = upper ? fma2(A[e], x[e], H[e]) : x[e];
+    return ok;
 }
+template <int PARTS> __device__ __forceinline__ void begin(Shared<PARTS>& sm) {
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < 3; ++s) mbar_init(&sm.full[s], 1);
+        for (int s = 0; s < 2; ++s) mbar_init(&sm.arrived[s], 1);
+        sm.abort_flag = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
+    if constexpr (PARTS > 1) cluster_arrive_wait();              // every CTA of the cluster runs, its barriers are set up
+}
+// Waits that have run out leave a flag and the loops run on without waiting (every thread still meets every barrier); copies that
+// may be under way then get time to land.
+template <int PARTS> __device__ __forceinline__ void finish(Shared<PARTS>& sm, bool ok, unsigned int* err) {
+    if (!ok) atomicOr(err, 1u);
+    __syncthreads();
+    if (*(volatile uint32_t*)&sm.abort_flag) {
+        for (int it = 0; it < 200; ++it) __nanosleep(1000);
+    }
+    if constexpr (PARTS > 1) cluster_arrive_wait();              // no CTA leaves before what others send it has arrived
+}
+// tokens of a step, of one CTA; bytes of a tile
+template <int TOK> __host__ __device__ constexpr int run_tokens() { return kGroups * TOK; }
+template <typename T, int TOK> __host__ __device__ constexpr uint32_t tile_bytes() { return run_tokens<TOK>() * kSlab * sizeof(T); }
 }  // namespace
 
-// grid: clusters of PARTS CTAs, one per sequence and slab of 8 pieces of channels; the CTAs of a cluster take runs of
-// 16 TOK tokens in turn.
+struct RecurrenceMaps {
+    CUtensorMap r, g, x, dout, out;
+};
+
+// grid: clusters of PARTS CTAs, one per sequence and slab of 64 channels; the CTAs of a cluster take runs of 8 TOK tokens in turn.
 template <typename T, int TOK, int PARTS>
 __global__ void __launch_bounds__(kThreads, 4)
-    gated_recurrence_kernel(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ g, const float* __restrict__ rate,
-                            const float* state_in, T* __restrict__ out, float* state_out, int N, int C, int slabs) {
-    constexpr int V = Piece<T>::V, P2 = V / 2, kRun = kGroups * TOK;
-    extern __shared__ uint4 stage[];                             // [2][3][TOK][kThreads]
-    __shared__ Joins<P2, PARTS> sm;
+    gated_recurrence_kernel(const __grid_constant__ RecurrenceMaps maps, const float* __restrict__ rate, const float* state_in,
+                            T* __restrict__ out, float* state_out, unsigned int* err, int N, int C, int slabs) {
+    constexpr int kRun = run_tokens<TOK>();
+    constexpr uint32_t kTile = tile_bytes<T, TOK>(), kRow = kSlab * sizeof(T);
+    extern __shared__ __align__(128) uint8_t stage[];            // [2][r, g, x][kRun][kSlab]
+    __shared__ Shared<PARTS> sm;
+    begin(sm);
     enter_dependent();
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & (kLanes - 1), group = tid / kLanes;
     const int rank = PARTS > 1 ? (int)cluster_rank() : 0;
-    const int work = blockIdx.x / PARTS, b = work / slabs;
-    const int c0 = (work - b * slabs) * (kLanes * V) + (lane & (kLanes - 1)) * V;
+    const int work = blockIdx.x / PARTS, b = work / slabs, slab0 = (work - b * slabs) * kSlab, c0 = slab0 + lane * kV;
     const bool mine = c0 < C;
-    const size_t base = (size_t)b * N * C + (mine ? c0 : 0);
-    const int group = tid / kLanes;
     const int steps = (int)(((long long)N + kRun * PARTS - 1) / (kRun * PARTS));
 
-    pair nrate[P2], h[P2];
-#pragma unroll
-    for (int e = 0; e < P2; ++e) nrate[e] = h[e] = 0;
-    if (mine) {
-        load_f32<P2>(rate + c0, nrate);
-#pragma unroll
-        for (int e = 0; e < P2; ++e) nrate[e] = neg2(nrate[e]);
-        if (state_in) load_f32<P2>(state_in + (size_t)b * C + c0, h);
-    }
-    bool small = true;
-#pragma unroll
-    for (int e = 0; e < P2; ++e) {
-        const float2 f = split(nrate[e]);
-        small = small && f.x > -0.25f && f.y > -0.25f;
-    }
-    small = __all_sync(0xffffffffu, small);
-
-    auto first_token = [&](int s) { return (s * (long long)PARTS + rank) * kRun + group * TOK; };
     auto fetch = [&](int s) {
-        const long long t0 = first_token(s);
-        uint4* to = stage + (size_t)(s & 1) * 3 * TOK * kThreads + tid;
-#pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-            const bool in = mine && t0 + j < N;
-            const size_t at = base + (in ? (size_t)(t0 + j) * C : 0);
-            copy_async16(to + (0 * TOK + j) * kThreads, r + at, in);
-            copy_async16(to + (1 * TOK + j) * kThreads, g + at, in);
-            copy_async16(to + (2 * TOK + j) * kThreads, x + at, in);
-        }
+        uint8_t* to = stage + (s & 1) * 3 * kTile;
+        const int t0 = (int)((s * (long long)PARTS + rank) * kRun);
+        mbar_arrive_expect_tx(&sm.full[s & 1], 3 * kTile);
+        tma_load_3d(to, &maps.r, &sm.full[s & 1], slab0, t0, b);
+        tma_load_3d(to + kTile, &maps.g, &sm.full[s & 1], slab0, t0, b);
+        tma_load_3d(to + 2 * kTile, &maps.x, &sm.full[s & 1], slab0, t0, b);
     };
-    fetch(0);
-    copy_async_commit();
-    if constexpr (PARTS > 1) cluster_arrive_wait();              // every CTA of the cluster runs: its shared memory may be written
+    if (tid == 0) {
+        fetch(0);
+        if (steps > 1) fetch(1);
+    }
+    pair nrate[kP] = {0, 0}, h[kP] = {0, 0};
+    if (mine) {
+        load_f32<kP>(rate + c0, nrate);
+        nrate[0] = neg2(nrate[0]);
+        nrate[1] = neg2(nrate[1]);
+        if (state_in) load_f32<kP>(state_in + (size_t)b * C + c0, h);
+    }
+    const bool small = all_small(nrate);
+    T* const to = out + (size_t)b * N * C + c0;
+    bool ok = true;
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch(s + 1);
-        copy_async_commit();
-        copy_async_wait<1>();
-        const uint4* from = stage + (size_t)(s & 1) * 3 * TOK * kThreads + tid;
-        const long long t0 = first_token(s);
-        pair a[TOK][P2], u[TOK][P2];                             // a_t, m_t i_t x_t
+        ok = mbar_wait(&sm.full[s & 1], (s >> 1) & 1, &sm.abort_flag) && ok;
+        const uint8_t* from = stage + (s & 1) * 3 * kTile + group * TOK * kRow + lane * kV * sizeof(T);
+        const long long t0 = (s * (long long)PARTS + rank) * kRun + group * TOK;
+        pair a[TOK][kP], u[TOK][kP];                             // a_t, m_t i_t x_t
         auto load = [&](auto small_tag) {
             constexpr bool SMALL = decltype(small_tag)::value;
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
-                pair rv[P2], gv[P2], xv[P2];
-                Piece<T>::unpack(from[(0 * TOK + j) * kThreads], rv);
-                Piece<T>::unpack(from[(1 * TOK + j) * kThreads], gv);
-                Piece<T>::unpack(from[(2 * TOK + j) * kThreads], xv);
-                const bool in = t0 + j < N;
+                pair rv[kP], gv[kP], xv[kP];
+                gate4<T>(from + j * kRow, rv);
+                gate4<T>(from + kTile + j * kRow, gv);
+                values4<T>(from + 2 * kTile + j * kRow, xv);
 #pragma unroll
-                for (int e = 0; e < P2; ++e) {
+                for (int e = 0; e < kP; ++e) {
                     const pair er = one_plus_exp_neg(rv[e]), eg = one_plus_exp_neg(gv[e]), q = rcp2(mul2(er, eg));
                     const pair p = exp_less_one<SMALL>(mul2(nrate[e], mul2(q, eg)));
                     const float2 m2 = split(one_less_square(p));
                     u[j][e] = mul2(make(root(m2.x), root(m2.y)), mul2(mul2(q, er), xv[e]));
-                    a[j][e] = in ? add2(p, both(1.f)) : both(1.f);   // (behind the sequence: nothing happens)
+                    a[j][e] = add2(p, both(1.f));
                 }
             }
         };
         if (small) load(std::true_type{});
         else load(std::false_type{});
-        pair A[P2], H[P2], first[P2];
+        if (t0 + TOK > N) {                                      // behind the sequence nothing happens (x reads as 0 there)
 #pragma unroll
-        for (int e = 0; e < P2; ++e) {
+            for (int j = 0; j < TOK; ++j)
+#pragma unroll
+                for (int e = 0; e < kP; ++e)
+                    if (t0 + j >= N) a[j][e] = both(1.f);
+        }
+        pair A[kP], H[kP], first[kP];
+#pragma unroll
+        for (int e = 0; e < kP; ++e) {
             A[e] = a[0][e];
             H[e] = u[0][e];
 #pragma unroll
@@ -314,99 +356,83 @@ __global__ void __launch_bounds__(kThreads, 4)
                 A[e] = mul2(A[e], a[j][e]);
             }
         }
-        join<P2, PARTS>(sm, s & 1, rank, A, H, h, first);
+        ok = join<PARTS>(sm, s, rank, A, H, h, first, [&] {      // (the stage has been read)
+            if (tid == 0 && s + 2 < steps) fetch(s + 2);
+        }) && ok;
 #pragma unroll
         for (int j = 0; j < TOK; ++j) {
 #pragma unroll
-            for (int e = 0; e < P2; ++e) first[e] = fma2(a[j][e], first[e], u[j][e]);
-            if (mine && t0 + j < N) __stcs(reinterpret_cast<uint4*>(out + base + (size_t)(t0 + j) * C), Piece<T>::pack(first));
+            for (int e = 0; e < kP; ++e) first[e] = fma2(a[j][e], first[e], u[j][e]);
+            if (mine && t0 + j < N) write4<T>(to + (size_t)(t0 + j) * C, first);
         }
     }
-    if (state_out && mine && rank == 0 && tid < kLanes) store_f32<P2>(state_out + (size_t)b * C + c0, h);
+    if (state_out && mine && rank == 0 && group == 0) store_f32<kP>(state_out + (size_t)b * C + c0, h);
+    finish(sm, ok, err);
 }
 
-// The scan from the last token to the first: "time" tau = N - 1 - t.  part: [sequences x PARTS][C] sums of drate
+// The scan from the last token to the first: "time" tau = N - 1 - t, tiles lie with the last token of a run below.  part: [sequences
+// x PARTS][C] sums of drate
 template <typename T, int TOK, int PARTS>
 __global__ void __launch_bounds__(kThreads, 4)
-    gated_recurrence_backward_kernel(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ g,
-                                     const float* __restrict__ rate, const float* __restrict__ state_in, const T* __restrict__ out,
-                                     const T* __restrict__ dout, const float* dstate_out, T* __restrict__ dx, T* __restrict__ dr,
-                                     T* __restrict__ dg, float* __restrict__ part, float* dstate_in, int N, int C, int slabs) {
-    constexpr int V = Piece<T>::V, P2 = V / 2, kRun = kGroups * TOK;
-    extern __shared__ uint4 stage[];                             // [2][5][TOK][kThreads]
-    __shared__ Joins<P2, PARTS> sm;
-    __shared__ pair sums[kWarps][P2][kLanes];
+    gated_recurrence_backward_kernel(const __grid_constant__ RecurrenceMaps maps, const float* __restrict__ rate,
+                                     const float* __restrict__ state_in, const float* dstate_out, T* __restrict__ dx, T* __restrict__ dr,
+                                     T* __restrict__ dg, float* __restrict__ part, float* dstate_in, unsigned int* err, int N, int C, int slabs) {
+    constexpr int kRun = run_tokens<TOK>();
+    constexpr uint32_t kTile = tile_bytes<T, TOK>(), kRow = kSlab * sizeof(T);
+    extern __shared__ __align__(128) uint8_t stage[];            // [3][r, dout, g, x, out of the token before][kRun][kSlab]
+    __shared__ Shared<PARTS> sm;
+    begin(sm);
     enter_dependent();
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & (kLanes - 1), group = tid / kLanes;
     const int rank = PARTS > 1 ? (int)cluster_rank() : 0;
-    const int work = blockIdx.x / PARTS, b = work / slabs;
-    const int c0 = (work - b * slabs) * (kLanes * V) + (lane & (kLanes - 1)) * V;
+    const int work = blockIdx.x / PARTS, b = work / slabs, slab0 = (work - b * slabs) * kSlab, c0 = slab0 + lane * kV;
     const bool mine = c0 < C;
-    const size_t base = (size_t)b * N * C + (mine ? c0 : 0);
-    const int group = tid / kLanes;
     const int steps = (int)(((long long)N + kRun * PARTS - 1) / (kRun * PARTS));
 
-    pair nrate[P2], E[P2], drate[P2];
-#pragma unroll
-    for (int e = 0; e < P2; ++e) nrate[e] = E[e] = drate[e] = 0;
-    if (mine) {
-        load_f32<P2>(rate + c0, nrate);
-#pragma unroll
-        for (int e = 0; e < P2; ++e) nrate[e] = neg2(nrate[e]);
-        if (dstate_out) load_f32<P2>(dstate_out + (size_t)b * C + c0, E);
-    }
-    bool small = true;
-#pragma unroll
-    for (int e = 0; e < P2; ++e) {
-        const float2 f = split(nrate[e]);
-        small = small && f.x > -0.25f && f.y > -0.25f;
-    }
-    small = __all_sync(0xffffffffu, small);
-
-    auto last_token = [&](int s) { return N - 1 - ((s * (long long)PARTS + rank) * kRun + group * TOK); };
     auto fetch = [&](int s) {
-        const long long t0 = last_token(s);
-        uint4* to = stage + (size_t)(s & 1) * 5 * TOK * kThreads + tid;
-#pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-            const bool in = mine && t0 - j >= 0, prev = mine && t0 - j >= 1;
-            const size_t at = base + (in ? (size_t)(t0 - j) * C : 0);
-            copy_async16(to + (0 * TOK + j) * kThreads, r + at, in);
-            copy_async16(to + (1 * TOK + j) * kThreads, dout + at, in);
-            copy_async16(to + (2 * TOK + j) * kThreads, g + at, in);
-            copy_async16(to + (3 * TOK + j) * kThreads, x + at, in);
-            copy_async16(to + (4 * TOK + j) * kThreads, out + (prev ? at - C : base), prev);
-        }
+        const int st = s % 3;
+        uint8_t* to = stage + st * 5 * kTile;
+        const int t0 = (int)(N - (s * (long long)PARTS + rank + 1) * kRun);       // (may be below 0: rows before the sequence read as 0)
+        mbar_arrive_expect_tx(&sm.full[st], 5 * kTile);
+        tma_load_3d(to, &maps.r, &sm.full[st], slab0, t0, b);
+        tma_load_3d(to + kTile, &maps.dout, &sm.full[st], slab0, t0, b);
+        tma_load_3d(to + 2 * kTile, &maps.g, &sm.full[st], slab0, t0, b);
+        tma_load_3d(to + 3 * kTile, &maps.x, &sm.full[st], slab0, t0, b);
+        tma_load_3d(to + 4 * kTile, &maps.out, &sm.full[st], slab0, t0 - 1, b);
     };
-    fetch(0);
-    copy_async_commit();
-    if constexpr (PARTS > 1) cluster_arrive_wait();              // every CTA of the cluster runs: its shared memory may be written
+    if (tid == 0) {
+        fetch(0);
+        if (steps > 1) fetch(1);
+    }
+    pair nrate[kP] = {0, 0}, E[kP] = {0, 0}, drate[kP] = {0, 0};
+    if (mine) {
+        load_f32<kP>(rate + c0, nrate);
+        nrate[0] = neg2(nrate[0]);
+        nrate[1] = neg2(nrate[1]);
+        if (dstate_out) load_f32<kP>(dstate_out + (size_t)b * C + c0, E);
+    }
+    const bool small = all_small(nrate);
+    const size_t base = (size_t)b * N * C + c0;
+    bool ok = true;
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch(s + 1);
-        copy_async_commit();
-        copy_async_wait<1>();
-        const uint4* from = stage + (size_t)(s & 1) * 5 * TOK * kThreads + tid;
-        const long long t0 = last_token(s);
-        pair p[TOK][P2], sg[TOK][P2];                            // a_t - 1, sigmoid(r_t)
-        pair A[P2], H[P2], first[P2];
-#pragma unroll
-        for (int e = 0; e < P2; ++e) {
-            A[e] = both(1.f);
-            H[e] = 0;
-        }
+        ok = mbar_wait(&sm.full[s % 3], (s / 3) & 1, &sm.abort_flag) && ok;
+        // the thread's tokens t0, t0 - 1, ...
+        const uint8_t* from = stage + (s % 3) * 5 * kTile + (kRun - 1 - group * TOK) * kRow + lane * kV * sizeof(T);
+        const long long t0 = N - 1 - ((s * (long long)PARTS + rank) * kRun + group * TOK);
+        pair p[TOK][kP], sg[TOK][kP];                            // a_t - 1, sigmoid(r_t)
+        pair A[kP] = {both(1.f), both(1.f)}, H[kP] = {0, 0}, first[kP];
         auto load = [&](auto small_tag) {
             constexpr bool SMALL = decltype(small_tag)::value;
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
-                pair rv[P2], dv[P2];
-                Piece<T>::unpack(from[(0 * TOK + j) * kThreads], rv);
-                Piece<T>::unpack(from[(1 * TOK + j) * kThreads], dv);
-                const bool in = t0 - j >= 0;
+                pair rv[kP], dv[kP];
+                gate4<T>(from - j * kRow, rv);
+                values4<T>(from + kTile - j * kRow, dv);
 #pragma unroll
-                for (int e = 0; e < P2; ++e) {
+                for (int e = 0; e < kP; ++e) {
                     sg[j][e] = rcp2(one_plus_exp_neg(rv[e]));
-                    const pair q = exp_less_one<SMALL>(mul2(nrate[e], sg[j][e]));
-                    p[j][e] = in ? q : 0;                        // (before the sequence: nothing happens)
+                    p[j][e] = exp_less_one<SMALL>(mul2(nrate[e], sg[j][e]));
+                    if (t0 - j < 0) p[j][e] = 0;                 // (before the sequence nothing happens)
                     const pair a = add2(p[j][e], both(1.f));
                     H[e] = mul2(a, add2(H[e], dv[e]));
                     A[e] = mul2(A[e], a);
@@ -415,103 +441,101 @@ __global__ void __launch_bounds__(kThreads, 4)
         };
         if (small) load(std::true_type{});
         else load(std::false_type{});
-        join<P2, PARTS>(sm, s & 1, rank, A, H, E, first);
+        ok = join<PARTS>(sm, s, rank, A, H, E, first, [&] {      // (the stage of the step before has been read)
+            if (tid == 0 && s + 2 < steps) fetch(s + 2);
+        }) && ok;
 #pragma unroll
         for (int j = 0; j < TOK; ++j) {
-            pair dv[P2], gv[P2], xv[P2], hv[P2], ox[P2], orr[P2], og[P2];
-            Piece<T>::unpack(from[(1 * TOK + j) * kThreads], dv);
-            Piece<T>::unpack(from[(2 * TOK + j) * kThreads], gv);
-            Piece<T>::unpack(from[(3 * TOK + j) * kThreads], xv);
-            Piece<T>::unpack(from[(4 * TOK + j) * kThreads], hv);
-            if (mine && t0 - j == 0 && state_in) load_f32<P2>(state_in + (size_t)b * C + c0, hv);
+            pair dv[kP], gv[kP], xv[kP], hv[kP], ox[kP], orr[kP], og[kP];
+            values4<T>(from + kTile - j * kRow, dv);
+            gate4<T>(from + 2 * kTile - j * kRow, gv);
+            values4<T>(from + 3 * kTile - j * kRow, xv);
+            values4<T>(from + 4 * kTile - j * kRow, hv);
             const bool in = mine && t0 - j >= 0;
+            if (in && t0 - j == 0 && state_in) load_f32<kP>(state_in + (size_t)b * C + c0, hv);
 #pragma unroll
-            for (int e = 0; e < P2; ++e) {
+            for (int e = 0; e < kP; ++e) {
                 const pair G = add2(dv[e], first[e]), a = add2(p[j][e], both(1.f));
                 const pair i = rcp2(one_plus_exp_neg(gv[e]));
                 const pair m2 = one_less_square(p[j][e]);
                 const float2 f = split(m2);
                 // 1 / m; where nothing decays (m = 0) a number so large that products with it stay finite
                 const pair im = make(rroot(max_nan(f.x, 1e-36f)), rroot(max_nan(f.y, 1e-36f)));
-                const pair Gi = mul2(G, i), Gmi = mul2(Gi, mul2(m2, im));
-                ox[e] = Gmi;
-                og[e] = mul2(mul2(Gmi, xv[e]), fma2(neg2(i), both(1.f), both(1.f)));
-                // dlog a = a (G h - a / m G i x)
-                const pair dla = mul2(a, fma2(G, hv[e], neg2(mul2(mul2(a, im), mul2(Gi, xv[e])))));
-                const pair ds = mul2(dla, sg[j][e]);
-                if (in) drate[e] = add2(drate[e], neg2(ds));
-                orr[e] = mul2(mul2(nrate[e], ds), fma2(neg2(sg[j][e]), both(1.f), both(1.f)));
+                const pair Gi = mul2(G, i), Gix = mul2(Gi, xv[e]), m = mul2(m2, im);
+                ox[e] = mul2(Gi, m);
+                og[e] = mul2(mul2(Gix, m), fma2(i, both(-1.f), both(1.f)));
+                // -dlog a = a (a / m G i x - G h)
                 first[e] = mul2(a, G);
+                const pair nd = fma2(mul2(a, a), mul2(im, Gix), neg2(mul2(first[e], hv[e])));
+                const pair ds = mul2(nd, sg[j][e]);
+                if (in) drate[e] = add2(drate[e], ds);
+                orr[e] = mul2(mul2(nrate[e], ds), fma2(sg[j][e], both(1.f), both(-1.f)));
             }
             if (in) {
                 const size_t at = base + (size_t)(t0 - j) * C;
-                __stcs(reinterpret_cast<uint4*>(dx + at), Piece<T>::pack(ox));
-                __stcs(reinterpret_cast<uint4*>(dr + at), Piece<T>::pack(orr));
-                __stcs(reinterpret_cast<uint4*>(dg + at), Piece<T>::pack(og));
+                write4<T>(dx + at, ox);
+                write4<T>(dr + at, orr);
+                write4<T>(dg + at, og);
             }
         }
     }
-    if (dstate_in && mine && rank == 0 && tid < kLanes) store_f32<P2>(dstate_in + (size_t)b * C + c0, E);
+    if (dstate_in && mine && rank == 0 && group == 0) store_f32<kP>(dstate_in + (size_t)b * C + c0, E);
     // drate over the CTA's tokens: the warp's groups, then the warps
 #pragma unroll
-    for (int e = 0; e < P2; ++e) {
-#pragma unroll
-        for (int d = kLanes; d < 32; d *= 2) drate[e] = add2(drate[e], __shfl_xor_sync(0xffffffffu, drate[e], d));
-        if (lane < kLanes) sums[tid >> 5][e][lane] = drate[e];
+    for (int e = 0; e < kP; ++e) {
+        drate[e] = add2(drate[e], __shfl_xor_sync(0xffffffffu, drate[e], kLanes));
+        if ((tid & 31) < kLanes) sm.sums[tid >> 5][e][lane] = drate[e];
     }
     __syncthreads();
-    if (tid < kLanes && mine) {
-        pair t[P2];
+    if (group == 0 && mine) {
+        pair t[kP];
 #pragma unroll
-        for (int e = 0; e < P2; ++e) t[e] = add2(add2(sums[0][e][tid], sums[1][e][tid]), add2(sums[2][e][tid], sums[3][e][tid]));
-        store_f32<P2>(part + ((size_t)b * PARTS + rank) * C + c0, t);
+        for (int e = 0; e < kP; ++e) t[e] = add2(add2(sm.sums[0][e][lane], sm.sums[1][e][lane]), add2(sm.sums[2][e][lane], sm.sums[3][e][lane]));
+        store_f32<kP>(part + ((size_t)b * PARTS + rank) * C + c0, t);
     }
+    finish(sm, ok, err);
 }
 
-// One token: 16 bytes of io values per thread
+// One token: 4 channels per thread
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-    gated_recurrence_step_kernel(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ g, const float* __restrict__ rate,
-                                 const float* state_in, T* __restrict__ out, float* state_out, long long pieces, int per_row) {
-    constexpr int V = Piece<T>::V, P2 = V / 2;
+    gated_recurrence_step_kernel(const Tokens x, const Tokens r, const Tokens g, const float* __restrict__ rate, const float* state_in,
+                                 T* __restrict__ out, float* state_out, long long pieces, int per_row) {
     enter_dependent();
     const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
     if (i >= pieces) return;
-    const int c0 = (int)(i % per_row) * V;
-    const uint4 ru = __ldcs(reinterpret_cast<const uint4*>(r) + i), gu = __ldcs(reinterpret_cast<const uint4*>(g) + i),
-                xu = __ldcs(reinterpret_cast<const uint4*>(x) + i);
-    pair h[P2], nrate[P2], rv[P2], gv[P2], xv[P2];
+    const long long b = i / per_row;
+    const int c0 = (int)(i - b * per_row) * kV;
+    using Raw = typename Four<T>::Raw;
+    auto at = [&](const Tokens& t) { return __ldcs(reinterpret_cast<const Raw*>(static_cast<const T*>(t.data) + b * t.batch_stride + c0)); };
+    const Raw ru = at(r), gu = at(g), xu = at(x);
+    pair h[kP] = {0, 0}, nrate[kP], rv[kP], gv[kP], xv[kP];
+    if (state_in) load_f32<kP>(state_in + i * kV, h);
+    load_f32<kP>(rate + c0, nrate);
+    Four<T>::values(Four<T>::gate(ru), rv);
+    Four<T>::values(Four<T>::gate(gu), gv);
+    Four<T>::values(xu, xv);
 #pragma unroll
-    for (int e = 0; e < P2; ++e) h[e] = 0;
-    if (state_in) load_f32<P2>(state_in + i * V, h);
-    load_f32<P2>(rate + c0, nrate);
-    Piece<T>::unpack(ru, rv);
-    Piece<T>::unpack(gu, gv);
-    Piece<T>::unpack(xu, xv);
-#pragma unroll
-    for (int e = 0; e < P2; ++e) {
+    for (int e = 0; e < kP; ++e) {
         const pair er = one_plus_exp_neg(rv[e]), eg = one_plus_exp_neg(gv[e]), q = rcp2(mul2(er, eg));
         const pair p = exp_less_one<false>(mul2(neg2(nrate[e]), mul2(q, eg)));
         const float2 m2 = split(one_less_square(p));
         h[e] = fma2(add2(p, both(1.f)), h[e], mul2(make(root(m2.x), root(m2.y)), mul2(mul2(q, er), xv[e])));
     }
-    if (state_out) store_f32<P2>(state_out + i * V, h);
-    __stcs(reinterpret_cast<uint4*>(out) + i, Piece<T>::pack(h));
+    if (state_out) store_f32<kP>(state_out + i * kV, h);
+    write4<T>(out + i * kV, h);
 }
 
 namespace {
-constexpr int kTok = 4;
+constexpr int kTokForward = 8, kTokBackward = 4;
 
 // CTAs per sequence and slab
-int parts_for(long long units, int N) {
+int parts_for(long long units, int N, int tok) {
     int parts = 1;
-    while (parts < 8 && units * parts < 4 * kSMs && (long long)parts * kGroups * kTok < N) parts *= 2;
+    while (parts < 8 && units * parts < 4 * kSMs && (long long)parts * kGroups * tok < N) parts *= 2;
     return parts;
 }
-int slabs_of(int C, based_dtype io) {
-    const int per = kLanes * (io == BASED_F32 ? 4 : 8);
-    return (int)(((long long)C + per - 1) / per);
-}
+int slabs_of(int C) { return (int)(((long long)C + kSlab - 1) / kSlab); }
 template <typename K> cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[64]) {
     int dev = 0;
     const cudaError_t e = cudaGetDevice(&dev);
@@ -529,43 +553,56 @@ template <typename F> based_status with_parts(int parts, F f) {
         default: return f(std::integral_constant<int, 8>{});
     }
 }
-template <int TOK> constexpr size_t stage_bytes(int arrays) { return (size_t)2 * arrays * TOK * kThreads * 16; }
 
 template <typename T>
-based_status forward_t(const void* x, const void* r, const void* g, const float* rate, const float* state_in, void* out,
-                       float* state_out, int B, int N, int C, based_dtype io, cudaStream_t stream) {
-    const int slabs = slabs_of(C, io);
-    return with_parts(parts_for((long long)B * slabs, N), [&](auto tag) {
+based_status forward_t(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, void* out,
+                       float* state_out, int B, int N, int C, cudaStream_t stream) {
+    constexpr bool f32 = sizeof(T) == 4;
+    const int slabs = slabs_of(C);
+    RecurrenceMaps maps;
+    unsigned int* err = nullptr;
+    constexpr int run = run_tokens<kTokForward>();
+    if (!make_tokens_map(&maps.r, r, f32, B, N, C, kSlab, run) || !make_tokens_map(&maps.g, g, f32, B, N, C, kSlab, run) ||
+        !make_tokens_map(&maps.x, x, f32, B, N, C, kSlab, run) || error_word_ptr(&err) != BASED_OK)
+        return BASED_ERR_CUDA;
+    maps.dout = maps.out = maps.x;
+    return with_parts(parts_for((long long)B * slabs, N, kTokForward), [&](auto tag) {
         constexpr int PARTS = decltype(tag)::value;
         static std::atomic<bool> ready[64];
-        constexpr size_t smem = stage_bytes<kTok>(3);
-        auto kernel = gated_recurrence_kernel<T, kTok, PARTS>;
+        constexpr size_t smem = 2 * 3 * tile_bytes<T, kTokForward>();
+        auto kernel = gated_recurrence_kernel<T, kTokForward, PARTS>;
         cudaError_t e = allow_smem(kernel, smem, ready);
         if (e == cudaSuccess)
-            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, true, stream,
-                          static_cast<const T*>(x), static_cast<const T*>(r), static_cast<const T*>(g), rate, state_in,
-                          static_cast<T*>(out), state_out, N, C, slabs);
+            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, true, stream, maps, rate,
+                          state_in, static_cast<T*>(out), state_out, err, N, C, slabs);
         note_launch();
         const based_status st = check_launch("gated_recurrence_kernel");
         return e == cudaSuccess ? st : BASED_ERR_CUDA;
     });
 }
 template <typename T>
-based_status backward_t(const void* x, const void* r, const void* g, const float* rate, const float* state_in, const void* out,
-                        const void* dout, const float* dstate_out, void* dx, void* dr, void* dg, float* drate, float* dstate_in,
-                        int B, int N, int C, float* part, based_dtype io, cudaStream_t stream) {
-    const int slabs = slabs_of(C, io), parts = parts_for((long long)B * slabs, N);
+based_status backward_t(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, const Tokens& out,
+                        const Tokens& dout, const float* dstate_out, void* dx, void* dr, void* dg, float* drate, float* dstate_in, int B,
+                        int N, int C, float* part, cudaStream_t stream) {
+    constexpr bool f32 = sizeof(T) == 4;
+    const int slabs = slabs_of(C), parts = parts_for((long long)B * slabs, N, kTokBackward);
+    RecurrenceMaps maps;
+    unsigned int* err = nullptr;
+    constexpr int run = run_tokens<kTokBackward>();
+    if (!make_tokens_map(&maps.r, r, f32, B, N, C, kSlab, run) || !make_tokens_map(&maps.g, g, f32, B, N, C, kSlab, run) ||
+        !make_tokens_map(&maps.x, x, f32, B, N, C, kSlab, run) || !make_tokens_map(&maps.out, out, f32, B, N, C, kSlab, run) ||
+        !make_tokens_map(&maps.dout, dout, f32, B, N, C, kSlab, run) || error_word_ptr(&err) != BASED_OK)
+        return BASED_ERR_CUDA;
     const based_status st = with_parts(parts, [&](auto tag) {
         constexpr int PARTS = decltype(tag)::value;
         static std::atomic<bool> ready[64];
-        constexpr size_t smem = stage_bytes<kTok>(5);
-        auto kernel = gated_recurrence_backward_kernel<T, kTok, PARTS>;
+        constexpr size_t smem = 3 * 5 * tile_bytes<T, kTokBackward>();
+        auto kernel = gated_recurrence_backward_kernel<T, kTokBackward, PARTS>;
         cudaError_t e = allow_smem(kernel, smem, ready);
         if (e == cudaSuccess)
-            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, true, stream,
-                          static_cast<const T*>(x), static_cast<const T*>(r), static_cast<const T*>(g), rate, state_in,
-                          static_cast<const T*>(out), static_cast<const T*>(dout), dstate_out, static_cast<T*>(dx),
-                          static_cast<T*>(dr), static_cast<T*>(dg), part, dstate_in, N, C, slabs);
+            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, true, stream, maps, rate,
+                          state_in, dstate_out, static_cast<T*>(dx), static_cast<T*>(dr), static_cast<T*>(dg), part, dstate_in, err, N, C,
+                          slabs);
         note_launch();
         const based_status s = check_launch("gated_recurrence_backward_kernel");
         return e == cudaSuccess ? s : BASED_ERR_CUDA;
@@ -575,27 +612,26 @@ based_status backward_t(const void* x, const void* r, const void* g, const float
 }
 }  // namespace
 
-long long gated_recurrence_blocks(int B, int N, int C, based_dtype io) {
-    const long long units = (long long)B * slabs_of(C, io);
-    return units * parts_for(units, N);
+long long gated_recurrence_blocks(int B, int N, int C) {
+    const long long units = (long long)B * slabs_of(C);
+    return units * (N > 1 ? parts_for(units, N, kTokBackward) : 1);
 }
-size_t gated_recurrence_backward_bytes(int B, int N, int C, based_dtype io) {
-    return (size_t)B * parts_for((long long)B * slabs_of(C, io), N) * C * sizeof(float);
+size_t gated_recurrence_backward_bytes(int B, int N, int C) {
+    return (size_t)B * parts_for((long long)B * slabs_of(C), N, kTokBackward) * C * sizeof(float);
 }
 
-based_status launch_gated_recurrence(const void* x, const void* r, const void* g, const float* rate, const float* state_in, void* out,
+based_status launch_gated_recurrence(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, void* out,
                                      float* state_out, int B, int N, int C, based_dtype io, cudaStream_t stream) {
     if (N > 1) {
-        return io == BASED_F32 ? forward_t<float>(x, r, g, rate, state_in, out, state_out, B, N, C, io, stream)
-                               : forward_t<__nv_bfloat16>(x, r, g, rate, state_in, out, state_out, B, N, C, io, stream);
+        return io == BASED_F32 ? forward_t<float>(x, r, g, rate, state_in, out, state_out, B, N, C, stream)
+                               : forward_t<__nv_bfloat16>(x, r, g, rate, state_in, out, state_out, B, N, C, stream);
     }
     auto step = [&](auto zero) {
         using T = decltype(zero);
-        const int per_row = C / Piece<T>::V;
+        const int per_row = C / kV;
         const long long pieces = (long long)B * per_row;
         return launch_ex(gated_recurrence_step_kernel<T>, dim3((unsigned)((pieces + kThreads - 1) / kThreads)), dim3(kThreads), 0, 1,
-                         true, stream, static_cast<const T*>(x), static_cast<const T*>(r), static_cast<const T*>(g), rate, state_in,
-                         static_cast<T*>(out), state_out, pieces, per_row);
+                         true, stream, x, r, g, rate, state_in, static_cast<T*>(out), state_out, pieces, per_row);
     };
     const cudaError_t e = io == BASED_F32 ? step(0.f) : step(__nv_bfloat16{});
     note_launch();
@@ -603,14 +639,14 @@ based_status launch_gated_recurrence(const void* x, const void* r, const void* g
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
 }
 
-based_status launch_gated_recurrence_backward(const void* x, const void* r, const void* g, const float* rate, const float* state_in,
-                                              const void* out, const void* dout, const float* dstate_out, void* dx, void* dr, void* dg,
+based_status launch_gated_recurrence_backward(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in,
+                                              const Tokens& out, const Tokens& dout, const float* dstate_out, void* dx, void* dr, void* dg,
                                               float* drate, float* dstate_in, int B, int N, int C, float* part, based_dtype io,
                                               cudaStream_t stream) {
     return io == BASED_F32 ? backward_t<float>(x, r, g, rate, state_in, out, dout, dstate_out, dx, dr, dg, drate, dstate_in, B, N, C,
-                                               part, io, stream)
+                                               part, stream)
                            : backward_t<__nv_bfloat16>(x, r, g, rate, state_in, out, dout, dstate_out, dx, dr, dg, drate, dstate_in, B,
-                                                       N, C, part, io, stream);
+                                                       N, C, part, stream);
 }
 
 }  // namespace based

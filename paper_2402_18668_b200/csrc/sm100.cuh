@@ -6,6 +6,8 @@
 #include <cuda.h>
 #include <stdint.h>
 
+#include "based.h"
+
 namespace based {
 
 // tensor map of a bf16 [BH][L][width] array with a [1][box_rows][box_w] box (box_w may exceed width: the rest is
@@ -17,6 +19,10 @@ bool make_rows_map_bf16(CUtensorMap* m, const void* base, int BH, int L, int wid
 // head % H, row, head / H; H 0: make_rows_map_bf16 (one kind of map for both cost the backward calls up to 1 % there)
 bool make_head_rows_map_bf16(CUtensorMap* m, const void* base, int BH, int H, int L, int width, int box_w, int box_rows,
                              CUtensorMapSwizzle sw);
+
+// tensor map of [B][N][C] bf16 or fp32 values with strides (elements; multiples of 16 bytes where there is more than one to step
+// over), [1][box_n][box_c] a box, rows side by side in shared memory
+bool make_tokens_map(CUtensorMap* m, const based_tokens& t, bool f32, int B, int N, int C, int box_c, int box_n);
 
 namespace sm100 {
 

@@ -26,12 +26,12 @@ EncodeTiledFn encode_fn() {
 }  // namespace
 
 static bool encode_map(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
-                       CUtensorMapSwizzle sw) {
+                       CUtensorMapSwizzle sw, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
     EncodeTiledFn enc = encode_fn();
     if (!enc) return false;
     cuuint32_t estr[4] = {1, 1, 1, 1};
     auto encode = [&] {
-        return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr,
+        return enc(m, type, rank, const_cast<void*>(base), dims, strides, box, estr,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
@@ -48,6 +48,16 @@ bool make_rows_map_bf16(CUtensorMap* m, const void* base, int BH, int L, int wid
     const cuuint64_t strides[2] = {(cuuint64_t)width * 2, (cuuint64_t)L * width * 2};
     const cuuint32_t box[3] = {(cuuint32_t)box_w, (cuuint32_t)box_rows, 1};
     return encode_map(m, base, 3, dims, strides, box, sw);
+}
+
+bool make_tokens_map(CUtensorMap* m, const based_tokens& t, bool f32, int B, int N, int C, int box_c, int box_n) {
+    const cuuint64_t e = f32 ? 4 : 2, row = ((cuuint64_t)C * e + 15) / 16 * 16;
+    const cuuint64_t token = N > 1 ? (cuuint64_t)t.token_stride * e : row, batch = B > 1 ? (cuuint64_t)t.batch_stride * e : token * (cuuint64_t)N;
+    const cuuint64_t dims[3] = {(cuuint64_t)C, (cuuint64_t)N, (cuuint64_t)B};
+    const cuuint64_t strides[2] = {token, batch};
+    const cuuint32_t box[3] = {(cuuint32_t)box_c, (cuuint32_t)box_n, 1};
+    return encode_map(m, t.data, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE,
+                      f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
 }
 
 bool make_head_rows_map_bf16(CUtensorMap* m, const void* base, int BH, int H, int L, int width, int box_w, int box_rows,

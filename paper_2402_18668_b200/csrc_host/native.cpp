@@ -489,6 +489,18 @@ int dim(const Tensor& t, int i) {
     if (n > 0x7fffffff) value_error("a dimension of 2^31 or more");
     return static_cast<int>(n);
 }
+// overlap() for tensors with strides: the whole stretch from the first element to the last
+bool stretches_overlap(const Tensor& a, const Tensor& b) {
+    auto end = [](const Tensor& t) {
+        int64_t last = 0;
+        for (int64_t i = 0; i < t.dim(); ++i) {
+            if (t.size(i) == 0) return static_cast<const char*>(t.const_data_ptr());
+            last += (t.size(i) - 1) * t.stride(i);
+        }
+        return static_cast<const char*>(t.const_data_ptr()) + (last + 1) * static_cast<int64_t>(t.element_size());
+    };
+    return static_cast<const char*>(a.const_data_ptr()) < end(b) && static_cast<const char*>(b.const_data_ptr()) < end(a);
+}
 // Every tensor of a call lies on one device, and what it writes overlaps nothing else of the call.  An undefined tensor is
 // passed over.
 void check_places(std::initializer_list<const Tensor*> in, std::initializer_list<const Tensor*> out) {
@@ -501,9 +513,9 @@ void check_places(std::initializer_list<const Tensor*> in, std::initializer_list
         if (!(*o)->defined()) continue;
         same(**o);
         for (const Tensor* t : in)
-            if (t->defined() && overlap(**o, *t)) value_error("an output overlaps an input");
+            if (t->defined() && stretches_overlap(**o, *t)) value_error("an output overlaps an input");
         for (auto p = out.begin(); p != o; ++p)
-            if ((*p)->defined() && overlap(**o, **p)) value_error("two outputs overlap");
+            if ((*p)->defined() && stretches_overlap(**o, **p)) value_error("two outputs overlap");
     }
 }
 // None: the current stream of the tensors' device
@@ -533,6 +545,16 @@ void check_like(const Tensor& t, const Tensor& like, const char* name, const cha
     if (t.defined() && (t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type()))
         value_error(std::string(name) + " must have the shape and dtype of " + whose);
 }
+// [B,N,C], or [B,C], as the library takes it: channels side by side, anything else evenly spaced
+const Tensor& tokens(PyObject* o, const char* name) {
+    const Tensor& t = tensor(o);
+    if (!t.defined()) throw TypeFault(std::string(name) + " is required");
+    if (!t.is_cuda()) value_error("libbased takes CUDA tensors only (there is no CPU path)");
+    if (t.dim() < 2 || t.dim() > 3) value_error(std::string(name) + " must be [B,N,C] (or [B,C] for one token)");
+    if (t.size(-1) > 1 && t.stride(-1) != 1) value_error(std::string(name) + " must have its channels side by side");
+    return t;
+}
+based_tokens as_tokens(const Tensor& t) { return {t.const_data_ptr(), t.stride(0), t.dim() == 3 ? t.stride(1) : t.size(-1)}; }
 void check_gates(const Tensor& x, const Tensor& r, const Tensor& g, const Tensor& rate) {
     check_like(r, x, "r", "x");
     check_like(g, x, "g", "x");
@@ -541,11 +563,11 @@ void check_gates(const Tensor& x, const Tensor& r, const Tensor& g, const Tensor
 Tensor recurrence_call(const Tensor& x, const Tensor& r, const Tensor& g, const Tensor& rate, const Tensor& in, Tensor out,
                        const Tensor& last, void* stream) {
     const bool step = x.dim() == 2;
-    if (!out.defined()) out = fresh(x);
+    if (!out.defined()) out = at::empty(x.sizes(), x.options());
     const int B = dim(x, 0), C = dim(x, static_cast<int>(x.dim()) - 1);
     const based_dtype io = dtype_code(x);
-    check(step ? based_gated_recurrence_step(cptr(x), cptr(r), cptr(g), f32(rate), f32(in), ptr(out), fptr(last), B, C, io, stream)
-               : based_gated_recurrence_forward(cptr(x), cptr(r), cptr(g), f32(rate), f32(in), ptr(out), fptr(last), B, dim(x, 1), C, io,
+    check(step ? based_gated_recurrence_step(as_tokens(x), as_tokens(r), as_tokens(g), f32(rate), f32(in), ptr(out), fptr(last), B, C, io, stream)
+               : based_gated_recurrence_forward(as_tokens(x), as_tokens(r), as_tokens(g), f32(rate), f32(in), ptr(out), fptr(last), B, dim(x, 1), C, io,
                                                 stream),
           step ? "based_gated_recurrence_step" : "based_gated_recurrence_forward");
     return out;
@@ -557,15 +579,16 @@ RecurrenceGradients recurrence_backward_call(const Tensor& x, const Tensor& r, c
     const int B = dim(x, 0), N = dim(x, 1), C = dim(x, 2);
     const based_dtype io = dtype_code(x);
     const Workspace ws(workspace, based_gated_recurrence_backward_workspace_bytes(B, N, C, io), x, stream);
-    RecurrenceGradients d{fresh(x), fresh(x), fresh(x), fresh(rate), in.defined() ? fresh(in) : Tensor()};
-    check(based_gated_recurrence_backward(cptr(x), cptr(r), cptr(g), f32(rate), f32(in), cptr(out), cptr(dout), f32(dlast), ptr(d.dx),
-                                          ptr(d.dr), ptr(d.dg), fptr(d.drate), fptr(d.dstate), B, N, C, io, ws.data, ws.bytes, stream),
+    RecurrenceGradients d{fresh(out), fresh(out), fresh(out), fresh(rate), in.defined() ? fresh(in) : Tensor()};
+    check(based_gated_recurrence_backward(as_tokens(x), as_tokens(r), as_tokens(g), f32(rate), f32(in), as_tokens(out), as_tokens(dout),
+                                          f32(dlast), ptr(d.dx), ptr(d.dr), ptr(d.dg), fptr(d.drate), fptr(d.dstate), B, N, C, io, ws.data,
+                                          ws.bytes, stream),
           "based_gated_recurrence_backward");
     return d;
 }
 // x, r, g, rate, state_in, out, state_out, stream; [B,N,C], or [B,C] for one token (whose states are required)
 PyObject* recurrence(PyObject* const* a) {
-    const Tensor &x = need(a[0], "x"), &r = need(a[1], "r"), &g = need(a[2], "g"), &rate = need(a[3], "rate"), &in = dev(a[4]),
+    const Tensor &x = tokens(a[0], "x"), &r = tokens(a[1], "r"), &g = tokens(a[2], "g"), &rate = need(a[3], "rate"), &in = dev(a[4]),
                  &out = dev(a[5]), &last = dev(a[6]);
     check_gates(x, r, g, rate);
     check_like(out, x, "out", "x");
@@ -581,8 +604,8 @@ PyObject* recurrence(PyObject* const* a) {
 }
 // x, r, g, rate, out, dout, state_in, dstate_out, workspace, stream -> dx, dr, dg, drate, dstate_in (None without state_in)
 PyObject* recurrence_backward(PyObject* const* a) {
-    const Tensor &x = need(a[0], "x"), &r = need(a[1], "r"), &g = need(a[2], "g"), &rate = need(a[3], "rate"), &out = need(a[4], "out"),
-                 &dout = need(a[5], "dout"), &in = dev(a[6]), &dlast = dev(a[7]), &ws = dev(a[8]);
+    const Tensor &x = tokens(a[0], "x"), &r = tokens(a[1], "r"), &g = tokens(a[2], "g"), &rate = need(a[3], "rate"),
+                 &out = tokens(a[4], "out"), &dout = tokens(a[5], "dout"), &in = dev(a[6]), &dlast = dev(a[7]), &ws = dev(a[8]);
     dims(x, 3, "x");
     check_gates(x, r, g, rate);
     check_like(out, x, "out", "x");
@@ -614,18 +637,6 @@ const Tensor& rows(PyObject* o, const char* name) {
     dims(t, 4, name);
     if (!evenly_spaced(t)) value_error(std::string(name) + " must be [B,L,H,d] with the heads of a token side by side and evenly spaced tokens");
     return t;
-}
-// overlap() for such rows, which reach beyond their number of bytes: the whole stretch from the first to the last
-bool stretches_overlap(const Tensor& a, const Tensor& b) {
-    auto end = [](const Tensor& t) {
-        int64_t last = 0;
-        for (int64_t i = 0; i < t.dim(); ++i) {
-            if (t.size(i) == 0) return static_cast<const char*>(t.const_data_ptr());
-            last += (t.size(i) - 1) * t.stride(i);
-        }
-        return static_cast<const char*>(t.const_data_ptr()) + (last + 1) * static_cast<int64_t>(t.element_size());
-    };
-    return static_cast<const char*>(a.const_data_ptr()) < end(b) && static_cast<const char*>(b.const_data_ptr()) < end(a);
 }
 struct Rotation {
     Tensor q, k, wq, wk, freqs, positions;
@@ -914,13 +925,22 @@ void on_gpu(const Tensor& t) {
 }
 Tensor packed(const std::optional<Tensor>& t) { return t ? t->contiguous() : Tensor(); }
 std::optional<Tensor> maybe(const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; }
+// a view with strides that the library takes, or a copy
+Tensor evenly(const Tensor& t) {
+    if (t.dim() != 3) return t.contiguous();
+    const int64_t per16 = 16 / static_cast<int64_t>(t.element_size()), B = t.size(0), N = t.size(1), C = t.size(2);
+    const bool as_it_lies = t.stride(2) == 1 && (reinterpret_cast<uintptr_t>(t.const_data_ptr()) & 15) == 0 &&
+                            (N == 1 || (t.stride(1) >= C && t.stride(1) % per16 == 0)) &&
+                            (B == 1 || (t.stride(0) >= (N > 1 ? (N - 1) * t.stride(1) : 0) + C && t.stride(0) % per16 == 0));
+    return as_it_lies ? t : t.contiguous();
+}
 struct GatedRecurrence : torch::autograd::Function<GatedRecurrence> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x_, const Tensor& r_,
                                                   const Tensor& g_, const Tensor& rate_, const std::optional<Tensor>& in_) {
         ctx->set_materialize_grads(false);
         on_gpu(x_);
-        const Tensor x = x_.contiguous(), r = r_.contiguous(), g = g_.contiguous(), rate = rate_.contiguous(), in = packed(in_);
-        dims(x, 3, "x");
+        dims(x_, 3, "x");
+        const Tensor x = evenly(x_), r = evenly(r_), g = evenly(g_), rate = rate_.contiguous(), in = packed(in_);
         check_gates(x, r, g, rate);
         check_f32(in, {x.size(0), x.size(2)}, "state");
         check_places({&x, &r, &g, &rate, &in}, {});
@@ -935,7 +955,7 @@ struct GatedRecurrence : torch::autograd::Function<GatedRecurrence> {
         const Tensor &x = saved[0], &in = saved[4];
         if (!grads[0].defined() && !grads[1].defined()) return {Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
         return node_backward(x, [&](void* stream) -> torch::autograd::variable_list {
-            const Tensor dout = grads[0].defined() ? as_input(grads[0], x) : at::zeros_like(x);
+            const Tensor dout = grads[0].defined() ? evenly(grads[0].to(x.scalar_type())) : at::zeros(x.sizes(), x.options());
             const RecurrenceGradients d = recurrence_backward_call(x, saved[1], saved[2], saved[3], in, saved[5], dout,
                                                                    as_input(grads[1], saved[3]), kNone, stream);
             return {d.dx, d.dr, d.dg, d.drate, d.dstate};

@@ -78,8 +78,8 @@ def test_large_gates(dtype):
     r[0, 5, 4], g[0, 5, 5] = float("inf"), -float("inf")
     want, a, m, i = recurrence(*f64(x, r, g, rate, h0))
     out = based.based_gated_recurrence_forward(x, r, g, rate, state_in=h0)
-    # (a shut gate counts as 2^-60: an m of up to sqrt(2 rate 2^-60) < 2^-29 in the place of a smaller one, times x < 8, 150 times)
-    off = 64 * U * 150 * channel_max(want, m * i * x.double(), h0) + 2.0 ** -29 * 8 * 150
+    # (a shut gate counts as 2^-59: an m of up to sqrt(2 rate 2^-59) < 2^-28.5 in the place of a smaller one, times x < 8, 150 times)
+    off = 64 * U * 150 * channel_max(want, m * i * x.double(), h0) + 2.0 ** -28.5 * 8 * 150
     close(out, want, off + half_step(x.dtype) * (want.abs() + off), "out")
     grads = based.based_gated_recurrence_backward(x, r, g, rate, out, dout, h0, dh)
     assert all(torch.isfinite(t).all() for t in grads)
@@ -216,6 +216,35 @@ def test_streams_graph_and_neighbours():
     want = based.based_gated_recurrence_forward(x, r, g, rate, state_in=h0)
     grads = based.based_gated_recurrence_backward(x, r, g, rate, want, dout, h0, dh)
     assert torch.equal(y, want) and all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_views_with_strides(dtype):
+    """Slices of a fused projection and of a longer batch, as they lie; the autograd node too."""
+    B, N, C = 3, 150, 72
+    x, r, g, rate, h0, dout, dh = draw(B, N, C, dtype, seed=8)
+    fused = torch.cat([r, g, x], -1)
+    longer = torch.nn.functional.pad(dout, (0, 0, 0, 50), value=float("nan"))
+    views = (fused[..., 2 * C:], fused[..., :C], fused[..., C:2 * C])
+    want = based.based_gated_recurrence_forward(x, r, g, rate, state_in=h0)
+    assert torch.equal(based.based_gated_recurrence_forward(*views, rate, state_in=h0), want)
+    out = torch.nn.functional.pad(want, (0, 0, 0, 7), value=float("nan"))[:, :N]
+    a = based.based_gated_recurrence_backward(x, r, g, rate, want, dout, h0, dh)
+    b = based.based_gated_recurrence_backward(*views, rate, out, longer[:, :N], h0, dh)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    leaf = fused.clone().requires_grad_(True)
+    y, _ = ag.gated_recurrence(leaf[..., 2 * C:], leaf[..., :C], leaf[..., C:2 * C], rate)
+    (d,) = torch.autograd.grad(y, leaf, longer[:, :N])
+    c = based.based_gated_recurrence_backward(x, r, g, rate, y.detach(), dout)
+    assert torch.equal(d, torch.cat([c[1], c[2], c[0]], -1))
+    state = h0.clone()
+    one = based.based_gated_recurrence_step(*(v[:, 3] for v in views), rate, state)
+    other = h0.clone()
+    assert torch.equal(one, based.based_gated_recurrence_step(*(v[:, 3].contiguous() for v in (x, r, g)), rate, other)) and torch.equal(state, other)
+    with pytest.raises(ValueError):
+        based.based_gated_recurrence_forward(x.transpose(1, 2), r.transpose(1, 2), g.transpose(1, 2), rate)
+    with pytest.raises(based.BasedError):                    # the same tokens for every sequence
+        based.based_gated_recurrence_forward(x[:1].expand(B, N, C), r, g, rate)
 
 
 def test_refusals():

@@ -20,21 +20,27 @@ U = ctypes.c_void_p(0x8008)
 INVALID, UNSUPPORTED, ALIGNMENT, WORKSPACE = 1, 2, 3, 6
 
 
+def T(p, batch=128, token=16):
+    from paper_2402_18668_b200.binding import Tokens
+    return Tokens(p, batch, token)
+
+
 def test_recurrence(lib):
-    def f(x=P(0), r=P(1), g=P(2), rate=P(3), si=None, out=P(4), so=None, B=1, N=8, C=16, io=1):
-        return lib.based_gated_recurrence_forward(x, r, g, rate, si, out, so, B, N, C, io, None)
+    def f(x=P(0), r=P(1), g=P(2), rate=P(3), si=None, out=P(4), so=None, B=2, N=8, C=16, io=1, batch=128, token=16):
+        return lib.based_gated_recurrence_forward(T(x, batch, token), T(r), T(g), rate, si, out, so, B, N, C, io, None)
     for k in ("x", "r", "g", "rate", "out"):
         assert f(**{k: None}) == INVALID
         assert f(**{k: U}) == ALIGNMENT
     assert f(si=U) == ALIGNMENT and f(so=U) == ALIGNMENT
     assert f(B=0) == f(N=0) == f(C=0) == f(N=-1) == f(io=2) == INVALID
-    assert f(C=12) == UNSUPPORTED
+    assert f(C=12) == f(token=20, batch=160) == f(batch=132) == f(io=0, batch=130) == UNSUPPORTED
+    assert f(token=8) == f(batch=120) == f(batch=0) == f(batch=-128) == f(token=-16) == INVALID
     assert f(out=P(0)) == f(out=P(1)) == f(out=P(2)) == f(so=P(3)) == f(so=P(4)) == f(si=P(4)) == INVALID
-    assert f(B=2**31 - 1, N=2, C=2**31 - 8) == UNSUPPORTED
+    assert f(B=2**31 - 1, N=2, C=2**31 - 8) == f(N=2**31 - 1) == UNSUPPORTED
     s = lib.based_gated_recurrence_step
-    assert s(P(0), P(1), P(2), P(3), None, P(4), P(5), 1, 16, 1, None) == INVALID
-    assert s(P(0), P(1), P(2), P(3), P(5), P(4), None, 1, 16, 1, None) == INVALID
-    assert s(P(0), P(1), P(2), P(3), P(5), P(4), P(5), 1, 20, 1, None) == UNSUPPORTED
+    assert s(T(P(0)), T(P(1)), T(P(2)), P(3), None, P(4), P(5), 1, 16, 1, None) == INVALID
+    assert s(T(P(0)), T(P(1)), T(P(2)), P(3), P(5), P(4), None, 1, 16, 1, None) == INVALID
+    assert s(T(P(0)), T(P(1)), T(P(2)), P(3), P(5), P(4), P(5), 1, 20, 1, None) == UNSUPPORTED
 
 
 def test_recurrence_backward(lib):
@@ -45,14 +51,15 @@ def test_recurrence_backward(lib):
     def f(ws=P(20), bytes_=need, B=2, N=8, C=16, io=1, **kw):
         names = ("x", "r", "g", "rate", "si", "out", "dout", "dso", "dx", "dr", "dg", "drate", "dsi")
         a = {n: P(i) for i, n in enumerate(names)} | kw
+        a |= {n: T(a[n]) for n in ("x", "r", "g", "out", "dout")}
         return lib.based_gated_recurrence_backward(*(a[n] for n in names), B, N, C, io, ws, bytes_, None)
     for k in ("x", "r", "g", "rate", "out", "dout", "dx", "dr", "dg", "drate"):
         assert f(**{k: None}) == INVALID
         assert f(**{k: U}) == ALIGNMENT
     assert f(dsi=U) == f(dso=U) == f(ws=U) == ALIGNMENT
     assert f(ws=None) == f(bytes_=need - 1) == WORKSPACE
-    assert f(dx=P(0)) == f(dr=P(8)) == f(drate=P(20)) == f(dg=P(7)) == INVALID
-    assert f(C=4) == UNSUPPORTED and f(io=3) == INVALID and f(N=0) == INVALID
+    assert f(dx=P(0)) == f(dr=P(8)) == f(drate=P(20)) == f(dg=P(7)) == f(dg=P(5)) == INVALID
+    assert f(C=4) == UNSUPPORTED and f(io=3) == INVALID and f(N=0) == INVALID and f(N=9) == INVALID
 
 
 def test_norm_rotate(lib):
