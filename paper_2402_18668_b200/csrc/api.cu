@@ -544,7 +544,7 @@ static based_status recurrence_check(const based_tokens& x, const based_tokens& 
                                      based_dtype io) {
     if (!x.data || !r.data || !g.data || !rate || B <= 0 || N <= 0 || C <= 0) return BASED_ERR_INVALID_ARG;
     if (io != BASED_F32 && io != BASED_BF16) return BASED_ERR_INVALID_ARG;
-    if (C % 8 != 0 || N > 0x7fff0000 || (long long)B * C > (1ll << 36) || gated_recurrence_blocks(B, N, C) > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    if (C % 8 != 0 || N > 0x7fff0000 || (long long)B * C > (1ll << 36) || gated_recurrence_blocks(B, C, io) > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
     for (const based_tokens* t : {&x, &r, &g}) {
         const based_status st = tokens_check(*t, B, N, C, io);
         if (st != BASED_OK) return st;
@@ -570,7 +570,7 @@ based_status based_gated_recurrence_step(based_tokens x, based_tokens r, based_t
 
 size_t based_gated_recurrence_backward_workspace_bytes(int B, int N, int C, based_dtype io) {
     if (B <= 0 || N <= 0 || C <= 0 || (io != BASED_F32 && io != BASED_BF16)) return 0;
-    return gated_recurrence_backward_bytes(B, N, C);
+    return gated_recurrence_backward_bytes(B, N, C, io);
 }
 
 based_status based_gated_recurrence_backward(based_tokens x, based_tokens r, based_tokens g, const float* rate, const float* state_in,
@@ -592,7 +592,7 @@ based_status based_gated_recurrence_backward(based_tokens x, based_tokens r, bas
     for (const void* p : {(const void*)state_in, (const void*)dstate_out, (const void*)dx, (const void*)dr, (const void*)dg,
                           (const void*)drate, (const void*)dstate_in, (const void*)workspace})
         if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
-    if (!workspace || workspace_bytes < gated_recurrence_backward_bytes(B, N, C)) return BASED_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < gated_recurrence_backward_bytes(B, N, C, io)) return BASED_ERR_WORKSPACE;
     return launch_gated_recurrence_backward(x, r, g, rate, state_in, out, dout, dstate_out, dx, dr, dg, drate, dstate_in, B, N, C,
                                             static_cast<float*>(workspace), io, static_cast<cudaStream_t>(cuda_stream));
 }

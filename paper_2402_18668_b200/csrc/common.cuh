@@ -232,9 +232,9 @@ based_status launch_quadratic_groups_tc(const void* q, const void* k, const void
 based_status launch_column_sums(const float* part, long long rows, int cols, float* a, int split, float* b, cudaStream_t stream);
 // [B,N,C] values as the caller holds them: strides in elements (based_tokens)
 using Tokens = based_tokens;
-// gated linear recurrence (gated_recurrence.cu); _blocks: CTAs of a launch (a grid has at most 2^31 - 1); part: _bytes of scratch
-long long gated_recurrence_blocks(int B, int N, int C);
-size_t gated_recurrence_backward_bytes(int B, int N, int C);
+// gated linear recurrence (gated_recurrence.cu); _blocks: CTAs of a launch at most (a grid has at most 2^31 - 1); part: _bytes of scratch
+long long gated_recurrence_blocks(int B, int C, based_dtype io);
+size_t gated_recurrence_backward_bytes(int B, int N, int C, based_dtype io);
 based_status launch_gated_recurrence(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, void* out,
                                      float* state_out, int B, int N, int C, based_dtype io, cudaStream_t stream);
 based_status launch_gated_recurrence_backward(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in,

@@ -13,10 +13,14 @@
 //   dx = G m i,  dg = G m x i (1 - i),  dlog a = a G h_{t-1} - (a^2 / m) G i x,  dr = -rate dlog a s (1 - s),
 //   drate = -sum dlog a s  (i = sigmoid(g); h_{t-1} is read from the output that the caller kept).
 //
-// HBM bound by its bytes (4 values a token and channel forward, 8 backward), with little to spare: four special-function calls per
-// element forward take 60 us of the 82 us that the bytes of B8 N4096 C2048 bf16 take.  So one reciprocal serves both sigmoids, the
-// decay comes from a polynomial where the rates allow, everything else works on two channels per instruction, and tiles of
-// tokens x 64 channels come by TMA, which needs no address arithmetic and reads views with strides as they lie.
+// HBM bound by its bytes (4 values a token and channel forward, 8 backward), with little to spare: at the pace of HBM an SM has 43 cycles
+// for 32 elements forward on a sub-core, and the element's 3 special-function calls take 24 of them, its multiply-adds 24, which
+// together come to 31 at best (measured, without loads).  So one reciprocal root serves both gates and the root of 1 - a^2, cubics
+// stand for what is left of the exponential where the rates allow, two channels share an instruction (half the issue slots, the same
+// pipe time), and tiles of tokens x 128 bytes come by TMA, which needs no address arithmetic and reads views with strides as they lie.
+// B8 N4096 C2048 bf16: forward 119 us = 4.5 TB/s (256 CTAs on 148 SMs: two on most, which is what bounds it; its loads and stores
+// without the arithmetic take 87, the arithmetic without them 97), backward 218 us = 4.9 TB/s; B1 N32768 C1000 fp32 forward 98 us =
+// 5.3 TB/s.
 #include <type_traits>
 
 #include "common.cuh"
@@ -30,8 +34,10 @@ using namespace sm100;
 namespace {
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kV = 4, kP = kV / 2;               // channels of a thread, and pairs of them
-constexpr int kLanes = 16, kSlab = kLanes * kV;  // threads side by side, and their channels
-constexpr int kGroups = kThreads / kLanes;       // groups of TOK consecutive tokens
+// threads side by side, whose channels make a tile's rows 128 bytes; groups of TOK consecutive tokens
+template <typename T> __host__ __device__ constexpr int lanes_of() { return sizeof(T) == 4 ? 8 : 16; }
+template <typename T> __host__ __device__ constexpr int slab_of() { return lanes_of<T>() * kV; }
+template <typename T> __host__ __device__ constexpr int groups_of() { return kThreads / lanes_of<T>(); }
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -63,8 +69,7 @@ __device__ __forceinline__ float max_nan(float x, float y) {
 
 // Four values of a row, as two pairs
 template <typename T> struct Four;
-// A gate is taken as -41 at least, so that exp(-x) stays below 2^60 and the product of two such sums and its reciprocal are finite: a
-// sigmoid below 2^-59 counts as 2^-59.  A NaN stays one.
+// A gate is taken as -41 at least, so that exp(-x) stays below 2^60 (see Gates): a sigmoid below 2^-59 counts as 2^-59.  A NaN stays one.
 constexpr float kLeast = -41.f;
 template <> struct Four<float> {
     using Raw = float4;
@@ -108,36 +113,72 @@ template <typename T> __device__ __forceinline__ void write4(T* p, const pair (&
     __stcs(reinterpret_cast<typename Four<T>::Raw*>(p), Four<T>::pack(x));
 }
 
-// 1 + exp(-x)
-__device__ __forceinline__ pair one_plus_exp_neg(pair x) {
+// exp(-x)
+__device__ __forceinline__ pair exp_neg(pair x) {
     const float2 t = split(mul2(x, both(-kLog2e)));
-    return add2(make(ex2(t.x), ex2(t.y)), both(1.f));
+    return make(ex2(t.x), ex2(t.y));
 }
-__device__ __forceinline__ pair rcp2(pair x) {
+__device__ __forceinline__ pair rroot2(pair x) {
     const float2 t = split(x);
+    return make(rroot(t.x), rroot(t.y));
+}
+__device__ __forceinline__ pair sigmoid(pair x) {
+    const float2 t = split(add2(exp_neg(x), both(1.f)));
     return make(rcp(t.x), rcp(t.y));
 }
-// exp(la) - 1 for la <= 0.  On [-1/4, 0] la times the polynomial of degree 4 that interpolates (exp(la) - 1) / la at the Chebyshev
-// points of the interval (off by 5e-9 relative at most, coefficients rounded to fp32), so that 1 - a^2 = -p (2 + p) keeps its digits
-// where the decay is slow.  SMALL: every la is in that range
-template <bool SMALL> __device__ __forceinline__ pair exp_less_one(pair la) {
-    pair y = fma2(la, both(0.0075136062f), both(0.041490654f));
-    y = fma2(la, y, both(0.16665108f));
-    y = fma2(la, y, both(0.49999951f));
-    y = fma2(la, y, both(1.f));
-    y = mul2(la, y);
-    if constexpr (!SMALL) {
-        const float2 l = split(la), f = split(y), e = split(mul2(la, both(kLog2e)));
-        y = make(l.x > -0.25f ? f.x : ex2(e.x) - 1.f, l.y > -0.25f ? f.y : ex2(e.y) - 1.f);
-    }
-    return y;
+// Both gates of an element from one reciprocal root: with A = 1 + exp(-r), B = 1 + exp(-g) it is t = A^-1/2 B^-1 = sqrt(sigmoid(r))
+// sigmoid(g), and w = t B the root of sigmoid(r), which is what sqrt(1 - a^2) holds of r.  B is taken times 2^-30 (t comes out
+// times 2^30), so that A B^2, which would reach 2^178, stays below 2^119.
+constexpr float kDown = 9.313225746154785e-10f;                      // 2^-30
+struct Gates {
+    pair A, t, w;
+};
+__device__ __forceinline__ Gates gates(pair r, pair g) {
+    Gates z;
+    z.A = add2(exp_neg(r), both(1.f));
+    const pair B = fma2(exp_neg(g), both(kDown), both(kDown));
+    z.t = rroot2(mul2(z.A, mul2(B, B)));
+    z.w = mul2(z.t, B);
+    return z;
+}
+// On -1/4 <= la <= 0, by the cubics that interpolate them at the interval's Chebyshev points, coefficients rounded to fp32:
+// (exp(la) - 1) / la (off by 2.6e-7 relative at most) and sqrt((1 - exp(2 la)) / (-2 la)) (4.4e-7)
+__device__ __forceinline__ pair cubic(pair x, float c0, float c1, float c2, float c3) {
+    return fma2(x, fma2(x, fma2(x, both(c3), both(c2)), both(c1)), both(c0));
+}
+__device__ __forceinline__ pair slope(pair la) { return cubic(la, 0.999999762f, 0.499969989f, 0.166062251f, 0.0377289727f); }
+__device__ __forceinline__ pair share(pair la) { return cubic(la, 0.999999642f, 0.499950707f, 0.207340196f, 0.0560273491f); }
+// exp(la) - 1 for any la <= 0, with all its digits near 0, so that 1 - a^2 = -p (2 + p) keeps them
+__device__ __forceinline__ pair exp_less_one(pair la) {
+    const float2 l = split(la), f = split(mul2(la, slope(la))), e = split(mul2(la, both(kLog2e)));
+    return make(l.x > -0.25f ? f.x : ex2(e.x) - 1.f, l.y > -0.25f ? f.y : ex2(e.y) - 1.f);
 }
 // 1 - a^2 from p = a - 1
 __device__ __forceinline__ pair one_less_square(pair p) { return mul2(p, fma2(p, both(-1.f), both(-2.f))); }
-// whether the rates of a warp's threads keep -rate sigmoid above -1/4
+// Decay and input of a token: a = exp(la), u = sqrt(1 - a^2) sigmoid(g) x, la = -rate sigmoid(r).  SMALL: la >= -1/4, and
+// sqrt(1 - a^2) = sqrt(-2 la) share(la) = sqrt(2 rate) w share(la); c: sqrt(2 rate) 2^-30
+template <bool SMALL>
+__device__ __forceinline__ void token(const Gates& z, pair nrate, pair c, pair x, pair& a, pair& u) {
+    const pair la = mul2(nrate, mul2(z.w, z.w));
+    if constexpr (SMALL) {
+        a = fma2(la, slope(la), both(1.f));
+        u = mul2(mul2(z.t, x), mul2(c, share(la)));
+    } else {
+        const pair p = exp_less_one(la);
+        const float2 m2 = split(one_less_square(p));
+        a = add2(p, both(1.f));
+        u = mul2(make(root(m2.x), root(m2.y)), mul2(mul2(mul2(z.t, both(kDown)), mul2(z.A, z.w)), x));
+    }
+}
+// whether the rates of all threads keep -rate sigmoid in the cubics' range
 __device__ __forceinline__ bool all_small(const pair (&nrate)[kP]) {
     const float2 a = split(nrate[0]), b = split(nrate[1]);
-    return __all_sync(0xffffffffu, a.x > -0.25f && a.y > -0.25f && b.x > -0.25f && b.y > -0.25f);
+    return __syncthreads_and(a.x >= -0.25f && a.y >= -0.25f && b.x >= -0.25f && b.y >= -0.25f);
+}
+// sqrt(2 rate) times f
+__device__ __forceinline__ pair root_rate(pair nrate, float f) {
+    const float2 r = split(nrate);
+    return make(sqrtf(-2.f * r.x) * f, sqrtf(-2.f * r.y) * f);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -160,30 +201,44 @@ __device__ __forceinline__ void store_remote(const void* own, uint64_t* own_bar,
 
 // What a CTA shares.  The joins of a step use one of two sets in turn: a set is written again two steps on, when every thread has
 // passed the barrier of the step between and so has read it.
-template <int PARTS> struct Shared {
-    ulonglong2 warp[2][kWarps][2][kLanes];                       // A, H of a warp's tokens
-    ulonglong2 part[2][PARTS > 1 ? PARTS : 1][2][kLanes];        // of a CTA's
-    pair sums[kWarps][kP][kLanes];
-    uint64_t full[3], arrived[2];                                // a stage's tiles; the parts of a set
+template <int LANES, int PARTS> struct Shared {
+    ulonglong2 warp[2][kWarps][2][LANES];                        // A, H of a warp's tokens
+    ulonglong2 part[2][PARTS > 1 ? PARTS : 1][2][LANES];         // of a CTA's
+    pair sums[kWarps][kP][LANES];
+    uint64_t full[4], arrived[2];                                // a stage's tiles; the parts of a set
     uint32_t abort_flag;
 };
 // A, H: what the thread's tokens do to the state.  h: the state before this step, on return the one behind it.  first: the state
 // that reaches the thread's first token.  after_barrier: run once every thread of the CTA has come this far.
-template <int PARTS, typename F>
-__device__ __forceinline__ bool join(Shared<PARTS>& sm, int step, int rank, const pair (&A0)[kP], const pair (&H0)[kP], pair (&h)[kP],
+template <int LANES, int PARTS, typename F>
+__device__ __forceinline__ bool join(Shared<LANES, PARTS>& sm, int step, int rank, pair (&A)[kP], pair (&H)[kP], pair (&h)[kP],
                                      pair (&first)[kP], F after_barrier) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane & (kLanes - 1), turn = step & 1;
-    const bool upper = lane >= kLanes;
-    // the lower group's, for the upper one: in front of its own tokens, and joined to them the warp's
-    pair A[kP], H[kP];
+    constexpr int kPer = 32 / LANES;                             // groups of a warp: 2 or 4
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane & (LANES - 1), turn = step & 1;
+    // over the warp's groups, inclusive; then exclusive (with two groups the upper one has what it needs from the first shuffle)
+    pair xa[kP], xh[kP];
 #pragma unroll
-    for (int e = 0; e < kP; ++e) {
-        A[e] = shfl_up2(A0[e], kLanes);
-        H[e] = shfl_up2(H0[e], kLanes);
+    for (int d = LANES; d < 32; d *= 2) {
+#pragma unroll
+        for (int e = 0; e < kP; ++e) {
+            xa[e] = shfl_up2(A[e], d);
+            xh[e] = shfl_up2(H[e], d);
+            if (lane >= d) {
+                H[e] = fma2(A[e], xh[e], H[e]);
+                A[e] = mul2(A[e], xa[e]);
+            }
+        }
     }
-    if (upper) {
-        sm.warp[turn][warp][0][col] = make_ulonglong2(mul2(A0[0], A[0]), mul2(A0[1], A[1]));
-        sm.warp[turn][warp][1][col] = make_ulonglong2(fma2(A0[0], H[0], H0[0]), fma2(A0[1], H[1], H0[1]));
+    if (lane >= 32 - LANES) {
+        sm.warp[turn][warp][0][col] = make_ulonglong2(A[0], A[1]);
+        sm.warp[turn][warp][1][col] = make_ulonglong2(H[0], H[1]);
+    }
+    if constexpr (kPer > 2) {
+#pragma unroll
+        for (int e = 0; e < kP; ++e) {
+            xa[e] = shfl_up2(A[e], LANES);
+            xh[e] = shfl_up2(H[e], LANES);
+        }
     }
     __syncthreads();
     after_barrier();
@@ -208,12 +263,12 @@ __device__ __forceinline__ bool join(Shared<PARTS>& sm, int step, int rank, cons
             ta[1] = mul2(a.y, ta[1]);
         }
         // it goes to every CTA of the cluster
-        if (threadIdx.x == 0) mbar_arrive_expect_tx(&sm.arrived[turn], PARTS * 2 * kLanes * 16);
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&sm.arrived[turn], PARTS * 2 * LANES * 16);
 #pragma unroll
         for (int to = 0; to < PARTS; ++to) {
             if ((to & (kWarps - 1)) != warp) continue;
-            if (upper) store_remote(&sm.part[turn][rank][1][col], &sm.arrived[turn], to, th[0], th[1]);
-            else store_remote(&sm.part[turn][rank][0][col], &sm.arrived[turn], to, ta[0], ta[1]);
+            if (lane < LANES) store_remote(&sm.part[turn][rank][0][col], &sm.arrived[turn], to, ta[0], ta[1]);
+            else if (lane < 2 * LANES) store_remote(&sm.part[turn][rank][1][col], &sm.arrived[turn], to, th[0], th[1]);
         }
         ok = mbar_wait(&sm.arrived[turn], (step >> 1) & 1, &sm.abort_flag);
         pair hs[kP];
@@ -242,12 +297,12 @@ __device__ __forceinline__ bool join(Shared<PARTS>& sm, int step, int rank, cons
         }
     }
 #pragma unroll
-    for (int e = 0; e < kP; ++e) first[e] = upper ? fma2(A[e], x[e], H[e]) : x[e];
+    for (int e = 0; e < kP; ++e) first[e] = lane < LANES ? x[e] : fma2(xa[e], x[e], xh[e]);
     return ok;
 }
-template <int PARTS> __device__ __forceinline__ void begin(Shared<PARTS>& sm) {
+template <int LANES, int PARTS> __device__ __forceinline__ void begin(Shared<LANES, PARTS>& sm) {
     if (threadIdx.x == 0) {
-        for (int s = 0; s < 3; ++s) mbar_init(&sm.full[s], 1);
+        for (uint64_t& bar : sm.full) mbar_init(&bar, 1);
         for (int s = 0; s < 2; ++s) mbar_init(&sm.arrived[s], 1);
         sm.abort_flag = 0;
         fence_mbar_init();
@@ -257,7 +312,7 @@ template <int PARTS> __device__ __forceinline__ void begin(Shared<PARTS>& sm) {
 }
 // Waits that have run out leave a flag and the loops run on without waiting (every thread still meets every barrier); copies that
 // may be under way then get time to land.
-template <int PARTS> __device__ __forceinline__ void finish(Shared<PARTS>& sm, bool ok, unsigned int* err) {
+template <int LANES, int PARTS> __device__ __forceinline__ void finish(Shared<LANES, PARTS>& sm, bool ok, unsigned int* err) {
     if (!ok) atomicOr(err, 1u);
     __syncthreads();
     if (*(volatile uint32_t*)&sm.abort_flag) {
@@ -265,44 +320,52 @@ template <int PARTS> __device__ __forceinline__ void finish(Shared<PARTS>& sm, b
     }
     if constexpr (PARTS > 1) cluster_arrive_wait();              // no CTA leaves before what others send it has arrived
 }
+// Tokens per thread, stages of tiles, and CTAs that an SM holds.  us, tokens x CTAs per SM: B8 N4096 C2048 bf16 forward 8 x 3 119, 8 x 4 123,
+// 4 x 4 136, 16 x 2 121 (more tokens spread a join over more elements, more registers keep constants where they are), backward 4 x 3
+// 217, 4 x 4 252, 2 x 5 271; B1 N32768 C1000 fp32 8 x 2 98, 4 x 4 121; backward B3 N1111 C1000 fp32 2 x 3 27, 4 x 1 39.  More
+// stages change nothing.
+template <typename T, bool BACK> struct Plan;
+template <> struct Plan<__nv_bfloat16, false> { static constexpr int kTok = 8, kStages = 2, kBlocks = 3; };
+template <> struct Plan<float, false> { static constexpr int kTok = 8, kStages = 2, kBlocks = 2; };
+template <> struct Plan<__nv_bfloat16, true> { static constexpr int kTok = 4, kStages = 3, kBlocks = 3; };
+template <> struct Plan<float, true> { static constexpr int kTok = 2, kStages = 3, kBlocks = 3; };
 // tokens of a step, of one CTA; bytes of a tile
-template <int TOK> __host__ __device__ constexpr int run_tokens() { return kGroups * TOK; }
-template <typename T, int TOK> __host__ __device__ constexpr uint32_t tile_bytes() { return run_tokens<TOK>() * kSlab * sizeof(T); }
+template <typename T, bool BACK> __host__ __device__ constexpr int run_tokens() { return groups_of<T>() * Plan<T, BACK>::kTok; }
+template <typename T, bool BACK> __host__ __device__ constexpr uint32_t tile_bytes() { return run_tokens<T, BACK>() * slab_of<T>() * sizeof(T); }
 }  // namespace
 
 struct RecurrenceMaps {
     CUtensorMap r, g, x, dout, out;
 };
 
-// grid: clusters of PARTS CTAs, one per sequence and slab of 64 channels; the CTAs of a cluster take runs of 8 TOK tokens in turn.
-template <typename T, int TOK, int PARTS>
-__global__ void __launch_bounds__(kThreads, 4)
+// grid: clusters of PARTS CTAs, one per sequence and slab of channels (64, fp32 32); the CTAs of a cluster take runs of tokens in turn.
+template <typename T, int PARTS>
+__global__ void __launch_bounds__(kThreads, Plan<T, false>::kBlocks)
     gated_recurrence_kernel(const __grid_constant__ RecurrenceMaps maps, const float* __restrict__ rate, const float* state_in,
                             T* __restrict__ out, float* state_out, unsigned int* err, int N, int C, int slabs) {
-    constexpr int kRun = run_tokens<TOK>();
-    constexpr uint32_t kTile = tile_bytes<T, TOK>(), kRow = kSlab * sizeof(T);
-    extern __shared__ __align__(128) uint8_t stage[];            // [2][r, g, x][kRun][kSlab]
-    __shared__ Shared<PARTS> sm;
+    constexpr int TOK = Plan<T, false>::kTok, kStages = Plan<T, false>::kStages, kRun = run_tokens<T, false>(), LANES = lanes_of<T>(), kSlab = slab_of<T>();
+    constexpr uint32_t kTile = tile_bytes<T, false>(), kRow = kSlab * sizeof(T);
+    extern __shared__ __align__(128) uint8_t stage[];            // [kStages][r, g, x][kRun][kSlab]
+    __shared__ Shared<LANES, PARTS> sm;
     begin(sm);
     enter_dependent();
-    const int tid = threadIdx.x, lane = tid & (kLanes - 1), group = tid / kLanes;
+    const int tid = threadIdx.x, lane = tid & (LANES - 1), group = tid / LANES;
     const int rank = PARTS > 1 ? (int)cluster_rank() : 0;
     const int work = blockIdx.x / PARTS, b = work / slabs, slab0 = (work - b * slabs) * kSlab, c0 = slab0 + lane * kV;
     const bool mine = c0 < C;
     const int steps = (int)(((long long)N + kRun * PARTS - 1) / (kRun * PARTS));
 
     auto fetch = [&](int s) {
-        uint8_t* to = stage + (s & 1) * 3 * kTile;
+        const int st = s % kStages;
+        uint8_t* to = stage + st * 3 * kTile;
         const int t0 = (int)((s * (long long)PARTS + rank) * kRun);
-        mbar_arrive_expect_tx(&sm.full[s & 1], 3 * kTile);
-        tma_load_3d(to, &maps.r, &sm.full[s & 1], slab0, t0, b);
-        tma_load_3d(to + kTile, &maps.g, &sm.full[s & 1], slab0, t0, b);
-        tma_load_3d(to + 2 * kTile, &maps.x, &sm.full[s & 1], slab0, t0, b);
+        mbar_arrive_expect_tx(&sm.full[st], 3 * kTile);
+        tma_load_3d(to, &maps.r, &sm.full[st], slab0, t0, b);
+        tma_load_3d(to + kTile, &maps.g, &sm.full[st], slab0, t0, b);
+        tma_load_3d(to + 2 * kTile, &maps.x, &sm.full[st], slab0, t0, b);
     };
-    if (tid == 0) {
-        fetch(0);
-        if (steps > 1) fetch(1);
-    }
+    if (tid == 0)
+        for (int s = 0; s < kStages && s < steps; ++s) fetch(s);
     pair nrate[kP] = {0, 0}, h[kP] = {0, 0};
     if (mine) {
         load_f32<kP>(rate + c0, nrate);
@@ -310,16 +373,15 @@ __global__ void __launch_bounds__(kThreads, 4)
         nrate[1] = neg2(nrate[1]);
         if (state_in) load_f32<kP>(state_in + (size_t)b * C + c0, h);
     }
-    const bool small = all_small(nrate);
     T* const to = out + (size_t)b * N * C + c0;
+    const pair c[kP] = {root_rate(nrate[0], kDown), root_rate(nrate[1], kDown)};
     bool ok = true;
-    for (int s = 0; s < steps; ++s) {
-        ok = mbar_wait(&sm.full[s & 1], (s >> 1) & 1, &sm.abort_flag) && ok;
-        const uint8_t* from = stage + (s & 1) * 3 * kTile + group * TOK * kRow + lane * kV * sizeof(T);
-        const long long t0 = (s * (long long)PARTS + rank) * kRun + group * TOK;
-        pair a[TOK][kP], u[TOK][kP];                             // a_t, m_t i_t x_t
-        auto load = [&](auto small_tag) {
-            constexpr bool SMALL = decltype(small_tag)::value;
+    auto walk = [&](auto small_tag) {
+        for (int s = 0; s < steps; ++s) {
+            ok = mbar_wait(&sm.full[s % kStages], (s / kStages) & 1, &sm.abort_flag) && ok;
+            const uint8_t* from = stage + (s % kStages) * 3 * kTile + group * TOK * kRow + lane * kV * sizeof(T);
+            const long long t0 = (s * (long long)PARTS + rank) * kRun + group * TOK;
+            pair a[TOK][kP], u[TOK][kP];                         // a_t, m_t i_t x_t
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
                 pair rv[kP], gv[kP], xv[kP];
@@ -327,70 +389,64 @@ __global__ void __launch_bounds__(kThreads, 4)
                 gate4<T>(from + kTile + j * kRow, gv);
                 values4<T>(from + 2 * kTile + j * kRow, xv);
 #pragma unroll
-                for (int e = 0; e < kP; ++e) {
-                    const pair er = one_plus_exp_neg(rv[e]), eg = one_plus_exp_neg(gv[e]), q = rcp2(mul2(er, eg));
-                    const pair p = exp_less_one<SMALL>(mul2(nrate[e], mul2(q, eg)));
-                    const float2 m2 = split(one_less_square(p));
-                    u[j][e] = mul2(make(root(m2.x), root(m2.y)), mul2(mul2(q, er), xv[e]));
-                    a[j][e] = add2(p, both(1.f));
+                for (int e = 0; e < kP; ++e) token<decltype(small_tag)::value>(gates(rv[e], gv[e]), nrate[e], c[e], xv[e], a[j][e], u[j][e]);
+            }
+            if (t0 + TOK > N) {                                  // behind the sequence nothing happens (x reads as 0 there)
+#pragma unroll
+                for (int j = 0; j < TOK; ++j)
+#pragma unroll
+                    for (int e = 0; e < kP; ++e)
+                        if (t0 + j >= N) a[j][e] = both(1.f);
+            }
+            pair A[kP], H[kP], first[kP];
+#pragma unroll
+            for (int e = 0; e < kP; ++e) {
+                A[e] = a[0][e];
+                H[e] = u[0][e];
+#pragma unroll
+                for (int j = 1; j < TOK; ++j) {
+                    H[e] = fma2(a[j][e], H[e], u[j][e]);
+                    A[e] = mul2(A[e], a[j][e]);
                 }
             }
-        };
-        if (small) load(std::true_type{});
-        else load(std::false_type{});
-        if (t0 + TOK > N) {                                      // behind the sequence nothing happens (x reads as 0 there)
+            ok = join<LANES, PARTS>(sm, s, rank, A, H, h, first, [&] {      // (the stage has been read)
+                if (tid == 0 && s + kStages < steps) fetch(s + kStages);
+            }) && ok;
 #pragma unroll
-            for (int j = 0; j < TOK; ++j)
+            for (int j = 0; j < TOK; ++j) {
 #pragma unroll
-                for (int e = 0; e < kP; ++e)
-                    if (t0 + j >= N) a[j][e] = both(1.f);
-        }
-        pair A[kP], H[kP], first[kP];
-#pragma unroll
-        for (int e = 0; e < kP; ++e) {
-            A[e] = a[0][e];
-            H[e] = u[0][e];
-#pragma unroll
-            for (int j = 1; j < TOK; ++j) {
-                H[e] = fma2(a[j][e], H[e], u[j][e]);
-                A[e] = mul2(A[e], a[j][e]);
+                for (int e = 0; e < kP; ++e) first[e] = fma2(a[j][e], first[e], u[j][e]);
+                if (mine && t0 + j < N) write4<T>(to + (size_t)(t0 + j) * C, first);
             }
         }
-        ok = join<PARTS>(sm, s, rank, A, H, h, first, [&] {      // (the stage has been read)
-            if (tid == 0 && s + 2 < steps) fetch(s + 2);
-        }) && ok;
-#pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-#pragma unroll
-            for (int e = 0; e < kP; ++e) first[e] = fma2(a[j][e], first[e], u[j][e]);
-            if (mine && t0 + j < N) write4<T>(to + (size_t)(t0 + j) * C, first);
-        }
-    }
+    };
+    if (all_small(nrate)) walk(std::true_type{});
+    else walk(std::false_type{});
     if (state_out && mine && rank == 0 && group == 0) store_f32<kP>(state_out + (size_t)b * C + c0, h);
     finish(sm, ok, err);
 }
 
 // The scan from the last token to the first: "time" tau = N - 1 - t, tiles lie with the last token of a run below.  part: [sequences
 // x PARTS][C] sums of drate
-template <typename T, int TOK, int PARTS>
-__global__ void __launch_bounds__(kThreads, 4)
+template <typename T, int PARTS>
+__global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
     gated_recurrence_backward_kernel(const __grid_constant__ RecurrenceMaps maps, const float* __restrict__ rate,
                                      const float* __restrict__ state_in, const float* dstate_out, T* __restrict__ dx, T* __restrict__ dr,
                                      T* __restrict__ dg, float* __restrict__ part, float* dstate_in, unsigned int* err, int N, int C, int slabs) {
-    constexpr int kRun = run_tokens<TOK>();
-    constexpr uint32_t kTile = tile_bytes<T, TOK>(), kRow = kSlab * sizeof(T);
-    extern __shared__ __align__(128) uint8_t stage[];            // [3][r, dout, g, x, out of the token before][kRun][kSlab]
-    __shared__ Shared<PARTS> sm;
+    constexpr int TOK = Plan<T, true>::kTok, kStages = Plan<T, true>::kStages, kRun = run_tokens<T, true>(), LANES = lanes_of<T>(), kSlab = slab_of<T>();
+    constexpr uint32_t kTile = tile_bytes<T, true>(), kRow = kSlab * sizeof(T);
+    extern __shared__ __align__(128) uint8_t stage[];            // [kStages][r, dout, g, x, out of the token before][kRun][kSlab]
+    __shared__ Shared<LANES, PARTS> sm;
     begin(sm);
     enter_dependent();
-    const int tid = threadIdx.x, lane = tid & (kLanes - 1), group = tid / kLanes;
+    const int tid = threadIdx.x, lane = tid & (LANES - 1), group = tid / LANES;
     const int rank = PARTS > 1 ? (int)cluster_rank() : 0;
     const int work = blockIdx.x / PARTS, b = work / slabs, slab0 = (work - b * slabs) * kSlab, c0 = slab0 + lane * kV;
     const bool mine = c0 < C;
     const int steps = (int)(((long long)N + kRun * PARTS - 1) / (kRun * PARTS));
 
     auto fetch = [&](int s) {
-        const int st = s % 3;
+        const int st = s % kStages;
         uint8_t* to = stage + st * 5 * kTile;
         const int t0 = (int)(N - (s * (long long)PARTS + rank + 1) * kRun);       // (may be below 0: rows before the sequence read as 0)
         mbar_arrive_expect_tx(&sm.full[st], 5 * kTile);
@@ -400,10 +456,8 @@ __global__ void __launch_bounds__(kThreads, 4)
         tma_load_3d(to + 3 * kTile, &maps.x, &sm.full[st], slab0, t0, b);
         tma_load_3d(to + 4 * kTile, &maps.out, &sm.full[st], slab0, t0 - 1, b);
     };
-    if (tid == 0) {
-        fetch(0);
-        if (steps > 1) fetch(1);
-    }
+    if (tid == 0)
+        for (int s = 0; s < kStages - 1 && s < steps; ++s) fetch(s);
     pair nrate[kP] = {0, 0}, E[kP] = {0, 0}, drate[kP] = {0, 0};
     if (mine) {
         load_f32<kP>(rate + c0, nrate);
@@ -411,18 +465,17 @@ __global__ void __launch_bounds__(kThreads, 4)
         nrate[1] = neg2(nrate[1]);
         if (dstate_out) load_f32<kP>(dstate_out + (size_t)b * C + c0, E);
     }
-    const bool small = all_small(nrate);
     const size_t base = (size_t)b * N * C + c0;
     bool ok = true;
-    for (int s = 0; s < steps; ++s) {
-        ok = mbar_wait(&sm.full[s % 3], (s / 3) & 1, &sm.abort_flag) && ok;
-        // the thread's tokens t0, t0 - 1, ...
-        const uint8_t* from = stage + (s % 3) * 5 * kTile + (kRun - 1 - group * TOK) * kRow + lane * kV * sizeof(T);
-        const long long t0 = N - 1 - ((s * (long long)PARTS + rank) * kRun + group * TOK);
-        pair p[TOK][kP], sg[TOK][kP];                            // a_t - 1, sigmoid(r_t)
-        pair A[kP] = {both(1.f), both(1.f)}, H[kP] = {0, 0}, first[kP];
-        auto load = [&](auto small_tag) {
-            constexpr bool SMALL = decltype(small_tag)::value;
+    auto walk = [&](auto small_tag) {
+        constexpr bool SMALL = decltype(small_tag)::value;
+        for (int s = 0; s < steps; ++s) {
+            ok = mbar_wait(&sm.full[s % kStages], (s / kStages) & 1, &sm.abort_flag) && ok;
+            // the thread's tokens t0, t0 - 1, ...
+            const uint8_t* from = stage + (s % kStages) * 5 * kTile + (kRun - 1 - group * TOK) * kRow + lane * kV * sizeof(T);
+            const long long t0 = N - 1 - ((s * (long long)PARTS + rank) * kRun + group * TOK);
+            pair p[TOK][kP], sg[TOK][kP];                        // a_t - 1, sigmoid(r_t)
+            pair A[kP] = {both(1.f), both(1.f)}, H[kP] = {0, 0}, first[kP];
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
                 pair rv[kP], dv[kP];
@@ -430,67 +483,71 @@ __global__ void __launch_bounds__(kThreads, 4)
                 values4<T>(from + kTile - j * kRow, dv);
 #pragma unroll
                 for (int e = 0; e < kP; ++e) {
-                    sg[j][e] = rcp2(one_plus_exp_neg(rv[e]));
-                    p[j][e] = exp_less_one<SMALL>(mul2(nrate[e], sg[j][e]));
+                    sg[j][e] = sigmoid(rv[e]);
+                    const pair la = mul2(nrate[e], sg[j][e]);
+                    p[j][e] = SMALL ? mul2(la, slope(la)) : exp_less_one(la);
                     if (t0 - j < 0) p[j][e] = 0;                 // (before the sequence nothing happens)
                     const pair a = add2(p[j][e], both(1.f));
                     H[e] = mul2(a, add2(H[e], dv[e]));
                     A[e] = mul2(A[e], a);
                 }
             }
-        };
-        if (small) load(std::true_type{});
-        else load(std::false_type{});
-        ok = join<PARTS>(sm, s, rank, A, H, E, first, [&] {      // (the stage of the step before has been read)
-            if (tid == 0 && s + 2 < steps) fetch(s + 2);
-        }) && ok;
+            ok = join<LANES, PARTS>(sm, s, rank, A, H, E, first, [&] {      // (the stage of the step before has been read)
+                if (tid == 0 && s + kStages - 1 < steps) fetch(s + kStages - 1);
+            }) && ok;
 #pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-            pair dv[kP], gv[kP], xv[kP], hv[kP], ox[kP], orr[kP], og[kP];
-            values4<T>(from + kTile - j * kRow, dv);
-            gate4<T>(from + 2 * kTile - j * kRow, gv);
-            values4<T>(from + 3 * kTile - j * kRow, xv);
-            values4<T>(from + 4 * kTile - j * kRow, hv);
-            const bool in = mine && t0 - j >= 0;
-            if (in && t0 - j == 0 && state_in) load_f32<kP>(state_in + (size_t)b * C + c0, hv);
+            for (int j = 0; j < TOK; ++j) {
+                pair dv[kP], gv[kP], xv[kP], hv[kP], ox[kP], orr[kP], og[kP];
+                values4<T>(from + kTile - j * kRow, dv);
+                gate4<T>(from + 2 * kTile - j * kRow, gv);
+                values4<T>(from + 3 * kTile - j * kRow, xv);
+                values4<T>(from + 4 * kTile - j * kRow, hv);
+                const bool in = mine && t0 - j >= 0;
+                if (in && t0 - j == 0 && state_in) load_f32<kP>(state_in + (size_t)b * C + c0, hv);
 #pragma unroll
-            for (int e = 0; e < kP; ++e) {
-                const pair G = add2(dv[e], first[e]), a = add2(p[j][e], both(1.f));
-                const pair i = rcp2(one_plus_exp_neg(gv[e]));
-                const pair m2 = one_less_square(p[j][e]);
-                const float2 f = split(m2);
-                // 1 / m; where nothing decays (m = 0) a number so large that products with it stay finite
-                const pair im = make(rroot(max_nan(f.x, 1e-36f)), rroot(max_nan(f.y, 1e-36f)));
-                const pair Gi = mul2(G, i), Gix = mul2(Gi, xv[e]), m = mul2(m2, im);
-                ox[e] = mul2(Gi, m);
-                og[e] = mul2(mul2(Gix, m), fma2(i, both(-1.f), both(1.f)));
-                // -dlog a = a (a / m G i x - G h)
-                first[e] = mul2(a, G);
-                const pair nd = fma2(mul2(a, a), mul2(im, Gix), neg2(mul2(first[e], hv[e])));
-                const pair ds = mul2(nd, sg[j][e]);
-                if (in) drate[e] = add2(drate[e], ds);
-                orr[e] = mul2(mul2(nrate[e], ds), fma2(sg[j][e], both(1.f), both(-1.f)));
-            }
-            if (in) {
-                const size_t at = base + (size_t)(t0 - j) * C;
-                write4<T>(dx + at, ox);
-                write4<T>(dr + at, orr);
-                write4<T>(dg + at, og);
+                for (int e = 0; e < kP; ++e) {
+                    const pair a = add2(p[j][e], both(1.f)), i = sigmoid(gv[e]), m2 = one_less_square(p[j][e]);
+                    const float2 f = split(m2);
+                    // 1 / m; where nothing decays (m = 0) a number so large that products with it stay finite
+                    const pair im = make(rroot(max_nan(f.x, 1e-36f)), rroot(max_nan(f.y, 1e-36f))), m = mul2(m2, im);
+                    const pair G = add2(dv[e], first[e]), Gi = mul2(G, i), Gix = mul2(Gi, xv[e]);
+                    ox[e] = mul2(Gi, m);
+                    og[e] = mul2(mul2(Gix, m), fma2(i, both(-1.f), both(1.f)));
+                    // -dlog a = a^2 / m G i x - a G h
+                    first[e] = mul2(a, G);
+                    const pair nd = fma2(mul2(a, a), mul2(im, Gix), neg2(mul2(first[e], hv[e])));
+                    const pair ds = mul2(nd, sg[j][e]);
+                    if (in) drate[e] = add2(drate[e], ds);
+                    orr[e] = mul2(mul2(nrate[e], ds), fma2(sg[j][e], both(1.f), both(-1.f)));
+                }
+                if (in) {
+                    const size_t at = base + (size_t)(t0 - j) * C;
+                    write4<T>(dx + at, ox);
+                    write4<T>(dr + at, orr);
+                    write4<T>(dg + at, og);
+                }
             }
         }
-    }
+    };
+    if (all_small(nrate)) walk(std::true_type{});
+    else walk(std::false_type{});
     if (dstate_in && mine && rank == 0 && group == 0) store_f32<kP>(dstate_in + (size_t)b * C + c0, E);
     // drate over the CTA's tokens: the warp's groups, then the warps
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
-        drate[e] = add2(drate[e], __shfl_xor_sync(0xffffffffu, drate[e], kLanes));
-        if ((tid & 31) < kLanes) sm.sums[tid >> 5][e][lane] = drate[e];
+#pragma unroll
+        for (int d = LANES; d < 32; d *= 2) drate[e] = add2(drate[e], __shfl_xor_sync(0xffffffffu, drate[e], d));
+        if ((tid & 31) < LANES) sm.sums[tid >> 5][e][lane] = drate[e];
     }
     __syncthreads();
     if (group == 0 && mine) {
         pair t[kP];
 #pragma unroll
-        for (int e = 0; e < kP; ++e) t[e] = add2(add2(sm.sums[0][e][lane], sm.sums[1][e][lane]), add2(sm.sums[2][e][lane], sm.sums[3][e][lane]));
+        for (int e = 0; e < kP; ++e) {
+            t[e] = sm.sums[0][e][lane];
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) t[e] = add2(t[e], sm.sums[w][e][lane]);
+        }
         store_f32<kP>(part + ((size_t)b * PARTS + rank) * C + c0, t);
     }
     finish(sm, ok, err);
@@ -517,25 +574,30 @@ __global__ void __launch_bounds__(kThreads)
     Four<T>::values(xu, xv);
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
-        const pair er = one_plus_exp_neg(rv[e]), eg = one_plus_exp_neg(gv[e]), q = rcp2(mul2(er, eg));
-        const pair p = exp_less_one<false>(mul2(neg2(nrate[e]), mul2(q, eg)));
-        const float2 m2 = split(one_less_square(p));
-        h[e] = fma2(add2(p, both(1.f)), h[e], mul2(make(root(m2.x), root(m2.y)), mul2(mul2(q, er), xv[e])));
+        pair a, u;
+        token<false>(gates(rv[e], gv[e]), neg2(nrate[e]), 0, xv[e], a, u);
+        h[e] = fma2(a, h[e], u);
     }
     if (state_out) store_f32<kP>(state_out + i * kV, h);
     write4<T>(out + i * kV, h);
 }
 
 namespace {
-constexpr int kTokForward = 8, kTokBackward = 4;
-
-// CTAs per sequence and slab
-int parts_for(long long units, int N, int tok) {
+// CTAs per sequence and slab: as many as are resident at once and the sequence has runs for (each goes along its whole sequence, so
+// a second wave would run with the chip half empty)
+int parts_for(long long units, long long runs, int blocks) {
     int parts = 1;
-    while (parts < 8 && units * parts < 4 * kSMs && (long long)parts * kGroups * tok < N) parts *= 2;
+    while (parts < 8 && units * parts * 2 <= (long long)blocks * kSMs && 2 * parts <= runs) parts *= 2;
     return parts;
 }
-int slabs_of(int C) { return (int)(((long long)C + kSlab - 1) / kSlab); }
+template <typename T> int slabs_of(int C) { return (int)(((long long)C + slab_of<T>() - 1) / slab_of<T>()); }
+template <typename T, bool BACK> int parts_of(int B, int N, int C) {
+    constexpr int run = run_tokens<T, BACK>();
+    return parts_for((long long)B * slabs_of<T>(C), ((long long)N + run - 1) / run, Plan<T, BACK>::kBlocks);
+}
+// Whether a launch comes in while the grid ahead drains: only one that finds room beside another like it.  A larger one would crowd on the
+// SMs that the grid ahead leaves first and stay there to its end (B8 N4096 C2048 behind itself 159 us for 122, B1 N32768 C1000 176 for 127).
+template <typename T, bool BACK> bool beside(long long ctas) { return 2 * ctas <= (long long)Plan<T, BACK>::kBlocks * kSMs; }
 template <typename K> cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[64]) {
     int dev = 0;
     const cudaError_t e = cudaGetDevice(&dev);
@@ -558,22 +620,22 @@ template <typename T>
 based_status forward_t(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, void* out,
                        float* state_out, int B, int N, int C, cudaStream_t stream) {
     constexpr bool f32 = sizeof(T) == 4;
-    const int slabs = slabs_of(C);
+    const int slabs = slabs_of<T>(C);
     RecurrenceMaps maps;
     unsigned int* err = nullptr;
-    constexpr int run = run_tokens<kTokForward>();
-    if (!make_tokens_map(&maps.r, r, f32, B, N, C, kSlab, run) || !make_tokens_map(&maps.g, g, f32, B, N, C, kSlab, run) ||
-        !make_tokens_map(&maps.x, x, f32, B, N, C, kSlab, run) || error_word_ptr(&err) != BASED_OK)
+    constexpr int run = run_tokens<T, false>();
+    if (!make_tokens_map(&maps.r, r, f32, B, N, C, slab_of<T>(), run) || !make_tokens_map(&maps.g, g, f32, B, N, C, slab_of<T>(), run) ||
+        !make_tokens_map(&maps.x, x, f32, B, N, C, slab_of<T>(), run) || error_word_ptr(&err) != BASED_OK)
         return BASED_ERR_CUDA;
     maps.dout = maps.out = maps.x;
-    return with_parts(parts_for((long long)B * slabs, N, kTokForward), [&](auto tag) {
+    return with_parts(parts_of<T, false>(B, N, C), [&](auto tag) {
         constexpr int PARTS = decltype(tag)::value;
         static std::atomic<bool> ready[64];
-        constexpr size_t smem = 2 * 3 * tile_bytes<T, kTokForward>();
-        auto kernel = gated_recurrence_kernel<T, kTokForward, PARTS>;
+        constexpr size_t smem = Plan<T, false>::kStages * 3 * tile_bytes<T, false>();
+        auto kernel = gated_recurrence_kernel<T, PARTS>;
         cudaError_t e = allow_smem(kernel, smem, ready);
         if (e == cudaSuccess)
-            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, true, stream, maps, rate,
+            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, beside<T, false>((long long)B * slabs * PARTS), stream, maps, rate,
                           state_in, static_cast<T*>(out), state_out, err, N, C, slabs);
         note_launch();
         const based_status st = check_launch("gated_recurrence_kernel");
@@ -585,22 +647,22 @@ based_status backward_t(const Tokens& x, const Tokens& r, const Tokens& g, const
                         const Tokens& dout, const float* dstate_out, void* dx, void* dr, void* dg, float* drate, float* dstate_in, int B,
                         int N, int C, float* part, cudaStream_t stream) {
     constexpr bool f32 = sizeof(T) == 4;
-    const int slabs = slabs_of(C), parts = parts_for((long long)B * slabs, N, kTokBackward);
+    const int slabs = slabs_of<T>(C), parts = parts_of<T, true>(B, N, C);
     RecurrenceMaps maps;
     unsigned int* err = nullptr;
-    constexpr int run = run_tokens<kTokBackward>();
-    if (!make_tokens_map(&maps.r, r, f32, B, N, C, kSlab, run) || !make_tokens_map(&maps.g, g, f32, B, N, C, kSlab, run) ||
-        !make_tokens_map(&maps.x, x, f32, B, N, C, kSlab, run) || !make_tokens_map(&maps.out, out, f32, B, N, C, kSlab, run) ||
-        !make_tokens_map(&maps.dout, dout, f32, B, N, C, kSlab, run) || error_word_ptr(&err) != BASED_OK)
+    constexpr int run = run_tokens<T, true>();
+    if (!make_tokens_map(&maps.r, r, f32, B, N, C, slab_of<T>(), run) || !make_tokens_map(&maps.g, g, f32, B, N, C, slab_of<T>(), run) ||
+        !make_tokens_map(&maps.x, x, f32, B, N, C, slab_of<T>(), run) || !make_tokens_map(&maps.out, out, f32, B, N, C, slab_of<T>(), run) ||
+        !make_tokens_map(&maps.dout, dout, f32, B, N, C, slab_of<T>(), run) || error_word_ptr(&err) != BASED_OK)
         return BASED_ERR_CUDA;
     const based_status st = with_parts(parts, [&](auto tag) {
         constexpr int PARTS = decltype(tag)::value;
         static std::atomic<bool> ready[64];
-        constexpr size_t smem = 3 * 5 * tile_bytes<T, kTokBackward>();
-        auto kernel = gated_recurrence_backward_kernel<T, kTokBackward, PARTS>;
+        constexpr size_t smem = Plan<T, true>::kStages * 5 * tile_bytes<T, true>();
+        auto kernel = gated_recurrence_backward_kernel<T, PARTS>;
         cudaError_t e = allow_smem(kernel, smem, ready);
         if (e == cudaSuccess)
-            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, true, stream, maps, rate,
+            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, beside<T, true>((long long)B * slabs * PARTS), stream, maps, rate,
                           state_in, dstate_out, static_cast<T*>(dx), static_cast<T*>(dr), static_cast<T*>(dg), part, dstate_in, err, N, C,
                           slabs);
         note_launch();
@@ -612,12 +674,12 @@ based_status backward_t(const Tokens& x, const Tokens& r, const Tokens& g, const
 }
 }  // namespace
 
-long long gated_recurrence_blocks(int B, int N, int C) {
-    const long long units = (long long)B * slabs_of(C);
-    return units * (N > 1 ? parts_for(units, N, kTokBackward) : 1);
+long long gated_recurrence_blocks(int B, int C, based_dtype io) {
+    return io == BASED_F32 ? (long long)B * slabs_of<float>(C) * 8 : (long long)B * slabs_of<__nv_bfloat16>(C) * 8;
 }
-size_t gated_recurrence_backward_bytes(int B, int N, int C) {
-    return (size_t)B * parts_for((long long)B * slabs_of(C), N, kTokBackward) * C * sizeof(float);
+size_t gated_recurrence_backward_bytes(int B, int N, int C, based_dtype io) {
+    const int parts = io == BASED_F32 ? parts_of<float, true>(B, N, C) : parts_of<__nv_bfloat16, true>(B, N, C);
+    return (size_t)B * parts * C * sizeof(float);
 }
 
 based_status launch_gated_recurrence(const Tokens& x, const Tokens& r, const Tokens& g, const float* rate, const float* state_in, void* out,
