@@ -28,6 +28,7 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "pairs.cuh"
 #include "sm100.cuh"
 
 namespace based {
@@ -61,8 +62,7 @@ constexpr uint32_t colX = 0, colAcc = 256;
 template <int PAD> constexpr uint32_t colDQ = PAD == 64 ? 192 : 0;   // PAD 128: over dP once that is read
 
 enum Bar {
-    bFullQ = 0, bEmptyQ = 2, bFullKV = 4, bEmptyKV = 10, bS = 16, bSread, bDP, bP, bPdone, bPS, bPSfree, bDQ, bDQfree, bAccFull, bAccFree = bAccFull + 2,
-    bCount = bAccFree + 2
+    bFullQ = 0, bEmptyQ = 2, bFullKV = 4, bEmptyKV = 10, bS = 16, bSread, bDP, bP, bPdone, bPS, bDone, bDQfree, bAccFree, bCount = bAccFree + 2
 };
 static_assert(bCount * 8 + 8 <= 256, "barrier area");
 
@@ -91,7 +91,6 @@ __device__ __forceinline__ bool pair_all(int id, bool pred) {
 
 struct Params {
     unsigned int* err;
-    __nv_bfloat16 *dq, *dk, *dv;
     int L, window, tiles_per_head, total_tiles;
     float scale, scale_log2e;
 };
@@ -122,42 +121,23 @@ struct Run {
     }
 };
 
-// 32 rows of 64 fp32 values in TMEM (a row per lane) to bf16 rows of 128 bytes in memory.  8 lanes exchange their 16-byte chunks so
-// that a store writes whole rows.  row0: the warp's first row (may lie outside [0, L))
-__device__ __forceinline__ void store_rows(uint32_t taddr, __nv_bfloat16* base, long long row0, int L, int lane) {
-    uint32_t c[8][4];
-    {
+// 32 rows of 64 fp32 values in TMEM (a row per lane) to bf16 rows of 128 bytes in shared memory, swizzled as the TMA store reads them
+__device__ __forceinline__ void stage_rows(uint32_t taddr, uint8_t* tile, int lane) {
+    uint8_t* row = tile + (lane >> 3) * 1024 + (lane & 7) * 128;
+    const uint32_t sw = lane & 7;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
         uint32_t t[32];
-        tmem_ld32(taddr, t);
+        tmem_ld32(taddr + 32 * h, t);
         tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) c[k >> 2][k & 3] = pack2(__uint_as_float(t[2 * k]), __uint_as_float(t[2 * k + 1]));
-        tmem_ld32(taddr + 32, t);
-        tmem_wait_ld();
+        for (int j = 0; j < 4; ++j) {
+            uint32_t w[4];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) c[4 + (k >> 2)][k & 3] = pack2(__uint_as_float(t[2 * k]), __uint_as_float(t[2 * k + 1]));
-    }
-#pragma unroll
-    for (int b = 1; b < 8; b *= 2) {
-        const bool up = lane & b;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (k & b) continue;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? c[k][w] : c[k | b][w], b);
-                if (up) c[k][w] = got;
-                else c[k | b][w] = got;
-            }
+            for (int k = 0; k < 4; ++k) w[k] = pack2(__uint_as_float(t[8 * j + 2 * k]), __uint_as_float(t[8 * j + 2 * k + 1]));
+            *reinterpret_cast<uint4*>(row + (((uint32_t)(4 * h + j) ^ sw) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    // lane (8 u + v) now holds chunk v of rows 8 u .. 8 u + 7
-    const long long r0 = row0 + (lane & 24);
-    __nv_bfloat16* to = base + r0 * kHD + (lane & 7) * 8;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (r0 + k >= 0 && r0 + k < L)
-            __stcs(reinterpret_cast<uint4*>(to + k * kHD), make_uint4(c[k][0], c[k][1], c[k][2], c[k][3]));
 }
 
 }  // namespace
@@ -165,7 +145,9 @@ __device__ __forceinline__ void store_rows(uint32_t taddr, __nv_bfloat16* base, 
 template <int PAD>
 __global__ void __launch_bounds__(kThreads, 1)
     swa_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                           const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o, const Params p) {
+                           const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
+                           const __grid_constant__ CUtensorMap tm_dq, const __grid_constant__ CUtensorMap tm_dk,
+                           const __grid_constant__ CUtensorMap tm_dv, const Params p) {
     using C = Cfg<PAD>;
     constexpr int NH = C::kHalves, NS = C::kSlots, NC = C::kCols;
     extern __shared__ uint8_t smem_raw[];
@@ -178,14 +160,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int N = run.count;
 
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(&bars[bFullQ + s], 1); mbar_init(&bars[bEmptyQ + s], 1);
-            mbar_init(&bars[bAccFull + s], 1); mbar_init(&bars[bAccFree + s], 128);
-        }
+        for (int s = 0; s < 2; ++s) { mbar_init(&bars[bFullQ + s], 1); mbar_init(&bars[bEmptyQ + s], 4); mbar_init(&bars[bAccFree + s], 128); }
         for (int s = 0; s < NS; ++s) { mbar_init(&bars[bFullKV + s], 1); mbar_init(&bars[bEmptyKV + s], 1); }
         mbar_init(&bars[bS], 1); mbar_init(&bars[bSread], 256); mbar_init(&bars[bDP], 1);
-        mbar_init(&bars[bP], 256); mbar_init(&bars[bPdone], 1); mbar_init(&bars[bPS], 256); mbar_init(&bars[bPSfree], 1);
-        mbar_init(&bars[bDQ], 1); mbar_init(&bars[bDQfree], 128);
+        mbar_init(&bars[bP], 256); mbar_init(&bars[bPdone], 1); mbar_init(&bars[bPS], 256);
+        mbar_init(&bars[bDone], 1); mbar_init(&bars[bDQfree], 128);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v); prefetch_tensormap(&tm_o);
@@ -253,8 +232,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!mbar_wait(&bars[bFullQ + (n & 1)], (n >> 1) & 1, abort_flag)) return false;
             for (int j = 0; j < NH; ++j)
                 if (!mbar_wait(&bars[bFullKV + (hb + j) % NS], ((hb + j) / NS) & 1, abort_flag)) return false;
-            if (PAD == 128 && n > run.halo)                          // dQ of the tile before lies over the scores
-                if (!mbar_wait(&bars[bDQfree], (n - run.halo - 1) & 1, abort_flag)) return false;
+            if (PAD == 128 && n > 0)                                 // dQ of the tile before lies over the scores
+                if (!mbar_wait(&bars[bDQfree], (n - 1) & 1, abort_flag)) return false;
             tc_fence_after();
             scores(qo(n), 0);
             mma_commit_w(lead, &bars[bS]);
@@ -278,117 +257,137 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         auto acc_col = [&](int a, int which) { return tb + colAcc + 128 * a + 64 * which; };     // 0: dK, 1: dV
         auto free_acc = [&](int a) { return uses[a] == 0 || mbar_wait(&bars[bAccFree + a], (uses[a] - 1) & 1, abort_flag); };
-        if (N > 0) ok = issue_s(0);
-        for (int n = 0; n < N && ok; ++n) {
-            const Tile t = run.tile(n);
-            const bool with_b = !t.end || t.last;                    // the next block is this run's too
-            ok = mbar_wait(&bars[bSread], n & 1, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            scores(qo(n) + kTileBytes, kHalfBytes);
-            mma_commit_w(lead, &bars[bDP]);
+        // step -1 only asks for the first scores; step n asks for tile n's dP, its gradients and the next tile's scores
+#pragma unroll 1
+        for (int n = -1; n < N && ok; ++n) {
+            Tile t{};
+            bool with_b = false, early = true;
+            if (n >= 0) {
+                t = run.tile(n);
+                with_b = !t.end || t.last;                           // the next block is this run's too
+                early = PAD == 64 && !t.end && !t.last;              // (a new head's halves wait for this tile's slots)
+                ok = mbar_wait(&bars[bSread], n & 1, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                scores(qo(n) + kTileBytes, kHalfBytes);
+                mma_commit_w(lead, &bars[bDP]);
+            }
             const uint32_t sQ = qo(n), sO = sQ + kTileBytes, sP = sm + C::offP, sD = sm + C::offD;
             auto begin_sets = [&]() -> bool {                        // the sets that this tile's products begin must have been read
                 if (!t.halo && t.first && !free_acc(acc)) return false;
-                if (with_b && !free_acc(acc ^ 1)) return false;
-                return true;
+                return !with_b || free_acc(acc ^ 1);
             };
-            auto products = [&](uint32_t x, uint32_t y, int which) {
-                if (!t.halo) block_a(x, y, acc_col(acc, which), t.first);
-                if (with_b) block_b(x, y, acc_col(acc ^ 1, which));
-            };
-            if constexpr (C::kShared) {
-                ok = mbar_wait(&bars[bP], n & 1, abort_flag) && begin_sets();
-                if (!ok) break;
-                tc_fence_after();
-                products(sP, sO, 1);
-                mma_commit_w(lead, &bars[bPdone]);
-            }
-            ok = mbar_wait(&bars[bPS], n & 1, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            const bool early = PAD == 64 && !t.end && !t.last;       // (a new head's halves wait for this tile's slots)
-            if (early) {
-                hb += 2;
-                ok = issue_s(n + 1);
-                hb -= 2;
-                if (!ok) break;
-            }
-            if (!t.halo) {
-                if (n > run.halo) ok = mbar_wait(&bars[bDQfree], (n - run.halo - 1) & 1, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t d = tb + colDQ<PAD>;
-                for (int j = 0; j < NH; ++j) {
-                    const uint32_t la = lo(d1, sD + C::block(j)), lb = lo(d1, kv(j));
-                    if (j == 0) mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
-                    else mma_ss_w<true>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
-#pragma unroll
-                    for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 128, desc_hi(d1), iQ);
+            // dV, or dV and dK
+            auto products = [&](int from, int to) {
+#pragma unroll 1
+                for (int which = from; which >= to; --which) {
+                    const uint32_t x = which ? sP : sD, y = which ? sO : sQ;
+                    if (!t.halo) block_a(x, y, acc_col(acc, which), t.first);
+                    if (with_b) block_b(x, y, acc_col(acc ^ 1, which));
                 }
-                mma_commit_w(lead, &bars[bDQ]);
+            };
+            if (n >= 0) {
+                if constexpr (C::kShared) {
+                    ok = mbar_wait(&bars[bP], n & 1, abort_flag) && begin_sets();
+                    if (!ok) break;
+                    tc_fence_after();
+                    products(1, 1);
+                    mma_commit_w(lead, &bars[bPdone]);
+                }
+                ok = mbar_wait(&bars[bPS], n & 1, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
             }
             const int drop = t.last ? NH : 2;                        // halves that the next tile does not use
-            for (int j = 0; j < drop; ++j) mma_commit_w(lead, &bars[bEmptyKV + (hb + j) % NS]);
-            if constexpr (!C::kShared) {
-                ok = begin_sets();
+#pragma unroll 1
+            for (int turn = 0; turn < 2 && ok; ++turn) {
+                if ((turn == 0) == early) {
+                    if (n + 1 >= N) continue;
+                    const int kept = hb;
+                    if (n >= 0 && early) hb += drop;
+                    ok = issue_s(n + 1);
+                    hb = kept;
+                    continue;
+                }
+                if (n < 0) continue;
+                // (also what keeps a tile's end from being told before the end of the tile before it was seen)
+                if (n > 0) ok = mbar_wait(&bars[bDQfree], (n - 1) & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                products(sP, sO, 1);
+                if (!t.halo) {
+                    const uint32_t d = tb + colDQ<PAD>;
+#pragma unroll
+                    for (int j = 0; j < NH; ++j) {
+                        const uint32_t la = lo(d1, sD + C::block(j)), lb = lo(d1, kv(j));
+                        if (j == 0) mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
+                        else mma_ss_w<true>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
+#pragma unroll
+                        for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 128, desc_hi(d1), iQ);
+                    }
+                }
+                for (int j = 0; j < drop; ++j) mma_commit_w(lead, &bars[bEmptyKV + (hb + j) % NS]);
+                if constexpr (!C::kShared) {
+                    ok = begin_sets();
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                products(C::kShared ? 0 : 1, 0);
+                mma_commit_w(lead, &bars[bDone]);
+                if (!t.halo && t.first) ++uses[acc];
+                if (with_b) ++uses[acc ^ 1];
+                if (!early) {                                        // (what follows is the next tile's)
+                    hb += drop;
+                    if (!t.last) acc ^= 1;
+                }
             }
-            products(sD, sQ, 0);
-            if (!t.halo) {
-                if (t.first) ++uses[acc];
-                mma_commit_w(lead, &bars[bAccFull + acc]);
+            if (n >= 0 && early) {
+                hb += drop;
+                if (!t.last) acc ^= 1;
             }
-            if (with_b) {
-                ++uses[acc ^ 1];
-                if (t.last) mma_commit_w(lead, &bars[bAccFull + (acc ^ 1)]);
-            }
-            mma_commit_w(lead, &bars[bEmptyQ + (n & 1)]);
-            mma_commit_w(lead, &bars[bPSfree]);
-            hb += drop;
-            if (!t.last) acc ^= 1;
-            if (!early && !t.end) ok = issue_s(n + 1);
         }
     } else if (warp >= kWarpOut) {
-        // ---- results: four warps, a TMEM lane per thread
+        // ---- results: four warps, a TMEM lane per thread.  Once a tile's products are done its slot of Q and dO holds the results on
+        // their way out (32 rows of two of them per warp); then it goes back to the loads
         const int u = warp & 3;
         const uint32_t lanes = (uint32_t)u * 32u;
-        int acc = 0, uses[2] = {0, 0}, nq = 0;
-        auto take = [&](int bar, uint32_t phase) {
-            ok = __all_sync(0xffffffffu, mbar_wait(&bars[bar], phase, abort_flag));
-            if (ok) tc_fence_after();
-            return ok;
-        };
-        // rows of a key block: lanes 0 .. 63 hold its keys 64 .. 127 and the other way round
-        auto keys_out = [&](int a, const Tile& t, int block) -> bool {
-            if (!take(bAccFull + a, (uses[a] - 1) & 1)) return false;
-            const long long row = (long long)block * kQT - PAD + (long long)(lanes ^ 64u);
-            const size_t head = (size_t)t.head * p.L * kHD;
-            store_rows(tmem_addr(tb, lanes, colAcc + 128 * a), p.dk + head, row, p.L, lane);
-            store_rows(tmem_addr(tb, lanes, colAcc + 128 * a + 64), p.dv + head, row, p.L, lane);
-            tc_fence_before();
-            mbar_arrive(&bars[bAccFree + a]);
-            return true;
-        };
+        int acc = 0;
         for (int n = 0; n < N && ok; ++n) {
             const Tile t = run.tile(n);
-            if (!t.halo) {
-                if (!take(bDQ, nq & 1)) break;
-                ++nq;
-                store_rows(tmem_addr(tb, lanes, colDQ<PAD>), p.dq + (size_t)t.head * p.L * kHD, (long long)t.i * kQT + lanes, p.L, lane);
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars[bDone], n & 1, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            uint8_t* slot = smem + C::offQ + (n & 1) * 2 * kTileBytes + u * 4096;
+            // dQ; dK, dV of the key block that this tile completes (lanes 0 .. 63 hold its keys 64 .. 127 and the other way round); of
+            // the one behind a head's last tile
+            if (t.halo) mbar_arrive(&bars[bDQfree]);
+            const int from = t.halo ? 5 : 0, to = t.halo || !t.last ? 3 : 5;
+#pragma unroll 1
+            for (int k = from; k < to; ++k) {
+                const int a = k < 3 ? acc : acc ^ 1, value = (k == 2 || k == 4);
+                uint8_t* tile = slot + (k & 1) * kTileBytes;
+                if (k >= 2) {                                        // (the store before last has read its rows)
+                    if (lane == 0) tma_store_wait_read<1>();
+                    __syncwarp();
+                }
+                stage_rows(tmem_addr(tb, lanes, k == 0 ? colDQ<PAD> : colAcc + 128 * a + 64 * value), tile, lane);
                 tc_fence_before();
-                mbar_arrive(&bars[bDQfree]);
-                if (t.first) ++uses[acc];
-                if (!keys_out(acc, t, t.i)) break;
+                if (k == 0) mbar_arrive(&bars[bDQfree]);
+                else if (value) mbar_arrive(&bars[bAccFree + a]);
+                fence_proxy_async_smem();
+                __syncwarp();
+                const int row = k == 0 ? t.i * kQT + (int)lanes : (k < 3 ? t.i : t.i + 1) * kQT - PAD + (int)(lanes ^ 64u);
+                if (lane == 0) {
+                    if (row >= 0 && row < p.L) tma_store_3d(k == 0 ? &tm_dq : value ? &tm_dv : &tm_dk, tile, 0, row, t.head);
+                    tma_store_commit();
+                }
             }
-            if (!t.end || t.last) {
-                ++uses[acc ^ 1];
-                if (t.last && !keys_out(acc ^ 1, t, t.i + 1)) break;
+            if (lane == 0) {
+                tma_store_wait_read<0>();
+                mbar_arrive(&bars[bEmptyQ + (n & 1)]);
             }
             if (!t.last) acc ^= 1;
         }
+        if (lane == 0) tma_store_wait<0>();
     } else {
         // ---- softmax: warps u and u + 4 share the rows of TMEM lanes 32 u .. 32 u + 31, half of their columns each
         const int u = warp & 3, half = warp >> 2;
@@ -400,11 +399,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto chunk = [&](uint32_t off, int c) {
             return smem + off + C::block(c >> 6) + (r >> 3) * 1024 + (r & 7) * 128 + ((((uint32_t)c >> 3 & 7u) ^ sw) << 4);
         };
+        constexpr int NP = NC / 2;                                   // pairs of columns
         for (int n = 0; n < N; ++n) {
             const Tile t = run.tile(n);
-            // visible columns: keys i - window + 1 .. i, and none before the head
-            const int hi = r + PAD - c0;
-            const int first = max(r + PAD + 1 - p.window, PAD - t.i * kQT) - c0;
+            // visible columns: keys i - window + 1 .. i, and none before the head; a bit each
+            const int hi = r + PAD - c0, first = max(r + PAD + 1 - p.window, PAD - t.i * kQT) - c0;
+            uint32_t seen[(NC + 31) / 32];
+#pragma unroll
+            for (int b = 0; b < (NC + 31) / 32; ++b) {
+                const int x = max(first - 32 * b, 0), y = min(hi - 32 * b, 31);
+                seen[b] = x > y ? 0u : (0xffffffffu >> (31 - (y - x))) << x;
+            }
             float e[NC];
             ok = mbar_wait(&bars[bS], n & 1, abort_flag);
             __syncwarp();
@@ -422,29 +427,43 @@ __global__ void __launch_bounds__(kThreads, 1)
             float mx = -INFINITY;
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
-                e[k] = k >= first && k <= hi ? e[k] : -INFINITY;
+                e[k] = (seen[k >> 5] >> (k & 31)) & 1u ? e[k] : -INFINITY;
                 mx = fmaxf(mx, e[k]);
             }
             const float m0 = mx == -INFINITY ? 0.f : mx;             // (no key in this half)
-            float l = 0.f;
+            pairs::pair l2 = 0, ep[NP];
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                e[k] = ex2((e[k] - m0) * p.scale_log2e);
-                l += e[k];
+            for (int k = 0; k < NP; ++k) {
+                const float2 x = pairs::split(pairs::mul2(pairs::add2(pairs::make(e[2 * k], e[2 * k + 1]), pairs::both(-m0)), pairs::both(p.scale_log2e)));
+                ep[k] = pairs::make(ex2(x.x), ex2(x.y));
+                l2 = pairs::add2(l2, ep[k]);
             }
             ok = mbar_wait(&bars[bDP], n & 1, abort_flag) && ok;
-            if (n > 0) ok = mbar_wait(&bars[bPSfree], (n - 1) & 1, abort_flag) && ok;
+            if (n > 0) ok = mbar_wait(&bars[bDone], (n - 1) & 1, abort_flag) && ok;
             __syncwarp();
             tc_fence_after();
-            float w = 0.f;
+            // dP: kept where there are registers for it, else read twice
+            constexpr bool kKeep = NC <= 48;
+            pairs::pair dp[kKeep ? NP : 1], w2 = 0;
 #pragma unroll
             for (int b = 0; b < NC; b += 16) {
                 uint32_t x[16];
                 tmem_ld16(tx + b, x);
+                if constexpr (!kKeep) tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const pairs::pair y = pairs::make(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
+                    if constexpr (kKeep) dp[b / 2 + k] = y;
+                    else w2 = pairs::fma2(ep[b / 2 + k], y, w2);
+                }
+            }
+            if constexpr (kKeep) {
                 tmem_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) w = fmaf(e[b + k], __uint_as_float(x[k]), w);
+                for (int k = 0; k < NP; ++k) w2 = pairs::fma2(ep[k], dp[k], w2);
             }
+            const float2 ls = pairs::split(l2), ws = pairs::split(w2);
+            const float l = ls.x + ls.y, w = ws.x + ws.y;
             // the partner's statistics lie in the first chunk that this thread itself overwrites, and the other way round
             *reinterpret_cast<float4*>(chunk(C::offP, c1)) = make_float4(mx, l, w, 0.f);
             ok = pair_all(1 + u, ok);
@@ -454,34 +473,44 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float f0 = ex2((mx - m) * p.scale_log2e), f1 = ex2((other.x - m) * p.scale_log2e);
             const float inv = 1.f / fmaf(l, f0, other.y * f1);
             const float D = fmaf(w, f0, other.z * f1) * inv;
-            const float pf = f0 * inv, df = p.scale;
+            const pairs::pair pf = pairs::both(f0 * inv), df = pairs::both(p.scale), nD = pairs::both(-D);
+            auto packed = [](pairs::pair x) {
+                const float2 f = pairs::split(x);
+                return pack2(f.x, f.y);
+            };
+#pragma unroll
+            for (int k = 0; k < NP; ++k) ep[k] = pairs::mul2(ep[k], pf);
             if constexpr (C::kShared) {
 #pragma unroll
-                for (int b = 0; b < NC; b += 8)
-                    *reinterpret_cast<uint4*>(chunk(C::offP, c0 + b)) =
-                        make_uint4(pack2(e[b] * pf, e[b + 1] * pf), pack2(e[b + 2] * pf, e[b + 3] * pf),
-                                   pack2(e[b + 4] * pf, e[b + 5] * pf), pack2(e[b + 6] * pf, e[b + 7] * pf));
+                for (int k = 0; k < NP; k += 4)
+                    *reinterpret_cast<uint4*>(chunk(C::offP, c0 + 2 * k)) = make_uint4(packed(ep[k]), packed(ep[k + 1]), packed(ep[k + 2]), packed(ep[k + 3]));
                 fence_proxy_async_smem();
                 mbar_arrive(&bars[bP]);
                 ok = pair_all(1 + u, mbar_wait(&bars[bPdone], n & 1, abort_flag));
                 if (!ok) break;
             }
 #pragma unroll
-            for (int b = 0; b < NC; b += 16) {
+            for (int b = 0; b < NP; b += 8) {
                 uint32_t x[16];
-                tmem_ld16(tx + b, x);
-                tmem_wait_ld();
+                if constexpr (!kKeep) {
+                    tmem_ld16(tx + 2 * b, x);
+                    tmem_wait_ld();
+                }
 #pragma unroll
-                for (int g = 0; g < 16; g += 8) {
-                    uint32_t ps[4], ds[4];
+                for (int g = 0; g < 8; g += 4) {
+                    uint32_t ds[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float p0 = e[b + g + 2 * k] * pf, p1 = e[b + g + 2 * k + 1] * pf;
-                        ps[k] = pack2(p0, p1);
-                        ds[k] = pack2(p0 * df * (__uint_as_float(x[g + 2 * k]) - D), p1 * df * (__uint_as_float(x[g + 2 * k + 1]) - D));
+                        pairs::pair y;
+                        if constexpr (kKeep) y = dp[b + g + k];
+                        else y = pairs::make(__uint_as_float(x[2 * (g + k)]), __uint_as_float(x[2 * (g + k) + 1]));
+                        ds[k] = packed(pairs::mul2(pairs::mul2(ep[b + g + k], df), pairs::add2(y, nD)));
                     }
-                    if constexpr (!C::kShared) *reinterpret_cast<uint4*>(chunk(C::offP, c0 + b + g)) = make_uint4(ps[0], ps[1], ps[2], ps[3]);
-                    *reinterpret_cast<uint4*>(chunk(C::offD, c0 + b + g)) = make_uint4(ds[0], ds[1], ds[2], ds[3]);
+                    const int c = c0 + 2 * (b + g);
+                    if constexpr (!C::kShared)
+                        *reinterpret_cast<uint4*>(chunk(C::offP, c)) =
+                            make_uint4(packed(ep[b + g]), packed(ep[b + g + 1]), packed(ep[b + g + 2]), packed(ep[b + g + 3]));
+                    *reinterpret_cast<uint4*>(chunk(C::offD, c)) = make_uint4(ds[0], ds[1], ds[2], ds[3]);
                 }
             }
             tc_fence_before();
@@ -504,16 +533,15 @@ template <int PAD>
 static based_status launch_pad(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, int BH, int L,
                                int window, float scale, cudaStream_t stream) {
     using C = Cfg<PAD>;
-    CUtensorMap tq, tk, tv, to;
+    CUtensorMap tq, tk, tv, to, tdq, tdk, tdv;
     const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B;
     if (!make_rows_map_bf16(&tq, q, BH, L, kHD, kHD, kQT, s128) || !make_rows_map_bf16(&tk, k, BH, L, kHD, kHD, 64, s128) ||
-        !make_rows_map_bf16(&tv, v, BH, L, kHD, kHD, 64, s128) || !make_rows_map_bf16(&to, dout, BH, L, kHD, kHD, kQT, s128))
+        !make_rows_map_bf16(&tv, v, BH, L, kHD, kHD, 64, s128) || !make_rows_map_bf16(&to, dout, BH, L, kHD, kHD, kQT, s128) ||
+        !make_rows_map_bf16(&tdq, dq, BH, L, kHD, kHD, 32, s128) || !make_rows_map_bf16(&tdk, dk, BH, L, kHD, kHD, 32, s128) ||
+        !make_rows_map_bf16(&tdv, dv, BH, L, kHD, kHD, 32, s128))
         return BASED_ERR_CUDA;
     Params p;
     if (error_word_ptr(&p.err) != BASED_OK) return BASED_ERR_CUDA;
-    p.dq = static_cast<__nv_bfloat16*>(dq);
-    p.dk = static_cast<__nv_bfloat16*>(dk);
-    p.dv = static_cast<__nv_bfloat16*>(dv);
     p.L = L;
     p.window = window;
     p.tiles_per_head = (int)(((long long)L + kQT - 1) / kQT);
@@ -533,7 +561,7 @@ static based_status launch_pad(const void* q, const void* k, const void* v, cons
         sm_count[dev].store(sms, std::memory_order_release);
     }
     const int grid = p.total_tiles < sms ? p.total_tiles : sms;
-    const cudaError_t e = launch_ex(swa_backward_tc_kernel<PAD>, dim3(grid), dim3(kThreads), C::kSmemBytes, 1, true, stream, tq, tk, tv, to, p);
+    const cudaError_t e = launch_ex(swa_backward_tc_kernel<PAD>, dim3(grid), dim3(kThreads), C::kSmemBytes, 1, true, stream, tq, tk, tv, to, tdq, tdk, tdv, p);
     note_launch();
     const based_status st = check_launch("swa_backward_tc_kernel");
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
