@@ -45,7 +45,7 @@ template <int PAD> struct Cfg {
     static constexpr int kSlots = PAD == 64 ? 5 : 6;                 // of the ring
     static constexpr int kCols = (32 + PAD) / 2;                     // columns per softmax thread: 48 or 80
     static constexpr bool kShared = PAD == 128;                      // P and dS in one array
-    static constexpr uint32_t offQ = kSlots * 2 * kHalfBytes;        // two slots of Q, dO
+    static constexpr uint32_t offQ = kSlots * 2 * kHalfBytes;        // two slots of Q and dO
     static constexpr uint32_t offP = offQ + 4 * kTileBytes;
     static constexpr uint32_t kPBytes = PAD == 64 ? 40960 : 65536;
     static constexpr uint32_t offD = kShared ? offP : offP + kPBytes;
@@ -62,7 +62,8 @@ constexpr uint32_t colX = 0, colAcc = 256;
 template <int PAD> constexpr uint32_t colDQ = PAD == 64 ? 192 : 0;   // PAD 128: over dP once that is read
 
 enum Bar {
-    bFullQ = 0, bEmptyQ = 2, bFullKV = 4, bEmptyKV = 10, bS = 16, bSread, bDP, bP, bPdone, bPS, bDone, bDQfree, bAccFree, bCount = bAccFree + 2
+    bFullQ = 0, bFullO = 2, bEmptyO = 4, bFullKV = 6, bEmptyKV = 12, bS = 18, bSread, bDP, bP, bPdone, bPS, bDone, bDQfree, bAccFree,
+    bCount = bAccFree + 2
 };
 static_assert(bCount * 8 + 8 <= 256, "barrier area");
 
@@ -121,22 +122,30 @@ struct Run {
     }
 };
 
-// 32 rows of 64 fp32 values in TMEM (a row per lane) to bf16 rows of 128 bytes in shared memory, swizzled as the TMA store reads them
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return r != 0;
+}
+// 32 rows of 32 fp32 values in TMEM (a row per lane) to bf16 rows of 64 bytes in shared memory, swizzled as the TMA store reads them
 __device__ __forceinline__ void stage_rows(uint32_t taddr, uint8_t* tile, int lane) {
-    uint8_t* row = tile + (lane >> 3) * 1024 + (lane & 7) * 128;
-    const uint32_t sw = lane & 7;
+    uint32_t t[32];
+    tmem_ld32(taddr, t);
+    tmem_wait_ld();
+    uint8_t* row = tile + lane * 64;
+    const uint32_t sw = (lane >> 1) & 3;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t t[32];
-        tmem_ld32(taddr + 32 * h, t);
-        tmem_wait_ld();
+    for (int j = 0; j < 4; ++j) {
+        uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t w[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = pack2(__uint_as_float(t[8 * j + 2 * k]), __uint_as_float(t[8 * j + 2 * k + 1]));
-            *reinterpret_cast<uint4*>(row + (((uint32_t)(4 * h + j) ^ sw) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int k = 0; k < 4; ++k) w[k] = pack2(__uint_as_float(t[8 * j + 2 * k]), __uint_as_float(t[8 * j + 2 * k + 1]));
+        *reinterpret_cast<uint4*>(row + (((uint32_t)j ^ sw) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -160,7 +169,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int N = run.count;
 
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) { mbar_init(&bars[bFullQ + s], 1); mbar_init(&bars[bEmptyQ + s], 4); mbar_init(&bars[bAccFree + s], 128); }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&bars[bFullQ + s], 1); mbar_init(&bars[bFullO + s], 1); mbar_init(&bars[bEmptyO + s], 4);
+            mbar_init(&bars[bAccFree + s], 128);
+        }
         for (int s = 0; s < NS; ++s) { mbar_init(&bars[bFullKV + s], 1); mbar_init(&bars[bEmptyKV + s], 1); }
         mbar_init(&bars[bS], 1); mbar_init(&bars[bSread], 256); mbar_init(&bars[bDP], 1);
         mbar_init(&bars[bP], 256); mbar_init(&bars[bPdone], 1); mbar_init(&bars[bPS], 256);
@@ -196,13 +208,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tma_load_3d(st + kHalfBytes, &tm_v, &bars[bFullKV + s], 0, key, t.head);
                 }
                 if (!ok) break;
+                // Q goes where the tile before last had it, once that tile's products are done; dO once its results are out, too
                 const int s = n & 1;
-                ok = mbar_wait(&bars[bEmptyQ + s], ((n >> 1) & 1) ^ 1, abort_flag);
+                if (n >= 2) ok = mbar_wait(&bars[bDone], (n - 2) & 1, abort_flag);
                 if (!ok) break;
                 uint8_t* st = smem + C::offQ + s * 2 * kTileBytes;
-                mbar_arrive_expect_tx(&bars[bFullQ + s], 2 * kTileBytes);
+                mbar_arrive_expect_tx(&bars[bFullQ + s], kTileBytes);
                 tma_load_3d(st, &tm_q, &bars[bFullQ + s], 0, t.i * kQT, t.head);
-                tma_load_3d(st + kTileBytes, &tm_o, &bars[bFullQ + s], 0, t.i * kQT, t.head);
+                ok = mbar_wait(&bars[bEmptyO + s], ((n >> 1) & 1) ^ 1, abort_flag);
+                if (!ok) break;
+                mbar_arrive_expect_tx(&bars[bFullO + s], kTileBytes);
+                tma_load_3d(st + kTileBytes, &tm_o, &bars[bFullO + s], 0, t.i * kQT, t.head);
             }
         }
     } else if (warp == kWarpMma) {
@@ -257,21 +273,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         auto acc_col = [&](int a, int which) { return tb + colAcc + 128 * a + 64 * which; };     // 0: dK, 1: dV
         auto free_acc = [&](int a) { return uses[a] == 0 || mbar_wait(&bars[bAccFree + a], (uses[a] - 1) & 1, abort_flag); };
-        // step -1 only asks for the first scores; step n asks for tile n's dP, its gradients and the next tile's scores
+        auto issue_dp = [&](int n) -> bool {
+            if (!mbar_wait(&bars[bSread], n & 1, abort_flag) || !mbar_wait(&bars[bFullO + (n & 1)], (n >> 1) & 1, abort_flag)) return false;
+            tc_fence_after();
+            scores(qo(n) + kTileBytes, kHalfBytes);
+            mma_commit_w(lead, &bars[bDP]);
+            return true;
+        };
+        bool dp_asked = false;
+        ok = issue_s(0);
 #pragma unroll 1
-        for (int n = -1; n < N && ok; ++n) {
-            Tile t{};
-            bool with_b = false, early = true;
-            if (n >= 0) {
-                t = run.tile(n);
-                with_b = !t.end || t.last;                           // the next block is this run's too
-                early = PAD == 64 && !t.end && !t.last;              // (a new head's halves wait for this tile's slots)
-                ok = mbar_wait(&bars[bSread], n & 1, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                scores(qo(n) + kTileBytes, kHalfBytes);
-                mma_commit_w(lead, &bars[bDP]);
-            }
+        for (int n = 0; n < N && ok; ++n) {
+            const Tile t = run.tile(n);
+            const bool with_b = !t.end || t.last;                    // the next block is this run's too
+            const bool early = PAD == 64 && !t.end && !t.last;       // (a new head's halves wait for this tile's slots)
+            const int drop = t.last ? NH : 2;                        // halves that the next tile does not use
             const uint32_t sQ = qo(n), sO = sQ + kTileBytes, sP = sm + C::offP, sD = sm + C::offD;
             auto begin_sets = [&]() -> bool {                        // the sets that this tile's products begin must have been read
                 if (!t.halo && t.first && !free_acc(acc)) return false;
@@ -286,68 +302,57 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (with_b) block_b(x, y, acc_col(acc ^ 1, which));
                 }
             };
-            if (n >= 0) {
-                if constexpr (C::kShared) {
-                    ok = mbar_wait(&bars[bP], n & 1, abort_flag) && begin_sets();
-                    if (!ok) break;
-                    tc_fence_after();
-                    products(1, 1);
-                    mma_commit_w(lead, &bars[bPdone]);
-                }
-                ok = mbar_wait(&bars[bPS], n & 1, abort_flag);
+            if (!dp_asked) ok = issue_dp(n);
+            if (!ok) break;
+            if constexpr (C::kShared) {
+                ok = mbar_wait(&bars[bP], n & 1, abort_flag) && begin_sets();
                 if (!ok) break;
                 tc_fence_after();
+                products(1, 1);
+                mma_commit_w(lead, &bars[bPdone]);
             }
-            const int drop = t.last ? NH : 2;                        // halves that the next tile does not use
-#pragma unroll 1
-            for (int turn = 0; turn < 2 && ok; ++turn) {
-                if ((turn == 0) == early) {
-                    if (n + 1 >= N) continue;
-                    const int kept = hb;
-                    if (n >= 0 && early) hb += drop;
-                    ok = issue_s(n + 1);
-                    hb = kept;
-                    continue;
-                }
-                if (n < 0) continue;
-                // (also what keeps a tile's end from being told before the end of the tile before it was seen)
-                if (n > 0) ok = mbar_wait(&bars[bDQfree], (n - 1) & 1, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                if (!t.halo) {
-                    const uint32_t d = tb + colDQ<PAD>;
-#pragma unroll
-                    for (int j = 0; j < NH; ++j) {
-                        const uint32_t la = lo(d1, sD + C::block(j)), lb = lo(d1, kv(j));
-                        if (j == 0) mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
-                        else mma_ss_w<true>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
-#pragma unroll
-                        for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 128, desc_hi(d1), iQ);
-                    }
-                }
-                for (int j = 0; j < drop; ++j) mma_commit_w(lead, &bars[bEmptyKV + (hb + j) % NS]);
-                if constexpr (!C::kShared) {
-                    ok = begin_sets();
-                    if (!ok) break;
-                    tc_fence_after();
-                }
-                products(C::kShared ? 0 : 1, 0);
-                mma_commit_w(lead, &bars[bDone]);
-                if (!t.halo && t.first) ++uses[acc];
-                if (with_b) ++uses[acc ^ 1];
-                if (!early) {                                        // (what follows is the next tile's)
-                    hb += drop;
-                    if (!t.last) acc ^= 1;
-                }
-            }
-            if (n >= 0 && early) {
+            ok = mbar_wait(&bars[bPS], n & 1, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            if (early) {
                 hb += drop;
-                if (!t.last) acc ^= 1;
+                ok = issue_s(n + 1);
+                hb -= drop;
             }
+            // (also what keeps a tile's end from being told before the end of the tile before it was seen)
+            if (ok && n > 0) ok = mbar_wait(&bars[bDQfree], (n - 1) & 1, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            if (!t.halo) {
+                const uint32_t d = tb + colDQ<PAD>;
+#pragma unroll
+                for (int j = 0; j < NH; ++j) {
+                    const uint32_t la = lo(d1, sD + C::block(j)), lb = lo(d1, kv(j));
+                    if (j == 0) mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
+                    else mma_ss_w<true>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
+#pragma unroll
+                    for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 128, desc_hi(d1), iQ);
+                }
+            }
+            for (int j = 0; j < drop; ++j) mma_commit_w(lead, &bars[bEmptyKV + (hb + j) % NS]);
+            hb += drop;
+            // the next tile's dP goes ahead of this one's products where its dO is there: its softmax waits for it, nothing of this tile does
+            dp_asked = early && __all_sync(0xffffffffu, mbar_test(&bars[bFullO + ((n + 1) & 1)], ((n + 1) >> 1) & 1));
+            if (dp_asked) ok = issue_dp(n + 1);
+            if constexpr (!C::kShared) ok = ok && begin_sets();
+            if (!ok) break;
+            tc_fence_after();
+            products(C::kShared ? 0 : 1, 0);
+            mma_commit_w(lead, &bars[bDone]);
+            if (!t.halo && t.first) ++uses[acc];
+            if (with_b) ++uses[acc ^ 1];
+            if (!t.last) acc ^= 1;
+            if (!early && !t.end) ok = issue_s(n + 1);
         }
     } else if (warp >= kWarpOut) {
-        // ---- results: four warps, a TMEM lane per thread.  Once a tile's products are done its slot of Q and dO holds the results on
-        // their way out (32 rows of two of them per warp); then it goes back to the loads
+        // ---- results: four warps, a TMEM lane per thread.  Once a tile's products are done, the place of its dO holds the results on
+        // their way out (per warp two pieces of 32 rows by 32 columns in turn); then it goes back to the loads.  (Stores from registers
+        // crowd out the softmax's accesses to shared memory, whose pipe they share.)
         const int u = warp & 3;
         const uint32_t lanes = (uint32_t)u * 32u;
         int acc = 0;
@@ -356,34 +361,35 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = __all_sync(0xffffffffu, mbar_wait(&bars[bDone], n & 1, abort_flag));
             if (!ok) break;
             tc_fence_after();
-            uint8_t* slot = smem + C::offQ + (n & 1) * 2 * kTileBytes + u * 4096;
+            if (t.halo) mbar_arrive(&bars[bDQfree]);
+            uint8_t* own = smem + C::offQ + (n & 1) * 2 * kTileBytes + kTileBytes + u * 4096;
             // dQ; dK, dV of the key block that this tile completes (lanes 0 .. 63 hold its keys 64 .. 127 and the other way round); of
             // the one behind a head's last tile
-            if (t.halo) mbar_arrive(&bars[bDQfree]);
-            const int from = t.halo ? 5 : 0, to = t.halo || !t.last ? 3 : 5;
+            const int from = t.halo ? 10 : 0, to = t.halo || !t.last ? 6 : 10;
 #pragma unroll 1
-            for (int k = from; k < to; ++k) {
-                const int a = k < 3 ? acc : acc ^ 1, value = (k == 2 || k == 4);
-                uint8_t* tile = slot + (k & 1) * kTileBytes;
-                if (k >= 2) {                                        // (the store before last has read its rows)
+            for (int q = from; q < to; ++q) {
+                const int k = q >> 1, col = (q & 1) * 32, a = k < 3 ? acc : acc ^ 1;
+                const bool value = k == 2 || k == 4;
+                uint8_t* tile = own + (q & 1) * 2048;
+                if (q > 1) {                                         // (the store before last has read its rows)
                     if (lane == 0) tma_store_wait_read<1>();
                     __syncwarp();
                 }
-                stage_rows(tmem_addr(tb, lanes, k == 0 ? colDQ<PAD> : colAcc + 128 * a + 64 * value), tile, lane);
+                stage_rows(tmem_addr(tb, lanes, (k == 0 ? colDQ<PAD> : colAcc + 128 * a + 64 * value) + col), tile, lane);
                 tc_fence_before();
-                if (k == 0) mbar_arrive(&bars[bDQfree]);
-                else if (value) mbar_arrive(&bars[bAccFree + a]);
+                if (q == 1) mbar_arrive(&bars[bDQfree]);
+                else if (value && (q & 1)) mbar_arrive(&bars[bAccFree + a]);
                 fence_proxy_async_smem();
                 __syncwarp();
                 const int row = k == 0 ? t.i * kQT + (int)lanes : (k < 3 ? t.i : t.i + 1) * kQT - PAD + (int)(lanes ^ 64u);
                 if (lane == 0) {
-                    if (row >= 0 && row < p.L) tma_store_3d(k == 0 ? &tm_dq : value ? &tm_dv : &tm_dk, tile, 0, row, t.head);
+                    if (row >= 0 && row < p.L) tma_store_3d(k == 0 ? &tm_dq : value ? &tm_dv : &tm_dk, tile, col, row, t.head);
                     tma_store_commit();
                 }
             }
             if (lane == 0) {
                 tma_store_wait_read<0>();
-                mbar_arrive(&bars[bEmptyQ + (n & 1)]);
+                mbar_arrive(&bars[bEmptyO + (n & 1)]);
             }
             if (!t.last) acc ^= 1;
         }
@@ -534,11 +540,11 @@ static based_status launch_pad(const void* q, const void* k, const void* v, cons
                                int window, float scale, cudaStream_t stream) {
     using C = Cfg<PAD>;
     CUtensorMap tq, tk, tv, to, tdq, tdk, tdv;
-    const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B;
+    const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B, s64 = CU_TENSOR_MAP_SWIZZLE_64B;
     if (!make_rows_map_bf16(&tq, q, BH, L, kHD, kHD, kQT, s128) || !make_rows_map_bf16(&tk, k, BH, L, kHD, kHD, 64, s128) ||
         !make_rows_map_bf16(&tv, v, BH, L, kHD, kHD, 64, s128) || !make_rows_map_bf16(&to, dout, BH, L, kHD, kHD, kQT, s128) ||
-        !make_rows_map_bf16(&tdq, dq, BH, L, kHD, kHD, 32, s128) || !make_rows_map_bf16(&tdk, dk, BH, L, kHD, kHD, 32, s128) ||
-        !make_rows_map_bf16(&tdv, dv, BH, L, kHD, kHD, 32, s128))
+        !make_rows_map_bf16(&tdq, dq, BH, L, kHD, 32, 32, s64) || !make_rows_map_bf16(&tdk, dk, BH, L, kHD, 32, 32, s64) ||
+        !make_rows_map_bf16(&tdv, dv, BH, L, kHD, 32, 32, s64))
         return BASED_ERR_CUDA;
     Params p;
     if (error_word_ptr(&p.err) != BASED_OK) return BASED_ERR_CUDA;
