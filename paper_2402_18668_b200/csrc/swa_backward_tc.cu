@@ -42,30 +42,39 @@ constexpr int kWarpOut = 8, kWarpTma = 12, kWarpMma = 13, kThreads = 448;
 constexpr uint32_t kTileBytes = kQT * kHD * 2, kHalfBytes = 64 * kHD * 2;       // 16 KB of Q or dO, 8 KB of 64 keys or values
 template <int PAD> struct Cfg {
     static constexpr int kHalves = 2 + PAD / 64;                     // 64-key halves under a tile: 3 or 4
-    static constexpr int kSlots = PAD == 64 ? 5 : 6;                 // of the ring
+    // Rings of halves: of K all that are under a tile and two for the next; of V, whose halves are done with early, four in all
+    static constexpr int kSlotsK = kHalves + 2, kSlotsV = 4;
+    static constexpr int kSlotsQ = 3, kSlotsO = 2;                   // tiles of Q, dO
     static constexpr int kCols = (32 + PAD) / 2;                     // columns per softmax thread: 48 or 80
     static constexpr bool kShared = PAD == 128;                      // P and dS in one array
-    static constexpr uint32_t offQ = kSlots * 2 * kHalfBytes;        // two slots of Q and dO
-    static constexpr uint32_t offP = offQ + 4 * kTileBytes;
-    static constexpr uint32_t kPBytes = PAD == 64 ? 40960 : 65536;
-    static constexpr uint32_t offD = kShared ? offP : offP + kPBytes;
-    static constexpr uint32_t offBars = offD + kPBytes;
-    static constexpr uint32_t kSmemBytes = offBars + 256 + 1024;
+    static constexpr uint32_t offV = kSlotsK * kHalfBytes;
+    static constexpr uint32_t offQ = offV + kSlotsV * kHalfBytes;
+    static constexpr uint32_t offO = offQ + kSlotsQ * kTileBytes;
+    static constexpr uint32_t offP = offO + kSlotsO * kTileBytes;    // P and dS
+    static constexpr uint32_t offBars = offP + (PAD == 64 ? 73728u : 65536u);
+    static constexpr uint32_t kSmemBytes = offBars + 512 + 1024;
     static_assert(kSmemBytes <= 232448, "shared memory budget");
-    // byte offset of row 0 of the block of 64 columns cb in P or dS (PAD 64, block 2: its rows 0 .. 63 are block 0's 64 .. 127)
-    static __host__ __device__ constexpr uint32_t block(int cb) {
-        return PAD == 64 ? (cb == 1 ? 0u : cb == 0 ? 16384u : 24576u) : (cb == 1 ? 0u : cb == 0 ? 16384u : cb == 3 ? 32768u : 49152u);
+    // Byte offset from offP of row 0 of the block of 64 columns cb in P or dS.  PAD 64: block 0 has rows 0 .. 63 only and block 2 rows
+    // 64 .. 127 only; one piece of 8 KB of zeros at kZero stands for what is missing.  It lies behind dS's block 0 and before its block
+    // 2, so that dQ's products read those with their missing rows; dK's and dV's reach it by their strides.
+    static constexpr uint32_t kZero = 49152;
+    static __host__ __device__ constexpr uint32_t block(bool ds, int cb) {
+        return PAD == 64 ? (ds ? (cb == 1 ? 24576u : cb == 0 ? 40960u : 49152u) : (cb == 1 ? 0u : cb == 0 ? 16384u : 57344u))
+                         : (cb == 1 ? 0u : cb == 0 ? 16384u : cb == 3 ? 32768u : 49152u);
     }
 };
 // TMEM columns: scores (and dP after them), dQ, two sets of (dK, dV)
 constexpr uint32_t colX = 0, colAcc = 256;
 template <int PAD> constexpr uint32_t colDQ = PAD == 64 ? 192 : 0;   // PAD 128: over dP once that is read
 
-enum Bar {
-    bFullQ = 0, bFullO = 2, bEmptyO = 4, bFullKV = 6, bEmptyKV = 12, bS = 18, bSread, bDP, bP, bPdone, bPS, bDone, bDQfree, bAccFree,
-    bCount = bAccFree + 2
-};
-static_assert(bCount * 8 + 8 <= 256, "barrier area");
+// One phase per tile each, of the pairs one in two tiles (so that nobody can be a whole turn behind):
+//   bFullA  Q and the new halves of K are there      bFullB  dO and the new halves of V are there
+//   bS, bDP  scores, dP are there                    bSread, bP, bPS  scores read; P (PAD 128), P and dS written
+//   bPdone  dV's products are done (PAD 128)         bKdone  so are dQ's, and with them the use of K
+//   bDone   all products are done                    bOut    the results have been read out of tensor memory
+// and for each of the three places of Q, bEmptyQ: the results that went out through it have left.
+enum Bar { bFullA = 0, bFullB = 2, bKdone = 4, bDone = 6, bEmptyQ = 8, bS = 11, bSread, bDP, bP, bPdone, bPS, bOut, bCount };
+static_assert(bCount * 8 + 8 <= 512, "barrier area");
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -133,20 +142,23 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
         : "memory");
     return r != 0;
 }
-// 32 rows of 32 fp32 values in TMEM (a row per lane) to bf16 rows of 64 bytes in shared memory, swizzled as the TMA store reads them
-__device__ __forceinline__ void stage_rows(uint32_t taddr, uint8_t* tile, int lane) {
-    uint32_t t[32];
-    tmem_ld32(taddr, t);
-    tmem_wait_ld();
-    uint8_t* row = tile + lane * 64;
-    const uint32_t sw = (lane >> 1) & 3;
+// A row of 64 fp32 values in TMEM per lane, rounded to bf16: 8 chunks of 16 bytes
+__device__ __forceinline__ void read_rows(uint32_t taddr, uint32_t (&c)[8][4]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t w[4];
+    for (int h = 0; h < 2; ++h) {
+        uint32_t t[32];
+        tmem_ld32(taddr + 32 * h, t);
+        tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = pack2(__uint_as_float(t[8 * j + 2 * k]), __uint_as_float(t[8 * j + 2 * k + 1]));
-        *reinterpret_cast<uint4*>(row + (((uint32_t)j ^ sw) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int k = 0; k < 16; ++k) c[4 * h + (k >> 2)][k & 3] = pack2(__uint_as_float(t[2 * k]), __uint_as_float(t[2 * k + 1]));
     }
+}
+// to a piece of shared memory, swizzled as the TMA store of 32 rows reads it
+__device__ __forceinline__ void stage_rows(const uint32_t (&c)[8][4], uint8_t* tile, int lane) {
+    uint8_t* row = tile + (lane >> 3) * 1024 + (lane & 7) * 128;
+    const uint32_t sw = lane & 7;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(row + (((uint32_t)j ^ sw) << 4)) = make_uint4(c[j][0], c[j][1], c[j][2], c[j][3]);
 }
 
 }  // namespace
@@ -158,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                            const __grid_constant__ CUtensorMap tm_dq, const __grid_constant__ CUtensorMap tm_dk,
                            const __grid_constant__ CUtensorMap tm_dv, const Params p) {
     using C = Cfg<PAD>;
-    constexpr int NH = C::kHalves, NS = C::kSlots, NC = C::kCols;
+    constexpr int NH = C::kHalves, NK = C::kSlotsK, NV = C::kSlotsV, NC = C::kCols;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
@@ -169,14 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int N = run.count;
 
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(&bars[bFullQ + s], 1); mbar_init(&bars[bFullO + s], 1); mbar_init(&bars[bEmptyO + s], 4);
-            mbar_init(&bars[bAccFree + s], 128);
-        }
-        for (int s = 0; s < NS; ++s) { mbar_init(&bars[bFullKV + s], 1); mbar_init(&bars[bEmptyKV + s], 1); }
-        mbar_init(&bars[bS], 1); mbar_init(&bars[bSread], 256); mbar_init(&bars[bDP], 1);
-        mbar_init(&bars[bP], 256); mbar_init(&bars[bPdone], 1); mbar_init(&bars[bPS], 256);
-        mbar_init(&bars[bDone], 1); mbar_init(&bars[bDQfree], 128);
+        for (int s = 0; s < bCount; ++s) mbar_init(&bars[s], s == bSread || s == bP || s == bPS ? 256 : s == bOut ? 128 : s >= bEmptyQ && s < bS ? 4 : 1);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v); prefetch_tensormap(&tm_o);
@@ -193,32 +198,30 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (warp == kWarpTma) {
         if (lane == 0) {
-            int hc = 0;                                              // halves loaded so far
-            for (int n = 0; n < N && ok; ++n) {
+            int hk = 0, hv = 0;                                      // halves of K, of V loaded so far
+            for (int n = 0; n < N; ++n) {
                 const Tile t = run.tile(n);
-                const bool fresh = n == 0 || t.first;                // all halves are new, else the last two
-                for (int j = fresh ? 0 : NH - 2; j < NH && ok; ++j, ++hc) {
-                    const int s = hc % NS;
-                    ok = mbar_wait(&bars[bEmptyKV + s], ((hc / NS) & 1) ^ 1, abort_flag);
-                    if (!ok) break;
-                    uint8_t* st = smem + s * 2 * kHalfBytes;
-                    const int key = t.i * kQT - PAD + 64 * j;        // (rows outside the head read as zeros)
-                    mbar_arrive_expect_tx(&bars[bFullKV + s], 2 * kHalfBytes);
-                    tma_load_3d(st, &tm_k, &bars[bFullKV + s], 0, key, t.head);
-                    tma_load_3d(st + kHalfBytes, &tm_v, &bars[bFullKV + s], 0, key, t.head);
-                }
+                const int from = n == 0 || t.first ? 0 : NH - 2;     // (all halves are new, or the last two; rows outside the head read as zeros)
+                const int o = n & 1, key = t.i * kQT - PAD;
+                // Q and K: where tile n - 3 had its Q, tile n - 2 the halves that tile n - 1 did not use (a new head: that tile n - 1 had)
+                const int sq = n % C::kSlotsQ;
+                if (n >= C::kSlotsQ) ok = mbar_wait(&bars[bEmptyQ + sq], (n / C::kSlotsQ - 1) & 1, abort_flag);
                 if (!ok) break;
-                // Q goes where the tile before last had it, once that tile's products are done; dO once its results are out, too
-                const int s = n & 1;
-                if (n >= 2) ok = mbar_wait(&bars[bDone], (n - 2) & 1, abort_flag);
+                if (n >= 2) ok = mbar_wait(&bars[bKdone + o], ((n - 2) >> 1) & 1, abort_flag);
+                if (ok && n > 0 && t.first) ok = mbar_wait(&bars[bKdone + (o ^ 1)], ((n - 1) >> 1) & 1, abort_flag);
                 if (!ok) break;
-                uint8_t* st = smem + C::offQ + s * 2 * kTileBytes;
-                mbar_arrive_expect_tx(&bars[bFullQ + s], kTileBytes);
-                tma_load_3d(st, &tm_q, &bars[bFullQ + s], 0, t.i * kQT, t.head);
-                ok = mbar_wait(&bars[bEmptyO + s], ((n >> 1) & 1) ^ 1, abort_flag);
+                mbar_arrive_expect_tx(&bars[bFullA + o], kTileBytes + (NH - from) * kHalfBytes);
+                tma_load_3d(smem + C::offQ + sq * kTileBytes, &tm_q, &bars[bFullA + o], 0, t.i * kQT, t.head);
+                for (int j = from; j < NH; ++j, ++hk)
+                    tma_load_3d(smem + (hk % NK) * kHalfBytes, &tm_k, &bars[bFullA + o], 0, key + 64 * j, t.head);
+                // dO and V: where tile n - 2 had its dO, and once tile n - 1 is done with V
+                if (n >= 2) ok = mbar_wait(&bars[bDone + o], ((n - 2) >> 1) & 1, abort_flag);
+                if (ok && n > 0) ok = mbar_wait(&bars[bDP], (n - 1) & 1, abort_flag);
                 if (!ok) break;
-                mbar_arrive_expect_tx(&bars[bFullO + s], kTileBytes);
-                tma_load_3d(st + kTileBytes, &tm_o, &bars[bFullO + s], 0, t.i * kQT, t.head);
+                mbar_arrive_expect_tx(&bars[bFullB + o], kTileBytes + (NH - from) * kHalfBytes);
+                tma_load_3d(smem + C::offO + o * kTileBytes, &tm_o, &bars[bFullB + o], 0, t.i * kQT, t.head);
+                for (int j = from; j < NH; ++j, ++hv)
+                    tma_load_3d(smem + C::offV + (hv % NV) * kHalfBytes, &tm_v, &bars[bFullB + o], 0, key + 64 * j, t.head);
             }
         }
     } else if (warp == kWarpMma) {
@@ -226,60 +229,73 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lead = elect_one();
         constexpr uint64_t d1 = make_smem_desc_base(16, 1024, kSwizzle128B);              // K-major rows, or one MN-major block of 64
         constexpr uint64_t dA = make_smem_desc_base(16384, 1024, kSwizzle128B);           // MN-major, blocks 1 and 0 (3 and 2)
-        constexpr uint64_t dB = make_smem_desc_base(PAD == 64 ? 8192 : 16384, 1024, kSwizzle128B);   // zeros and block 2 (blocks 3, 2)
-        constexpr uint32_t iS = make_idesc_bf16(128, 64, 0, 0), iQ = make_idesc_bf16(128, 64, 0, 1), iK = make_idesc_bf16(128, 64, 1, 1);
+        constexpr uint32_t iS0 = make_idesc_bf16(128, 0, 0, 0), iQ = make_idesc_bf16(128, 64, 0, 1), iK = make_idesc_bf16(128, 64, 1, 1);
         const uint32_t sm = smem_u32(smem);
+        // (the same answer for the whole warp, and known to be: what depends on it stays in uniform registers)
+        auto wait = [&](int bar, int phase) -> bool { return __all_sync(0xffffffffu, mbar_wait(&bars[bar], phase & 1, abort_flag)); };
         auto lo = [](uint64_t base, uint32_t addr) { return desc_lo(base) + (addr >> 4); };
         int hb = 0;                                                  // the tile's first half, counted as they are loaded
-        int acc = 0, uses[2] = {0, 0};                               // the set its key block is in; times a set was begun
-        auto kv = [&](int j) { return sm + ((hb + j) % NS) * 2 * kHalfBytes; };
-        auto qo = [&](int n) { return sm + C::offQ + (n & 1) * 2 * kTileBytes; };
-        // scores or dP: rows of `a` (Q or dO) by the halves of K or V, `off` bytes into a half's slot
-        auto scores = [&](uint32_t a, uint32_t off) {
+        int acc = 0;                                                 // the set its key block is in
+        auto tile_q = [&](int n) { return sm + C::offQ + (n % C::kSlotsQ) * kTileBytes; };
+        auto tile_o = [&](int n) { return sm + C::offO + (n & 1) * kTileBytes; };
+        // scores or dP: rows of `a` (Q or dO) by the halves in a ring of NR slots, as many at a time as lie side by side: a product reads `a`
+        // once however many they are, and shared memory's bandwidth is what bounds the products
+        auto scores = [&](uint32_t a, uint32_t ring, int NR) {
             const uint32_t la = lo(d1, a);
-            for (int j = 0; j < NH; ++j) {
-                const uint32_t lb = lo(d1, kv(j) + off), d = tb + colX + 64 * j;
-                mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iS);
+            const int s0 = hb % NR, side = min(NH, NR - s0);
+#pragma unroll 1
+            for (int j = 0, count = side; j < NH; j += count, count = NH - side) {
+                const uint32_t lb = lo(d1, ring + (j == 0 ? s0 : 0) * kHalfBytes), d = tb + colX + 64 * j;
+                const uint32_t i = iS0 | (uint32_t)(8 * count) << 17;
+                mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), i);
 #pragma unroll
-                for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 2, desc_hi(d1), iS);
+                for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 2, desc_hi(d1), i);
             }
         };
         auto issue_s = [&](int n) -> bool {
-            if (!mbar_wait(&bars[bFullQ + (n & 1)], (n >> 1) & 1, abort_flag)) return false;
-            for (int j = 0; j < NH; ++j)
-                if (!mbar_wait(&bars[bFullKV + (hb + j) % NS], ((hb + j) / NS) & 1, abort_flag)) return false;
-            if (PAD == 128 && n > 0)                                 // dQ of the tile before lies over the scores
-                if (!mbar_wait(&bars[bDQfree], (n - 1) & 1, abort_flag)) return false;
+            // (PAD 128: dQ of the tile before lies over the scores)
+            if (!wait(bFullA + (n & 1), n >> 1) || (PAD == 128 && n > 0 && !wait(bOut, n - 1))) return false;
             tc_fence_after();
-            scores(qo(n), 0);
+            scores(tile_q(n), sm, NK);
             mma_commit_w(lead, &bars[bS]);
             return true;
         };
-        // X^T Y of the tile's key block A (completing its accumulators) and of block B (starting the next one's)
-        auto block_a = [&](uint32_t x, uint32_t y, uint32_t d, bool begin) {
-            const uint32_t lx = lo(dA, x), ly = lo(d1, y);
-            if (begin) mma_ss_w<false>(lead, d, lx, desc_hi(dA), ly, desc_hi(d1), iK);
-            else mma_ss_w<true>(lead, d, lx, desc_hi(dA), ly, desc_hi(d1), iK);
-#pragma unroll
-            for (int k = 1; k < 8; ++k) mma_ss_w<true>(lead, d, lx + k * 128, desc_hi(dA), ly + k * 128, desc_hi(d1), iK);
-        };
-        auto block_b = [&](uint32_t x, uint32_t y, uint32_t d) {
-            // (PAD 64: only rows 64 .. 127 see block 2; block(2) is where their zeros lie)
-            constexpr int k0 = PAD == 64 ? 4 : 0;
-            const uint32_t lx = lo(dB, x + C::block(PAD == 64 ? 2 : 3)), ly = lo(d1, y) + k0 * 128;
-            mma_ss_w<false>(lead, d, lx, desc_hi(dB), ly, desc_hi(d1), iK);
-#pragma unroll
-            for (int k = 1; k < 8 - k0; ++k) mma_ss_w<true>(lead, d, lx + k * 128, desc_hi(dB), ly + k * 128, desc_hi(d1), iK);
-        };
-        auto acc_col = [&](int a, int which) { return tb + colAcc + 128 * a + 64 * which; };     // 0: dK, 1: dV
-        auto free_acc = [&](int a) { return uses[a] == 0 || mbar_wait(&bars[bAccFree + a], (uses[a] - 1) & 1, abort_flag); };
         auto issue_dp = [&](int n) -> bool {
-            if (!mbar_wait(&bars[bSread], n & 1, abort_flag) || !mbar_wait(&bars[bFullO + (n & 1)], (n >> 1) & 1, abort_flag)) return false;
+            if (!wait(bSread, n) || !wait(bFullB + (n & 1), n >> 1)) return false;
             tc_fence_after();
-            scores(qo(n) + kTileBytes, kHalfBytes);
+            scores(tile_o(n), sm + C::offV, NV);
             mma_commit_w(lead, &bars[bDP]);
             return true;
         };
+        // X^T Y of the tile's key block A (completing its accumulators) and of block B (starting the next one's); x: offset of P or dS
+        auto part = [&](uint32_t x, uint32_t stride, uint32_t y, uint32_t d, int steps, bool begin) {
+            const uint64_t base = make_smem_desc_base(stride, 1024, kSwizzle128B);
+            const uint32_t lx = lo(base, x), ly = lo(d1, y);
+            if (begin) mma_ss_w<false>(lead, d, lx, desc_hi(dA), ly, desc_hi(d1), iK);
+            else mma_ss_w<true>(lead, d, lx, desc_hi(dA), ly, desc_hi(d1), iK);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, lx + k * 128, desc_hi(dA), ly + k * 128, desc_hi(d1), iK);
+            if (steps == 8) {
+#pragma unroll
+                for (int k = 4; k < 8; ++k) mma_ss_w<true>(lead, d, lx + k * 128, desc_hi(dA), ly + k * 128, desc_hi(d1), iK);
+            }
+        };
+        auto block_a = [&](bool ds, uint32_t y, uint32_t d, bool begin) {
+            const uint32_t x = sm + C::offP + C::block(ds, 1);
+            if constexpr (PAD == 64) {                               // rows 64 .. 127 have no block 0: zeros
+                part(x, 16384, y, d, 4, begin);
+                part(x + 8192, C::kZero - C::block(ds, 1) - 8192, y + 8192, d, 4, false);
+            } else {
+                part(x, 16384, y, d, 8, begin);
+            }
+        };
+        auto block_b = [&](bool ds, uint32_t y, uint32_t d) {
+            if constexpr (PAD == 64)                                 // only rows 64 .. 127 see block 2; no block 3: zeros
+                part(sm + C::offP + C::kZero, C::block(ds, 2) + 8192 - C::kZero, y + 8192, d, 4, true);
+            else
+                part(sm + C::offP + C::block(ds, 3), 16384, y, d, 8, true);
+        };
+        auto acc_col = [&](int a, int which) { return tb + colAcc + 128 * a + 64 * which; };     // 0: dK, 1: dV
         bool dp_asked = false;
         ok = issue_s(0);
 #pragma unroll 1
@@ -288,30 +304,25 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool with_b = !t.end || t.last;                    // the next block is this run's too
             const bool early = PAD == 64 && !t.end && !t.last;       // (a new head's halves wait for this tile's slots)
             const int drop = t.last ? NH : 2;                        // halves that the next tile does not use
-            const uint32_t sQ = qo(n), sO = sQ + kTileBytes, sP = sm + C::offP, sD = sm + C::offD;
-            auto begin_sets = [&]() -> bool {                        // the sets that this tile's products begin must have been read
-                if (!t.halo && t.first && !free_acc(acc)) return false;
-                return !with_b || free_acc(acc ^ 1);
-            };
-            // dV, or dV and dK
+            // dV, or dV and dK.  What they begin was last used by the tile before and has been read out
             auto products = [&](int from, int to) {
 #pragma unroll 1
                 for (int which = from; which >= to; --which) {
-                    const uint32_t x = which ? sP : sD, y = which ? sO : sQ;
-                    if (!t.halo) block_a(x, y, acc_col(acc, which), t.first);
-                    if (with_b) block_b(x, y, acc_col(acc ^ 1, which));
+                    const uint32_t y = which ? tile_o(n) : tile_q(n);
+                    if (!t.halo) block_a(!which, y, acc_col(acc, which), t.first);
+                    if (with_b) block_b(!which, y, acc_col(acc ^ 1, which));
                 }
             };
             if (!dp_asked) ok = issue_dp(n);
             if (!ok) break;
             if constexpr (C::kShared) {
-                ok = mbar_wait(&bars[bP], n & 1, abort_flag) && begin_sets();
+                ok = wait(bP, n);
                 if (!ok) break;
                 tc_fence_after();
                 products(1, 1);
                 mma_commit_w(lead, &bars[bPdone]);
             }
-            ok = mbar_wait(&bars[bPS], n & 1, abort_flag);
+            ok = wait(bPS, n);
             if (!ok) break;
             tc_fence_after();
             if (early) {
@@ -319,77 +330,79 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = issue_s(n + 1);
                 hb -= drop;
             }
-            // (also what keeps a tile's end from being told before the end of the tile before it was seen)
-            if (ok && n > 0) ok = mbar_wait(&bars[bDQfree], (n - 1) & 1, abort_flag);
+            if (PAD == 64 && ok && n > 0) ok = wait(bOut, n - 1);
             if (!ok) break;
             tc_fence_after();
             if (!t.halo) {
                 const uint32_t d = tb + colDQ<PAD>;
 #pragma unroll
                 for (int j = 0; j < NH; ++j) {
-                    const uint32_t la = lo(d1, sD + C::block(j)), lb = lo(d1, kv(j));
+                    const uint32_t la = lo(d1, sm + C::offP + C::block(true, j)), lb = lo(d1, sm + ((hb + j) % NK) * kHalfBytes);
                     if (j == 0) mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
                     else mma_ss_w<true>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), iQ);
 #pragma unroll
                     for (int k = 1; k < 4; ++k) mma_ss_w<true>(lead, d, la + k * 2, desc_hi(d1), lb + k * 128, desc_hi(d1), iQ);
                 }
             }
-            for (int j = 0; j < drop; ++j) mma_commit_w(lead, &bars[bEmptyKV + (hb + j) % NS]);
+            mma_commit_w(lead, &bars[bKdone + (n & 1)]);
             hb += drop;
-            // the next tile's dP goes ahead of this one's products where its dO is there: its softmax waits for it, nothing of this tile does
-            dp_asked = early && __all_sync(0xffffffffu, mbar_test(&bars[bFullO + ((n + 1) & 1)], ((n + 1) >> 1) & 1));
+            // the next tile's dP goes ahead of this one's products where its dO and V are there: its softmax waits for it, nothing of
+            // this tile does
+            dp_asked = early && __all_sync(0xffffffffu, mbar_test(&bars[bFullB + ((n + 1) & 1)], ((n + 1) >> 1) & 1));
             if (dp_asked) ok = issue_dp(n + 1);
-            if constexpr (!C::kShared) ok = ok && begin_sets();
             if (!ok) break;
-            tc_fence_after();
             products(C::kShared ? 0 : 1, 0);
-            mma_commit_w(lead, &bars[bDone]);
-            if (!t.halo && t.first) ++uses[acc];
-            if (with_b) ++uses[acc ^ 1];
+            mma_commit_w(lead, &bars[bDone + (n & 1)]);
             if (!t.last) acc ^= 1;
             if (!early && !t.end) ok = issue_s(n + 1);
         }
     } else if (warp >= kWarpOut) {
-        // ---- results: four warps, a TMEM lane per thread.  Once a tile's products are done, the place of its dO holds the results on
-        // their way out (per warp two pieces of 32 rows by 32 columns in turn); then it goes back to the loads.  (Stores from registers
-        // crowd out the softmax's accesses to shared memory, whose pipe they share.)
+        // ---- results: four warps, a TMEM lane per thread.  dQ; dK, dV of the key block that a tile completes (lanes 0 .. 63 hold its
+        // keys 64 .. 127 and the other way round); of the one behind a head's last tile
         const int u = warp & 3;
         const uint32_t lanes = (uint32_t)u * 32u;
         int acc = 0;
         for (int n = 0; n < N && ok; ++n) {
             const Tile t = run.tile(n);
-            ok = __all_sync(0xffffffffu, mbar_wait(&bars[bDone], n & 1, abort_flag));
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars[bDone + (n & 1)], (n >> 1) & 1, abort_flag));
             if (!ok) break;
             tc_fence_after();
-            if (t.halo) mbar_arrive(&bars[bDQfree]);
-            uint8_t* own = smem + C::offQ + (n & 1) * 2 * kTileBytes + kTileBytes + u * 4096;
-            // dQ; dK, dV of the key block that this tile completes (lanes 0 .. 63 hold its keys 64 .. 127 and the other way round); of
-            // the one behind a head's last tile
-            const int from = t.halo ? 10 : 0, to = t.halo || !t.last ? 6 : 10;
-#pragma unroll 1
-            for (int q = from; q < to; ++q) {
-                const int k = q >> 1, col = (q & 1) * 32, a = k < 3 ? acc : acc ^ 1;
-                const bool value = k == 2 || k == 4;
-                uint8_t* tile = own + (q & 1) * 2048;
-                if (q > 1) {                                         // (the store before last has read its rows)
-                    if (lane == 0) tma_store_wait_read<1>();
-                    __syncwarp();
-                }
-                stage_rows(tmem_addr(tb, lanes, (k == 0 ? colDQ<PAD> : colAcc + 128 * a + 64 * value) + col), tile, lane);
-                tc_fence_before();
-                if (q == 1) mbar_arrive(&bars[bDQfree]);
-                else if (value && (q & 1)) mbar_arrive(&bars[bAccFree + a]);
+            const int key = t.i * kQT - PAD + (int)(lanes ^ 64u);
+            // out through the place of the tile's Q, which three tiles share: 32 rows a time per warp
+            uint8_t* own = smem + C::offQ + (n % C::kSlotsQ) * kTileBytes + u * 4096;
+            auto send = [&](const uint32_t (&c)[8][4], const CUtensorMap& map, int row) {
+                if (lane == 0) tma_store_wait_read<0>();             // (the one before has been read)
+                __syncwarp();
+                stage_rows(c, own, lane);
                 fence_proxy_async_smem();
                 __syncwarp();
-                const int row = k == 0 ? t.i * kQT + (int)lanes : (k < 3 ? t.i : t.i + 1) * kQT - PAD + (int)(lanes ^ 64u);
                 if (lane == 0) {
-                    if (row >= 0 && row < p.L) tma_store_3d(k == 0 ? &tm_dq : value ? &tm_dv : &tm_dk, tile, col, row, t.head);
+                    if (row >= 0 && row < p.L) tma_store_3d(&map, own, 0, row, t.head);
                     tma_store_commit();
                 }
+            };
+            uint32_t c[3][8][4];
+            if (t.last) {
+                read_rows(tmem_addr(tb, lanes, colAcc + 128 * (acc ^ 1)), c[0]);
+                send(c[0], tm_dk, key + kQT);
+                read_rows(tmem_addr(tb, lanes, colAcc + 128 * (acc ^ 1) + 64), c[0]);
+                send(c[0], tm_dv, key + kQT);
+            }
+            if (!t.halo) {
+                read_rows(tmem_addr(tb, lanes, colDQ<PAD>), c[0]);
+                read_rows(tmem_addr(tb, lanes, colAcc + 128 * acc), c[1]);
+                read_rows(tmem_addr(tb, lanes, colAcc + 128 * acc + 64), c[2]);
+            }
+            tc_fence_before();
+            mbar_arrive(&bars[bOut]);
+            if (!t.halo) {
+                send(c[0], tm_dq, t.i * kQT + (int)lanes);
+                send(c[1], tm_dk, key);
+                send(c[2], tm_dv, key);
             }
             if (lane == 0) {
                 tma_store_wait_read<0>();
-                mbar_arrive(&bars[bEmptyO + (n & 1)]);
+                mbar_arrive(&bars[bEmptyQ + n % C::kSlotsQ]);
             }
             if (!t.last) acc ^= 1;
         }
@@ -402,8 +415,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t tx = tmem_addr(tb, (uint32_t)u * 32u, colX + c0);
         const uint32_t sw = r & 7;
         // the 16 bytes of columns c .. c + 7 of this row in P or dS
-        auto chunk = [&](uint32_t off, int c) {
-            return smem + off + C::block(c >> 6) + (r >> 3) * 1024 + (r & 7) * 128 + ((((uint32_t)c >> 3 & 7u) ^ sw) << 4);
+        auto chunk = [&](bool ds, int c) {
+            return smem + C::offP + C::block(ds, c >> 6) + (r >> 3) * 1024 + (r & 7) * 128 + ((((uint32_t)c >> 3 & 7u) ^ sw) << 4);
         };
         constexpr int NP = NC / 2;                                   // pairs of columns
         for (int n = 0; n < N; ++n) {
@@ -445,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 l2 = pairs::add2(l2, ep[k]);
             }
             ok = mbar_wait(&bars[bDP], n & 1, abort_flag) && ok;
-            if (n > 0) ok = mbar_wait(&bars[bDone], (n - 1) & 1, abort_flag) && ok;
+            if (n > 0) ok = mbar_wait(&bars[bDone + ((n - 1) & 1)], ((n - 1) >> 1) & 1, abort_flag) && ok;
             __syncwarp();
             tc_fence_after();
             // dP: kept where there are registers for it, else read twice
@@ -471,10 +484,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float2 ls = pairs::split(l2), ws = pairs::split(w2);
             const float l = ls.x + ls.y, w = ws.x + ws.y;
             // the partner's statistics lie in the first chunk that this thread itself overwrites, and the other way round
-            *reinterpret_cast<float4*>(chunk(C::offP, c1)) = make_float4(mx, l, w, 0.f);
+            *reinterpret_cast<float4*>(chunk(false, c1)) = make_float4(mx, l, w, 0.f);
             ok = pair_all(1 + u, ok);
             if (!ok) break;
-            const float4 other = *reinterpret_cast<const float4*>(chunk(C::offP, c0));
+            const float4 other = *reinterpret_cast<const float4*>(chunk(false, c0));
             const float m = fmaxf(mx, other.x);                      // (finite: a row sees its own key)
             const float f0 = ex2((mx - m) * p.scale_log2e), f1 = ex2((other.x - m) * p.scale_log2e);
             const float inv = 1.f / fmaf(l, f0, other.y * f1);
@@ -489,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (C::kShared) {
 #pragma unroll
                 for (int k = 0; k < NP; k += 4)
-                    *reinterpret_cast<uint4*>(chunk(C::offP, c0 + 2 * k)) = make_uint4(packed(ep[k]), packed(ep[k + 1]), packed(ep[k + 2]), packed(ep[k + 3]));
+                    *reinterpret_cast<uint4*>(chunk(false, c0 + 2 * k)) = make_uint4(packed(ep[k]), packed(ep[k + 1]), packed(ep[k + 2]), packed(ep[k + 3]));
                 fence_proxy_async_smem();
                 mbar_arrive(&bars[bP]);
                 ok = pair_all(1 + u, mbar_wait(&bars[bPdone], n & 1, abort_flag));
@@ -514,9 +527,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     const int c = c0 + 2 * (b + g);
                     if constexpr (!C::kShared)
-                        *reinterpret_cast<uint4*>(chunk(C::offP, c)) =
+                        *reinterpret_cast<uint4*>(chunk(false, c)) =
                             make_uint4(packed(ep[b + g]), packed(ep[b + g + 1]), packed(ep[b + g + 2]), packed(ep[b + g + 3]));
-                    *reinterpret_cast<uint4*>(chunk(C::offD, c)) = make_uint4(ds[0], ds[1], ds[2], ds[3]);
+                    *reinterpret_cast<uint4*>(chunk(true, c)) = make_uint4(ds[0], ds[1], ds[2], ds[3]);
                 }
             }
             tc_fence_before();
@@ -540,11 +553,11 @@ static based_status launch_pad(const void* q, const void* k, const void* v, cons
                                int window, float scale, cudaStream_t stream) {
     using C = Cfg<PAD>;
     CUtensorMap tq, tk, tv, to, tdq, tdk, tdv;
-    const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B, s64 = CU_TENSOR_MAP_SWIZZLE_64B;
+    const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B;
     if (!make_rows_map_bf16(&tq, q, BH, L, kHD, kHD, kQT, s128) || !make_rows_map_bf16(&tk, k, BH, L, kHD, kHD, 64, s128) ||
         !make_rows_map_bf16(&tv, v, BH, L, kHD, kHD, 64, s128) || !make_rows_map_bf16(&to, dout, BH, L, kHD, kHD, kQT, s128) ||
-        !make_rows_map_bf16(&tdq, dq, BH, L, kHD, 32, 32, s64) || !make_rows_map_bf16(&tdk, dk, BH, L, kHD, 32, 32, s64) ||
-        !make_rows_map_bf16(&tdv, dv, BH, L, kHD, 32, 32, s64))
+        !make_rows_map_bf16(&tdq, dq, BH, L, kHD, kHD, 32, s128) || !make_rows_map_bf16(&tdk, dk, BH, L, kHD, kHD, 32, s128) ||
+        !make_rows_map_bf16(&tdv, dv, BH, L, kHD, kHD, 32, s128))
         return BASED_ERR_CUDA;
     Params p;
     if (error_word_ptr(&p.err) != BASED_OK) return BASED_ERR_CUDA;
