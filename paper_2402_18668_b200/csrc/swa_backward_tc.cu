@@ -131,17 +131,6 @@ struct Run {
     }
 };
 
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(r)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return r != 0;
-}
 // A row of 64 fp32 values in TMEM per lane, rounded to bf16: 8 chunks of 16 bytes
 __device__ __forceinline__ void read_rows(uint32_t taddr, uint32_t (&c)[8][4]) {
 #pragma unroll
@@ -296,8 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 part(sm + C::offP + C::block(ds, 3), 16384, y, d, 8, true);
         };
         auto acc_col = [&](int a, int which) { return tb + colAcc + 128 * a + 64 * which; };     // 0: dK, 1: dV
-        bool dp_asked = false;
-        ok = issue_s(0);
+        ok = issue_s(0) && issue_dp(0);
 #pragma unroll 1
         for (int n = 0; n < N && ok; ++n) {
             const Tile t = run.tile(n);
@@ -313,8 +301,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (with_b) block_b(!which, y, acc_col(acc ^ 1, which));
                 }
             };
-            if (!dp_asked) ok = issue_dp(n);
-            if (!ok) break;
             if constexpr (C::kShared) {
                 ok = wait(bP, n);
                 if (!ok) break;
@@ -346,15 +332,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             mma_commit_w(lead, &bars[bKdone + (n & 1)]);
             hb += drop;
-            // the next tile's dP goes ahead of this one's products where its dO and V are there: its softmax waits for it, nothing of
-            // this tile does
-            dp_asked = early && __all_sync(0xffffffffu, mbar_test(&bars[bFullB + ((n + 1) & 1)], ((n + 1) >> 1) & 1));
-            if (dp_asked) ok = issue_dp(n + 1);
-            if (!ok) break;
             products(C::kShared ? 0 : 1, 0);
             mma_commit_w(lead, &bars[bDone + (n & 1)]);
             if (!t.last) acc ^= 1;
-            if (!early && !t.end) ok = issue_s(n + 1);
+            if (!t.end) ok = (early || issue_s(n + 1)) && issue_dp(n + 1);
         }
     } else if (warp >= kWarpOut) {
         // ---- results: four warps, a TMEM lane per thread.  dQ; dK, dV of the key block that a tile completes (lanes 0 .. 63 hold its
