@@ -605,7 +605,7 @@ static based_status norm_rotate_check(const NormRotate& a, int positions_per_seq
     const long long width_q = (long long)a.Hq * a.d, width_k = (long long)a.Hk * a.d, per16 = 16 / (long long)esize(io);
     if (a.q_stride < width_q || a.k_stride < width_k) return BASED_ERR_INVALID_ARG;
     if (a.d % 16 != 0 || a.d > 256 || a.n % 8 != 0 || 2 * a.n > a.d || a.q_stride % per16 != 0 || a.k_stride % per16 != 0 ||
-        width_q > 0x7fffffffLL || width_k > 0x7fffffffLL || (long long)a.B * a.L > 0x7fffffffLL)
+        width_q > 0x7fffffffLL || width_k > 0x7fffffffLL || (long long)a.B * a.L > 0x7fffff00LL)
         return BASED_ERR_UNSUPPORTED;
     if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.wq) || !aligned16(a.wk)) return BASED_ERR_ALIGNMENT;
     if ((reinterpret_cast<uintptr_t>(a.freqs) & 7u) || (reinterpret_cast<uintptr_t>(a.positions) & 3u)) return BASED_ERR_ALIGNMENT;

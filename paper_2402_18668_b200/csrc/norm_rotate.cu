@@ -9,12 +9,18 @@
 //
 //   e = turned back dy,  dw = sum over rows of e x inv,  dx = inv (w e - x inv^2 mean(w e x)),   inv = 1 / sqrt(mean(x^2) + eps).
 //
-// One pass over rows of 32 to 512 bytes: bound by HBM bandwidth.  A row is shared by d / (2 V) threads, each with two 16-byte
-// pieces (V values) that hold both elements of its pairs, so only the row's sums cross threads.  A CTA takes a few
+// One pass over rows of 32 bytes to 1 KB: bound by HBM bandwidth.  A row is shared by d / (2 V) threads, each with two 16-byte
+// pieces (V values) that hold both elements of its pairs, so only the row's sums cross threads.  A CTA takes up to 32
 // consecutive tokens and all their heads: a warp reads pieces of rows that lie a token stride apart and writes rows that lie
 // side by side, and the angles of the tokens, the same for all heads, are taken once, into shared memory.  An angle is a
 // product in fp64, reduced to a part of a turn there (a far position's angle in fp32 would be off by position x 6e-8), and only
-// that part is rounded to fp32 for the sine and cosine.
+// that part is rounded to fp32 for the sine and cosine.  What is left of HBM's rate goes to the start of each CTA, where it
+// waits for the angles and its first rows: those rows are asked for before the angles, and a turn ahead after that.
+//
+// Measured: bf16, 2 x 32768 tokens, 16 + 16 heads of 64, rotating: 106 us (77 % of the copy rate; 115 with 8 tokens per CTA, 165
+// with 4); fp32, 3 x 777 tokens, 16 + 4 heads of 128, 64 of them rotating: 8.6 us (85 %); backward, bf16, 4 x 2048 tokens of
+// 16 + 16 heads of 64: 30 us (51 %: latency, 16 warps of 116 registers per SM).  A form with a TMA pipeline through shared memory (4 stages, results stored by TMA) took 117,
+// 17 and 50: its rows pass through shared memory twice, and short grids fill no pipeline.
 #include <type_traits>
 
 #include "common.cuh"
@@ -32,25 +38,38 @@ __device__ __forceinline__ pair swap2(pair a) { return (a >> 32) | (a << 32); }
 struct Grid {
     int T, TP;                     // threads that share a row, and the power of two they are spaced by
     int TB;                        // tokens per block, a power of two
-    long long blocks;              // blocks of tokens
+    int NP;                        // the angles of a token are spaced by that many threads, a power of two
+    int blocks;                    // blocks of tokens
 };
-
-// The angles of TB tokens from m0 on: cos and sin [TB][n] in shared memory
-__device__ __forceinline__ void fill_angles(const NormRotate& a, long long m0, int TB, float2* table) {
-    const long long rows = (long long)a.B * a.L;
-    for (int i = threadIdx.x; i < TB * a.n; i += kThreads) {
-        const int tok = i / a.n, j = i - tok * a.n;
-        const long long m = m0 + tok;
-        float2 cs = make_float2(1.f, 0.f);
-        if (m < rows) {
-            const long long b = m / a.L, t = m - b * a.L;
-            const long long pos = a.positions ? (a.per_token ? (long long)a.positions[m] : a.positions[b] + t) : a.start + t;
-            const double turns = (double)pos * (a.freqs[j] * kTurnsPerRadian);
-            float s, c;
-            sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-            cs = make_float2(c, s);
+// Sine and cosine of x half turns, |x| <= 1.  For bf16 io the fast ones (off by 2^-20.5, where the result is rounded by 2^-9 of it)
+template <typename T> __device__ __forceinline__ float2 cos_sin(float x) {
+    float2 r;
+    if constexpr (sizeof(T) == 2) {
+        const float a = x * 3.14159265f;
+        asm("cos.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(a));
+        asm("sin.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(a));
+    } else {
+        sincospif(x, &r.y, &r.x);
+    }
+    return r;
+}
+// The angles of TB tokens from token m0 of the batch on: cos and sin [TB][n] in shared memory
+template <typename T> __device__ __forceinline__ void fill_angles(const NormRotate& a, const Grid& gr, int m0, float2* table) {
+    const int j = threadIdx.x & (gr.NP - 1), step = kThreads / gr.NP;
+    if (j >= a.n) return;
+    const double freq = a.freqs[j] * kTurnsPerRadian;
+    for (int tok = threadIdx.x / gr.NP; tok < gr.TB; tok += step) {
+        const int m = m0 + tok;
+        if (m >= a.B * a.L) return;
+        double pos;
+        if (a.positions && a.per_token) {
+            pos = (double)a.positions[m];
+        } else {
+            const int b = m / a.L, t = m - b * a.L;
+            pos = (a.positions ? (double)a.positions[b] : (double)a.start) + (double)t;
         }
-        table[i] = cs;
+        const double turns = pos * freq;
+        table[tok * a.n + j] = cos_sin<T>((float)(2.0 * (turns - rint(turns))));
     }
 }
 
@@ -126,203 +145,213 @@ template <int P2> __device__ __forceinline__ void weights(const float* w, int va
 }
 }  // namespace
 
-// a block: TB tokens and all their heads
+// grid: blocks of TB tokens; queries and keys
 template <typename T, bool PAIRS>
-__global__ void __launch_bounds__(kThreads) norm_rotate_kernel(const NormRotate a, const Grid gr, T* __restrict__ out_q, T* __restrict__ out_k) {
-    constexpr int V = Piece<T>::V, P2 = V / 2, U = 4;
+__global__ void __launch_bounds__(kThreads, 4) norm_rotate_kernel(const NormRotate a, const Grid gr, T* __restrict__ out_q, T* __restrict__ out_k) {
+    constexpr int V = Piece<T>::V, P2 = V / 2, U = 2;
     extern __shared__ float2 table[];
     enter_dependent();
     const int tid = threadIdx.x, j = tid & (gr.TP - 1), slot = tid / gr.TP;
     const int tok = slot & (gr.TB - 1), h0 = slot / gr.TB, hs = kThreads / gr.TP / gr.TB;
-    const long long m = (long long)blockIdx.x * gr.TB + tok, rows = (long long)a.B * a.L;
-    if (a.n) {
-        fill_angles(a, (long long)blockIdx.x * gr.TB, gr.TB, table);
-        __syncthreads();
-    }
+    const int m0 = blockIdx.x * gr.TB, m = m0 + tok;             // (B L < 2^31 - 2^4)
+    const bool keys = blockIdx.y != 0;
+    const int H = keys ? a.Hk : a.Hq;
     Place<T, PAIRS> at;
     at.set(j, gr.T, a.n);
-    at.angles(table + tok * a.n);
-    const bool live = at.in && m < rows;
-    const long long b = m / a.L, t = m - b * a.L;
+    const bool live = at.in && m < a.B * a.L;
+    const int b = m / a.L, t = m - b * a.L;
     const float per_d = 1.f / (float)a.d;
-    auto heads = [&](const T* x, long long stride, const float* w, T* y, int H) {
-        pair wa[P2], wb[P2];
-        weights<P2>(w, at.va, at.vb, at.in, wa, wb);
-        const T* row = x + m * stride;
-        T* to = y + (b * H * a.L + t) * a.d;
-        for (int hb = 0; hb < H; hb += U * hs) {                 // (every thread: the sums cross lanes)
-            uint4 ua[U], ub[U];
+    const T* row = static_cast<const T*>(keys ? a.k : a.q) + m * (keys ? a.k_stride : a.q_stride);
+    T* to = (keys ? out_k : out_q) + ((size_t)b * H * a.L + t) * a.d;
+    // rows of U heads at a time, those of the next turn under way while this one's are worked on; the first ones before the angles
+    uint4 ua[U], ub[U];
+    auto fetch = [&](int hb) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = hb + u * hs + h0;
-                ua[u] = ub[u] = make_uint4(0, 0, 0, 0);
-                if (live && h < H) {
-                    ua[u] = __ldcs(reinterpret_cast<const uint4*>(row + (size_t)h * a.d) + at.va);
-                    ub[u] = __ldcs(reinterpret_cast<const uint4*>(row + (size_t)h * a.d) + at.vb);
-                }
-            }
-            float ss[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                pair xa[P2], xb[P2];
-                Piece<T>::unpack(ua[u], xa);
-                Piece<T>::unpack(ub[u], xb);
-                ss[u] = dot<P2>(xa, xb, xa, xb);
-            }
-            for (int d = gr.TP / 2; d > 0; d /= 2)
-#pragma unroll
-                for (int u = 0; u < U; ++u) ss[u] += __shfl_xor_sync(0xffffffffu, ss[u], d);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = hb + u * hs + h0;
-                if (!live || h >= H) continue;
-                const pair inv = both(rsqrtf(fmaf(ss[u], per_d, a.eps)));
-                pair xa[P2], xb[P2];
-                Piece<T>::unpack(ua[u], xa);
-                Piece<T>::unpack(ub[u], xb);
-#pragma unroll
-                for (int e = 0; e < P2; ++e) {
-                    xa[e] = mul2(mul2(xa[e], inv), wa[e]);
-                    xb[e] = mul2(mul2(xb[e], inv), wb[e]);
-                }
-                at.template turn<false>(xa, xb);
-                uint4* dst = reinterpret_cast<uint4*>(to + (size_t)h * a.L * a.d);
-                __stcs(dst + at.va, Piece<T>::pack(xa));
-                __stcs(dst + at.vb, Piece<T>::pack(xb));
+        for (int u = 0; u < U; ++u) {
+            const int h = hb + u * hs + h0;
+            ua[u] = ub[u] = make_uint4(0, 0, 0, 0);
+            if (live && h < H) {
+                ua[u] = __ldcs(reinterpret_cast<const uint4*>(row + (size_t)h * a.d) + at.va);
+                ub[u] = __ldcs(reinterpret_cast<const uint4*>(row + (size_t)h * a.d) + at.vb);
             }
         }
     };
-    heads(static_cast<const T*>(a.q), a.q_stride, a.wq, out_q, a.Hq);
-    heads(static_cast<const T*>(a.k), a.k_stride, a.wk, out_k, a.Hk);
+    fetch(0);
+    pair wa[P2], wb[P2];
+    weights<P2>(keys ? a.wk : a.wq, at.va, at.vb, at.in, wa, wb);
+    if (a.n) {
+        fill_angles<T>(a, gr, m0, table);
+        __syncthreads();
+    }
+    at.angles(table + tok * a.n);
+    for (int hb = 0; hb < H; hb += U * hs) {                     // (every thread: the sums cross lanes)
+        pair xa[U][P2], xb[U][P2];
+        float ss[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            Piece<T>::unpack(ua[u], xa[u]);
+            Piece<T>::unpack(ub[u], xb[u]);
+        }
+        if (hb + U * hs < H) fetch(hb + U * hs);
+#pragma unroll
+        for (int u = 0; u < U; ++u) ss[u] = dot<P2>(xa[u], xb[u], xa[u], xb[u]);
+        for (int d = gr.TP / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int u = 0; u < U; ++u) ss[u] += __shfl_xor_sync(0xffffffffu, ss[u], d);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = hb + u * hs + h0;
+            const pair inv = both(rsqrtf(fmaf(ss[u], per_d, a.eps)));
+#pragma unroll
+            for (int e = 0; e < P2; ++e) {
+                xa[u][e] = mul2(mul2(xa[u][e], inv), wa[e]);
+                xb[u][e] = mul2(mul2(xb[u][e], inv), wb[e]);
+            }
+            at.template turn<false>(xa[u], xb[u]);
+            if (live && h < H) {
+                uint4* dst = reinterpret_cast<uint4*>(to + (size_t)h * a.L * a.d);
+                __stcs(dst + at.va, Piece<T>::pack(xa[u]));
+                __stcs(dst + at.vb, Piece<T>::pack(xb[u]));
+            }
+        }
+    }
 }
 
-// the same rows backward; part: a row of 2 d sums per CTA (null: the weights' gradients are not wanted)
+// The same rows backward.  part: a row of 2 d sums per block, the queries' and the keys' (null: the weights' gradients are not wanted)
 template <typename T, bool PAIRS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
     norm_rotate_backward_kernel(const NormRotate a, const Grid gr, const T* __restrict__ gq, const T* __restrict__ gk, T* __restrict__ dq,
                                 long long dq_stride, T* __restrict__ dk, long long dk_stride, float* __restrict__ part) {
-    constexpr int V = Piece<T>::V, P2 = V / 2, U = 2;
+    constexpr int V = Piece<T>::V, P2 = V / 2, U = 1;
     extern __shared__ float2 table[];
-    __shared__ pair sums[kThreads / 32][2][2][P2][32];           // warp, query or key, piece, pair, thread of a row
+    __shared__ pair sums[kThreads / 32][2][P2][32];              // warp, piece, pair, thread of a row
     enter_dependent();
     const int tid = threadIdx.x, j = tid & (gr.TP - 1), slot = tid / gr.TP;
     const int tok = slot & (gr.TB - 1), h0 = slot / gr.TB, hs = kThreads / gr.TP / gr.TB;
-    const long long rows = (long long)a.B * a.L;
+    const bool keys = blockIdx.y != 0;
+    const int H = keys ? a.Hk : a.Hq;
+    const T *x = static_cast<const T*>(keys ? a.k : a.q), *g = keys ? gk : gq;
+    T* dx = keys ? dk : dq;
+    const long long stride = keys ? a.k_stride : a.q_stride, dx_stride = keys ? dk_stride : dq_stride;
     Place<T, PAIRS> at;
     at.set(j, gr.T, a.n);
+    pair wa[P2], wb[P2], sa[P2], sb[P2];
+    weights<P2>(keys ? a.wk : a.wq, at.va, at.vb, at.in, wa, wb);
     const float per_d = 1.f / (float)a.d;
-    pair acc[2][2][P2];
 #pragma unroll
-    for (int i = 0; i < 4 * P2; ++i) (&acc[0][0][0])[i] = 0;
-    for (long long blk = blockIdx.x; blk < gr.blocks; blk += gridDim.x) {
-        const long long m = blk * gr.TB + tok;
-        if (a.n) {
-            __syncthreads();
-            fill_angles(a, blk * gr.TB, gr.TB, table);
-            __syncthreads();
-        }
-        at.angles(table + tok * a.n);
-        const bool live = at.in && m < rows;
-        const long long b = m / a.L, t = m - b * a.L;
-        auto heads = [&](const T* x, long long stride, const float* w, const T* g, T* dx, long long dx_stride, int H, pair (&sa)[P2],
-                         pair (&sb)[P2]) {
-            pair wa[P2], wb[P2];
-            weights<P2>(w, at.va, at.vb, at.in, wa, wb);
-            const T* row = x + m * stride;
-            const T* from = g + (b * H * a.L + t) * a.d;
-            for (int hb = 0; hb < H; hb += U * hs) {
-                uint4 ux[U][2], ug[U][2];
+    for (int e = 0; e < P2; ++e) sa[e] = sb[e] = 0;
+    for (int blk = blockIdx.x; blk < gr.blocks; blk += gridDim.x) {
+        const int m0 = blk * gr.TB, m = m0 + tok;
+        const bool live = at.in && m < a.B * a.L;
+        const int b = m / a.L, t = m - b * a.L;
+        const T *row = x + m * stride, *from = g + ((size_t)b * H * a.L + t) * a.d;
+        uint4 ux[U][2], ug[U][2];
+        auto fetch = [&](int hb) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int h = hb + u * hs + h0;
-                    ux[u][0] = ux[u][1] = ug[u][0] = ug[u][1] = make_uint4(0, 0, 0, 0);
-                    if (live && h < H) {
-                        const uint4 *px = reinterpret_cast<const uint4*>(row + (size_t)h * a.d),
-                                    *pg = reinterpret_cast<const uint4*>(from + (size_t)h * a.L * a.d);
-                        ux[u][0] = __ldcs(px + at.va);
-                        ux[u][1] = __ldcs(px + at.vb);
-                        ug[u][0] = __ldcs(pg + at.va);
-                        ug[u][1] = __ldcs(pg + at.vb);
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int h = hb + u * hs + h0;
-                    pair xa[P2], xb[P2], ea[P2], eb[P2], na[P2], nb[P2];
-                    Piece<T>::unpack(ux[u][0], xa);
-                    Piece<T>::unpack(ux[u][1], xb);
-                    Piece<T>::unpack(ug[u][0], ea);
-                    Piece<T>::unpack(ug[u][1], eb);
-                    at.template turn<true>(ea, eb);
-#pragma unroll
-                    for (int e = 0; e < P2; ++e) {
-                        na[e] = mul2(ea[e], wa[e]);
-                        nb[e] = mul2(eb[e], wb[e]);
-                    }
-                    float ss = dot<P2>(xa, xb, xa, xb), sd = dot<P2>(na, nb, xa, xb);
-                    for (int d = gr.TP / 2; d > 0; d /= 2) {
-                        ss += __shfl_xor_sync(0xffffffffu, ss, d);
-                        sd += __shfl_xor_sync(0xffffffffu, sd, d);
-                    }
-                    if (!live || h >= H) continue;
-                    const float inv = rsqrtf(fmaf(ss, per_d, a.eps));
-                    const pair i2 = both(inv), c = both(-inv * inv * sd * per_d);
-#pragma unroll
-                    for (int e = 0; e < P2; ++e) {
-                        sa[e] = fma2(mul2(ea[e], i2), xa[e], sa[e]);
-                        sb[e] = fma2(mul2(eb[e], i2), xb[e], sb[e]);
-                        na[e] = mul2(i2, fma2(xa[e], c, na[e]));
-                        nb[e] = mul2(i2, fma2(xb[e], c, nb[e]));
-                    }
-                    uint4* dst = reinterpret_cast<uint4*>(dx + m * dx_stride + (size_t)h * a.d);
-                    __stcs(dst + at.va, Piece<T>::pack(na));
-                    __stcs(dst + at.vb, Piece<T>::pack(nb));
+            for (int u = 0; u < U; ++u) {
+                const int h = hb + u * hs + h0;
+                ux[u][0] = ux[u][1] = ug[u][0] = ug[u][1] = make_uint4(0, 0, 0, 0);
+                if (live && h < H) {
+                    const uint4 *px = reinterpret_cast<const uint4*>(row + (size_t)h * a.d),
+                                *pg = reinterpret_cast<const uint4*>(from + (size_t)h * a.L * a.d);
+                    ux[u][0] = __ldcs(px + at.va);
+                    ux[u][1] = __ldcs(px + at.vb);
+                    ug[u][0] = __ldcs(pg + at.va);
+                    ug[u][1] = __ldcs(pg + at.vb);
                 }
             }
         };
-        heads(static_cast<const T*>(a.q), a.q_stride, a.wq, gq, dq, dq_stride, a.Hq, acc[0][0], acc[0][1]);
-        heads(static_cast<const T*>(a.k), a.k_stride, a.wk, gk, dk, dk_stride, a.Hk, acc[1][0], acc[1][1]);
+        fetch(0);
+        if (a.n) {
+            __syncthreads();
+            fill_angles<T>(a, gr, m0, table);
+            __syncthreads();
+        }
+        at.angles(table + tok * a.n);
+        for (int hb = 0; hb < H; hb += U * hs) {
+            pair xa[U][P2], xb[U][P2], ea[U][P2], eb[U][P2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                Piece<T>::unpack(ux[u][0], xa[u]);
+                Piece<T>::unpack(ux[u][1], xb[u]);
+                Piece<T>::unpack(ug[u][0], ea[u]);
+                Piece<T>::unpack(ug[u][1], eb[u]);
+            }
+            if (hb + U * hs < H) fetch(hb + U * hs);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = hb + u * hs + h0;
+                pair na[P2], nb[P2];
+                at.template turn<true>(ea[u], eb[u]);
+#pragma unroll
+                for (int e = 0; e < P2; ++e) {
+                    na[e] = mul2(ea[u][e], wa[e]);
+                    nb[e] = mul2(eb[u][e], wb[e]);
+                }
+                float ss = dot<P2>(xa[u], xb[u], xa[u], xb[u]), sd = dot<P2>(na, nb, xa[u], xb[u]);
+                for (int d = gr.TP / 2; d > 0; d /= 2) {
+                    ss += __shfl_xor_sync(0xffffffffu, ss, d);
+                    sd += __shfl_xor_sync(0xffffffffu, sd, d);
+                }
+                if (!live || h >= H) continue;
+                const float inv = rsqrtf(fmaf(ss, per_d, a.eps));
+                const pair i2 = both(inv), c = both(-inv * inv * sd * per_d);
+#pragma unroll
+                for (int e = 0; e < P2; ++e) {
+                    sa[e] = fma2(mul2(ea[u][e], i2), xa[u][e], sa[e]);
+                    sb[e] = fma2(mul2(eb[u][e], i2), xb[u][e], sb[e]);
+                    na[e] = mul2(i2, fma2(xa[u][e], c, na[e]));
+                    nb[e] = mul2(i2, fma2(xb[u][e], c, nb[e]));
+                }
+                uint4* dst = reinterpret_cast<uint4*>(dx + m * dx_stride + (size_t)h * a.d);
+                __stcs(dst + at.va, Piece<T>::pack(na));
+                __stcs(dst + at.vb, Piece<T>::pack(nb));
+            }
+        }
     }
     if (!part) return;
     // over the rows of the warp, then over the warps: always in the same order
     const int lane = tid & 31;
 #pragma unroll
-    for (int i = 0; i < 4 * P2; ++i) {
-        pair v = (&acc[0][0][0])[i];
+    for (int i = 0; i < 2 * P2; ++i) {
+        pair v = i < P2 ? sa[i] : sb[i - P2];
         for (int d = 16; d >= gr.TP; d /= 2) v = add2(v, __shfl_xor_sync(0xffffffffu, v, d));
-        if (lane < gr.TP) (&sums[tid / 32][0][0][0][0])[i * 32 + lane] = v;
+        if (lane < gr.TP) (&sums[tid / 32][0][0][0])[i * 32 + lane] = v;
     }
     __syncthreads();
-    for (int i = tid; i < 4 * P2 * gr.T; i += kThreads) {
-        const int x = i % gr.T, e = i / gr.T;                    // e: (query or key, piece, pair)
-        pair v = (&sums[0][0][0][0][0])[e * 32 + x];
+    for (int i = tid; i < 2 * P2 * gr.T; i += kThreads) {
+        const int col = i % gr.T, e = i / gr.T;                  // e: (piece, pair)
+        pair v = (&sums[0][0][0][0])[e * 32 + col];
 #pragma unroll
-        for (int w = 1; w < kThreads / 32; ++w) v = add2(v, (&sums[w][0][0][0][0])[e * 32 + x]);
+        for (int w = 1; w < kThreads / 32; ++w) v = add2(v, (&sums[w][0][0][0])[e * 32 + col]);
         Place<T, PAIRS> pl;
-        pl.set(x, gr.T, a.n);
-        const int piece = (e / P2) & 1 ? pl.vb : pl.va;
+        pl.set(col, gr.T, a.n);
         const float2 f = split(v);
-        float* to = part + (size_t)blockIdx.x * 2 * a.d + (e / (2 * P2)) * a.d + piece * V + 2 * (e % P2);
+        float* to = part + ((size_t)blockIdx.x * 2 + keys) * a.d + (e / P2 ? pl.vb : pl.va) * V + 2 * (e % P2);
         to[0] = f.x;
         to[1] = f.y;
     }
 }
 
 namespace {
-Grid grid_for(int B, int L, int d, based_dtype io) {
+Grid grid_for(int B, int L, int d, int n, based_dtype io) {
     Grid g;
     g.T = d / (io == BASED_F32 ? 8 : 16);
     g.TP = 1;
     while (g.TP < g.T) g.TP *= 2;
-    const long long rows = (long long)B * L;
-    // up to 8 tokens per block, so that a head's rows are written in runs; fewer where the chip would not be filled
-    g.TB = 8;
+    g.NP = 1;
+    while (g.NP < n) g.NP *= 2;
+    const int rows = B * L;
+    // up to 32 tokens per block, so that a head's rows are written in runs; fewer where there would not be two blocks of the
+    // queries' and two of the keys' per SM (with twice that, the fp32 case above takes 10.4 us)
+    g.TB = 32;
     while (g.TB > kThreads / g.TP) g.TB /= 2;
-    while (g.TB > 1 && rows < (long long)g.TB * 4 * kSMs) g.TB /= 2;
-    g.blocks = (rows + g.TB - 1) / g.TB;
+    while (g.TB > 1 && rows < (long long)g.TB * 2 * kSMs) g.TB /= 2;
+    g.blocks = (int)(((long long)rows + g.TB - 1) / g.TB);
     return g;
 }
-unsigned backward_blocks(const Grid& g) { return (unsigned)(g.blocks < 4 * kSMs ? g.blocks : 4 * kSMs); }
+// blocks along the tokens backward: as many as are resident at once, of the queries and of the keys
+int backward_blocks(const Grid& g) { return g.blocks < 2 * kSMs ? g.blocks : 2 * kSMs; }
 
 template <typename F> cudaError_t with_kinds(based_dtype io, int pairs, F f) {
     using Yes = std::true_type;
@@ -333,15 +362,14 @@ template <typename F> cudaError_t with_kinds(based_dtype io, int pairs, F f) {
 }  // namespace
 
 size_t norm_rotate_backward_bytes(int B, int L, int d, based_dtype io) {
-    return (size_t)backward_blocks(grid_for(B, L, d, io)) * 2 * d * sizeof(float);
+    return (size_t)backward_blocks(grid_for(B, L, d, 0, io)) * 2 * d * sizeof(float);
 }
 
 based_status launch_norm_rotate(const NormRotate& a, void* out_q, void* out_k, based_dtype io, cudaStream_t stream) {
-    const Grid g = grid_for(a.B, a.L, a.d, io);
-    if (g.blocks > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    const Grid g = grid_for(a.B, a.L, a.d, a.n, io);
     const cudaError_t e = with_kinds(io, a.pairs, [&](auto zero, auto pairs) {
         using T = decltype(zero);
-        return launch_ex(norm_rotate_kernel<T, decltype(pairs)::value>, dim3((unsigned)g.blocks), dim3(kThreads),
+        return launch_ex(norm_rotate_kernel<T, decltype(pairs)::value>, dim3(g.blocks, 2), dim3(kThreads),
                          (size_t)g.TB * a.n * sizeof(float2), 1, true, stream, a, g, static_cast<T*>(out_q), static_cast<T*>(out_k));
     });
     note_launch();
@@ -351,11 +379,11 @@ based_status launch_norm_rotate(const NormRotate& a, void* out_q, void* out_k, b
 
 based_status launch_norm_rotate_backward(const NormRotate& a, const void* gq, const void* gk, void* dq, long long dq_stride, void* dk,
                                          long long dk_stride, float* dwq, float* dwk, float* part, based_dtype io, cudaStream_t stream) {
-    const Grid g = grid_for(a.B, a.L, a.d, io);
-    const unsigned blocks = backward_blocks(g);
+    const Grid g = grid_for(a.B, a.L, a.d, a.n, io);
+    const int blocks = backward_blocks(g);
     const cudaError_t e = with_kinds(io, a.pairs, [&](auto zero, auto pairs) {
         using T = decltype(zero);
-        return launch_ex(norm_rotate_backward_kernel<T, decltype(pairs)::value>, dim3(blocks), dim3(kThreads),
+        return launch_ex(norm_rotate_backward_kernel<T, decltype(pairs)::value>, dim3(blocks, 2), dim3(kThreads),
                          (size_t)g.TB * a.n * sizeof(float2), 1, true, stream, a, g, static_cast<const T*>(gq), static_cast<const T*>(gk),
                          static_cast<T*>(dq), dq_stride, static_cast<T*>(dk), dk_stride, dwq ? part : static_cast<float*>(nullptr));
     });
