@@ -5,7 +5,7 @@
 //
 // Persistent CTAs (one per SM) walk contiguous runs of tiles of 128 queries.  The tile at i0 sees the keys from i0 - PAD on
 // (PAD = 64 for windows up to 65, else 128): 128 + PAD columns.  Per tile
-//   S, then dP   [128, 128 + PAD] into the same TMEM columns, 64 keys at a time
+//   S, then dP   [128, 128 + PAD] into the same TMEM columns
 //   softmax      two threads per query row, each with half of the 32 + PAD columns its warp's rows can touch; the statistics
 //                m, l, sum P dP join through shared memory; P and dS go to shared memory as bf16
 //   dQ           dS K, dS read with the queries as rows
@@ -15,16 +15,24 @@
 // and no gradient is added into memory.  A run that starts inside a head first recomputes the tile before it, for the
 // block that it completes next.
 //
-// Shared memory (227 KB, which is why there is one CTA per SM): a ring of 64-key halves of K and V, of which two are the next
-// tile's; two slots of Q and dO; P and dS.  Rows of warp u (32 of them) touch columns 32 u .. 32 u + 31 + PAD only, what lies outside
-// is zeroed once and never written.  With PAD 64, P and dS have 40 KB each: column blocks 1 and 0 of 64 by all 128 rows, then the
-// lower half of block 2; the zeros that stand for its upper half (as rows, in dQ) and for the missing block 3 (as columns, in
-// dK and dV) are block 0's lower half, which lies where either view looks for them.  With PAD 128, P and dS take turns in one array of
-// 64 KB.
+// P and dS are rounded to bf16 for the products (half an ulp, 2^-9 of each weight); scores, dP, statistics and sums are fp32.
 //
-// Work per tile at PAD 64: five products of 128 x 192 x 64 (and the zeros: 2200 cycles of the tensor pipe) and 7 x 16 KB of HBM
-// traffic (2.6 us of an SM's share): bound by HBM where the chain load - S - softmax - dP - products - store of a tile
-// overlaps its neighbours'.  S of the next tile is issued ahead of this one's gradients, four warps of their own write results out.
+// Shared memory (226 KB, which is why there is one CTA per SM): rings of 64-key halves of K (those under a tile and two of the
+// next) and V (four), three places for Q, two for dO; P and dS.  A tile's results leave through its place of Q, once the products
+// have read that: 32 rows a time and warp, by TMA.  Rows of warp u (32 of them) touch columns 32 u .. 32 u + 31 + PAD only; what
+// lies outside is zeroed once and never written.  With PAD 64, P and dS have 32 KB each (column block 1 by all rows, the upper
+// half of block 0, the lower half of block 2) and share one piece of 8 KB of zeros that stands for the blocks' other halves.
+// With PAD 128 they take turns in one array of 64 KB, and dQ lies over dP in TMEM: the next tile's S starts with the three
+// halves beside it, while dQ is read out.
+//
+// Order of the products of tile n: [PAD 64: S of n + 1,] dQ, [PAD 128: dV ahead of it, S of n + 1 after it,] dV, dK, then dP of
+// n + 1, so that the softmax warps find S of the next tile when they are done with this one.
+//
+// Measured, bf16: 2 x 16 heads x 32768 queries, window 64: 178 us over 50 calls, 208 in a long run at the power limit (69 %
+// of the copy rate; the chain S - softmax - dP - dS - products of a tile, some 5900 cycles where HBM's share is 4700).  3 x 16
+// heads x 1777 queries, window 128: 36 us, some 8900 cycles per tile, 5.5 tiles per SM with the recomputed ones; of them 2300 for
+// the exponentials, 1500 each for writing P and dS.  It was 51 us with S of the next tile behind all of this one's results and dS
+// worked out behind dV's products; four softmax threads per row took 39.5 (80 registers, spills), and 248 with PAD 64.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -73,7 +81,7 @@ template <int PAD> constexpr uint32_t colDQ = PAD == 64 ? 192 : 0;   // PAD 128:
 //   bPdone  dV's products are done (PAD 128)         bKdone  so are dQ's, and with them the use of K
 //   bDone   all products are done                    bOut    the results have been read out of tensor memory
 // and for each of the three places of Q, bEmptyQ: the results that went out through it have left.
-enum Bar { bFullA = 0, bFullB = 2, bKdone = 4, bDone = 6, bEmptyQ = 8, bS = 11, bSread, bDP, bP, bPdone, bPS, bOut, bCount };
+enum Bar { bFullA = 0, bFullB = 2, bKdone = 4, bDone = 6, bEmptyQ = 8, bS = 11, bSread, bDP, bP, bPdone, bPS, bOutQ, bOut, bCount };
 static_assert(bCount * 8 + 8 <= 512, "barrier area");
 
 __device__ __forceinline__ float ex2(float x) {
@@ -134,12 +142,12 @@ struct Run {
 // A row of 64 fp32 values in TMEM per lane, rounded to bf16: 8 chunks of 16 bytes
 __device__ __forceinline__ void read_rows(uint32_t taddr, uint32_t (&c)[8][4]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t t[32];
-        tmem_ld32(taddr + 32 * h, t);
+    for (int h = 0; h < 4; ++h) {
+        uint32_t t[16];
+        tmem_ld16(taddr + 16 * h, t);
         tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) c[4 * h + (k >> 2)][k & 3] = pack2(__uint_as_float(t[2 * k]), __uint_as_float(t[2 * k + 1]));
+        for (int k = 0; k < 8; ++k) c[2 * h + (k >> 2)][k & 3] = pack2(__uint_as_float(t[2 * k]), __uint_as_float(t[2 * k + 1]));
     }
 }
 // to a piece of shared memory, swizzled as the TMA store of 32 rows reads it
@@ -170,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int N = run.count;
 
     if (tid == 0) {
-        for (int s = 0; s < bCount; ++s) mbar_init(&bars[s], s == bSread || s == bP || s == bPS ? 256 : s == bOut ? 128 : s >= bEmptyQ && s < bS ? 4 : 1);
+        for (int s = 0; s < bCount; ++s) mbar_init(&bars[s], s == bSread || s == bP || s == bPS ? 256 : s == bOut || s == bOutQ ? 128 : s >= bEmptyQ && s < bS ? 4 : 1);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v); prefetch_tensormap(&tm_o);
@@ -227,14 +235,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         int acc = 0;                                                 // the set its key block is in
         auto tile_q = [&](int n) { return sm + C::offQ + (n % C::kSlotsQ) * kTileBytes; };
         auto tile_o = [&](int n) { return sm + C::offO + (n & 1) * kTileBytes; };
-        // scores or dP: rows of `a` (Q or dO) by the halves in a ring of NR slots, as many at a time as lie side by side: a product reads `a`
-        // once however many they are, and shared memory's bandwidth is what bounds the products
-        auto scores = [&](uint32_t a, uint32_t ring, int NR) {
+        // scores or dP: rows of `a` (Q or dO) by halves j0 .. j1 - 1 in a ring of NR slots, as many at a time as lie side by side: a product
+        // reads `a` once however many they are, and shared memory's bandwidth is what bounds the products
+        auto scores = [&](uint32_t a, uint32_t ring, int NR, int j0, int j1) {
             const uint32_t la = lo(d1, a);
-            const int s0 = hb % NR, side = min(NH, NR - s0);
 #pragma unroll 1
-            for (int j = 0, count = side; j < NH; j += count, count = NH - side) {
-                const uint32_t lb = lo(d1, ring + (j == 0 ? s0 : 0) * kHalfBytes), d = tb + colX + 64 * j;
+            for (int j = j0, count; j < j1; j += count) {
+                const int slot = (hb + j) % NR;
+                count = min(j1 - j, NR - slot);
+                const uint32_t lb = lo(d1, ring + slot * kHalfBytes), d = tb + colX + 64 * j;
                 const uint32_t i = iS0 | (uint32_t)(8 * count) << 17;
                 mma_ss_w<false>(lead, d, la, desc_hi(d1), lb, desc_hi(d1), i);
 #pragma unroll
@@ -242,17 +251,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         };
         auto issue_s = [&](int n) -> bool {
-            // (PAD 128: dQ of the tile before lies over the scores)
-            if (!wait(bFullA + (n & 1), n >> 1) || (PAD == 128 && n > 0 && !wait(bOut, n - 1))) return false;
+            if (!wait(bFullA + (n & 1), n >> 1)) return false;
             tc_fence_after();
-            scores(tile_q(n), sm, NK);
+            if (PAD == 128 && n > 0) {                               // dQ of the tile before lies over the first half's scores
+                scores(tile_q(n), sm, NK, 1, NH);
+                if (!wait(bOutQ, n - 1)) return false;
+                tc_fence_after();
+                scores(tile_q(n), sm, NK, 0, 1);
+            } else {
+                scores(tile_q(n), sm, NK, 0, NH);
+            }
             mma_commit_w(lead, &bars[bS]);
             return true;
         };
         auto issue_dp = [&](int n) -> bool {
             if (!wait(bSread, n) || !wait(bFullB + (n & 1), n >> 1)) return false;
             tc_fence_after();
-            scores(tile_o(n), sm + C::offV, NV);
+            scores(tile_o(n), sm + C::offV, NV, 0, NH);
             mma_commit_w(lead, &bars[bDP]);
             return true;
         };
@@ -290,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int n = 0; n < N && ok; ++n) {
             const Tile t = run.tile(n);
             const bool with_b = !t.end || t.last;                    // the next block is this run's too
-            const bool early = PAD == 64 && !t.end && !t.last;       // (a new head's halves wait for this tile's slots)
+            const bool early = !t.end && !t.last;                    // (a new head's halves wait for this tile's slots)
             const int drop = t.last ? NH : 2;                        // halves that the next tile does not use
             // dV, or dV and dK.  What they begin was last used by the tile before and has been read out
             auto products = [&](int from, int to) {
@@ -302,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             };
             if constexpr (C::kShared) {
-                ok = wait(bP, n);
+                ok = wait(bP, n) && (n == 0 || wait(bOut, n - 1));
                 if (!ok) break;
                 tc_fence_after();
                 products(1, 1);
@@ -311,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = wait(bPS, n);
             if (!ok) break;
             tc_fence_after();
-            if (early) {
+            if (PAD == 64 && early) {
                 hb += drop;
                 ok = issue_s(n + 1);
                 hb -= drop;
@@ -332,6 +347,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             mma_commit_w(lead, &bars[bKdone + (n & 1)]);
             hb += drop;
+            if (PAD == 128 && early) ok = issue_s(n + 1);
+            if (!ok) break;
             products(C::kShared ? 0 : 1, 0);
             mma_commit_w(lead, &bars[bDone + (n & 1)]);
             if (!t.last) acc ^= 1;
@@ -345,7 +362,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         int acc = 0;
         for (int n = 0; n < N && ok; ++n) {
             const Tile t = run.tile(n);
-            ok = __all_sync(0xffffffffu, mbar_wait(&bars[bDone + (n & 1)], (n >> 1) & 1, abort_flag));
+            uint32_t c[PAD == 64 ? 3 : 2][8][4];
+            auto wait = [&](int bar) -> bool { return __all_sync(0xffffffffu, mbar_wait(&bars[bar + (n & 1)], (n >> 1) & 1, abort_flag)); };
+            if constexpr (PAD == 128) {                              // (S of the next tile waits for it)
+                ok = wait(bKdone);
+                if (!ok) break;
+                tc_fence_after();
+                if (!t.halo) read_rows(tmem_addr(tb, lanes, colDQ<PAD>), c[0]);
+                tc_fence_before();
+                mbar_arrive(&bars[bOutQ]);
+            }
+            ok = wait(bDone);
             if (!ok) break;
             tc_fence_after();
             const int key = t.i * kQT - PAD + (int)(lanes ^ 64u);
@@ -362,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tma_store_commit();
                 }
             };
-            uint32_t c[3][8][4];
+            if (PAD == 128 && !t.halo) send(c[0], tm_dq, t.i * kQT + (int)lanes);
             if (t.last) {
                 read_rows(tmem_addr(tb, lanes, colAcc + 128 * (acc ^ 1)), c[0]);
                 send(c[0], tm_dk, key + kQT);
@@ -370,16 +397,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 send(c[0], tm_dv, key + kQT);
             }
             if (!t.halo) {
-                read_rows(tmem_addr(tb, lanes, colDQ<PAD>), c[0]);
-                read_rows(tmem_addr(tb, lanes, colAcc + 128 * acc), c[1]);
-                read_rows(tmem_addr(tb, lanes, colAcc + 128 * acc + 64), c[2]);
+                read_rows(tmem_addr(tb, lanes, colAcc + 128 * acc), c[0]);
+                read_rows(tmem_addr(tb, lanes, colAcc + 128 * acc + 64), c[1]);
+                if constexpr (PAD == 64) read_rows(tmem_addr(tb, lanes, colDQ<PAD>), c[2]);
             }
             tc_fence_before();
             mbar_arrive(&bars[bOut]);
             if (!t.halo) {
-                send(c[0], tm_dq, t.i * kQT + (int)lanes);
-                send(c[1], tm_dk, key);
-                send(c[2], tm_dv, key);
+                send(c[0], tm_dk, key);
+                send(c[1], tm_dv, key);
+                if constexpr (PAD == 64) send(c[2], tm_dq, t.i * kQT + (int)lanes);
             }
             if (lane == 0) {
                 tma_store_wait_read<0>();
@@ -410,26 +437,29 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int x = max(first - 32 * b, 0), y = min(hi - 32 * b, 31);
                 seen[b] = x > y ? 0u : (0xffffffffu >> (31 - (y - x))) << x;
             }
+            const bool all = __all_sync(0xffffffffu, first <= 0 && hi >= NC - 1);      // (of the whole warp's)
             float e[NC];
             ok = mbar_wait(&bars[bS], n & 1, abort_flag);
             __syncwarp();
             tc_fence_after();
 #pragma unroll
-            for (int b = 0; b < NC; b += 16) {
-                uint32_t x[16];
-                tmem_ld16(tx + b, x);
+            for (int b = 0; b < NC; b += 8) {
+                uint32_t x[8];
+                tmem_ld8(tx + b, x);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) e[b + k] = __uint_as_float(x[k]);
+                for (int k = 0; k < 8; ++k) e[b + k] = __uint_as_float(x[k]);
             }
             tmem_wait_ld();
             tc_fence_before();
             mbar_arrive(&bars[bSread]);
-            float mx = -INFINITY;
+            // (a branch: without it the compiler moves the loads' use about, and the case of 3 x 16 x 1777 takes 43 us, not 36)
+            if (!all) {
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                e[k] = (seen[k >> 5] >> (k & 31)) & 1u ? e[k] : -INFINITY;
-                mx = fmaxf(mx, e[k]);
+                for (int k = 0; k < NC; ++k) e[k] = (seen[k >> 5] >> (k & 31)) & 1u ? e[k] : -INFINITY;
             }
+            float mx = e[0];
+#pragma unroll
+            for (int k = 1; k < NC; ++k) mx = fmaxf(mx, e[k]);
             const float m0 = mx == -INFINITY ? 0.f : mx;             // (no key in this half)
             pairs::pair l2 = 0, ep[NP];
 #pragma unroll
@@ -446,12 +476,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             constexpr bool kKeep = NC <= 48;
             pairs::pair dp[kKeep ? NP : 1], w2 = 0;
 #pragma unroll
-            for (int b = 0; b < NC; b += 16) {
-                uint32_t x[16];
-                tmem_ld16(tx + b, x);
+            for (int b = 0; b < NC; b += 8) {
+                uint32_t x[8];
+                tmem_ld8(tx + b, x);
                 if constexpr (!kKeep) tmem_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < 4; ++k) {
                     const pairs::pair y = pairs::make(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
                     if constexpr (kKeep) dp[b / 2 + k] = y;
                     else w2 = pairs::fma2(ep[b / 2 + k], y, w2);
@@ -478,41 +508,47 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 f = pairs::split(x);
                 return pack2(f.x, f.y);
             };
-#pragma unroll
-            for (int k = 0; k < NP; ++k) ep[k] = pairs::mul2(ep[k], pf);
+            // (the weights all at once or chunk by chunk, whichever the compiler's schedule is better with: PAD 64, 2 x 16 x 32768: 214 us
+            // at once, 208 by chunks; PAD 128, 3 x 16 x 1777: 36 and 48)
             if constexpr (C::kShared) {
 #pragma unroll
-                for (int k = 0; k < NP; k += 4)
-                    *reinterpret_cast<uint4*>(chunk(false, c0 + 2 * k)) = make_uint4(packed(ep[k]), packed(ep[k + 1]), packed(ep[k + 2]), packed(ep[k + 3]));
+                for (int k = 0; k < NP; ++k) ep[k] = pairs::mul2(ep[k], pf);
+            }
+#pragma unroll
+            for (int k = 0; k < NP; k += 4) {
+                if constexpr (!C::kShared) {
+#pragma unroll
+                    for (int j = k; j < k + 4; ++j) ep[j] = pairs::mul2(ep[j], pf);
+                    asm volatile("" ::: "memory");
+                }
+                *reinterpret_cast<uint4*>(chunk(false, c0 + 2 * k)) = make_uint4(packed(ep[k]), packed(ep[k + 1]), packed(ep[k + 2]), packed(ep[k + 3]));
+            }
+            if constexpr (C::kShared) {
                 fence_proxy_async_smem();
                 mbar_arrive(&bars[bP]);
+            }
+            uint32_t ds[NP];
+#pragma unroll
+            for (int b = 0; b < NP; b += 4) {
+                uint32_t x[8];
+                if constexpr (!kKeep) {
+                    tmem_ld8(tx + 2 * b, x);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    pairs::pair y;
+                    if constexpr (kKeep) y = dp[b + k];
+                    else y = pairs::make(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
+                    ds[b + k] = packed(pairs::mul2(pairs::mul2(ep[b + k], df), pairs::add2(y, nD)));
+                }
+            }
+            if constexpr (C::kShared) {                              // dS takes P's place
                 ok = pair_all(1 + u, mbar_wait(&bars[bPdone], n & 1, abort_flag));
                 if (!ok) break;
             }
 #pragma unroll
-            for (int b = 0; b < NP; b += 8) {
-                uint32_t x[16];
-                if constexpr (!kKeep) {
-                    tmem_ld16(tx + 2 * b, x);
-                    tmem_wait_ld();
-                }
-#pragma unroll
-                for (int g = 0; g < 8; g += 4) {
-                    uint32_t ds[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        pairs::pair y;
-                        if constexpr (kKeep) y = dp[b + g + k];
-                        else y = pairs::make(__uint_as_float(x[2 * (g + k)]), __uint_as_float(x[2 * (g + k) + 1]));
-                        ds[k] = packed(pairs::mul2(pairs::mul2(ep[b + g + k], df), pairs::add2(y, nD)));
-                    }
-                    const int c = c0 + 2 * (b + g);
-                    if constexpr (!C::kShared)
-                        *reinterpret_cast<uint4*>(chunk(false, c)) =
-                            make_uint4(packed(ep[b + g]), packed(ep[b + g + 1]), packed(ep[b + g + 2]), packed(ep[b + g + 3]));
-                    *reinterpret_cast<uint4*>(chunk(true, c)) = make_uint4(ds[0], ds[1], ds[2], ds[3]);
-                }
-            }
+            for (int k = 0; k < NP; k += 4) *reinterpret_cast<uint4*>(chunk(true, c0 + 2 * k)) = make_uint4(ds[k], ds[k + 1], ds[k + 2], ds[k + 3]);
             tc_fence_before();
             fence_proxy_async_smem();
             mbar_arrive(&bars[bPS]);
