@@ -4,52 +4,81 @@
 //   P_ij = exp(c (s_ij - m_i)) / l_i,  dP_ij = dout_i . v_j,  D_i = sum_j P_ij dP_ij,  dS_ij = c P_ij (dP_ij - D_i),
 //   dq_i = sum_j dS_ij k_j,   dk_j = sum_i dS_ij q_i,   dv_j = sum_i P_ij dout_i        (s = q k^T)
 //
-// Two kernels on tiles of 64 x 64 pairs, 4 x 4 of them per thread, operands as padded fp32 rows in shared memory.  The first
-// takes 64 queries: their scores and dP against all the keys they see (two or three tiles of 64, held in registers) give the
-// row statistics m, 1/l, D, then dS and dq.  The second takes 64 keys and recomputes P and dS of the queries that see them
-// from the statistics.  Neither adds into memory that another CTA writes, so results do not depend on any order.
+// Two kernels of 256 threads on 64 rows each, in four strips of 16: 64 threads work on a strip and the NB blocks of 16 rows of
+// the other side that it meets (the queries i meet the keys i - 64 .. i: 80 of them for windows up to 65, 144 for those up to
+// 128), 4 x NB pairs per thread in registers.  The first kernel takes queries: scores and dP give the row statistics m, 1/l, D,
+// then dS and dq.  The second takes keys and recomputes P and dS of the queries that see them from the statistics.  Neither adds
+// into memory that another CTA writes, so results do not depend on any order.
+//
+// Bound by the multiply-adds (7 products of 16 x 16 NB x 64 per strip) and the shared-memory reads that feed them, 0.7 of the
+// multiply-adds' time; scores and dP take even and odd elements in pairs, which halves their instructions.
+// Measured: 16 heads x 1000 queries, window 64: 40 us, window 128: 74; 32 x 4096: 256 and 511 (57 % of the multiply-adds' rate with
+// window 64).  On tiles of 64 x 64, half of whose pairs lie outside the band, these took 68, 98, 511 and 709.
 #include "common.cuh"
+#include "pairs.cuh"
 
 namespace based {
+using namespace pairs;
 
 namespace {
-constexpr int kT = 64, kHD = 64, kStride = kHD + 4, kThreads = 256;
-constexpr int kTile = kT * kStride;
-constexpr size_t kSmemQ = 5 * kTile * sizeof(float), kSmemK = 6 * kTile * sizeof(float) + kT * sizeof(float4);
+constexpr int kT = 64, kS = 16, kHD = 64, kStride = kHD + 4, kThreads = 256;
+template <int NB> struct Cfg {
+    static constexpr int kFar = kT - kS + kS * NB;                   // rows of the other side: those of four strips
+    static constexpr int kPStride = kS * NB + 4;                     // of a row of P or dS
+    static constexpr int kNear = 2 * kT * kStride, kWeights = 2 * kT * kPStride;
+    static constexpr size_t kSmemQ = (kNear + 2 * kFar * kStride) * sizeof(float);
+    static constexpr size_t kSmemK = ((kNear > kWeights ? kNear : kWeights) + 2 * kFar * kStride) * sizeof(float) + kFar * sizeof(float4);
+    static_assert(kT * kPStride <= kFar * kStride && kSmemK <= 232448 && kSmemQ <= 232448, "shared memory");
+};
 
-// rows r0 .. r0 + 63 of [L][64] into a padded tile, zeros outside [0, L)
-__device__ __forceinline__ void load_tile(float* dst, const float* src, int r0, int L) {
-    for (int i = threadIdx.x; i < kT * kHD / 4; i += kThreads) {
-        const int row = i / (kHD / 4), col = (i % (kHD / 4)) * 4;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r0 + row >= 0 && r0 + row < L) x = *reinterpret_cast<const float4*>(src + (size_t)(r0 + row) * kHD + col);
-        *reinterpret_cast<float4*>(dst + row * kStride + col) = x;
+// ROWS rows from r0 on of [L][64] into padded rows, zeros outside [0, L)
+template <int ROWS> __device__ __forceinline__ void load_rows(float* dst, const float* src, int r0, int L) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < ROWS * kHD / 4; i += kThreads) {
+        const int row = i / (kHD / 4), col = (i % (kHD / 4)) * 4, r = r0 + row;
+        const bool in = r >= 0 && r < L;
+        copy_async16(dst + row * kStride + col, src + (size_t)(in ? r : 0) * kHD + col, in);
     }
 }
+// the 64 threads of a strip
+__device__ __forceinline__ void strip_sync(int strip) { asm volatile("bar.sync %0, 64;" ::"r"(1 + strip) : "memory"); }
 __device__ __forceinline__ float4 lds(const float* p) { return *reinterpret_cast<const float4*>(p); }
-// acc[i][j] += a[row ty + 16 i] . b[row tx + 16 j] over 64
-__device__ __forceinline__ void dots(float (&acc)[4][4], const float* a, const float* b, int ty, int tx) {
-#pragma unroll 4
+// out[i][j] = a[row ty + 4 i] . b[row tx + 16 j] over 64
+template <int NB> __device__ __forceinline__ void dots(float (&out)[4][NB], const float* a, const float* b, int ty, int tx) {
+    pair acc[4][NB];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = 0;
+#pragma unroll 2
     for (int d = 0; d < kHD; d += 4) {
-        float4 x[4], y[4];
+        ulonglong2 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = lds(a + (ty + 16 * i) * kStride + d);
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(a + (ty + 4 * i) * kStride + d);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = lds(b + (tx + 16 * j) * kStride + d);
+        for (int j = 0; j < NB; ++j) {
+            const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(b + (tx + 16 * j) * kStride + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, acc[i][j]))));
+            for (int i = 0; i < 4; ++i) acc[i][j] = fma2(x[i].y, y.y, fma2(x[i].x, y.x, acc[i][j]));
+        }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const float2 f = split(acc[i][j]);
+            out[i][j] = f.x + f.y;
+        }
 }
-// acc[i][0..3] += sum_k a[row ty + 16 i][k] b[k][4 tx ..]
-__device__ __forceinline__ void product(float (&acc)[4][4], const float* a, const float* b, int ty, int tx) {
+// acc[i][0..3] = sum over the strip's 16 NB of a[row ty + 4 i][k] b[k][4 tx ..]
+template <int NB> __device__ __forceinline__ void product(float (&acc)[4][4], const float* a, const float* b, int ty, int tx) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i >> 2][i & 3] = 0.f;
 #pragma unroll 4
-    for (int k = 0; k < kT; k += 4) {
+    for (int k = 0; k < kS * NB; k += 4) {
         float4 x[4], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = lds(a + (ty + 16 * i) * kStride + k);
+        for (int i = 0; i < 4; ++i) x[i] = lds(a + (ty + 4 * i) * Cfg<NB>::kPStride + k);
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = lds(b + (k + j) * kStride + 4 * tx);
 #pragma unroll
@@ -68,7 +97,7 @@ __device__ __forceinline__ void product(float (&acc)[4][4], const float* a, cons
 __device__ __forceinline__ void store_rows(float* dst, const float (&acc)[4][4], int r0, int L, int ty, int tx) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int row = r0 + ty + 16 * i;
+        const int row = r0 + ty + 4 * i;
         if (row >= L) continue;
         *reinterpret_cast<float4*>(dst + (size_t)row * kHD + 4 * tx) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
     }
@@ -85,143 +114,131 @@ __device__ __forceinline__ float sum16(float x) {
 }
 }  // namespace
 
-// 64 queries against TILES tiles of 64 keys (the last of them their own); stats: (m, 1 / l, D, 0) per row
-template <int TILES>
-__global__ void __launch_bounds__(kThreads) swa_backward_queries_kernel(const float* __restrict__ q, const float* __restrict__ k,
-                                                                        const float* __restrict__ v, const float* __restrict__ dout,
-                                                                        float* __restrict__ dq, float4* __restrict__ stats, int L, int window,
-                                                                        float scale) {
+// 64 queries; stats: (m, 1 / l, D, 0) per row
+template <int NB>
+__global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
+    swa_backward_queries_kernel(const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
+                                const float* __restrict__ dout, float* __restrict__ dq, float4* __restrict__ stats, int L, int window,
+                                float scale) {
+    using C = Cfg<NB>;
     extern __shared__ __align__(16) float smem[];
-    float *sQ = smem, *sO = sQ + kTile, *sK = sO + kTile, *sV = sK + kTile, *sD = sV + kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, i0 = blockIdx.x * kT;
+    float *sQ = smem, *sO = sQ + kT * kStride, *sK = sO + kT * kStride, *sV = sK + C::kFar * kStride, *sD = sV;      // (dS over V)
+    const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 3, strip = threadIdx.x >> 6, i0 = blockIdx.x * kT;
     const size_t head = (size_t)blockIdx.y * L * kHD;
+    const int r0 = kS * strip, first = i0 + r0 - kS * (NB - 1);      // the strip's first row, and its first key
     enter_dependent();
-    load_tile(sQ, q + head, i0, L);
-    load_tile(sO, dout + head, i0, L);
-    float s[TILES][4][4], dp[TILES][4][4];
+    load_rows<kT>(sQ, q + head, i0, L);
+    load_rows<C::kFar>(sK, k + head, i0 - kS * (NB - 1), L);
+    copy_async_commit();
+    load_rows<kT>(sO, dout + head, i0, L);
+    load_rows<C::kFar>(sV, v + head, i0 - kS * (NB - 1), L);
+    copy_async_commit();
+    copy_async_wait<1>();
+    __syncthreads();
+    float s[4][NB], dp[4][NB];
+    dots<NB>(s, sQ + r0 * kStride, sK + r0 * kStride, ty, tx);
+    copy_async_wait<0>();
+    __syncthreads();
+    dots<NB>(dp, sO + r0 * kStride, sV + r0 * kStride, ty, tx);
+    __syncthreads();                                                 // (everyone is done with V)
     const float c = scale * 1.4426950408889634f;
-    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-        const int j0 = i0 - (TILES - 1 - t) * kT;
-        __syncthreads();
-        load_tile(sK, k + head, j0, L);
-        load_tile(sV, v + head, j0, L);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i >> 2][i & 3] = dp[t][i >> 2][i & 3] = 0.f;
-        dots(s[t], sQ, sK, ty, tx);
-        dots(dp[t], sO, sV, ty, tx);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int qi = i0 + ty + 16 * i, kj = j0 + tx + 16 * j;
-                const bool seen = kj >= 0 && kj <= qi && kj > qi - window;
-                s[t][i][j] = seen ? s[t][i][j] : -INFINITY;
-                dp[t][i][j] = seen ? dp[t][i][j] : 0.f;
-                mx[i] = fmaxf(mx[i], s[t][i][j]);
-            }
-    }
-    float inv[4], D[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        mx[i] = max16(mx[i]);                                    // (finite: a row sees its own key)
+        const int qi = i0 + r0 + ty + 4 * i;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int kj = first + tx + 16 * j;
+            const bool seen = kj >= 0 && kj <= qi && kj > qi - window;
+            s[i][j] = seen ? s[i][j] : -INFINITY;
+            dp[i][j] = seen ? dp[i][j] : 0.f;
+            mx = fmaxf(mx, s[i][j]);
+        }
+        mx = max16(mx);                                              // (finite: a row sees its own key)
         float l = 0.f, w = 0.f;
 #pragma unroll
-        for (int t = 0; t < TILES; ++t)
+        for (int j = 0; j < NB; ++j) {
+            s[i][j] = exp2f((s[i][j] - mx) * c);
+            l += s[i][j];
+            w = fmaf(s[i][j], dp[i][j], w);
+        }
+        const float inv = 1.f / sum16(l), D = sum16(w) * inv;
+        if (tx == 0 && qi < L) stats[(size_t)blockIdx.y * L + qi] = make_float4(mx, inv, D, 0.f);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s[t][i][j] = exp2f((s[t][i][j] - mx[i]) * c);
-                l += s[t][i][j];
-                w = fmaf(s[t][i][j], dp[t][i][j], w);
-            }
-        inv[i] = 1.f / sum16(l);
-        D[i] = sum16(w) * inv[i];
-        if (tx == 0 && i0 + ty + 16 * i < L)
-            stats[(size_t)blockIdx.y * L + i0 + ty + 16 * i] = make_float4(mx[i], inv[i], D[i], 0.f);
+        for (int j = 0; j < NB; ++j) sD[(r0 + ty + 4 * i) * C::kPStride + tx + 16 * j] = s[i][j] * inv * (dp[i][j] - D) * scale;
     }
-    float acc[4][4] = {};
-    // the last tile of keys is still in shared memory
-#pragma unroll
-    for (int t = TILES - 1; t >= 0; --t) {
-        __syncthreads();
-        if (t < TILES - 1) load_tile(sK, k + head, i0 - (TILES - 1 - t) * kT, L);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                sD[(ty + 16 * i) * kStride + tx + 16 * j] = s[t][i][j] * inv[i] * (dp[t][i][j] - D[i]) * scale;
-        __syncthreads();
-        product(acc, sD, sK, ty, tx);
-    }
-    store_rows(dq + head, acc, i0, L, ty, tx);
+    strip_sync(strip);
+    float acc[4][4];
+    product<NB>(acc, sD + r0 * C::kPStride, sK + r0 * kStride, ty, tx);
+    store_rows(dq + head, acc, i0 + r0, L, ty, tx);
 }
 
-// 64 keys and the TILES tiles of queries that see them (the first of them their own)
-template <int TILES>
-__global__ void __launch_bounds__(kThreads) swa_backward_keys_kernel(const float* __restrict__ q, const float* __restrict__ k,
-                                                                     const float* __restrict__ v, const float* __restrict__ dout,
-                                                                     const float4* __restrict__ stats, float* __restrict__ dk,
-                                                                     float* __restrict__ dv, int L, int window, float scale) {
+// 64 keys and the queries that see them
+template <int NB>
+__global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
+    swa_backward_keys_kernel(const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
+                             const float* __restrict__ dout, const float4* __restrict__ stats, float* __restrict__ dk, float* __restrict__ dv,
+                             int L, int window, float scale) {
+    using C = Cfg<NB>;
     extern __shared__ __align__(16) float smem[];
-    float *sK = smem, *sV = sK + kTile, *sQ = sV + kTile, *sO = sQ + kTile, *sP = sO + kTile, *sD = sP + kTile;
-    float4* sS = reinterpret_cast<float4*>(sD + kTile);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, j0 = blockIdx.x * kT;
+    float *sQ = smem, *sO = sQ + C::kFar * kStride, *sK = sO + C::kFar * kStride + C::kFar * 4, *sV = sK + kT * kStride;
+    float *sP = sK, *sD = sP + kT * C::kPStride;                     // (over K and V)
+    float4* sS = reinterpret_cast<float4*>(sO + C::kFar * kStride);
+    const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 3, strip = threadIdx.x >> 6, j0 = blockIdx.x * kT, r0 = kS * strip;
     const size_t head = (size_t)blockIdx.y * L * kHD;
     enter_dependent();
-    load_tile(sK, k + head, j0, L);
-    load_tile(sV, v + head, j0, L);
+    load_rows<kT>(sK, k + head, j0, L);
+    load_rows<C::kFar>(sQ, q + head, j0, L);
+    copy_async_commit();
+    load_rows<kT>(sV, v + head, j0, L);
+    load_rows<C::kFar>(sO, dout + head, j0, L);
+    for (int i = threadIdx.x; i < C::kFar; i += kThreads) copy_async16(sS + i, stats + (size_t)blockIdx.y * L + min(j0 + i, L - 1), j0 + i < L);
+    copy_async_commit();
+    copy_async_wait<1>();
+    __syncthreads();
+    float s[4][NB], dp[4][NB];
+    dots<NB>(s, sK + r0 * kStride, sQ + r0 * kStride, ty, tx);
+    copy_async_wait<0>();
+    __syncthreads();
+    dots<NB>(dp, sV + r0 * kStride, sO + r0 * kStride, ty, tx);
+    __syncthreads();                                                 // (everyone is done with K and V)
     const float c = scale * 1.4426950408889634f;
-    float ak[4][4] = {}, av[4][4] = {};
-    for (int t = 0; t < TILES; ++t) {
-        const int i0 = j0 + t * kT;
-        if (i0 >= L) break;
-        __syncthreads();
-        load_tile(sQ, q + head, i0, L);
-        load_tile(sO, dout + head, i0, L);
-        if (threadIdx.x < kT)
-            sS[threadIdx.x] = i0 + threadIdx.x < L ? stats[(size_t)blockIdx.y * L + i0 + threadIdx.x] : make_float4(0.f, 0.f, 0.f, 0.f);
-        __syncthreads();
-        float s[4][4] = {}, dp[4][4] = {};
-        dots(s, sQ, sK, ty, tx);
-        dots(dp, sO, sV, ty, tx);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int qi = j0 + r0 + tx + 16 * j;
+        const float4 st = sS[r0 + tx + 16 * j];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4 st = sS[ty + 16 * i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int qi = i0 + ty + 16 * i, kj = j0 + tx + 16 * j;
-                const bool seen = kj <= qi && kj > qi - window && qi < L;
-                const float P = seen ? exp2f((s[i][j] - st.x) * c) * st.y : 0.f;
-                const int at = (tx + 16 * j) * kStride + ty + 16 * i;          // [key][query]
-                sP[at] = P;
-                sD[at] = seen ? P * (dp[i][j] - st.z) * scale : 0.f;
-            }
+            const int kj = j0 + r0 + ty + 4 * i, at = (r0 + ty + 4 * i) * C::kPStride + tx + 16 * j;
+            const bool seen = kj <= qi && kj > qi - window && qi < L;
+            const float P = seen ? exp2f((s[i][j] - st.x) * c) * st.y : 0.f;
+            sP[at] = P;
+            sD[at] = seen ? P * (dp[i][j] - st.z) * scale : 0.f;
         }
-        __syncthreads();
-        product(av, sP, sO, ty, tx);
-        product(ak, sD, sQ, ty, tx);
     }
-    store_rows(dk + head, ak, j0, L, ty, tx);
-    store_rows(dv + head, av, j0, L, ty, tx);
+    strip_sync(strip);
+    float acc[4][4];
+    product<NB>(acc, sP + r0 * C::kPStride, sO + r0 * kStride, ty, tx);
+    store_rows(dv + head, acc, j0 + r0, L, ty, tx);
+    product<NB>(acc, sD + r0 * C::kPStride, sQ + r0 * kStride, ty, tx);
+    store_rows(dk + head, acc, j0 + r0, L, ty, tx);
 }
 
-template <int TILES>
-static based_status launch_tiles(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, float* stats,
+template <int NB>
+static based_status launch_blocks(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, float* stats,
                                  int BH, int L, int window, float scale, cudaStream_t stream) {
-    auto kq = swa_backward_queries_kernel<TILES>;
-    auto kk = swa_backward_keys_kernel<TILES>;
+    auto kq = swa_backward_queries_kernel<NB>;
+    auto kk = swa_backward_keys_kernel<NB>;
     // per-device attributes; setting them on every call keeps multi-device processes correct
-    if (cudaFuncSetAttribute(kq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemQ) != cudaSuccess ||
-        cudaFuncSetAttribute(kk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemK) != cudaSuccess)
+    if (cudaFuncSetAttribute(kq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<NB>::kSmemQ) != cudaSuccess ||
+        cudaFuncSetAttribute(kk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<NB>::kSmemK) != cudaSuccess)
         return BASED_ERR_CUDA;
     const dim3 grid((L + kT - 1) / kT, BH);
     auto in = [](const void* p) { return static_cast<const float*>(p); };
-    cudaError_t e = launch_ex(kq, grid, dim3(kThreads), kSmemQ, 1, true, stream, in(q), in(k), in(v), in(dout), static_cast<float*>(dq),
+    cudaError_t e = launch_ex(kq, grid, dim3(kThreads), Cfg<NB>::kSmemQ, 1, true, stream, in(q), in(k), in(v), in(dout), static_cast<float*>(dq),
                               reinterpret_cast<float4*>(stats), L, window, scale);
     if (e == cudaSuccess)
-        e = launch_ex(kk, grid, dim3(kThreads), kSmemK, 1, true, stream, in(q), in(k), in(v), in(dout),
+        e = launch_ex(kk, grid, dim3(kThreads), Cfg<NB>::kSmemK, 1, true, stream, in(q), in(k), in(v), in(dout),
                       reinterpret_cast<const float4*>(stats), static_cast<float*>(dk), static_cast<float*>(dv), L, window, scale);
     note_launch();
     note_launch();
@@ -231,9 +248,9 @@ static based_status launch_tiles(const void* q, const void* k, const void* v, co
 
 based_status launch_swa_backward_f32(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
                                      float* stats, int BH, int L, int window, float scale, cudaStream_t stream) {
-    // a query's first key lies window - 1 before it: one tile of 64 back, or two
-    return window <= kT + 1 ? launch_tiles<2>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream)
-                            : launch_tiles<3>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
+    // a query's first key lies window - 1 before it: 64 / 16 blocks back, or 128 / 16
+    return window <= 65 ? launch_blocks<5>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream)
+                        : launch_blocks<9>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
 }
 
 }  // namespace based
