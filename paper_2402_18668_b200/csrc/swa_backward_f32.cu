@@ -12,7 +12,7 @@
 //
 // Bound by the multiply-adds (7 products of 16 x 16 NB x 64 per strip) and the shared-memory reads that feed them, 0.7 of the
 // multiply-adds' time; scores and dP take even and odd elements in pairs, which halves their instructions.
-// Measured: 16 heads x 1000 queries, window 64: 40 us, window 128: 74; 32 x 4096: 256 and 511 (57 % of the multiply-adds' rate with
+// Measured: 16 heads x 1000 queries, window 64: 40 us, window 128: 74; 32 x 4096: 256 and 511 (51 % of the multiply-adds' rate with
 // window 64).  On tiles of 64 x 64, half of whose pairs lie outside the band, these took 68, 98, 511 and 709.
 #include "common.cuh"
 #include "pairs.cuh"
