@@ -6,6 +6,9 @@ autograd, routes the output gradient through based_prefill_backward (with the sa
 output, which lets the bf16 path merge two of its passes).  The node itself is native
 (csrc_host/native.cpp), so neither direction waits for the interpreter; both run in the library's
 kernels.
+
+A backward pass can be captured into a CUDA graph under torch's own rule for that: no eager graph of the same leaves may be alive
+(their gradients would be accumulated on the stream that it was built on, which the capture refuses with an error).
 """
 from __future__ import annotations
 

@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks)
     };
     auto start = [&](Cursor& c) {
         c.count = min(gr.TB, m_end - c.m0);
-        c.left = (c.count * H + groups - 1) / groups;
+        c.left = (int)(((long long)c.count * H + groups - 1) / groups);       // (H up to 2^27)
         c.h = slot / c.count;
         c.tok = slot - c.h * c.count;
         c.dh = groups / c.count;
