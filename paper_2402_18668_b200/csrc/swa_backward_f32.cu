@@ -4,7 +4,7 @@
 //   P_ij = exp(c (s_ij - m_i)) / l_i,  dP_ij = dout_i . v_j,  D_i = sum_j P_ij dP_ij,  dS_ij = c P_ij (dP_ij - D_i),
 //   dq_i = sum_j dS_ij k_j,   dk_j = sum_i dS_ij q_i,   dv_j = sum_i P_ij dout_i        (s = q k^T)
 //
-// Two kernels of 256 threads on 64 rows each, in four strips of 16: 64 threads work on a strip and the NB blocks of 16 rows of
+// Two kernels of 64, 128 or 256 threads on one, two or four strips of 16 rows: 64 threads work on a strip and the NB blocks of 16 rows of
 // the other side that it meets (the queries i meet the keys i - 64 .. i: 80 of them for windows up to 65, 144 for those up to
 // 128), 4 x NB pairs per thread in registers.  The first kernel takes queries: scores and dP give the row statistics m, 1/l, D,
 // then dS and dq.  The second takes keys and recomputes P and dS of the queries that see them from the statistics.  Neither adds
@@ -21,8 +21,9 @@ namespace based {
 using namespace pairs;
 
 namespace {
-constexpr int kT = 64, kS = 16, kHD = 64, kStride = kHD + 4, kThreads = 256;
-template <int NB> struct Cfg {
+constexpr int kS = 16, kHD = 64, kStride = kHD + 4;
+template <int NB, int STRIPS> struct Cfg {
+    static constexpr int kT = kS * STRIPS, kThreads = 64 * STRIPS;   // rows of a CTA, threads
     static constexpr int kFar = kT - kS + kS * NB;                   // rows of the other side: those of four strips
     static constexpr int kPStride = kS * NB + 4;                     // of a row of P or dS
     static constexpr int kNear = 2 * kT * kStride, kWeights = 2 * kT * kPStride;
@@ -32,9 +33,9 @@ template <int NB> struct Cfg {
 };
 
 // ROWS rows from r0 on of [L][64] into padded rows, zeros outside [0, L)
-template <int ROWS> __device__ __forceinline__ void load_rows(float* dst, const float* src, int r0, int L) {
+template <int ROWS, int THREADS> __device__ __forceinline__ void load_rows(float* dst, const float* src, int r0, int L) {
 #pragma unroll 8
-    for (int i = threadIdx.x; i < ROWS * kHD / 4; i += kThreads) {
+    for (int i = threadIdx.x; i < ROWS * kHD / 4; i += THREADS) {
         const int row = i / (kHD / 4), col = (i % (kHD / 4)) * 4, r = r0 + row;
         const bool in = r >= 0 && r < L;
         copy_async16(dst + row * kStride + col, src + (size_t)(in ? r : 0) * kHD + col, in);
@@ -78,7 +79,7 @@ template <int NB> __device__ __forceinline__ void product(float (&acc)[4][4], co
     for (int k = 0; k < kS * NB; k += 4) {
         float4 x[4], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = lds(a + (ty + 4 * i) * Cfg<NB>::kPStride + k);
+        for (int i = 0; i < 4; ++i) x[i] = lds(a + (ty + 4 * i) * (kS * NB + 4) + k);
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = lds(b + (k + j) * kStride + 4 * tx);
 #pragma unroll
@@ -114,24 +115,25 @@ __device__ __forceinline__ float sum16(float x) {
 }
 }  // namespace
 
-// 64 queries; stats: (m, 1 / l, D, 0) per row
-template <int NB>
-__global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
+// 16 STRIPS queries; stats: (m, 1 / l, D, 0) per row
+template <int NB, int STRIPS>
+__global__ void __launch_bounds__(64 * STRIPS, NB == 5 ? 8 / STRIPS : 4 / STRIPS)
     swa_backward_queries_kernel(const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
                                 const float* __restrict__ dout, float* __restrict__ dq, float4* __restrict__ stats, int L, int window,
                                 float scale) {
-    using C = Cfg<NB>;
+    using C = Cfg<NB, STRIPS>;
+    constexpr int kT = C::kT, kThreads = C::kThreads;
     extern __shared__ __align__(16) float smem[];
     float *sQ = smem, *sO = sQ + kT * kStride, *sK = sO + kT * kStride, *sV = sK + C::kFar * kStride, *sD = sV;      // (dS over V)
     const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 3, strip = threadIdx.x >> 6, i0 = blockIdx.x * kT;
     const size_t head = (size_t)blockIdx.y * L * kHD;
     const int r0 = kS * strip, first = i0 + r0 - kS * (NB - 1);      // the strip's first row, and its first key
     enter_dependent();
-    load_rows<kT>(sQ, q + head, i0, L);
-    load_rows<C::kFar>(sK, k + head, i0 - kS * (NB - 1), L);
+    load_rows<kT, kThreads>(sQ, q + head, i0, L);
+    load_rows<C::kFar, kThreads>(sK, k + head, i0 - kS * (NB - 1), L);
     copy_async_commit();
-    load_rows<kT>(sO, dout + head, i0, L);
-    load_rows<C::kFar>(sV, v + head, i0 - kS * (NB - 1), L);
+    load_rows<kT, kThreads>(sO, dout + head, i0, L);
+    load_rows<C::kFar, kThreads>(sV, v + head, i0 - kS * (NB - 1), L);
     copy_async_commit();
     copy_async_wait<1>();
     __syncthreads();
@@ -173,13 +175,14 @@ __global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
     store_rows(dq + head, acc, i0 + r0, L, ty, tx);
 }
 
-// 64 keys and the queries that see them
-template <int NB>
-__global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
+// 16 STRIPS keys and the queries that see them
+template <int NB, int STRIPS>
+__global__ void __launch_bounds__(64 * STRIPS, NB == 5 ? 8 / STRIPS : 4 / STRIPS)
     swa_backward_keys_kernel(const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
                              const float* __restrict__ dout, const float4* __restrict__ stats, float* __restrict__ dk, float* __restrict__ dv,
                              int L, int window, float scale) {
-    using C = Cfg<NB>;
+    using C = Cfg<NB, STRIPS>;
+    constexpr int kT = C::kT, kThreads = C::kThreads;
     extern __shared__ __align__(16) float smem[];
     float *sQ = smem, *sO = sQ + C::kFar * kStride, *sK = sO + C::kFar * kStride + C::kFar * 4, *sV = sK + kT * kStride;
     float *sP = sK, *sD = sP + kT * C::kPStride;                     // (over K and V)
@@ -187,11 +190,11 @@ __global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
     const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 3, strip = threadIdx.x >> 6, j0 = blockIdx.x * kT, r0 = kS * strip;
     const size_t head = (size_t)blockIdx.y * L * kHD;
     enter_dependent();
-    load_rows<kT>(sK, k + head, j0, L);
-    load_rows<C::kFar>(sQ, q + head, j0, L);
+    load_rows<kT, kThreads>(sK, k + head, j0, L);
+    load_rows<C::kFar, kThreads>(sQ, q + head, j0, L);
     copy_async_commit();
-    load_rows<kT>(sV, v + head, j0, L);
-    load_rows<C::kFar>(sO, dout + head, j0, L);
+    load_rows<kT, kThreads>(sV, v + head, j0, L);
+    load_rows<C::kFar, kThreads>(sO, dout + head, j0, L);
     for (int i = threadIdx.x; i < C::kFar; i += kThreads) copy_async16(sS + i, stats + (size_t)blockIdx.y * L + min(j0 + i, L - 1), j0 + i < L);
     copy_async_commit();
     copy_async_wait<1>();
@@ -224,21 +227,22 @@ __global__ void __launch_bounds__(kThreads, NB == 5 ? 2 : 1)
     store_rows(dk + head, acc, j0 + r0, L, ty, tx);
 }
 
-template <int NB>
-static based_status launch_blocks(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, float* stats,
+template <int NB, int STRIPS>
+static based_status launch_strips(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv, float* stats,
                                  int BH, int L, int window, float scale, cudaStream_t stream) {
-    auto kq = swa_backward_queries_kernel<NB>;
-    auto kk = swa_backward_keys_kernel<NB>;
+    using C = Cfg<NB, STRIPS>;
+    auto kq = swa_backward_queries_kernel<NB, STRIPS>;
+    auto kk = swa_backward_keys_kernel<NB, STRIPS>;
     // per-device attributes; setting them on every call keeps multi-device processes correct
-    if (cudaFuncSetAttribute(kq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<NB>::kSmemQ) != cudaSuccess ||
-        cudaFuncSetAttribute(kk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<NB>::kSmemK) != cudaSuccess)
+    if (cudaFuncSetAttribute(kq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemQ) != cudaSuccess ||
+        cudaFuncSetAttribute(kk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemK) != cudaSuccess)
         return BASED_ERR_CUDA;
-    const dim3 grid((L + kT - 1) / kT, BH);
+    const dim3 grid((L + C::kT - 1) / C::kT, BH);
     auto in = [](const void* p) { return static_cast<const float*>(p); };
-    cudaError_t e = launch_ex(kq, grid, dim3(kThreads), Cfg<NB>::kSmemQ, 1, true, stream, in(q), in(k), in(v), in(dout), static_cast<float*>(dq),
+    cudaError_t e = launch_ex(kq, grid, dim3(C::kThreads), C::kSmemQ, 1, true, stream, in(q), in(k), in(v), in(dout), static_cast<float*>(dq),
                               reinterpret_cast<float4*>(stats), L, window, scale);
     if (e == cudaSuccess)
-        e = launch_ex(kk, grid, dim3(kThreads), Cfg<NB>::kSmemK, 1, true, stream, in(q), in(k), in(v), in(dout),
+        e = launch_ex(kk, grid, dim3(C::kThreads), C::kSmemK, 1, true, stream, in(q), in(k), in(v), in(dout),
                       reinterpret_cast<const float4*>(stats), static_cast<float*>(dk), static_cast<float*>(dv), L, window, scale);
     note_launch();
     note_launch();
@@ -248,9 +252,17 @@ static based_status launch_blocks(const void* q, const void* k, const void* v, c
 
 based_status launch_swa_backward_f32(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
                                      float* stats, int BH, int L, int window, float scale, cudaStream_t stream) {
-    // a query's first key lies window - 1 before it: 64 / 16 blocks back, or 128 / 16
-    return window <= 65 ? launch_blocks<5>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream)
-                        : launch_blocks<9>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
+    // A query's first key lies window - 1 before it: 64 / 16 blocks back, or 128 / 16.  Strips per CTA: four where the chip is full of
+    // such CTAs, fewer (more CTAs, less for each) where they are few.  us with 1 / 2 / 4, heads x queries, window 64: 4 x 100 16 / 16 / 23,
+    // 8 x 700 25 / 32 / 40, 16 x 700 39 / 33 / 41, 16 x 1000 46 / 44 / 40; window 128: 8 x 300 27 / 31 / 38, 8 x 700 48 / 43 / 38
+    const long long fours = ((long long)L + 63) / 64 * BH;
+    if (window <= 65) {
+        if (4 * fours <= 3 * kSMs) return launch_strips<5, 1>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
+        if (2 * fours <= 3 * kSMs) return launch_strips<5, 2>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
+        return launch_strips<5, 4>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
+    }
+    if (2 * fours <= kSMs) return launch_strips<9, 1>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
+    return launch_strips<9, 4>(q, k, v, dout, dq, dk, dv, stats, BH, L, window, scale, stream);
 }
 
 }  // namespace based

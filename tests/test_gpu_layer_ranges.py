@@ -20,7 +20,8 @@ def test_rotation_in_several_rounds(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,H,L,w", [(2, 40, 1300, 128), (2, 40, 1283, 64), (1, 3, 5003, 100), (4, 64, 130, 127), (300, 1, 129, 64)])
+@pytest.mark.parametrize("B,H,L,w", [(2, 40, 1300, 128), (2, 40, 1283, 64), (1, 3, 5003, 100), (4, 64, 130, 127), (300, 1, 129, 64),
+                                     (1, 8, 700, 64), (1, 8, 1100, 60), (2, 4, 290, 128), (1, 8, 700, 128)])
 def test_window_in_several_rounds(B, H, L, w, dtype):
     t = sliding.draw(B, H, L, dtype, seed=11)
     got = based.swa_backward(*t, window=w)
