@@ -10,9 +10,10 @@
 // then dS and dq.  The second takes keys and recomputes P and dS of the queries that see them from the statistics.  Neither adds
 // into memory that another CTA writes, so results do not depend on any order.
 //
-// Bound by the multiply-adds (7 products of 16 x 16 NB x 64 per strip) and the shared-memory reads that feed them, 0.7 of the
-// multiply-adds' time; scores and dP take even and odd elements in pairs, which halves their instructions.
-// Measured: 16 heads x 1000 queries, window 64: 40 us, window 128: 74; 32 x 4096: 256 and 511 (51 % of the multiply-adds' rate with
+// Bound by shared memory's reads, four fifths of the time, and the multiply-adds that they feed (7 products of 16 x 16 NB x 64 per
+// strip).  Scores and dP take even and odd elements in pairs, which halves their instructions.  Lanes that read the same 16 bytes are
+// neighbours, which serves half a warp at a time (half-warps that read the same rows: 40 us for 38, 255 for 235).
+// Measured: 16 heads x 1000 queries, window 64: 38 us, window 128: 70; 32 x 4096: 235 and 481 (56 % of the multiply-adds' rate with
 // window 64).  On tiles of 64 x 64, half of whose pairs lie outside the band, these took 68, 98, 511 and 709.
 #include "common.cuh"
 #include "pairs.cuh"
@@ -105,12 +106,12 @@ __device__ __forceinline__ void store_rows(float* dst, const float (&acc)[4][4],
 }
 __device__ __forceinline__ float max16(float x) {
 #pragma unroll
-    for (int o = 8; o > 0; o /= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    for (int o = 16; o > 1; o /= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
     return x;
 }
 __device__ __forceinline__ float sum16(float x) {
 #pragma unroll
-    for (int o = 8; o > 0; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
+    for (int o = 16; o > 1; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
 }  // namespace
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(64 * STRIPS, NB == 5 ? 8 / STRIPS : 4 / STRIPS
     constexpr int kT = C::kT, kThreads = C::kThreads;
     extern __shared__ __align__(16) float smem[];
     float *sQ = smem, *sO = sQ + kT * kStride, *sK = sO + kT * kStride, *sV = sK + C::kFar * kStride, *sD = sV;      // (dS over V)
-    const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 3, strip = threadIdx.x >> 6, i0 = blockIdx.x * kT;
+    const int tx = (threadIdx.x >> 1) & 15, ty = (threadIdx.x & 1) + ((threadIdx.x >> 4) & 2), strip = threadIdx.x >> 6, i0 = blockIdx.x * kT;
     const size_t head = (size_t)blockIdx.y * L * kHD;
     const int r0 = kS * strip, first = i0 + r0 - kS * (NB - 1);      // the strip's first row, and its first key
     enter_dependent();
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(64 * STRIPS, NB == 5 ? 8 / STRIPS : 4 / STRIPS
     float *sQ = smem, *sO = sQ + C::kFar * kStride, *sK = sO + C::kFar * kStride + C::kFar * 4, *sV = sK + kT * kStride;
     float *sP = sK, *sD = sP + kT * C::kPStride;                     // (over K and V)
     float4* sS = reinterpret_cast<float4*>(sO + C::kFar * kStride);
-    const int tx = threadIdx.x & 15, ty = (threadIdx.x >> 4) & 3, strip = threadIdx.x >> 6, j0 = blockIdx.x * kT, r0 = kS * strip;
+    const int tx = (threadIdx.x >> 1) & 15, ty = (threadIdx.x & 1) + ((threadIdx.x >> 4) & 2), strip = threadIdx.x >> 6, j0 = blockIdx.x * kT, r0 = kS * strip;
     const size_t head = (size_t)blockIdx.y * L * kHD;
     enter_dependent();
     load_rows<kT, kThreads>(sK, k + head, j0, L);
