@@ -584,26 +584,30 @@ __global__ void __launch_bounds__(kThreads)
 
 namespace {
 // CTAs per sequence and slab: as many as are resident at once and the sequence has runs for (each goes along its whole sequence, so
-// a second wave would run with the chip half empty)
+// a second wave would run with the chip half empty).  Up to 8, the clusters that every launch may have; 16 where each CTA has an SM to
+// itself (us, 8 / 16: B1 N32000 C256 bf16 forward 108 / 70, backward 205 / 122; with two CTAs per SM, B1 N2000 C1024 backward 20 / 23,
+// B3 N1000 C512 7 / 10)
 int parts_for(long long units, long long runs, int blocks) {
     int parts = 1;
     while (parts < 8 && units * parts * 2 <= (long long)blocks * kSMs && 2 * parts <= runs) parts *= 2;
-    return parts;
+    return parts == 8 && units * 16 <= kSMs && 16 <= runs ? 16 : parts;
 }
 template <typename T> int slabs_of(int C) { return (int)(((long long)C + slab_of<T>() - 1) / slab_of<T>()); }
 template <typename T, bool BACK> int parts_of(int B, int N, int C) {
     constexpr int run = run_tokens<T, BACK>();
     return parts_for((long long)B * slabs_of<T>(C), ((long long)N + run - 1) / run, Plan<T, BACK>::kBlocks);
 }
-// Whether a launch comes in while the grid ahead drains: only one that finds room beside another like it.  A larger one would crowd on the
-// SMs that the grid ahead leaves first and stay there to its end (B8 N4096 C2048 behind itself 159 us for 122, B1 N32768 C1000 176 for 127).
-template <typename T, bool BACK> bool beside(long long ctas) { return 2 * ctas <= (long long)Plan<T, BACK>::kBlocks * kSMs; }
-template <typename K> cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[64]) {
+// Whether a launch comes in while the grid ahead drains: only one with at most a CTA per SM, and backward of a step or two.  Others crowd on the SMs
+// that the grid ahead leaves first and stay there to their end (us behind itself, dependent / plain: bf16 B1 N16000 C1600 97 / 74, backward
+// 166 / 133; B8 N4096 C2048 159 / 122; backward B1 N8000 C512 73 / 55, B2 N2000 C512 24 / 20; but B1 N128 C512 3.1 / 3.7, backward 4.4 / 4.9)
+template <bool BACK> bool beside(long long ctas, long long steps) { return ctas <= kSMs && (!BACK || steps <= 2); }
+template <typename K> cudaError_t allow(K kernel, size_t bytes, int cluster, std::atomic<bool> (&done)[64]) {
     int dev = 0;
     const cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || dev < 0 || dev >= 64) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
     if (done[dev].load(std::memory_order_acquire)) return cudaSuccess;
-    const cudaError_t f = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t f = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (f == cudaSuccess && cluster > 8) f = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (f == cudaSuccess) done[dev].store(true, std::memory_order_release);
     return f;
 }
@@ -612,7 +616,8 @@ template <typename F> based_status with_parts(int parts, F f) {
         case 1: return f(std::integral_constant<int, 1>{});
         case 2: return f(std::integral_constant<int, 2>{});
         case 4: return f(std::integral_constant<int, 4>{});
-        default: return f(std::integral_constant<int, 8>{});
+        case 8: return f(std::integral_constant<int, 8>{});
+        default: return f(std::integral_constant<int, 16>{});
     }
 }
 
@@ -633,9 +638,9 @@ based_status forward_t(const Tokens& x, const Tokens& r, const Tokens& g, const 
         static std::atomic<bool> ready[64];
         constexpr size_t smem = Plan<T, false>::kStages * 3 * tile_bytes<T, false>();
         auto kernel = gated_recurrence_kernel<T, PARTS>;
-        cudaError_t e = allow_smem(kernel, smem, ready);
+        cudaError_t e = allow(kernel, smem, PARTS, ready);
         if (e == cudaSuccess)
-            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, beside<T, false>((long long)B * slabs * PARTS), stream, maps, rate,
+            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, beside<false>((long long)B * slabs * PARTS, 0), stream, maps, rate,
                           state_in, static_cast<T*>(out), state_out, err, N, C, slabs);
         note_launch();
         const based_status st = check_launch("gated_recurrence_kernel");
@@ -660,9 +665,10 @@ based_status backward_t(const Tokens& x, const Tokens& r, const Tokens& g, const
         static std::atomic<bool> ready[64];
         constexpr size_t smem = Plan<T, true>::kStages * 5 * tile_bytes<T, true>();
         auto kernel = gated_recurrence_backward_kernel<T, PARTS>;
-        cudaError_t e = allow_smem(kernel, smem, ready);
+        cudaError_t e = allow(kernel, smem, PARTS, ready);
         if (e == cudaSuccess)
-            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS, beside<T, true>((long long)B * slabs * PARTS), stream, maps, rate,
+            e = launch_ex(kernel, dim3((unsigned)((long long)B * slabs * PARTS)), dim3(kThreads), smem, PARTS,
+                          beside<true>((long long)B * slabs * PARTS, ((long long)N + run * PARTS - 1) / (run * PARTS)), stream, maps, rate,
                           state_in, dstate_out, static_cast<T*>(dx), static_cast<T*>(dr), static_cast<T*>(dg), part, dstate_in, err, N, C,
                           slabs);
         note_launch();
