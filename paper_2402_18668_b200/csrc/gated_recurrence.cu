@@ -162,7 +162,7 @@ __device__ __forceinline__ void token(const Gates& z, pair nrate, pair c, pair x
     const pair la = mul2(nrate, mul2(z.w, z.w));
     if constexpr (SMALL) {
         a = fma2(la, slope(la), both(1.f));
-        u = mul2(mul2(z.t, x), mul2(c, share(la)));
+        u = mul2(mul2(z.t, c), mul2(x, share(la)));              // (t's 2^30 never meets x, which may be large)
     } else {
         const pair p = exp_less_one(la);
         const float2 m2 = split(one_less_square(p));
