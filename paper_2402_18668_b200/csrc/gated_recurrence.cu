@@ -148,10 +148,35 @@ __device__ __forceinline__ pair cubic(pair x, float c0, float c1, float c2, floa
 }
 __device__ __forceinline__ pair slope(pair la) { return cubic(la, 0.999999762f, 0.499969989f, 0.166062251f, 0.0377289727f); }
 __device__ __forceinline__ pair share(pair la) { return cubic(la, 0.999999642f, 0.499950707f, 0.207340196f, 0.0560273491f); }
-// exp(la) - 1 for any la <= 0, with all its digits near 0, so that 1 - a^2 = -p (2 + p) keeps them
-__device__ __forceinline__ pair exp_less_one(pair la) {
-    const float2 l = split(la), f = split(mul2(la, slope(la))), e = split(mul2(la, both(kLog2e)));
-    return make(l.x > -0.25f ? f.x : ex2(e.x) - 1.f, l.y > -0.25f ? f.y : ex2(e.y) - 1.f);
+// A decay a = exp(la) and p = a - 1, both with all their digits: p near a = 1, so that 1 - a^2 = -p (2 + p) keeps them, and a below la =
+// -1/4, where 1 + (a - 1) would be off by 2^-25, which is all there is of a fast decay
+__device__ __forceinline__ void decay(pair la, pair& a, pair& p) {
+    const pair f2 = mul2(la, slope(la)), f1 = add2(f2, both(1.f));
+    const float2 l = split(la), f = split(f2), g = split(f1), e = split(mul2(la, both(kLog2e)));
+    const pair x2 = make(ex2(e.x), ex2(e.y)), y2 = add2(x2, both(-1.f));
+    const float2 x = split(x2), y = split(y2);
+    const bool u = l.x > -0.25f, v = l.y > -0.25f;
+    a = make(u ? g.x : x.x, v ? g.y : x.y);
+    p = make(u ? f.x : y.x, v ? f.y : y.y);
+}
+// The one of the two that has them, to keep in one register: p has its sign bit set, -0 included, and a has not.  (No rate is taken as
+// +0 for that, see minus_rate.)  SMALL: la >= -1/4, always p
+template <bool SMALL> __device__ __forceinline__ pair decay_kept(pair la) {
+    const pair f2 = mul2(la, slope(la));
+    if constexpr (SMALL) return f2;
+    const float2 l = split(la), f = split(f2), e = split(mul2(la, both(kLog2e)));
+    return make(l.x > -0.25f ? f.x : ex2(e.x), l.y > -0.25f ? f.y : ex2(e.y));
+}
+// 1 where a - 1 is kept, else 0
+template <bool SMALL> __device__ __forceinline__ pair decay_one(pair v) {
+    if constexpr (SMALL) return both(1.f);
+    const float2 x = split(v);
+    return make(__int_as_float((__float_as_int(x.x) >> 31) & 0x3f800000), __int_as_float((__float_as_int(x.y) >> 31) & 0x3f800000));
+}
+template <bool SMALL> __device__ __forceinline__ pair decay_stay() { return SMALL ? 0 : 0x8000000080000000ull; }      // a = 1
+__device__ __forceinline__ pair minus_rate(pair rate) {
+    const float2 r = split(rate);
+    return make(r.x == 0.f ? -0.f : -r.x, r.y == 0.f ? -0.f : -r.y);
 }
 // 1 - a^2 from p = a - 1
 __device__ __forceinline__ pair one_less_square(pair p) { return mul2(p, fma2(p, both(-1.f), both(-2.f))); }
@@ -164,9 +189,9 @@ __device__ __forceinline__ void token(const Gates& z, pair nrate, pair c, pair x
         a = fma2(la, slope(la), both(1.f));
         u = mul2(mul2(z.t, c), mul2(x, share(la)));              // (t's 2^30 never meets x, which may be large)
     } else {
-        const pair p = exp_less_one(la);
+        pair p;
+        decay(la, a, p);
         const float2 m2 = split(one_less_square(p));
-        a = add2(p, both(1.f));
         u = mul2(make(root(m2.x), root(m2.y)), mul2(mul2(mul2(z.t, both(kDown)), mul2(z.A, z.w)), x));
     }
 }
@@ -369,8 +394,8 @@ __global__ void __launch_bounds__(kThreads, Plan<T, false>::kBlocks)
     pair nrate[kP] = {0, 0}, h[kP] = {0, 0};
     if (mine) {
         load_f32<kP>(rate + c0, nrate);
-        nrate[0] = neg2(nrate[0]);
-        nrate[1] = neg2(nrate[1]);
+        nrate[0] = minus_rate(nrate[0]);
+        nrate[1] = minus_rate(nrate[1]);
         if (state_in) load_f32<kP>(state_in + (size_t)b * C + c0, h);
     }
     T* const to = out + (size_t)b * N * C + c0;
@@ -461,8 +486,8 @@ __global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
     pair nrate[kP] = {0, 0}, E[kP] = {0, 0}, drate[kP] = {0, 0};
     if (mine) {
         load_f32<kP>(rate + c0, nrate);
-        nrate[0] = neg2(nrate[0]);
-        nrate[1] = neg2(nrate[1]);
+        nrate[0] = minus_rate(nrate[0]);
+        nrate[1] = minus_rate(nrate[1]);
         if (dstate_out) load_f32<kP>(dstate_out + (size_t)b * C + c0, E);
     }
     const size_t base = (size_t)b * N * C + c0;
@@ -474,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
             // the thread's tokens t0, t0 - 1, ...
             const uint8_t* from = stage + (s % kStages) * 5 * kTile + (kRun - 1 - group * TOK) * kRow + lane * kV * sizeof(T);
             const long long t0 = N - 1 - ((s * (long long)PARTS + rank) * kRun + group * TOK);
-            pair p[TOK][kP], sg[TOK][kP];                        // a_t - 1, sigmoid(r_t)
+            pair v[TOK][kP], sg[TOK][kP];                        // the decay, sigmoid(r_t)
             pair A[kP] = {both(1.f), both(1.f)}, H[kP] = {0, 0}, first[kP];
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
@@ -484,10 +509,9 @@ __global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
 #pragma unroll
                 for (int e = 0; e < kP; ++e) {
                     sg[j][e] = sigmoid(rv[e]);
-                    const pair la = mul2(nrate[e], sg[j][e]);
-                    p[j][e] = SMALL ? mul2(la, slope(la)) : exp_less_one(la);
-                    if (t0 - j < 0) p[j][e] = 0;                 // (before the sequence nothing happens)
-                    const pair a = add2(p[j][e], both(1.f));
+                    v[j][e] = decay_kept<SMALL>(mul2(nrate[e], sg[j][e]));
+                    if (t0 - j < 0) v[j][e] = decay_stay<SMALL>();             // (before the sequence nothing happens)
+                    const pair a = add2(v[j][e], decay_one<SMALL>(v[j][e]));
                     H[e] = mul2(a, add2(H[e], dv[e]));
                     A[e] = mul2(A[e], a);
                 }
@@ -506,7 +530,8 @@ __global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
                 if (in && t0 - j == 0 && state_in) load_f32<kP>(state_in + (size_t)b * C + c0, hv);
 #pragma unroll
                 for (int e = 0; e < kP; ++e) {
-                    const pair a = add2(p[j][e], both(1.f)), i = sigmoid(gv[e]), m2 = one_less_square(p[j][e]);
+                    const pair one = decay_one<SMALL>(v[j][e]), a = add2(v[j][e], one), i = sigmoid(gv[e]);
+                    const pair m2 = one_less_square(SMALL ? v[j][e] : add2(v[j][e], add2(one, both(-1.f))));
                     const float2 f = split(m2);
                     // 1 / m; where nothing decays (m = 0) a number so large that products with it stay finite
                     const pair im = make(rroot(max_nan(f.x, 1e-36f)), rroot(max_nan(f.y, 1e-36f))), m = mul2(m2, im);
@@ -575,7 +600,7 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
         pair a, u;
-        token<false>(gates(rv[e], gv[e]), neg2(nrate[e]), 0, xv[e], a, u);
+        token<false>(gates(rv[e], gv[e]), minus_rate(nrate[e]), 0, xv[e], a, u);
         h[e] = fma2(a, h[e], u);
     }
     if (state_out) store_f32<kP>(state_out + i * kV, h);
