@@ -696,13 +696,14 @@ struct Rotation {
         const Workspace ws(workspace, weights ? based_qk_norm_rotate_backward_workspace_bytes(B, L, Hq, Hk, d, io) : 0, q, stream);
         if (!dq.defined()) dq = blank({B, L, Hq, d}, q.scalar_type());
         if (!dk.defined()) dk = blank({B, L, Hk, d}, q.scalar_type());
-        if (weights) {
-            dwq = blank({d}, at::kFloat);
-            dwk = blank({d}, at::kFloat);
-        }
+        if (weights && wq.defined()) dwq = blank({d}, at::kFloat);
+        if (weights && wk.defined()) dwk = blank({d}, at::kFloat);
+        // the library writes both: one that nobody is given is scratch, of the call's own stream like the workspace
+        const Workspace unwanted(kNone, weights && dwq.defined() != dwk.defined() ? d * sizeof(float) : 0, q, stream);
+        auto to = [&](const Tensor& t) { return weights && !t.defined() ? static_cast<float*>(unwanted.data) : fptr(t); };
         check(based_qk_norm_rotate_backward(cptr(q), cptr(k), token_stride(q), token_stride(k), f32(wq), f32(wk), f(), p(), per, start,
-                                            cptr(gq), cptr(gk), ptr(dq), ptr(dk), token_stride(dq), token_stride(dk), fptr(dwq),
-                                            fptr(dwk), B, L, Hq, Hk, d, n, eps, io, flags, ws.data, ws.bytes, stream),
+                                            cptr(gq), cptr(gk), ptr(dq), ptr(dk), token_stride(dq), token_stride(dk), to(dwq), to(dwk), B, L,
+                                            Hq, Hk, d, n, eps, io, flags, ws.data, ws.bytes, stream),
               "based_qk_norm_rotate_backward");
     }
 };
@@ -747,7 +748,7 @@ PyObject* rotate_backward(PyObject* const* a) {
     void* stream = stream_on(a[14], o.q);
     Tensor dwq, dwk;
     away(o.q, [&] { o.backward(gq, gk, dq, dk, o.wq.defined() || o.wk.defined(), dwq, dwk, ws, stream); });
-    return wrap({dq, dk, o.wq.defined() ? dwq : Tensor(), o.wk.defined() ? dwk : Tensor()});
+    return wrap({dq, dk, dwq, dwk});
 }
 
 Gradients swa_backward_call(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& dout, const Tensor& workspace, int window,
@@ -997,7 +998,7 @@ struct NormRotation : torch::autograd::Function<NormRotation> {
         return node_backward(o.q, [&](void* stream) -> torch::autograd::variable_list {
             Tensor dq, dk, dwq, dwk;
             o.backward(as_input(grads[0], o.q), as_input(grads[1], o.k), dq, dk, ctx->saved_data["weights"].toBool(), dwq, dwk, kNone, stream);
-            return {dq, dk, o.wq.defined() ? dwq : Tensor(), o.wk.defined() ? dwk : Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+            return {dq, dk, dwq, dwk, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
         });
     }
 };
