@@ -343,7 +343,9 @@ template <int LANES, int PARTS> __device__ __forceinline__ void finish(Shared<LA
     if (*(volatile uint32_t*)&sm.abort_flag) {
         for (int it = 0; it < 200; ++it) __nanosleep(1000);
     }
-    if constexpr (PARTS > 1) cluster_arrive_wait();              // no CTA leaves before what others send it has arrived
+    // No CTA leaves before what others send it has arrived; and every thread of the cluster has read the state that it started from, whose
+    // place the new one may take
+    if constexpr (PARTS > 1) cluster_arrive_wait();
 }
 // Tokens per thread, stages of tiles, and CTAs that an SM holds.  us, tokens x CTAs per SM: B8 N4096 C2048 bf16 forward 8 x 3 119, 8 x 4 123,
 // 4 x 4 136, 16 x 2 121 (more tokens spread a join over more elements, more registers keep constants where they are), backward 4 x 3
@@ -447,8 +449,8 @@ __global__ void __launch_bounds__(kThreads, Plan<T, false>::kBlocks)
     };
     if (all_small(nrate)) walk(std::true_type{});
     else walk(std::false_type{});
-    if (state_out && mine && rank == 0 && group == 0) store_f32<kP>(state_out + (size_t)b * C + c0, h);
     finish(sm, ok, err);
+    if (state_out && mine && rank == 0 && group == 0) store_f32<kP>(state_out + (size_t)b * C + c0, h);
 }
 
 // The scan from the last token to the first: "time" tau = N - 1 - t, tiles lie with the last token of a run below.  part: [sequences
@@ -556,7 +558,6 @@ __global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
     };
     if (all_small(nrate)) walk(std::true_type{});
     else walk(std::false_type{});
-    if (dstate_in && mine && rank == 0 && group == 0) store_f32<kP>(dstate_in + (size_t)b * C + c0, E);
     // drate over the CTA's tokens: the warp's groups, then the warps
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
@@ -576,6 +577,7 @@ __global__ void __launch_bounds__(kThreads, Plan<T, true>::kBlocks)
         store_f32<kP>(part + ((size_t)b * PARTS + rank) * C + c0, t);
     }
     finish(sm, ok, err);
+    if (dstate_in && mine && rank == 0 && group == 0) store_f32<kP>(dstate_in + (size_t)b * C + c0, E);
 }
 
 // One token: 4 channels per thread
