@@ -53,11 +53,13 @@ const Tensor& need(PyObject* o, const char* name) {
     return t;
 }
 int integer(PyObject* o) {
-    const long x = PyLong_AsLong(o);
+    int beyond = 0;
+    const long x = PyLong_AsLongAndOverflow(o, &beyond);
     if (x == -1 && PyErr_Occurred()) {
         PyErr_Clear();
         throw TypeFault("expected an integer");
     }
+    if (beyond || x != static_cast<int>(x)) value_error("an integer argument does not fit 32 bits");
     return static_cast<int>(x);
 }
 float number(PyObject* o) {
