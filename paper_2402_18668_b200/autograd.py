@@ -7,6 +7,9 @@ output, which lets the bf16 path merge two of its passes).  The node itself is n
 (csrc_host/native.cpp), so neither direction waits for the interpreter; both run in the library's
 kernels.
 
+The layers' functions take tensors however they lie: what the kernels can read as it lies is not copied (contiguous ones, and slices of a
+fused projection whose rows start on 16-byte boundaries), anything else is.
+
 A backward pass can be captured into a CUDA graph under torch's own rule for that: no eager graph of the same leaves may be alive
 (their gradients would be accumulated on the stream that it was built on, which the capture refuses with an error).
 """

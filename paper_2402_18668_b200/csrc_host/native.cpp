@@ -930,20 +930,34 @@ template <typename F> torch::autograd::variable_list node_backward(const Tensor&
         throw err;
     }
 }
-Tensor as_input(const Tensor& g, const Tensor& like) { return g.defined() ? g.contiguous().to(like.scalar_type()) : Tensor(); }
+// The nodes take any tensor of their shapes: what the kernels cannot read as it lies is copied.
+bool on_16_bytes(const Tensor& t) { return (reinterpret_cast<uintptr_t>(t.const_data_ptr()) & 15) == 0; }
+// contiguous, from a 16-byte boundary on
+Tensor packed(const Tensor& t) {
+    if (!t.defined()) return t;
+    const Tensor c = t.contiguous();
+    return on_16_bytes(c) ? c : c.clone();
+}
+Tensor as_input(const Tensor& g, const Tensor& like) { return g.defined() ? packed(g.to(like.scalar_type())) : Tensor(); }
 void on_gpu(const Tensor& t) {
     if (!t.is_cuda()) value_error("libbased takes CUDA tensors only (there is no CPU path)");
 }
-Tensor packed(const std::optional<Tensor>& t) { return t ? t->contiguous() : Tensor(); }
+Tensor packed(const std::optional<Tensor>& t) { return t ? packed(*t) : Tensor(); }
 std::optional<Tensor> maybe(const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; }
 // a view with strides that the library takes, or a copy
 Tensor evenly(const Tensor& t) {
-    if (t.dim() != 3) return t.contiguous();
+    if (t.dim() != 3) return packed(t);
     const int64_t per16 = 16 / static_cast<int64_t>(t.element_size()), B = t.size(0), N = t.size(1), C = t.size(2);
-    const bool as_it_lies = t.stride(2) == 1 && (reinterpret_cast<uintptr_t>(t.const_data_ptr()) & 15) == 0 &&
+    const bool as_it_lies = t.stride(2) == 1 && on_16_bytes(t) &&
                             (N == 1 || (t.stride(1) >= C && t.stride(1) % per16 == 0)) &&
                             (B == 1 || (t.stride(0) >= (N > 1 ? (N - 1) * t.stride(1) : 0) + C && t.stride(0) % per16 == 0));
-    return as_it_lies ? t : t.contiguous();
+    return as_it_lies ? t : packed(t);
+}
+// the same of a projection [B,L,H,d]
+Tensor evenly_rows(const Tensor& t) {
+    const bool as_it_lies = evenly_spaced(t) && on_16_bytes(t) && token_stride(t) >= t.size(2) * t.size(3) &&
+                            token_stride(t) * static_cast<int64_t>(t.element_size()) % 16 == 0;
+    return as_it_lies ? t : packed(t);
 }
 struct GatedRecurrence : torch::autograd::Function<GatedRecurrence> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x_, const Tensor& r_,
@@ -951,7 +965,7 @@ struct GatedRecurrence : torch::autograd::Function<GatedRecurrence> {
         ctx->set_materialize_grads(false);
         on_gpu(x_);
         dims(x_, 3, "x");
-        const Tensor x = evenly(x_), r = evenly(r_), g = evenly(g_), rate = rate_.contiguous(), in = packed(in_);
+        const Tensor x = evenly(x_), r = evenly(r_), g = evenly(g_), rate = packed(rate_), in = packed(in_);
         check_gates(x, r, g, rate);
         check_f32(in, {x.size(0), x.size(2)}, "state");
         check_places({&x, &r, &g, &rate, &in}, {});
@@ -981,8 +995,8 @@ struct NormRotation : torch::autograd::Function<NormRotation> {
         on_gpu(k_);
         dims(q_, 4, "q");
         dims(k_, 4, "k");
-        const Rotation o(evenly_spaced(q_) ? q_ : q_.contiguous(), evenly_spaced(k_) ? k_ : k_.contiguous(), packed(wq), packed(wk),
-                         packed(freqs), packed(positions), static_cast<float>(eps), static_cast<int>(flags), static_cast<int>(start));
+        const Rotation o(evenly_rows(q_), evenly_rows(k_), packed(wq), packed(wk), packed(freqs), packed(positions), static_cast<float>(eps),
+                         static_cast<int>(flags), static_cast<int>(start));
         const c10::cuda::CUDAGuard device(o.q.device());
         Tensor oq, ok;
         o.forward(oq, ok, c10::cuda::getCurrentCUDAStream(o.q.get_device()).stream());
@@ -1008,7 +1022,7 @@ struct SlidingWindow : torch::autograd::Function<SlidingWindow> {
     static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& q_, const Tensor& k_, const Tensor& v_, int64_t window,
                           double scale) {
         on_gpu(q_);
-        const Tensor q = q_.contiguous(), k = k_.contiguous(), v = v_.contiguous();
+        const Tensor q = packed(q_), k = packed(k_), v = packed(v_);
         dims(q, 4, "q");
         check_qkv(q, k, v, kNone);
         if (v.sizes() != q.sizes()) value_error("the sliding-window mixer takes q, k, v of one shape");
