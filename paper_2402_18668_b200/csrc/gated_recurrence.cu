@@ -638,6 +638,29 @@ template <typename K> cudaError_t allow(K kernel, size_t bytes, int cluster, std
     if (f == cudaSuccess) done[dev].store(true, std::memory_order_release);
     return f;
 }
+// Whether the device has room for a cluster of 16 of the kernel's CTAs: a whole chip has, the share of one that a process may be given
+// need not
+template <typename K> bool holds_16(K kernel, size_t bytes, std::atomic<bool> (&known)[64]) {
+    int dev = 0, clusters = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if (known[dev].load(std::memory_order_acquire)) return true;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 16;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    const bool held = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess &&
+                      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                      cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0;
+    if (held) known[dev].store(true, std::memory_order_release);
+    else (void)cudaGetLastError();
+    return held;
+}
 template <typename F> based_status with_parts(int parts, F f) {
     switch (parts) {
         case 1: return f(std::integral_constant<int, 1>{});
@@ -660,10 +683,13 @@ based_status forward_t(const Tokens& x, const Tokens& r, const Tokens& g, const 
         !make_tokens_map(&maps.x, x, f32, B, N, C, slab_of<T>(), run) || error_word_ptr(&err) != BASED_OK)
         return BASED_ERR_CUDA;
     maps.dout = maps.out = maps.x;
-    return with_parts(parts_of<T, false>(B, N, C), [&](auto tag) {
+    constexpr size_t smem = Plan<T, false>::kStages * 3 * tile_bytes<T, false>();
+    static std::atomic<bool> known16[64];
+    int parts = parts_of<T, false>(B, N, C);
+    if (parts == 16 && !holds_16(gated_recurrence_kernel<T, 16>, smem, known16)) parts = 8;
+    return with_parts(parts, [&](auto tag) {
         constexpr int PARTS = decltype(tag)::value;
         static std::atomic<bool> ready[64];
-        constexpr size_t smem = Plan<T, false>::kStages * 3 * tile_bytes<T, false>();
         auto kernel = gated_recurrence_kernel<T, PARTS>;
         cudaError_t e = allow(kernel, smem, PARTS, ready);
         if (e == cudaSuccess)
@@ -679,7 +705,7 @@ based_status backward_t(const Tokens& x, const Tokens& r, const Tokens& g, const
                         const Tokens& dout, const float* dstate_out, void* dx, void* dr, void* dg, float* drate, float* dstate_in, int B,
                         int N, int C, float* part, cudaStream_t stream) {
     constexpr bool f32 = sizeof(T) == 4;
-    const int slabs = slabs_of<T>(C), parts = parts_of<T, true>(B, N, C);
+    const int slabs = slabs_of<T>(C);
     RecurrenceMaps maps;
     unsigned int* err = nullptr;
     constexpr int run = run_tokens<T, true>();
@@ -687,10 +713,13 @@ based_status backward_t(const Tokens& x, const Tokens& r, const Tokens& g, const
         !make_tokens_map(&maps.x, x, f32, B, N, C, slab_of<T>(), run) || !make_tokens_map(&maps.out, out, f32, B, N, C, slab_of<T>(), run) ||
         !make_tokens_map(&maps.dout, dout, f32, B, N, C, slab_of<T>(), run) || error_word_ptr(&err) != BASED_OK)
         return BASED_ERR_CUDA;
+    constexpr size_t smem = Plan<T, true>::kStages * 5 * tile_bytes<T, true>();
+    static std::atomic<bool> known16[64];
+    int parts = parts_of<T, true>(B, N, C);                      // (the scratch is for that many, or more than needed)
+    if (parts == 16 && !holds_16(gated_recurrence_backward_kernel<T, 16>, smem, known16)) parts = 8;
     const based_status st = with_parts(parts, [&](auto tag) {
         constexpr int PARTS = decltype(tag)::value;
         static std::atomic<bool> ready[64];
-        constexpr size_t smem = Plan<T, true>::kStages * 5 * tile_bytes<T, true>();
         auto kernel = gated_recurrence_backward_kernel<T, PARTS>;
         cudaError_t e = allow(kernel, smem, PARTS, ready);
         if (e == cudaSuccess)
