@@ -72,3 +72,21 @@ def test_what_fast_decays_leave_of_a_state(dtype):
     for t in range(N):
         y = based.based_gated_recurrence_step(x[:, t], r[:, t], g[:, t], rate, state)
         close(y, want[:, t], (rel[:, t] + half_step(x.dtype) * (1 + rel[:, t])) * want[:, t].abs(), f"token {t}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,N,C", [(2, 203, 64), (1, 3001, 72)])
+def test_rates_of_zero_beside_fast_ones(B, N, C, dtype):
+    """Of either sign: the state stays as it is to the last bit, and its gradient gathers the outputs' (N sums in fp32 in any order)."""
+    x, r, g, _, h0, dout, dh = draw(B, N, C, dtype, seed=23)
+    rate = rates("fast", C)
+    rate[::8], rate[1::8] = 0.0, -0.0
+    still = (rate == 0).nonzero()[:, 0]
+    last = torch.empty_like(h0)
+    out = based.based_gated_recurrence_forward(x, r, g, rate, state_in=h0, state_out=last)
+    assert torch.equal(last[:, still], h0[:, still])
+    assert torch.equal(out[..., still], h0[:, None, still].expand(B, N, -1).to(out.dtype))
+    dx, _, dg, _, dh0 = based.based_gated_recurrence_backward(x, r, g, rate, out, dout, state_in=h0, dstate_out=dh)
+    assert (dx[..., still] == 0).all() and (dg[..., still] == 0).all()
+    want = dout.double().sum(1) + dh.double()
+    close(dh0[:, still], want[:, still], (N + 1) * U * (dout.double().abs().sum(1) + dh.double().abs())[:, still], "dstate_in")
