@@ -444,8 +444,9 @@ size_t based_static_scratch_bytes(void);
 
 /*
  * [B,N,C] values that need not lie contiguous: element (b, n, c) at data + b * batch_stride + n * token_stride + c.  Slices of a
- * fused projection or of a longer batch are taken as they lie.  Strides in elements, multiples of 16 bytes, tokens and sequences not
- * overlapping (a stride along a dimension of size 1 is not looked at).
+ * fused projection or of a longer batch are taken as they lie.  Strides in elements, multiples of 16 bytes; tokens do not overlap, and a
+ * sequence's tokens all lie ahead of the next sequence's: token_stride >= C, batch_stride >= (N - 1) token_stride + C (a stride along a
+ * dimension of size 1 is not looked at).
  */
 typedef struct { const void* data; long long batch_stride, token_stride; } based_tokens;
 

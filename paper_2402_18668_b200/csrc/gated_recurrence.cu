@@ -16,11 +16,12 @@
 // HBM bound by its bytes (4 values a token and channel forward, 8 backward), with little to spare: at the pace of HBM an SM has 43 cycles
 // for 32 elements forward on a sub-core, and the element's 3 special-function calls take 24 of them, its multiply-adds 24, which
 // together come to 31 at best (measured, without loads).  So one reciprocal root serves both gates and the root of 1 - a^2, cubics
-// stand for what is left of the exponential where the rates allow, two channels share an instruction (half the issue slots, the same
-// pipe time), and tiles of tokens x 128 bytes come by TMA, which needs no address arithmetic and reads views with strides as they lie.
-// B8 N4096 C2048 bf16: forward 119 us = 4.5 TB/s (256 CTAs on 148 SMs: two on most, which is what bounds it; its loads and stores
-// without the arithmetic take 87, the arithmetic without them 97), backward 218 us = 4.9 TB/s; B1 N32768 C1000 fp32 forward 98 us =
-// 5.3 TB/s.
+// stand for what is left of the exponential where all rates of a slab are at most 1/4 (else 5 calls), two channels share an instruction
+// (half the issue slots, the same pipe time), and tiles of tokens x 128 bytes come by TMA, which needs no address arithmetic and reads
+// views with strides as they lie.
+// B8 N4096 C2048 bf16, on two cards: forward 114 and 119 us = 4.7 and 4.5 TB/s (256 CTAs on 148 SMs: two on most, which is what bounds
+// it; its loads and stores without the arithmetic take 87, the arithmetic without them 97), backward 204 and 222 us = 5.3 and 4.8 TB/s;
+// with rates up to 1 on the first card 139 and 235 us.  B1 N32768 C1000 fp32 forward 92 and 99 us = 5.7 and 5.3 TB/s.
 #include <type_traits>
 
 #include "common.cuh"

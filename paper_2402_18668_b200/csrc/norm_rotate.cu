@@ -20,7 +20,8 @@
 //
 // Measured: bf16, 2 x 32768 tokens, 16 + 16 heads of 64, rotating: 94 us (87 % of the copy rate; 106 with the next step's rows in
 // registers); fp32, 3 x 777 tokens, 16 + 4 heads of 128, 64 elements of them rotating: 8.4 us (87 %); backward, bf16, 4 x 2048 tokens of
-// 16 + 16 heads of 64: 26 us (58 %; 3.6 of them the second launch, which joins the weights' gradients), 4 x 8192: 84 us (73 %).
+// 16 + 16 heads of 64: 26 us (58 %; 3.6 of them the second launch, which joins the weights' gradients), 4 x 8192: 85 us (72 %);
+// in fp32 45 us (68 %) and 165 (75 %).
 #include <type_traits>
 
 #include "common.cuh"
@@ -43,7 +44,7 @@ struct Grid {
     int TB;                        // tokens per block, a power of two.  Backward: whose angles are there at once
     int blocks;                    // blocks of tokens.  Backward: even shares of them
 };
-// Sine and cosine of x half turns, |x| <= 1.  For bf16 io the fast ones (off by 2^-20.5, where the result is rounded by 2^-9 of it)
+// Sine and cosine of x half turns, |x| <= 1.  For bf16 io the fast ones (off by 2^-20.5, where the result is rounded by up to 2^-8 of it)
 template <typename T> __device__ __forceinline__ float2 cos_sin(float x) {
     float2 r;
     if constexpr (sizeof(T) == 2) {

@@ -10,9 +10,10 @@
 // then dS and dq.  The second takes keys and recomputes P and dS of the queries that see them from the statistics.  Neither adds
 // into memory that another CTA writes, so results do not depend on any order.
 //
-// Bound by shared memory's reads, four fifths of the time, and the multiply-adds that they feed (7 products of 16 x 16 NB x 64 per
-// strip).  Scores and dP take even and odd elements in pairs, which halves their instructions.  Lanes that read the same 16 bytes are
-// neighbours, which serves half a warp at a time (half-warps that read the same rows: 40 us for 38, 255 for 235).
+// Bound by the multiply-adds (7 products of 16 x 16 NB x 64 per strip; their pipe is what issue waits for most), with shared memory's
+// reads, at 53 and 58 % of their peak, close behind.  Scores and dP take even and odd elements in pairs, which halves their
+// instructions.  Lanes that read the same 16 bytes are neighbours, which serves half a warp at a time (half-warps that read the same
+// rows: 40 us for 38, 255 for 235).
 // Measured: 16 heads x 1000 queries, window 64: 38 us, window 128: 70; 32 x 4096: 235 and 481 (56 % of the multiply-adds' rate with
 // window 64).  On tiles of 64 x 64, half of whose pairs lie outside the band, these took 68, 98, 511 and 709.
 #include "common.cuh"
