@@ -540,6 +540,60 @@ based_status swa_backward(const void* q, const void* k, const void* v, const voi
 size_t swa_backward_workspace_bytes(int B, int H, int L, int window, based_dtype io);
 
 /*
+ * [B,H,L,d] values that need not lie contiguous: element (b, h, t, c) at data + b * batch_stride + h * head_stride + t * token_stride + c.
+ * The heads of a projection, [B,L,H,d], and slices of a fused one are taken as they lie.  Strides in elements, at least d and multiples
+ * of 16 bytes (one along a dimension of size 1 is not looked at).  An output is given in the same way; its elements lie apart.
+ */
+typedef struct { const void* data; long long batch_stride, head_stride, token_stride; } based_heads;
+
+/*
+ * Linear attention with a decay per head (the fixed per-head decay of App. "Extended Architecture", on plain queries and keys).  Per sequence
+ * and head, with a = exp(-rate[h]), from S = state_in (NULL: zeros):
+ *
+ *   S_t = a S_{t-1} + k_t v_t^T,     out_t = scale q_t S_t
+ *
+ * q, k [B,H,L,d_k], v, out [B,H,L,d_v] in the io dtype; rate [H] fp32, >= 0 (not checked; 0: no decay); state_in, state_out
+ * [B,H,d_k,d_v] fp32: the states before token 0 and behind token L-1 (NULL: not wanted), which must not be one array.  scale <= 0:
+ * 1 / sqrt(d_k).
+ * documents [B,L] int32, or NULL: a token whose document is negative is padding, and passed over as if it were not there (its
+ * inputs are not used, its output is 0); one whose document is not that of the last token before it that counts starts from an
+ * empty state.  A sequence's first document continues state_in, whatever its number.
+ * fp32 io: fp32 multiply-adds.  bf16 io: the faded scores and the state as operands of products with q are rounded to bf16 once; sums, the
+ * state itself and what goes into it are fp32 (16 bits of every faded v).  Where a value that counts is not finite, the outputs of its
+ * sequence and head from up to 127 tokens ahead of it on may not be either, in other documents too.
+ * Supported: d_k, d_v multiples of 8 up to 128; io in {F32, BF16}; 1 <= L <= 2^31 - 2^16.
+ * workspace: based_decay_attention_workspace_bytes (with_documents: whether documents is given; 0 bytes are possible).  Outputs must not
+ * alias inputs.
+ */
+based_status based_decay_attention_forward(based_heads q, based_heads k, based_heads v, const float* rate, const int* documents,
+                                           const float* state_in, based_heads out, float* state_out, int B, int H, int L, int d_k, int d_v,
+                                           float scale, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t based_decay_attention_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io);
+
+/*
+ * The same for one new token per sequence (generation): q, k [B,H,d_k], v, out [B,H,d_v], contiguous; state_in and state_out required,
+ * and may be one array.  Supported and scale as above.
+ */
+based_status based_decay_attention_step(const void* q, const void* k, const void* v, const float* rate, const float* state_in, void* out,
+                                        float* state_out, int B, int H, int d_k, int d_v, float scale, based_dtype io, void* cuda_stream);
+
+/*
+ * Its backward pass.  dout: the gradient of out, dstate_out [B,H,d_k,d_v] fp32: that of state_out (NULL: zeros).  With R = dstate_out behind
+ * the last token, from the last token to the first,
+ *
+ *   R += scale q_t dout_t^T,   dk_t = R v_t,   dv_t = R^T k_t,   dq_t = scale S_t dout_t,   then R <- a R;    dstate_in = R,
+ *
+ * where padding is passed over (its gradients are 0) and R starts anew ahead of a document's first token, as S does.  dq, dk, dv: like q, k, v, with
+ * strides of their own; dstate_in fp32 (NULL: not wanted).  The rates are constants: they have no gradient here.  workspace:
+ * based_decay_attention_backward_workspace_bytes.  Rounding, limits and the reach of values that are not finite (both ways) as above.
+ */
+based_status based_decay_attention_backward(based_heads q, based_heads k, based_heads v, const float* rate, const int* documents,
+                                            const float* state_in, based_heads dout, const float* dstate_out, based_heads dq, based_heads dk,
+                                            based_heads dv, float* dstate_in, int B, int H, int L, int d_k, int d_v, float scale,
+                                            based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t based_decay_attention_backward_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io);
+
+/*
  * Synchronises the stream and returns the sticky device-side status: BASED_OK, or
  * BASED_ERR_DEVICE_TIMEOUT if a kernel abandoned a bounded wait (its outputs are then
  * undefined), or BASED_ERR_CUDA if the stream reported a CUDA error.  Clears the flag.

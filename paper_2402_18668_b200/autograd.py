@@ -40,3 +40,10 @@ def gated_recurrence(x, r, g, rate, state=None):
     """based_gated_recurrence_forward, differentiable with respect to x, r, g [B,N,C], rate [C] and state [B,C].  Returns
     (out, the state behind the last token), both differentiable."""
     return _b.native().gated_recurrence(x, r, g, rate, state)
+
+
+def decay_attention(q, k, v, rate, documents=None, state=None, scale: float = 0.0):
+    """based_decay_attention_forward, differentiable with respect to q, k [B,H,L,d_k], v [B,H,L,d_v] and state [B,H,d_k,d_v]; the
+    rates [H] are constants (one that requires a gradient is refused).  Returns (out, the state behind the last token), both
+    differentiable."""
+    return _b.native().decay_attention(q, k, v, rate, documents, state, float(scale))

@@ -38,6 +38,8 @@ EXPORTS = (
     "based_prefill_backward_tokens_first_with_out", "based_gated_recurrence_forward", "based_gated_recurrence_step",
     "based_gated_recurrence_backward", "based_gated_recurrence_backward_workspace_bytes", "based_qk_norm_rotate",
     "based_qk_norm_rotate_backward", "based_qk_norm_rotate_backward_workspace_bytes", "swa_backward", "swa_backward_workspace_bytes",
+    "based_decay_attention_forward", "based_decay_attention_workspace_bytes", "based_decay_attention_step", "based_decay_attention_backward",
+    "based_decay_attention_backward_workspace_bytes",
 )
 
 _lib = None
@@ -47,6 +49,12 @@ _native_module = None
 class Tokens(ctypes.Structure):
     """based_tokens: [B,N,C] values with strides, in elements."""
     _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_longlong), ("token_stride", ctypes.c_longlong)]
+
+
+class Heads(ctypes.Structure):
+    """based_heads: [B,H,L,d] values with strides, in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
+                ("token_stride", ctypes.c_longlong)]
 
 
 class BasedError(RuntimeError):
@@ -141,6 +149,16 @@ def lib() -> ctypes.CDLL:
         L.swa_backward.argtypes = [vp] * 7 + [i, i, i, i, i, f, i, vp, sz, vp]
         L.swa_backward_workspace_bytes.restype = sz
         L.swa_backward_workspace_bytes.argtypes = [i, i, i, i, i]
+        L.based_decay_attention_forward.restype = i
+        L.based_decay_attention_forward.argtypes = [Heads, Heads, Heads, vp, vp, vp, Heads, vp, i, i, i, i, i, f, i, vp, sz, vp]
+        L.based_decay_attention_step.restype = i
+        L.based_decay_attention_step.argtypes = [vp] * 7 + [i, i, i, i, f, i, vp]
+        L.based_decay_attention_backward.restype = i
+        L.based_decay_attention_backward.argtypes = [Heads, Heads, Heads, vp, vp, vp, Heads, vp, Heads, Heads, Heads, vp, i, i, i, i, i, f, i, vp,
+                                                     sz, vp]
+        for name in ("based_decay_attention_workspace_bytes", "based_decay_attention_backward_workspace_bytes"):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = [i] * 7
         L.based_poll_error.restype = i
         L.based_poll_error.argtypes = [vp]
         L.based_status_string.restype = ctypes.c_char_p
@@ -447,6 +465,31 @@ def based_qk_norm_rotate_backward(q, k, dout_q, dout_k, q_weight=None, k_weight=
 def swa_backward(q, k, v, dout, window: int = 64, softmax_scale: float = 0.0, workspace=None, stream=None):
     """Gradients (dq, dk, dv) of swa_forward(q, k, v, window=window, softmax_scale=softmax_scale) for the output gradient dout."""
     return (_native_module or native()).swa_grad(q, k, v, dout, int(window), float(softmax_scale), workspace, _handle(stream))
+
+
+def based_decay_attention_forward(q, k, v, rate, documents=None, state_in=None, out=None, state_out=None, scale: float = 0.0, workspace=None,
+                                  stream=None):
+    """S_t = exp(-rate) S_{t-1} + k_t v_t^T, out_t = scale q_t S_t per head: q, k [B,H,L,d_k], v [B,H,L,d_v] (the heads of a projection,
+    [B,L,H,d] transposed, and slices of a fused one are taken as they lie), rate [H] fp32; scale <= 0: 1/sqrt(d_k).  documents int32
+    [B,L]: a negative one marks padding, which is passed over; where it changes the state starts anew.  state_in, state_out
+    [B,H,d_k,d_v] fp32 (state_out is written).  Returns out [B,H,L,d_v]."""
+    return (_native_module or native()).decay_forward(q, k, v, rate, documents, state_in, out, state_out, float(scale), workspace,
+                                                      _handle(stream))
+
+
+def based_decay_attention_step(q, k, v, rate, state, out=None, state_out=None, scale: float = 0.0, stream=None):
+    """The same for one token: q, k [B,H,d_k], v [B,H,d_v]; state [B,H,d_k,d_v] fp32 is updated in place, or left as it is and the new
+    one written to state_out."""
+    return (_native_module or native()).decay_step(q, k, v, rate, state, out, state if state_out is None else state_out, float(scale),
+                                                   _handle(stream))
+
+
+def based_decay_attention_backward(q, k, v, rate, dout, documents=None, state_in=None, dstate_out=None, scale: float = 0.0, workspace=None,
+                                   stream=None):
+    """Gradients (dq, dk, dv, dstate_in) of based_decay_attention_forward for the gradients dout of its output and dstate_out of its
+    state_out.  dstate_in is None without state_in; the rates are constants."""
+    return (_native_module or native()).decay_backward(q, k, v, rate, documents, state_in, dout, dstate_out, float(scale), workspace,
+                                                       _handle(stream))
 
 
 def based_selftest_bounded_wait(limit_ms: int = 20, stream=None) -> None:

@@ -2,12 +2,14 @@
 // contract of every entry point.
 #include <atomic>
 #include <mutex>
+#include <cmath>
 #include <cstdio>
 #include <initializer_list>
 #include <new>
 #include <vector>
 
 #include "common.cuh"
+#include "decay.cuh"
 
 namespace based {
 
@@ -694,6 +696,133 @@ based_status swa_backward(const void* q, const void* k, const void* v, const voi
         if (st != BASED_OK) return st;
     }
     return BASED_OK;
+}
+
+static based_status heads_check(const based_heads& t, int B, int H, int L, int d, based_dtype io, bool written) {
+    if (!t.data) return BASED_ERR_INVALID_ARG;
+    const long long per16 = 16 / (long long)esize(io);
+    struct { long long stride; int size; } dim[3] = {{t.token_stride, L}, {t.head_stride, H}, {t.batch_stride, B}};
+    for (const auto& x : dim)
+        if (x.size > 1 && x.stride < d) return BASED_ERR_INVALID_ARG;
+    for (const auto& x : dim)      // (tensor maps hold strides below 2^40 bytes)
+        if (x.size > 1 && (x.stride % per16 != 0 || x.stride >= 1ll << 37)) return BASED_ERR_UNSUPPORTED;
+    if (written) {                 // from the smallest stride on, each steps over all that lies inside it
+        long long extent = d;
+        for (int turn = 0; turn < 3; ++turn) {
+            int least = -1;
+            for (int i = 0; i < 3; ++i)
+                if (dim[i].size > 1 && (least < 0 || dim[i].stride < dim[least].stride)) least = i;
+            if (least < 0) break;
+            if (dim[least].stride < extent) return BASED_ERR_INVALID_ARG;
+            extent += dim[least].stride * (dim[least].size - 1);
+            dim[least].size = 0;
+        }
+    }
+    return aligned16(t.data) ? BASED_OK : BASED_ERR_ALIGNMENT;
+}
+static based_status decay_sizes_check(int B, int H, int L, int d_k, int d_v, based_dtype io) {
+    if (B <= 0 || H <= 0 || L <= 0 || d_k <= 0 || d_v <= 0 || (io != BASED_F32 && io != BASED_BF16)) return BASED_ERR_INVALID_ARG;
+    if (d_k % 8 || d_v % 8 || d_k > kDecayMaxWidth || d_v > kDecayMaxWidth || L > 0x7fff0000 || (long long)B * H > 0x7fffffffLL ||
+        (long long)B * ((L + 63) / 64) > 0x7fffffffLL || (long long)B * H * d_k * d_v > 1ll << 40)
+        return BASED_ERR_UNSUPPORTED;
+    return BASED_OK;
+}
+static DecayPlan decay_plan_of(int passes, int B, int H, int L, int d_k, int d_v, bool documents, based_dtype io) {
+    DecayCall c{};
+    c.passes = passes;
+    for (int i = 0; i < passes; ++i) c.pass[i].dc = passes == 1 ? d_k : (d_k > d_v ? d_k : d_v);
+    const int de = passes == 1 ? d_v : (d_k > d_v ? d_k : d_v);
+    (void)io;
+    return decay_plan(passes, de, B, H, L, documents, kDecayBlockF32, decay_f32_slots(c));
+}
+static based_status decay_run(const DecayCall& c, const DecayPlan& plan, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (plan.ctas > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    if (!aligned16(workspace)) return BASED_ERR_ALIGNMENT;
+    if (plan.bytes() && (!workspace || workspace_bytes < plan.bytes())) return BASED_ERR_WORKSPACE;
+    if (io != BASED_F32) return BASED_ERR_UNSUPPORTED;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    return launch_decay_f32(c, plan, workspace, stream);
+}
+
+size_t based_decay_attention_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {
+    if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
+    return decay_plan_of(1, B, H, L, d_k, d_v, with_documents != 0, io).bytes();
+}
+size_t based_decay_attention_backward_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {
+    if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
+    return decay_plan_of(3, B, H, L, d_k, d_v, with_documents != 0, io).bytes();
+}
+
+based_status based_decay_attention_forward(based_heads q, based_heads k, based_heads v, const float* rate, const int* documents,
+                                           const float* state_in, based_heads out, float* state_out, int B, int H, int L, int d_k, int d_v,
+                                           float scale, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!q.data || !k.data || !v.data || !out.data || !rate) return BASED_ERR_INVALID_ARG;
+    based_status st = decay_sizes_check(B, H, L, d_k, d_v, io);
+    if (st != BASED_OK) return st;
+    if (is_one_of(out.data, {q.data, k.data, v.data, rate, documents, state_in, state_out, workspace}) ||
+        is_one_of(state_out, {q.data, k.data, v.data, rate, documents, state_in, workspace}))
+        return BASED_ERR_INVALID_ARG;
+    st = heads_check(q, B, H, L, d_k, io, false);
+    if (st == BASED_OK) st = heads_check(k, B, H, L, d_k, io, false);
+    if (st == BASED_OK) st = heads_check(v, B, H, L, d_v, io, false);
+    if (st == BASED_OK) st = heads_check(out, B, H, L, d_v, io, true);
+    if (st != BASED_OK) return st;
+    if (!aligned16(rate) || !aligned16(state_in) || !aligned16(state_out) || (reinterpret_cast<uintptr_t>(documents) & 3)) return BASED_ERR_ALIGNMENT;
+    DecayCall c{};
+    c.passes = 1;
+    c.pass[0] = {q, k, v, out, d_k, d_v, state_in, state_out, 0, 0, 1.f, 1.f};
+    c.rate = rate;
+    c.documents = documents;
+    c.B = B; c.H = H; c.L = L;
+    c.factor = scale > 0.f ? scale : 1.f / sqrtf((float)d_k);
+    return decay_run(c, decay_plan_of(1, B, H, L, d_k, d_v, documents != nullptr, io), io, workspace, workspace_bytes, cuda_stream);
+}
+
+based_status based_decay_attention_step(const void* q, const void* k, const void* v, const float* rate, const float* state_in, void* out,
+                                        float* state_out, int B, int H, int d_k, int d_v, float scale, based_dtype io, void* cuda_stream) {
+    if (!q || !k || !v || !rate || !state_in || !out || !state_out) return BASED_ERR_INVALID_ARG;
+    const based_status st = decay_sizes_check(B, H, 1, d_k, d_v, io);
+    if (st != BASED_OK) return st;
+    if (is_one_of(out, {q, k, v, rate, state_in, state_out}) || is_one_of(state_out, {q, k, v, rate})) return BASED_ERR_INVALID_ARG;
+    for (const void* p : {q, k, v, (const void*)rate, (const void*)state_in, (const void*)out, (const void*)state_out})
+        if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
+    return launch_decay_step(q, k, v, rate, state_in, out, state_out, (long long)B * H, H, d_k, d_v,
+                             scale > 0.f ? scale : 1.f / sqrtf((float)d_k), io, static_cast<cudaStream_t>(cuda_stream));
+}
+
+based_status based_decay_attention_backward(based_heads q, based_heads k, based_heads v, const float* rate, const int* documents,
+                                            const float* state_in, based_heads dout, const float* dstate_out, based_heads dq, based_heads dk,
+                                            based_heads dv, float* dstate_in, int B, int H, int L, int d_k, int d_v, float scale,
+                                            based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!q.data || !k.data || !v.data || !dout.data || !dq.data || !dk.data || !dv.data || !rate) return BASED_ERR_INVALID_ARG;
+    based_status st = decay_sizes_check(B, H, L, d_k, d_v, io);
+    if (st != BASED_OK) return st;
+    const void* outs[] = {dq.data, dk.data, dv.data, dstate_in};
+    for (int i = 0; i < 4; ++i) {
+        if (is_one_of(outs[i], {q.data, k.data, v.data, dout.data, rate, documents, state_in, dstate_out, workspace})) return BASED_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (is_one_of(outs[i], {outs[j]})) return BASED_ERR_INVALID_ARG;
+    }
+    const struct { const based_heads* t; int d; bool written; } all[] = {{&q, d_k, false}, {&k, d_k, false}, {&v, d_v, false}, {&dout, d_v, false},
+                                                                         {&dq, d_k, true}, {&dk, d_k, true}, {&dv, d_v, true}};
+    for (const auto& x : all) {
+        st = heads_check(*x.t, B, H, L, x.d, io, x.written);
+        if (st != BASED_OK) return st;
+    }
+    for (const void* p : {(const void*)rate, (const void*)state_in, (const void*)dstate_out, (const void*)dstate_in})
+        if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
+    if (reinterpret_cast<uintptr_t>(documents) & 3) return BASED_ERR_ALIGNMENT;
+    DecayCall c{};
+    c.passes = 3;
+    c.factor = scale > 0.f ? scale : 1.f / sqrtf((float)d_k);
+    // R of the backward passes is kept without the scale
+    c.pass[0] = {dout, v, k, dq, d_v, d_k, state_in, nullptr, 1, 0, 1.f, 1.f};
+    c.pass[1] = {v, dout, q, dk, d_v, d_k, dstate_out, nullptr, 1, 1, 1.f / c.factor, c.factor};
+    c.pass[2] = {k, q, dout, dv, d_k, d_v, dstate_out, dstate_in, 0, 1, 1.f / c.factor, c.factor};
+    c.rate = rate;
+    c.documents = documents;
+    c.B = B; c.H = H; c.L = L;
+    return decay_run(c, decay_plan_of(3, B, H, L, d_k, d_v, documents != nullptr, io), io, workspace, workspace_bytes, cuda_stream);
 }
 
 size_t based_prefill_backward_workspace_bytes(int B, int H, int L, int d_v, based_dtype io) {

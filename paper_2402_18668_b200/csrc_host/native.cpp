@@ -781,6 +781,110 @@ PyObject* swa_grad(PyObject* const* a) {
     return wrap({g.dq, g.dk, g.dv});
 }
 
+// ---------------------------------------------------------------------------------------------- decay attention
+// [B,H,L,d] as the library takes it: the elements of a row side by side
+const Tensor& heads(PyObject* o, const char* name) {
+    const Tensor& t = tensor(o);
+    if (!t.defined()) throw TypeFault(std::string(name) + " is required");
+    if (!t.is_cuda()) value_error("libbased takes CUDA tensors only (there is no CPU path)");
+    dims(t, 4, name);
+    if (t.size(3) > 1 && t.stride(3) != 1) value_error(std::string(name) + " must have the elements of a row side by side");
+    return t;
+}
+based_heads as_heads(const Tensor& t) { return {t.const_data_ptr(), t.stride(0), t.stride(1), t.stride(2)}; }
+void check_int32(const Tensor& t, at::IntArrayRef shape, const char* name) {
+    if (!t.defined()) return;
+    if (t.scalar_type() != at::kInt) throw TypeFault(std::string(name) + " is int32");
+    if (!shape_is(t, shape)) value_error(std::string(name) + " must be " + text(shape) + ", got " + text(t.sizes()));
+}
+struct Decay {
+    Tensor q, k, v, rate, documents, in;
+    float scale;
+    int B, H, L, dk, dv;
+    based_dtype io;
+    Decay(Tensor q_, Tensor k_, Tensor v_, Tensor rate_, Tensor documents_, Tensor in_, float scale_)
+        : q(std::move(q_)), k(std::move(k_)), v(std::move(v_)), rate(std::move(rate_)), documents(std::move(documents_)), in(std::move(in_)),
+          scale(scale_) {
+        check_qkv(q, k, v, kNone);
+        B = dim(q, 0); H = dim(q, 1); L = dim(q, 2); dk = dim(q, 3); dv = dim(v, 3);
+        check_f32(rate, {H}, "rate");
+        check_int32(documents, {B, L}, "documents");
+        state(in, "state_in");
+        io = dtype_code(q);
+    }
+    void state(const Tensor& t, const char* name) const { check_f32(t, {B, H, dk, dv}, name); }
+    const int* ids() const { return static_cast<const int*>(cptr(documents)); }
+    Tensor forward(Tensor out, const Tensor& last, const Tensor& workspace, void* stream) const {
+        if (!out.defined()) out = blank({B, H, L, dv}, q.scalar_type());
+        const Workspace ws(workspace, based_decay_attention_workspace_bytes(B, H, L, dk, dv, documents.defined(), io), q, stream);
+        check(based_decay_attention_forward(as_heads(q), as_heads(k), as_heads(v), f32(rate), ids(), f32(in), as_heads(out), fptr(last), B, H, L,
+                                            dk, dv, scale, io, ws.data, ws.bytes, stream),
+              "based_decay_attention_forward");
+        return out;
+    }
+    struct Grads { Tensor dq, dk, dv, dstate; };
+    Grads backward(const Tensor& dout, const Tensor& dlast, const Tensor& workspace, void* stream) const {
+        const at::ScalarType type = q.scalar_type();
+        Grads g{blank({B, H, L, dk}, type), blank({B, H, L, dk}, type), blank({B, H, L, dv}, type),
+                in.defined() ? blank({B, H, dk, dv}, at::kFloat) : Tensor()};
+        const Workspace ws(workspace, based_decay_attention_backward_workspace_bytes(B, H, L, dk, dv, documents.defined(), io), q, stream);
+        check(based_decay_attention_backward(as_heads(q), as_heads(k), as_heads(v), f32(rate), ids(), f32(in), as_heads(dout), f32(dlast),
+                                             as_heads(g.dq), as_heads(g.dk), as_heads(g.dv), fptr(g.dstate), B, H, L, dk, dv, scale, io,
+                                             ws.data, ws.bytes, stream),
+              "based_decay_attention_backward");
+        return g;
+    }
+};
+// q, k, v, rate, documents, state_in, out, state_out, scale, workspace, stream
+PyObject* decay_forward(PyObject* const* a) {
+    const Decay o(heads(a[0], "q"), heads(a[1], "k"), heads(a[2], "v"), need(a[3], "rate"), dev(a[4]), dev(a[5]), number(a[8]));
+    const Tensor out = a[6] == Py_None ? Tensor() : heads(a[6], "out");
+    const Tensor &last = dev(a[7]), &ws = dev(a[9]);
+    check_like(out, o.v, "out", "v");
+    o.state(last, "state_out");
+    check_places({&o.q, &o.k, &o.v, &o.rate, &o.documents, &o.in}, {&out, &last, &ws});
+    void* stream = stream_on(a[10], o.q);
+    Tensor y;
+    away(o.q, [&] { y = o.forward(out, last, ws, stream); });
+    return wrap(y);
+}
+// q, k, v, rate, state_in, out, state_out, scale, stream; one token: q, k [B,H,d_k], v [B,H,d_v]
+PyObject* decay_step(PyObject* const* a) {
+    const Tensor &q = need(a[0], "q"), &k = need(a[1], "k"), &v = need(a[2], "v"), &rate = need(a[3], "rate"), &in = need(a[4], "state"),
+                 &last = need(a[6], "state_out");
+    Tensor out = dev(a[5]);
+    dims(q, 3, "q");
+    check_qkv(q, k, v, out);
+    const int B = dim(q, 0), H = dim(q, 1), dk = dim(q, 2), dv = dim(v, 2);
+    check_f32(rate, {H}, "rate");
+    check_f32(in, {B, H, dk, dv}, "state");
+    check_f32(last, {B, H, dk, dv}, "state_out");
+    const bool in_place = in.const_data_ptr() == last.const_data_ptr();
+    if (in_place) check_places({&q, &k, &v, &rate}, {&out, &last});
+    else check_places({&q, &k, &v, &rate, &in}, {&out, &last});
+    const float scale = number(a[7]);
+    const based_dtype io = dtype_code(q);
+    void* stream = stream_on(a[8], q);
+    away(q, [&] {
+        if (!out.defined()) out = blank(v.sizes(), v.scalar_type());
+        check(based_decay_attention_step(cptr(q), cptr(k), cptr(v), f32(rate), f32(in), ptr(out), fptr(last), B, H, dk, dv, scale, io, stream),
+              "based_decay_attention_step");
+    });
+    return wrap(out);
+}
+// q, k, v, rate, documents, state_in, dout, dstate_out, scale, workspace, stream -> dq, dk, dv, dstate_in (None without state_in)
+PyObject* decay_backward(PyObject* const* a) {
+    const Decay o(heads(a[0], "q"), heads(a[1], "k"), heads(a[2], "v"), need(a[3], "rate"), dev(a[4]), dev(a[5]), number(a[8]));
+    const Tensor &dout = heads(a[6], "dout"), &dlast = dev(a[7]), &ws = dev(a[9]);
+    check_like(dout, o.v, "dout", "v");
+    o.state(dlast, "dstate_out");
+    check_places({&o.q, &o.k, &o.v, &o.rate, &o.documents, &o.in, &dout, &dlast}, {&ws});
+    void* stream = stream_on(a[10], o.q);
+    Decay::Grads g;
+    away(o.q, [&] { g = o.backward(dout, dlast, ws, stream); });
+    return wrap({g.dq, g.dk, g.dv, g.dstate});
+}
+
 // Python's exception for a status of the library
 void set_status_error(const StatusFault& e) {
     PyObject* mod = PyImport_ImportModule("paper_2402_18668_b200.binding");
@@ -1048,6 +1152,44 @@ struct SlidingWindow : torch::autograd::Function<SlidingWindow> {
         });
     }
 };
+// a view [B,H,L,d] with strides that the library takes, or a copy
+Tensor as_rows(const Tensor& t) {
+    if (t.dim() != 4) return packed(t);
+    const int64_t per16 = 16 / static_cast<int64_t>(t.element_size()), d = t.size(3);
+    bool as_it_lies = (d == 1 || t.stride(3) == 1) && on_16_bytes(t);
+    for (int i = 0; i < 3; ++i) as_it_lies = as_it_lies && (t.size(i) == 1 || (t.stride(i) >= d && t.stride(i) % per16 == 0));
+    return as_it_lies ? t : packed(t);
+}
+struct DecayAttention : torch::autograd::Function<DecayAttention> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& q_, const Tensor& k_, const Tensor& v_,
+                                                  const Tensor& rate_, const std::optional<Tensor>& documents,
+                                                  const std::optional<Tensor>& in, double scale) {
+        ctx->set_materialize_grads(false);
+        on_gpu(q_);
+        on_gpu(k_);
+        on_gpu(v_);
+        if (rate_.requires_grad()) value_error("the rates are constants: rate must not require a gradient");
+        dims(q_, 4, "q");
+        const Decay o(as_rows(q_), as_rows(k_), as_rows(v_), packed(rate_), packed(documents), packed(in), static_cast<float>(scale));
+        check_places({&o.q, &o.k, &o.v, &o.rate, &o.documents, &o.in}, {});
+        const c10::cuda::CUDAGuard device(o.q.device());
+        const Tensor last = blank({o.B, o.H, o.dk, o.dv}, at::kFloat);
+        const Tensor out = o.forward(Tensor(), last, kNone, c10::cuda::getCurrentCUDAStream(o.q.get_device()).stream());
+        ctx->save_for_backward({o.q, o.k, o.v, o.rate, o.documents, o.in});
+        ctx->saved_data["scale"] = scale;
+        return {out, last};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        const auto s = ctx->get_saved_variables();
+        if (!grads[0].defined() && !grads[1].defined()) return {Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        const Decay o(s[0], s[1], s[2], s[3], s[4], s[5], static_cast<float>(ctx->saved_data["scale"].toDouble()));
+        return node_backward(o.q, [&](void* stream) -> torch::autograd::variable_list {
+            const Tensor dout = grads[0].defined() ? as_rows(grads[0].to(o.v.scalar_type())) : at::zeros(o.v.sizes(), o.v.options());
+            const Decay::Grads g = o.backward(dout, as_input(grads[1], o.rate), kNone, stream);
+            return {g.dq, g.dk, g.dv, Tensor(), Tensor(), g.dstate, Tensor()};
+        });
+    }
+};
 // a call of a node, without the interpreter lock
 template <typename F> auto applied(F f) {
     decltype(f()) r;
@@ -1091,6 +1233,15 @@ PyObject* sliding_window(PyObject* const* a) {
     return wrap(applied([&] { return SlidingWindow::apply(q, k, v, window, scale); }));
 }
 
+// q, k, v, rate, documents, state, scale
+PyObject* decay_attention(PyObject* const* a) {
+    const Tensor q = given(a[0], "q"), k = given(a[1], "k"), v = given(a[2], "v"), rate = given(a[3], "rate");
+    const auto documents = maybe(tensor(a[4])), in = maybe(tensor(a[5]));
+    const double scale = number(a[6]);
+    const auto y = applied([&] { return DecayAttention::apply(q, k, v, rate, documents, in, scale); });
+    return wrap({y[0], y[1]});
+}
+
 // ---------------------------------------------------------------------------------------------- module
 // Everything but the faults of this file is torch's to translate: its own error types, and Python exceptions that passed
 // through C++ (python_error, from a saved-tensor hook for instance), which go on as they are.
@@ -1127,7 +1278,9 @@ PyMethodDef methods[] = {method<prefill, 9>("prefill"), method<prefill_backward,
                          method<recurrence, 8>("recurrence"), method<recurrence_backward, 10>("recurrence_backward"),
                          method<rotate, 12>("rotate"), method<rotate_backward, 15>("rotate_backward"),
                          method<swa_grad, 8>("swa_grad"), method<gated_recurrence, 5>("gated_recurrence"),
-                         method<qk_norm_rotate, 9>("qk_norm_rotate"), method<sliding_window, 5>("sliding_window"), {nullptr, nullptr, 0, nullptr}};
+                         method<qk_norm_rotate, 9>("qk_norm_rotate"), method<sliding_window, 5>("sliding_window"),
+                         method<decay_forward, 11>("decay_forward"), method<decay_step, 9>("decay_step"), method<decay_backward, 11>("decay_backward"),
+                         method<decay_attention, 7>("decay_attention"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 
