@@ -732,16 +732,15 @@ static DecayPlan decay_plan_of(int passes, int B, int H, int L, int d_k, int d_v
     c.passes = passes;
     for (int i = 0; i < passes; ++i) c.pass[i].dc = passes == 1 ? d_k : (d_k > d_v ? d_k : d_v);
     const int de = passes == 1 ? d_v : (d_k > d_v ? d_k : d_v);
-    (void)io;
-    return decay_plan(passes, de, B, H, L, documents, kDecayBlockF32, decay_f32_slots(c));
+    return io == BASED_F32 ? decay_plan(passes, de, B, H, L, documents, kDecayBlockF32, decay_f32_slots(c))
+                           : decay_plan(passes, de, B, H, L, documents, kDecayBlockTc, decay_tc_slots());
 }
 static based_status decay_run(const DecayCall& c, const DecayPlan& plan, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (plan.ctas > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
     if (!aligned16(workspace)) return BASED_ERR_ALIGNMENT;
     if (plan.bytes() && (!workspace || workspace_bytes < plan.bytes())) return BASED_ERR_WORKSPACE;
-    if (io != BASED_F32) return BASED_ERR_UNSUPPORTED;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    return launch_decay_f32(c, plan, workspace, stream);
+    return io == BASED_F32 ? launch_decay_f32(c, plan, workspace, stream) : launch_decay_tc(c, plan, workspace, stream);
 }
 
 size_t based_decay_attention_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {

@@ -24,6 +24,10 @@ bool make_head_rows_map_bf16(CUtensorMap* m, const void* base, int BH, int H, in
 // over), [1][box_n][box_c] a box, rows side by side in shared memory
 bool make_tokens_map(CUtensorMap* m, const based_tokens& t, bool f32, int B, int N, int C, int box_c, int box_n);
 
+// tensor map of bf16 [B,H,L,width] values with strides (based_heads): coordinates x, token, head, sequence; 64 columns x box_rows tokens a box,
+// swizzled by 128 bytes, what lies outside zero-filled on load and clipped on store
+bool make_heads_map_bf16(CUtensorMap* m, const based_heads& t, int B, int H, int L, int width, int box_rows);
+
 namespace sm100 {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
@@ -165,6 +169,11 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void*
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* smem_src, int x, int y) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
                  ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(smem_src))
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void* smem_src, int x, int y, int z, int w) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map),
+                 "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(smem_src))
                  : "memory");
 }
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }

@@ -60,6 +60,15 @@ bool make_tokens_map(CUtensorMap* m, const based_tokens& t, bool f32, int B, int
                       f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
 }
 
+bool make_heads_map_bf16(CUtensorMap* m, const based_heads& t, int B, int H, int L, int width, int box_rows) {
+    const cuuint64_t row = (cuuint64_t)width * 2;                    // (stands for the stride of a dimension of size 1)
+    const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)L, (cuuint64_t)H, (cuuint64_t)B};
+    const cuuint64_t strides[3] = {L > 1 ? (cuuint64_t)t.token_stride * 2 : row, H > 1 ? (cuuint64_t)t.head_stride * 2 : row,
+                                   B > 1 ? (cuuint64_t)t.batch_stride * 2 : row};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
+    return encode_map(m, t.data, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
 bool make_head_rows_map_bf16(CUtensorMap* m, const void* base, int BH, int H, int L, int width, int box_w, int box_rows,
                              CUtensorMapSwizzle sw) {
     if (H == 0) return make_rows_map_bf16(m, base, BH, L, width, box_w, box_rows, sw);
