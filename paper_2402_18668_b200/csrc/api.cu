@@ -727,15 +727,23 @@ static based_status decay_sizes_check(int B, int H, int L, int d_k, int d_v, bas
         return BASED_ERR_UNSUPPORTED;
     return BASED_OK;
 }
-static DecayPlan decay_plan_of(int passes, int B, int H, int L, int d_k, int d_v, bool documents, based_dtype io) {
+static DecayPlan decay_plan_of(const DecayCall& c, based_dtype io) { return io == BASED_F32 ? decay_plan_f32(c) : decay_plan_tc(c); }
+// the sizes of a call's passes, without its arrays
+static DecayCall decay_call(int passes, int B, int H, int L, int d_k, int d_v, bool documents) {
+    static const int given = 0;
     DecayCall c{};
     c.passes = passes;
-    for (int i = 0; i < passes; ++i) c.pass[i].dc = passes == 1 ? d_k : (d_k > d_v ? d_k : d_v);
-    const int de = passes == 1 ? d_v : (d_k > d_v ? d_k : d_v);
-    return io == BASED_F32 ? decay_plan(passes, de, B, H, L, documents, kDecayBlockF32, decay_f32_slots(c))
-                           : decay_plan(passes, de, B, H, L, documents, kDecayBlockTc, decay_tc_slots());
+    c.B = B; c.H = H; c.L = L;
+    c.documents = documents ? &given : nullptr;
+    const int dc[2][3] = {{d_k, 0, 0}, {d_v, d_v, d_k}}, de[2][3] = {{d_v, 0, 0}, {d_k, d_k, d_v}};
+    for (int i = 0; i < passes; ++i) {
+        c.pass[i].dc = dc[passes == 3][i];
+        c.pass[i].de = de[passes == 3][i];
+    }
+    return c;
 }
-static based_status decay_run(const DecayCall& c, const DecayPlan& plan, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+static based_status decay_run(const DecayCall& c, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    const DecayPlan plan = decay_plan_of(c, io);
     if (plan.ctas > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
     if (!aligned16(workspace)) return BASED_ERR_ALIGNMENT;
     if (plan.bytes() && (!workspace || workspace_bytes < plan.bytes())) return BASED_ERR_WORKSPACE;
@@ -745,11 +753,11 @@ static based_status decay_run(const DecayCall& c, const DecayPlan& plan, based_d
 
 size_t based_decay_attention_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {
     if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
-    return decay_plan_of(1, B, H, L, d_k, d_v, with_documents != 0, io).bytes();
+    return decay_plan_of(decay_call(1, B, H, L, d_k, d_v, with_documents != 0), io).bytes();
 }
 size_t based_decay_attention_backward_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {
     if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
-    return decay_plan_of(3, B, H, L, d_k, d_v, with_documents != 0, io).bytes();
+    return decay_plan_of(decay_call(3, B, H, L, d_k, d_v, with_documents != 0), io).bytes();
 }
 
 based_status based_decay_attention_forward(based_heads q, based_heads k, based_heads v, const float* rate, const int* documents,
@@ -774,7 +782,7 @@ based_status based_decay_attention_forward(based_heads q, based_heads k, based_h
     c.documents = documents;
     c.B = B; c.H = H; c.L = L;
     c.factor = scale > 0.f ? scale : 1.f / sqrtf((float)d_k);
-    return decay_run(c, decay_plan_of(1, B, H, L, d_k, d_v, documents != nullptr, io), io, workspace, workspace_bytes, cuda_stream);
+    return decay_run(c, io, workspace, workspace_bytes, cuda_stream);
 }
 
 based_status based_decay_attention_step(const void* q, const void* k, const void* v, const float* rate, const float* state_in, void* out,
@@ -821,7 +829,7 @@ based_status based_decay_attention_backward(based_heads q, based_heads k, based_
     c.rate = rate;
     c.documents = documents;
     c.B = B; c.H = H; c.L = L;
-    return decay_run(c, decay_plan_of(3, B, H, L, d_k, d_v, documents != nullptr, io), io, workspace, workspace_bytes, cuda_stream);
+    return decay_run(c, io, workspace, workspace_bytes, cuda_stream);
 }
 
 size_t based_prefill_backward_workspace_bytes(int B, int H, int L, int d_v, based_dtype io) {

@@ -17,7 +17,6 @@
 
 namespace based {
 
-constexpr int kDecayTile = 64;             // columns of z and of the output that a CTA works on
 constexpr int kDecayMaxWidth = 128;        // d_k, d_v at most
 
 // one pass: x, y [B,H,L,dc], z, out [B,H,L,de]
@@ -50,18 +49,19 @@ __device__ __forceinline__ int place_run(uint32_t w) { return (int)(w >> 8 & 255
 __device__ __forceinline__ float faded(float rate2, int n) { return n == 0 ? 1.f : exp2f(-rate2 * (float)n); }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// How a call is cut: every pass and head into tiles of 64 output columns, every one of those into segments of whole blocks of tokens.
+// How a call is cut: every pass and head into tiles of `width` output columns, every one of those into segments of whole blocks of tokens.
 // More than one segment: a launch ahead writes every segment's own state.
 struct DecayPlan {
-    int T;                                 // tokens in a block
+    int T, width;                          // tokens in a block, columns of z and of the output that a CTA works on
     int blocks, segments;                  // blocks of a sequence, segments they are cut into
-    int tiles;                             // tiles of 64 columns of the widest pass
+    int tiles;                             // tiles of the widest pass
     long long ctas;                        // passes x tiles x segments x heads
+    double time;                           // what the choice went by
     size_t places_bytes, states_bytes, factors_bytes;
     size_t bytes() const { return places_bytes + states_bytes + factors_bytes; }
 };
-// slots: CTAs that the device holds at a time
-DecayPlan decay_plan(int passes, int max_de, int B, int H, int L, bool documents, int T, int slots);
+// slots: CTAs that the device holds at a time; per_block: a block's time at this width, in blocks of width 64
+DecayPlan decay_plan(int passes, int max_de, int B, int H, int L, bool documents, int T, int width, int slots, double per_block);
 // the first block of a segment
 __host__ __device__ inline int decay_first(int blocks, int segments, int s) { return (int)((long long)blocks * s / segments); }
 
@@ -76,17 +76,17 @@ struct DecayItem {
         head = i / segments;
     }
 };
-// the segments' states and factors in the workspace: [pass][head][tile][segment - 1 of them][128][64], the last not kept
+// the segments' states and factors in the workspace, of all but the last: states [128][width] each
 __host__ __device__ inline long long decay_slot(int pass, int passes, long long head, int tiles, int tile, int segments, int segment) {
     return ((head * passes + pass) * tiles + tile) * (segments - 1) + segment;
 }
 
 // places [B][blocks * T] of the tokens (decay_places.cu)
 based_status launch_decay_places(const int* documents, uint32_t* places, int B, int L, int T, cudaStream_t stream);
-// fp32 io on multiply-adds (decay_f32.cu), bf16 io on tensor cores (decay_tc.cu); slots: what their plans take
-int decay_f32_slots(const DecayCall& c);
+// fp32 io on multiply-adds (decay_f32.cu), bf16 io on tensor cores (decay_tc.cu)
+DecayPlan decay_plan_f32(const DecayCall& c);
 based_status launch_decay_f32(const DecayCall& c, const DecayPlan& plan, void* workspace, cudaStream_t stream);
-int decay_tc_slots();
+DecayPlan decay_plan_tc(const DecayCall& c);
 based_status launch_decay_tc(const DecayCall& c, const DecayPlan& plan, void* workspace, cudaStream_t stream);
 // one token (decay_step.cu): state [B,H,dk,dv] read, updated, written
 based_status launch_decay_step(const void* q, const void* k, const void* v, const float* rate, const float* state_in, void* out,

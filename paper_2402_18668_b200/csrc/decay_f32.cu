@@ -11,9 +11,9 @@ namespace based {
 
 namespace {
 
-constexpr int kT = kDecayBlockF32, kThreads = 256;
+constexpr int kT = kDecayBlockF32, kTile = 64, kThreads = 256;
 template <int DC> struct Cfg {
-    static constexpr int kX = DC + 4, kZ = kDecayTile + 4;          // floats per row
+    static constexpr int kX = DC + 4, kZ = kTile + 4;          // floats per row
     static constexpr int offY = kT * kX, offZ = 2 * kT * kX, offS = offZ + kT * kZ, offP = offS + DC * kZ, offW = offP + kT * kZ;
     static constexpr size_t bytes = sizeof(float) * (offW + 3 * kT);
 };
@@ -51,22 +51,22 @@ __global__ void __launch_bounds__(kThreads, DC == 64 ? 2 : 1) decay_f32_kernel(c
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const DecayItem it(blockIdx.x, a.c.passes, a.tiles, STATES ? a.segments - 1 : a.segments);
     const DecayPass& p = a.c.pass[it.pass];
-    const int e0 = it.tile * kDecayTile, L = a.c.L;
+    const int e0 = it.tile * kTile, L = a.c.L;
     enter_dependent();
     if (e0 >= p.de) return;
     const int b = (int)(it.head / a.c.H), h = (int)(it.head % a.c.H);
     const float rate2 = a.c.rate[h] * kLog2e;
 
     // the state that the segment begins with
-    for (int i = tid; i < DC * kDecayTile; i += kThreads) {
-        const int c = i / kDecayTile, e = i % kDecayTile;
+    for (int i = tid; i < DC * kTile; i += kThreads) {
+        const int c = i / kTile, e = i % kTile;
         float s = 0.f;
         if (!STATES) {
             if (p.state_in && c < p.dc && e0 + e < p.de)
                 s = p.in_factor * p.state_in[it.head * p.dc * p.de + (p.turned ? (long long)(e0 + e) * p.dc + c : (long long)c * p.de + e0 + e)];
             for (int g = 0; g < it.segment; ++g) {
                 const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, g);
-                s = fmaf(a.factors[slot], s, a.states[slot * kDecayMaxWidth * kDecayTile + i]);
+                s = fmaf(a.factors[slot], s, a.states[slot * kDecayMaxWidth * kTile + i]);
             }
         }
         sS[c * C::kZ + e] = s;
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, DC == 64 ? 2 : 1) decay_f32_kernel(c
         }
         if (!STATES) load_rows<DC>(p.x, b, h, t0, L, 0, p.dc, pl, sX);
         load_rows<DC>(p.y, b, h, t0, L, 0, p.dc, pl, sY);
-        load_rows<kDecayTile>(p.z, b, h, t0, L, e0, p.de, pl, sZ);
+        load_rows<kTile>(p.z, b, h, t0, L, e0, p.de, pl, sZ);
         __syncthreads();
         if (!STATES) {
             {   // scores of rows ty + 16 i and columns tx + 16 j
@@ -208,13 +208,13 @@ __global__ void __launch_bounds__(kThreads, DC == 64 ? 2 : 1) decay_f32_kernel(c
     }
     if (STATES) {
         const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, it.segment);
-        for (int i = tid; i < DC * kDecayTile; i += kThreads)
-            a.states[slot * kDecayMaxWidth * kDecayTile + i] = sS[i / kDecayTile * C::kZ + i % kDecayTile];
+        for (int i = tid; i < DC * kTile; i += kThreads)
+            a.states[slot * kDecayMaxWidth * kTile + i] = sS[i / kTile * C::kZ + i % kTile];
         if (tid == 0) a.factors[slot] = whole;
     } else if (p.state_out && it.segment == a.segments - 1) {
-        for (int i = tid; i < p.dc * kDecayTile; i += kThreads) {
+        for (int i = tid; i < p.dc * kTile; i += kThreads) {
             // (neighbouring threads along the state's rows, whichever way it lies)
-            const int c = p.turned ? i % p.dc : i / kDecayTile, e = p.turned ? i / p.dc : i % kDecayTile;
+            const int c = p.turned ? i % p.dc : i / kTile, e = p.turned ? i / p.dc : i % kTile;
             if (e0 + e < p.de)
                 p.state_out[it.head * p.dc * p.de + (p.turned ? (long long)(e0 + e) * p.dc + c : (long long)c * p.de + e0 + e)] =
                     p.out_factor * sS[c * C::kZ + e];
@@ -246,7 +246,11 @@ bool wide(const DecayCall& c) {
 
 }  // namespace
 
-int decay_f32_slots(const DecayCall& c) { return wide(c) ? kSMs : 2 * kSMs; }
+DecayPlan decay_plan_f32(const DecayCall& c) {
+    int de = 0;
+    for (int i = 0; i < c.passes; ++i) de = c.pass[i].de > de ? c.pass[i].de : de;
+    return decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, kTile, wide(c) ? kSMs : 2 * kSMs, 1.0);
+}
 
 based_status launch_decay_f32(const DecayCall& c, const DecayPlan& plan, void* workspace, cudaStream_t stream) {
     char* ws = static_cast<char*>(workspace);
