@@ -40,10 +40,13 @@ struct DecayCall {
 };
 
 // A token's place in its block of kT tokens: bits 0-7 how many tokens up to it count, bits 8-15 how many documents have begun up to it
-// (0: the one that reaches over the block's border), bit 31: it is padding.  Past the sequence: padding.
-constexpr uint32_t kPadding = 0x80000000u;
+// (0: the one that reaches over the block's border), bits 16-22 and 23-29 the first and the last token of its document in the
+// block, bit 30: no padding lies between the block's tokens that count, bit 31: it is padding.  Past the sequence: padding.
+constexpr uint32_t kPadding = 0x80000000u, kCompact = 0x40000000u;
 __device__ __forceinline__ int place_count(uint32_t w) { return (int)(w & 255u); }
 __device__ __forceinline__ int place_run(uint32_t w) { return (int)(w >> 8 & 255u); }
+__device__ __forceinline__ int place_from(uint32_t w) { return (int)(w >> 16 & 127u); }
+__device__ __forceinline__ int place_to(uint32_t w) { return (int)(w >> 23 & 127u); }
 
 // exp(-rate n) for a rate held as rate log2(e); n = 0 gives 1 whatever the rate
 __device__ __forceinline__ float faded(float rate2, int n) { return n == 0 ? 1.f : exp2f(-rate2 * (float)n); }

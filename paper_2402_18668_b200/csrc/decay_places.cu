@@ -14,7 +14,7 @@ __global__ void __launch_bounds__(128) decay_places_kernel(const int* __restrict
     enter_dependent();
     const int b = blockIdx.x / blocks, n = blockIdx.x % blocks, t = n * T + threadIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int* ids = documents + (long long)b * L;
-    __shared__ int s_last[4], s_any[4], s_count[4], s_begun[4];
+    __shared__ int s_last[4], s_any[4];
     const bool in = (int)threadIdx.x < T;
     const int id = in && t < L ? ids[t] : -1;
     const bool counts = id >= 0;
@@ -26,7 +26,6 @@ __global__ void __launch_bounds__(128) decay_places_kernel(const int* __restrict
     if (lane == 0) {
         s_any[warp] = m != 0;
         s_last[warp] = last;
-        s_count[warp] = __popc(m);
     }
     __syncthreads();
     bool known = prev_lane >= 0;
@@ -71,14 +70,47 @@ __global__ void __launch_bounds__(128) decay_places_kernel(const int* __restrict
     if (!known) prev = before;                         // (-1: nothing before it counts, and the state given goes on)
     const bool begins = counts && prev >= 0 && prev != id;
     const uint32_t mb = __ballot_sync(0xffffffffu, begins), upto = 0xffffffffu >> (31 - lane);
-    if (lane == 0) s_begun[warp] = __popc(mb);
-    __syncthreads();
-    int count = __popc(m & upto), run = __popc(mb & upto);
-    for (int w = 0; w < warp; ++w) {
-        count += s_count[w];
-        run += s_begun[w];
+    __shared__ uint32_t s_counts[4], s_begins[4];
+    if (lane == 0) {
+        s_counts[warp] = m;
+        s_begins[warp] = mb;
     }
-    if (in) places[((long long)b * blocks + n) * T + threadIdx.x] = (uint32_t)count | (uint32_t)run << 8 | (counts ? 0u : kPadding);
+    __syncthreads();
+    int count = __popc(m & upto), run = __popc(mb & upto), first = 128, last_one = -1, all = 0;
+    for (int w = 0; w < 4; ++w) {
+        if (w < warp) {
+            count += __popc(s_counts[w]);
+            run += __popc(s_begins[w]);
+        }
+        all += __popc(s_counts[w]);
+        if (s_counts[w]) {
+            first = min(first, 32 * w + __ffs(s_counts[w]) - 1);
+            last_one = 32 * w + 31 - __clz(s_counts[w]);
+        }
+    }
+    // this token's document: from the last beginning up to it (or the block's first token that counts) to the token that counts ahead of the
+    // next beginning (or the last one)
+    int from = first, to = last_one;
+    const uint32_t mine = mb & upto, after = mb & ~upto;
+    if (mine) {
+        from = 32 * warp + 31 - __clz(mine);
+    } else {
+        for (int w = warp - 1; w >= 0; --w)
+            if (s_begins[w]) {
+                from = 32 * w + 31 - __clz(s_begins[w]);
+                break;
+            }
+    }
+    int next = after ? 32 * warp + __ffs(after) - 1 : 128;
+    for (int w = warp + 1; w < 4 && next == 128; ++w)
+        if (s_begins[w]) next = 32 * w + __ffs(s_begins[w]) - 1;
+    if (next < 128) {                                  // (with padding ahead of it, a token that does not count: no matter)
+        to = next - 1;
+    }
+    const bool compact = all == last_one - first + 1;
+    if (in)
+        places[((long long)b * blocks + n) * T + threadIdx.x] = (uint32_t)count | (uint32_t)run << 8 | (uint32_t)(from & 127) << 16 |
+                                                                 (uint32_t)(to & 127) << 23 | (compact ? kCompact : 0u) | (counts ? 0u : kPadding);
 }
 
 }  // namespace

@@ -5,9 +5,8 @@
 //   turn    Y = y^T            [DC,128]    by products with a 16 x 16 identity: a row per dimension, a column per token, in TMEM, where
 //           one thread per row fades the columns and leaves them as bf16 parts that add up to 16 (24) bits
 //   O = x S  [128, E], S rounded to bf16 in shared memory; then O <- take O by one thread per row, and O += P z
-//   dS = (give Y) z            [DC, E], fp32; the state S <- f S + dS is held in registers, a row per thread, so that no
-//           block's products wait for the block before it
-//   out     factor O -> bf16 -> the place of z -> TMA store
+//   S += (give Y) z            [DC, E], fp32 in TMEM, after one thread per row has multiplied it by f and left it in bf16 for x S
+//   out     O -> bf16 -> the place of z -> TMA store (the factor of the outputs lies in P and take)
 // One bf16 part of the faded y would put a second rounding beside that of S into every output, and 2^-9 into a state that is
 // returned: two parts where S is only an operand, three where the call returns a state.
 //
@@ -17,11 +16,13 @@
 // With give z written to shared memory in two parts (the first form of this kernel) there was room for two stages that a
 // block held to its end: 224 us for B8 H16 L4096 128/128.
 //
-// Warps: 0-3 scores (E = 128: and results), 4-7 feed (fades Y), 8-11 state, 12-15 results (E = 128: the state's columns 64 ..), 16 loads,
-// 17 products, 18 stores.
+// Warps: 0-3 scores, 4-7 feed (fades Y), 8-11 state, 12-15 results, then one each for loads, products and stores.  The groups' work
+// is counted in instructions and ways to tensor memory and back, 32 columns a time: with the state in registers, loads ahead of
+// stores, or unrolled loops that the instruction caches do not hold, a block took up to twice as long.
 #include <cuda_bf16.h>
 
 #include "decay.cuh"
+#include "pairs.cuh"
 #include "sm100.cuh"
 
 namespace based {
@@ -30,7 +31,7 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kT = kDecayBlockTc, kThreads = 608;
+constexpr int kT = kDecayBlockTc, kThreads = 640;
 constexpr int kWarpTma = 16, kWarpMma = 17, kWarpStore = 18;
 constexpr uint32_t kPanel = kT * 128;                                // 128 tokens x 64 columns, bf16: 16 KB
 
@@ -43,21 +44,24 @@ template <int DC, int E, bool STATES> struct Cfg {
     static constexpr uint32_t offS = offZ + kStages * kZ * kPanel;
     static constexpr uint32_t offUnit = offS + (STATES ? 0 : kZ * kSPanel);
     static constexpr uint32_t offBars = offUnit + 512;
-    static constexpr uint32_t offPow = offBars + 320;                // a^0 .. a^128
+    static constexpr uint32_t offPow = offBars + 352;                // a^0 .. a^128
     static constexpr uint32_t offGive = offPow + 528;
-    static constexpr uint32_t offNear = offGive + 512;               // a^(steps to the near end of 32 columns)
-    static constexpr uint32_t offPlaces = offNear + 128;
+    static constexpr uint32_t offPlaces = offGive + 512;
     static constexpr uint32_t kBytes = offPlaces + kStages * kT * 4;
     static_assert(kBytes <= 232448, "shared memory budget");
 };
-// TMEM columns: scores (P, and the third part of the faded y behind it), the turned y, O, dS
+// TMEM columns: scores (P, and the third part of the faded y behind it), the turned y, O, S
 constexpr uint32_t colX = 0, colY = 128, colO = 256;
+// Where there is room, two turned y in turn; where only states are wanted, two third parts too
+template <int E, bool STATES> constexpr bool kTwoY = STATES || E == 64;
+template <int E, bool STATES> __device__ __forceinline__ uint32_t col_y(int i) { return kTwoY<E, STATES> && (i & 1) ? (E == 128 ? colO : 384u) : colY; }
+template <bool STATES> __device__ __forceinline__ uint32_t col_third(int i) { return STATES ? colX + 64u * (i & 1) : colX + 64u; }
 
-// Rings: full and empty places of x, y, z.  One phase a block: bX, bP scores there, P written; bClean padding out of y, z; bTurn, bFeed y
-// turned, faded; bDS, bDSread; bS the state ahead of the block in shared memory; bXS, bTake x S there, faded; bO, bOread all of O
-// there, read; bOut the output in z's place.
-enum Bar { bFullX = 0, bFullY = 4, bFullZ = 8, bEmptyX = 12, bEmptyY = 16, bEmptyZ = 20, bX = 24, bP, bClean, bTurn, bFeed, bDS, bDSread, bS, bXS, bTake, bO, bOread, bOut, bCount };
-static_assert(bCount * 8 + 8 <= 320, "barrier area");
+// Rings: full and empty places of x, y, z, and the output in z's place.  One phase a block (bTurn, bFeed: of two in turn where there are two
+// turned y): bTurn, bFeed y turned, faded; bX, bP scores there, P written; bClean padding out of y, z; bDS the state behind the
+// block there; bS the state ahead of it in shared memory, and faded by the block in TMEM; bXS, bTake x S there, faded; bO, bOread all of O there, read.
+enum Bar { bFullX = 0, bFullY = 4, bFullZ = 8, bEmptyX = 12, bEmptyY = 16, bEmptyZ = 20, bOut = 24, bTurn = 28, bFeed = 30, bX = 32, bP, bClean, bDS, bS, bXS, bTake, bO, bOread, bCount };
+static_assert(bCount * 8 + 8 <= 352, "barrier area");
 
 struct alignas(64) Maps { CUtensorMap m[3][4]; };                    // [pass] x, y, z, out
 struct Args {
@@ -73,8 +77,52 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&v);
 }
-__device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ pairs::pair as_pair(uint32_t lo, uint32_t hi) { return pairs::make(__uint_as_float(lo), __uint_as_float(hi)); }
+// A row of y^T (one dimension's 128 tokens) in TMEM, every token faded: near[k] a^steps inside 16 tokens and a power more for each 16, or
+// `give` where the block is not a whole plain one; left as PARTS bf16 parts, 8 columns each behind one another (a third one at tx): all but the
+// last cut off, that one rounded.  32 tokens a turn: what takes time is the way to tensor memory and back, not the arithmetic (loads
+// ahead of the stores before them are no help: 680 cycles per 16 tokens for 370).
+template <int PARTS, bool WHOLE>
+__device__ __forceinline__ void feed_row(uint32_t ty, uint32_t tx, const pairs::pair (&near)[8], float rate2, bool back, const float* give) {
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        uint32_t x[32];
+        tmem_ld32(ty + c, x);
+        pairs::pair f2[2] = {0, 0};
+        if (WHOLE) {
+            f2[0] = pairs::both(exp2f(-rate2 * (float)(back ? c + 1 : 112 - c)));
+            f2[1] = pairs::both(exp2f(-rate2 * (float)(back ? c + 17 : 96 - c)));
+        }
+        tmem_wait_ld();
+        uint32_t out[32];                                            // (hi, lo) of 16 tokens, (hi, lo) of the next
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            pairs::pair q;
+            if constexpr (WHOLE) q = pairs::mul2(f2[k >> 3], near[k & 7]);
+            else q = *reinterpret_cast<const pairs::pair*>(give + c + 2 * k);
+            const float2 v = pairs::split(pairs::mul2(pairs::make(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), q));
+            const uint32_t a = __float_as_uint(v.x), b = __float_as_uint(v.y);
+            const int at = (k >> 3) * 16 + (k & 7);
+            out[at] = __byte_perm(a, b, 0x7632);
+            const float y0 = v.x - __uint_as_float(a & 0xffff0000u), y1 = v.y - __uint_as_float(b & 0xffff0000u);
+            if constexpr (PARTS == 2) {
+                out[at + 8] = pack2(y0, y1);
+            } else {
+                const uint32_t l0 = __float_as_uint(y0), l1 = __float_as_uint(y1);
+                out[at + 8] = __byte_perm(l0, l1, 0x7632);
+                x[k] = pack2(y0 - __uint_as_float(l0 & 0xffff0000u), y1 - __uint_as_float(l1 & 0xffff0000u));
+            }
+        }
+        tmem_st32(ty + c, out);
+        if constexpr (PARTS == 3) {
+            uint32_t third[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) third[k] = x[k];
+            tmem_st16(tx + c / 2, third);
+        }
+    }
+    tmem_wait_st();
+}
 // barrier of a group of 128 threads that also tells whether all of them say yes
 __device__ __forceinline__ bool group_all(int id, bool pred) {
     uint32_t r;
@@ -95,6 +143,7 @@ template <int DC, int E, bool STATES, bool DOCS>
 __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
     using C = Cfg<DC, E, STATES>;
     constexpr int NS = C::kStages;
+    constexpr bool kTwo = kTwoY<E, STATES>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
     uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(bars + bCount);
@@ -114,9 +163,8 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
 
     if (tid == 0) {
         for (int s = 0; s < bCount; ++s) {
-            const bool groups = s == bDSread || s == bS;             // as many groups as the state has
-            const bool group = s == bP || s == bClean || s == bFeed || s == bTake || s == bOread || s == bOut;
-            mbar_init(&bars[s], groups ? 128 * C::kZ : group ? 128 : 1);
+            const bool group = s == bP || s == bClean || (s >= bFeed && s < bFeed + 2) || s == bS || s == bTake || s == bOread || (s >= bOut && s < bOut + 4);
+            mbar_init(&bars[s], group ? 128 : 1);
         }
         *abort_flag = 0;
         fence_mbar_init();
@@ -133,7 +181,6 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
     enter_dependent();
     const float rate2 = a.c.rate[h] * kLog2e;
     if (tid <= kT) pw[tid] = faded(rate2, tid);
-    if (tid < 32) reinterpret_cast<float*>(smem + C::offNear)[tid] = faded(rate2, back ? tid : 31 - tid);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -165,6 +212,36 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         cut = from > 0;
         if (!back) first += from;
         count -= from;
+    }
+    // Blocks of padding alone at either end: nothing but zeros to write
+    int lead_in = 0, lead_out = 0;                                   // so many from `first` on, so many behind
+    if (DOCS) {
+        for (int i = 0; i < count; i += 32) {
+            const uint32_t m = __ballot_sync(0xffffffffu, i + lane < count && place_count(end_of(first + i + lane)) != 0);
+            if (m) {
+                lead_in = i + __ffs(m) - 1;
+                break;
+            }
+            lead_in = count;
+        }
+        for (int i = count; i > lead_in; i -= 32) {
+            const uint32_t m = __ballot_sync(0xffffffffu, i - 1 - lane >= lead_in && place_count(end_of(first + i - 1 - lane)) != 0);
+            if (m) {
+                lead_out = count - (i - (__ffs(m) - 1));
+                break;
+            }
+        }
+        first += lead_in;
+        count -= lead_in + lead_out;
+        if (!STATES && lead_in + lead_out > 0 && warp >= 12 && warp < 16) {
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(const_cast<void*>(p.out.data)) + b * p.out.batch_stride + h * p.out.head_stride + e0;
+            const int chunks = min(E, p.de - e0) / 8;
+            for (int part = 0; part < 2; ++part) {
+                const int t0 = (part ? first + count : first - lead_in) * kT, t1 = min(t0 + (part ? lead_out : lead_in) * kT, L);
+                for (long long k = tid & 127; k < (long long)(t1 - t0) * chunks; k += 128)
+                    *reinterpret_cast<uint4*>(out + (t0 + k / chunks) * p.out.token_stride + k % chunks * 8) = make_uint4(0, 0, 0, 0);
+            }
+        }
     }
     auto block_of = [&](int i) { return back ? first + count - 1 - i : first + i; };
     auto wait = [&](int bar, int phase) -> bool { return __all_sync(0xffffffffu, mbar_wait(&bars[bar], phase & 1, abort_flag)); };
@@ -200,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         if (!STATES && lane == 0) {
             for (int i = 0; i < count; ++i) {
                 const int s = i % NS;
-                ok = mbar_wait(&bars[bOut], i & 1, abort_flag);
+                ok = mbar_wait(&bars[bOut + s], (i / NS) & 1, abort_flag);
                 if (!ok) break;
 #pragma unroll
                 for (int j = 0; j < C::kZ; ++j)
@@ -220,277 +297,362 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         constexpr uint64_t dS = make_smem_desc_base(C::kSPanel, 1024, kSwizzle128B);
         constexpr uint64_t dU = make_smem_desc_base(16, 256, kSwizzle32B);               // K-major [16][16]
         constexpr uint32_t iX = make_idesc_bf16(128, 128, 0, 0), iT = make_idesc_bf16(128, 16, 1, 0), iO = make_idesc_bf16(128, E, 0, 1);
-        constexpr uint32_t colDS = colO + E;
+        constexpr uint32_t colS = colO + E;
         const uint32_t sm = smem_u32(smem);
         auto lo = [](uint64_t base, uint32_t addr) { return desc_lo(base) + (addr >> 4); };
-#pragma unroll 1
-        for (int i = 0; i < count && ok; ++i) {
-            const int s = i % NS, turn = i / NS;
-            const uint32_t y = sm + C::offY + s * C::kX * kPanel;
-            const uint32_t lx = lo(dK, sm + s * C::kX * kPanel), ly = lo(dK, y), lz = lo(dZ, sm + C::offZ + s * C::kZ * kPanel);
-            ok = wait(bFullY + s, turn) && (STATES || wait(bFullX + s, turn));
-            if (!ok) break;
+        auto x_of = [&](int i) { return lo(dK, sm + (i % NS) * C::kX * kPanel); };
+        auto y_of = [&](int i) { return sm + C::offY + (i % NS) * C::kX * kPanel; };
+        auto z_of = [&](int i) { return lo(dZ, sm + C::offZ + (i % NS) * C::kZ * kPanel); };
+        // y^T; products have 128 rows: those past the dimensions of a narrow y hold what lies behind it, and nobody reads them
+        auto turn = [&](int i) -> bool {
+            if (!wait(bFullY + i % NS, i / NS) || (DOCS && !wait(bClean, i))) return false;
             tc_fence_after();
-            if (!STATES) {
+            const uint32_t lt = lo(dZ, y_of(i)), lu = lo(dU, sm + C::offUnit), d = tb + col_y<E, STATES>(i);
 #pragma unroll
-                for (int k = 0; k < DC / 16; ++k) {
-                    const uint32_t at = (k >> 2) * (kPanel >> 4) + (k & 3) * 2;
-                    if (k == 0) mma_ss_w<false>(lead, tb + colX, lx, desc_hi(dK), ly, desc_hi(dK), iX);
-                    else mma_ss_w<true>(lead, tb + colX, lx + at, desc_hi(dK), ly + at, desc_hi(dK), iX);
-                }
-                mma_commit_w(lead, &bars[bX]);
-            }
-            if (DOCS) {
-                ok = wait(bClean, i);
-                if (!ok) break;
-                tc_fence_after();
-            }
-            {   // (products have 128 rows: those past the dimensions of a narrow y hold what lies behind it, and nobody reads them)
-                const uint32_t lt = lo(dZ, y);
-                const uint32_t lu = lo(dU, sm + C::offUnit);
-#pragma unroll
-                for (int k = 0; k < kT / 16; ++k) mma_ss_w<false>(lead, tb + colY + 16 * k, lt + k * 128, desc_hi(dZ), lu, desc_hi(dU), iT);
-                mma_commit_w(lead, &bars[bTurn]);
-                mma_commit_w(lead, &bars[bEmptyY + s]);
-            }
-            if (!STATES) {
-                ok = wait(bS, i) && (i == 0 || wait(bOread, i - 1));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t ls = lo(dS, sm + C::offS);
-#pragma unroll
-                for (int k = 0; k < DC / 16; ++k) {
-                    const uint32_t at = (k >> 2) * (kPanel >> 4) + (k & 3) * 2;
-                    if (k == 0) mma_ss_w<false>(lead, tb + colO, lx, desc_hi(dK), ls, desc_hi(dS), iO);
-                    else mma_ss_w<true>(lead, tb + colO, lx + at, desc_hi(dK), ls + k * 128, desc_hi(dS), iO);
-                }
-                mma_commit_w(lead, &bars[bXS]);
-                mma_commit_w(lead, &bars[bEmptyX + s]);
-            }
-            ok = wait(bFullZ + s, turn) && wait(bFeed, i) && (i == 0 || wait(bDSread, i - 1));
-            if (!ok) break;
+            for (int k = 0; k < kT / 16; ++k) mma_ss_w<false>(lead, d + 16 * k, lt + k * 128, desc_hi(dZ), lu, desc_hi(dU), iT);
+            mma_commit_w(lead, &bars[bTurn + (kTwo ? i & 1 : 0)]);
+            if (STATES) mma_commit_w(lead, &bars[bEmptyY + i % NS]);
+            return true;
+        };
+        auto delta = [&](int i) -> bool {
+            if (!wait(bFullZ + i % NS, i / NS) || !wait(bFeed + (kTwo ? i & 1 : 0), kTwo ? i >> 1 : i) || !wait(bS, i)) return false;
             tc_fence_after();
+            const uint32_t lz = z_of(i), ty = tb + col_y<E, STATES>(i);
 #pragma unroll
             for (int k = 0; k < kT / 16; ++k) {
-                const uint32_t at = colY + 32 * (k >> 1) + 8 * (k & 1);
-                if (k == 0) mma_ts_w<false>(lead, tb + colDS, tb + at, lz, desc_hi(dZ), iO);
-                else mma_ts_w<true>(lead, tb + colDS, tb + at, lz + k * 128, desc_hi(dZ), iO);
-                mma_ts_w<true>(lead, tb + colDS, tb + at + 16, lz + k * 128, desc_hi(dZ), iO);
+                const uint32_t at = ty + 16 * k;
+                mma_ts_w<true>(lead, tb + colS, at, lz + k * 128, desc_hi(dZ), iO);
+                mma_ts_w<true>(lead, tb + colS, at + 8, lz + k * 128, desc_hi(dZ), iO);
             }
             if (a.parts == 3) {
+                const uint32_t t3 = tb + col_third<STATES>(i);
 #pragma unroll
-                for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, tb + colDS, tb + colX + 64 + 8 * k, lz + k * 128, desc_hi(dZ), iO);
+                for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, tb + colS, t3 + 8 * k, lz + k * 128, desc_hi(dZ), iO);
             }
             mma_commit_w(lead, &bars[bDS]);
-            if (STATES) {
-                mma_commit_w(lead, &bars[bEmptyZ + s]);
-            } else {
-                ok = wait(bP, i) && wait(bTake, i);
-                if (!ok) break;
-                tc_fence_after();
+            if (STATES) mma_commit_w(lead, &bars[bEmptyZ + i % NS]);
+            return true;
+        };
+        auto scores = [&](int i) -> bool {
+            if (!wait(bFullX + i % NS, i / NS)) return false;
+            tc_fence_after();
+            const uint32_t lx = x_of(i), ly = lo(dK, y_of(i));
 #pragma unroll
-                for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, tb + colO, tb + colX + k * 8, lz + k * 128, desc_hi(dZ), iO);
-                mma_commit_w(lead, &bars[bO]);
+            for (int k = 0; k < DC / 16; ++k) {
+                const uint32_t at = (k >> 2) * (kPanel >> 4) + (k & 3) * 2;
+                if (k == 0) mma_ss_w<false>(lead, tb + colX, lx, desc_hi(dK), ly, desc_hi(dK), iX);
+                else mma_ss_w<true>(lead, tb + colX, lx + at, desc_hi(dK), ly + at, desc_hi(dK), iX);
+            }
+            mma_commit_w(lead, &bars[bX]);
+            mma_commit_w(lead, &bars[bEmptyY + i % NS]);
+            return true;
+        };
+        auto before = [&](int i) -> bool {
+            if (!wait(bS, i) || (i > 0 && !wait(bOread, i - 1))) return false;
+            tc_fence_after();
+            const uint32_t lx = x_of(i), ls = lo(dS, sm + C::offS);
+#pragma unroll
+            for (int k = 0; k < DC / 16; ++k) {
+                const uint32_t at = (k >> 2) * (kPanel >> 4) + (k & 3) * 2;
+                if (k == 0) mma_ss_w<false>(lead, tb + colO, lx, desc_hi(dK), ls, desc_hi(dS), iO);
+                else mma_ss_w<true>(lead, tb + colO, lx + at, desc_hi(dK), ls + k * 128, desc_hi(dS), iO);
+            }
+            mma_commit_w(lead, &bars[bXS]);
+            mma_commit_w(lead, &bars[bEmptyX + i % NS]);
+            return true;
+        };
+        auto inside = [&](int i) -> bool {
+            if (!wait(bP, i) || !wait(bTake, i)) return false;
+            tc_fence_after();
+            const uint32_t lz = z_of(i);
+#pragma unroll
+            for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, tb + colO, tb + colX + k * 8, lz + k * 128, desc_hi(dZ), iO);
+            mma_commit_w(lead, &bars[bO]);
+            return true;
+        };
+        // Products run in the order of their issue, so one that overwrites what one before it reads waits for nobody.
+        if (count == 0) {
+        } else if constexpr (STATES) {
+            ok = turn(0);
+#pragma unroll 1
+            for (int i = 0; i < count && ok; ++i) ok = (i + 1 == count || turn(i + 1)) && delta(i);
+        } else {
+            ok = turn(0) && scores(0) && before(0);
+#pragma unroll 1
+            for (int i = 0; i < count && ok; ++i) {
+                const bool more = i + 1 < count;
+                if (kTwo) ok = (!more || turn(i + 1)) && delta(i) && inside(i);
+                else ok = delta(i) && (!more || turn(i + 1)) && inside(i);
+                if (more && ok) ok = scores(i + 1) && before(i + 1);
             }
         }
-    } else if (warp < 4 || (E == 64 && warp >= 12 && warp < 16)) {
-        // ---- scores and results: thread = row of the block, TMEM lane; two groups where there is one to spare
+    } else if (warp < 4) {
+        // ---- scores: thread = row of the block, TMEM lane
         if constexpr (!STATES) {
-            const bool do_scores = warp < 4, do_results = E == 128 || warp >= 12;
-            const int w = warp & 3, r = 32 * w + lane;
+            const int w = warp, r = tid;
             const uint32_t tl = tmem_addr(tb, (uint32_t)w * 32u, 0);
-            const float* near = reinterpret_cast<const float*>(smem + C::offNear);
-            const uint32_t sw = r & 7;
             const float factor = a.c.factor;
+            // a^steps from column k of 16 to the end that is nearer to rows outside, and factor a^steps to a row among the 16 (0: the row does
+            // not see it), in registers: a load from shared memory takes long while the products read it all the time
+            pairs::pair near[8], among[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int l = lane & 15, j = 2 * k, s0 = back ? j - l : l - j, s1 = back ? j + 1 - l : l - j - 1;
+                near[k] = pairs::make(faded(rate2, back ? j : 15 - j), faded(rate2, back ? j + 1 : 14 - j));
+                among[k] = pairs::make(s0 >= 0 ? factor * faded(rate2, s0) : 0.f, s1 >= 0 ? factor * faded(rate2, s1) : 0.f);
+            }
             for (int i = 0; i < count; ++i) {
                 const int n = block_of(i), s = i % NS;
                 const uint32_t end = end_of(n);
                 const bool simple = plain(end, n);
                 const uint32_t own = DOCS && !simple ? places_of(n)[r] : 0u;
-                if (do_scores) {
-                    const uint32_t* pl = reinterpret_cast<const uint32_t*>(smem + C::offPlaces + s * kT * 4);
-                    ok = wait(bX, i) && (simple || wait(bFullZ + s, i / NS));      // (the places come with z)
-                    if (!ok) break;
-                    tc_fence_after();
+                const uint32_t* pl = reinterpret_cast<const uint32_t*>(smem + C::offPlaces + s * kT * 4);
+                ok = wait(bX, i) && (simple || (end & kCompact) || wait(bFullZ + s, i / NS));      // (the places come with z)
+                if (!ok) break;
+                tc_fence_after();
+                // 32 columns a time; P goes over columns that this row has read, or does not need
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {                    // 32 columns a time
-                        uint32_t pk[16];
-                        if (back ? c < w : c > w) {
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pk[16];
+                    if (back ? c < w : c > w) {
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) pk[k] = 0u;
-                        } else {
-                            uint32_t x[32];
-                            tmem_ld32(tl + colX + 32 * c, x);
+                        for (int k = 0; k < 16; ++k) pk[k] = 0u;
+                    } else {
+                        uint32_t v[32];
+                        tmem_ld32(tl + colX + 32 * c, v);
+                        if (!DOCS || simple || (end & kCompact)) {
+                            const int steps = back ? 32 * c - r : r - 32 * c - 15;             // to the nearer end of the first 16 columns
+                            pairs::pair f0 = pairs::both(factor * exp2f(-rate2 * (float)steps)), f1 = pairs::both(factor * exp2f(-rate2 * (float)(back ? steps + 16 : steps - 16)));
                             tmem_wait_ld();
-                            if (simple) {
-                                if (c == w) {
+                            if (c != w) {
 #pragma unroll
-                                    for (int k = 0; k < 32; ++k) {
-                                        const int steps = back ? k - lane : lane - k;
-                                        x[k] = steps >= 0 ? __float_as_uint(__uint_as_float(x[k]) * pw[steps]) : 0u;
-                                    }
-                                } else {                             // steps from the row to the nearer end of the columns, and on from there
-                                    const float f = pw[back ? 32 * c - r : r - 32 * c - 31];
-#pragma unroll
-                                    for (int k = 0; k < 32; k += 4) {
-                                        const float4 q = *reinterpret_cast<const float4*>(near + k);
-                                        x[k] = __float_as_uint(__uint_as_float(x[k]) * f * q.x);
-                                        x[k + 1] = __float_as_uint(__uint_as_float(x[k + 1]) * f * q.y);
-                                        x[k + 2] = __float_as_uint(__uint_as_float(x[k + 2]) * f * q.z);
-                                        x[k + 3] = __float_as_uint(__uint_as_float(x[k + 3]) * f * q.w);
-                                    }
+                                for (int k = 0; k < 16; ++k) {
+                                    const float2 y = pairs::split(pairs::mul2(as_pair(v[2 * k], v[2 * k + 1]), pairs::mul2(k < 8 ? f0 : f1, near[k & 7])));
+                                    pk[k] = pack2(y.x, y.y);
                                 }
-                            } else {
+                            } else {                                 // of either 16 the row is one, or it sees them all, or none
+                                const bool high = lane >= 16;
+                                if (back ? high : !high) f0 = f1 = 0;
+                                if (back) f0 = 0;
+                                else f1 = 0;
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) {
-                                    const uint32_t q = pl[32 * c + k];
-                                    const int steps = back ? place_count(q) - place_count(own) : place_count(own) - place_count(q);
-                                    const bool seen = ((q ^ own) & (kPadding | 0xff00u)) == 0 && !(own & kPadding) && (c != w || (back ? k >= lane : k <= lane));
-                                    x[k] = seen ? __float_as_uint(__uint_as_float(x[k]) * pw[max(steps, 0)]) : 0u;
+                                for (int k = 0; k < 16; ++k) {
+                                    const pairs::pair t = pairs::mul2(k < 8 ? f0 : f1, near[k & 7]);
+                                    const float2 y = pairs::split(pairs::mul2(as_pair(v[2 * k], v[2 * k + 1]), high == (k >= 8) ? among[k & 7] : t));
+                                    pk[k] = pack2(y.x, y.y);
                                 }
                             }
+                            if (DOCS && !simple) {                   // the row's document alone: columns lo .. hi of these 32, two a register
+                                const int lo = own & kPadding ? 32 : (back ? 0 : max(place_from(own) - 32 * c, 0)), hi = back ? min(place_to(own) - 32 * c, 31) : 31;
+                                const uint32_t m = lo > hi ? 0u : (0xffffffffu >> (31 - hi)) & (0xffffffffu << lo);
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) pk[k] = pack2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
+                                for (int k = 0; k < 16; ++k) {
+                                    if (!((m >> (2 * k)) & 1u)) pk[k] &= 0xffff0000u;
+                                    if (!((m >> (2 * k + 1)) & 1u)) pk[k] &= 0x0000ffffu;
+                                }
+                            }
+                        } else {
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                const uint32_t q = pl[32 * c + k];
+                                const int steps = back ? place_count(q) - place_count(own) : place_count(own) - place_count(q);
+                                const bool seen = ((q ^ own) & (kPadding | 0xff00u)) == 0 && !(own & kPadding) && (c != w || (back ? k >= lane : k <= lane));
+                                const float f = pw[max(steps, 0)] * factor;
+                                v[k] = seen ? __float_as_uint(__uint_as_float(v[k]) * f) : 0u;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) pk[k] = pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
                         }
-                        tmem_st16(tl + colX + 16 * c, pk);           // (over columns that this row has read, or does not need)
                     }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(&bars[bP]);
+                    tmem_st16(tl + colX + 16 * c, pk);
                 }
-                if (do_results) {
-                    float take;
-                    if (simple) take = back ? pw[max(place_count(end) - 1 - r, 0)] : pw[r + 1];
-                    else
-                        take = own & kPadding ? 0.f
-                               : back         ? (place_run(own) == place_run(end) ? pw[place_count(end) - place_count(own)] : 0.f)
-                                              : (place_run(own) == 0 ? pw[place_count(own)] : 0.f);
-                    ok = wait(bXS, i);
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int c = 0; c < E; c += 32) {
-                        uint32_t x[32];
-                        tmem_ld32(tl + colO + c, x);
-                        tmem_wait_ld();
-                        // (no product with a weight of 0: there the state's share need not be finite)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] = take == 0.f ? 0u : __float_as_uint(__uint_as_float(x[k]) * take);
-                        tmem_st32(tl + colO + c, x);
-                    }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(&bars[bTake]);
-                    ok = wait(bO, i);
-                    if (!ok) break;
-                    tc_fence_after();
-                    uint8_t* row = smem + C::offZ + s * C::kZ * kPanel + r * 128;
-#pragma unroll 1
-                    for (int c = 0; c < E; c += 32) {
-                        uint32_t x[32];
-                        tmem_ld32(tl + colO + c, x);
-                        tmem_wait_ld();
-                        if (c + 32 == E) {
-                            tc_fence_before();
-                            mbar_arrive(&bars[bOread]);
-                        }
-                        uint8_t* panel = row + (c >> 6) * kPanel;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t v[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(x[8 * j + 2 * k]) * factor, __uint_as_float(x[8 * j + 2 * k + 1]) * factor);
-                            *reinterpret_cast<uint4*>(panel + (((uint32_t)((c & 32) / 8 + j) ^ sw) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                        }
-                    }
-                    fence_proxy_async_smem();
-                    mbar_arrive(&bars[bOut]);
-                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&bars[bP]);
             }
         }
-    } else if (warp >= 8 && warp < 16) {
-        // ---- state: thread = row of the state, TMEM lane, 64 of its columns
-        const int w = warp & 3, c = 32 * w + lane, at = warp < 12 ? 0 : 64, e1 = e0 + at;
+    } else if (warp >= 8 && warp < 12) {
+        // ---- state: thread = row of the state, TMEM lane
+        const int w = warp & 3, c = 32 * w + lane;
         const bool rows = w * 32 < DC;                               // (the whole warp's)
-        float s[64];
-#pragma unroll
-        for (int e = 0; e < 64; ++e) s[e] = 0.f;
-        if (!STATES && rows) {
-            if (p.state_in && c < p.dc) {
-                const float* in = p.state_in + it.head * p.dc * p.de;
-#pragma unroll
-                for (int e = 0; e < 64; ++e)
-                    if (e1 + e < p.de) s[e] = p.in_factor * in[p.turned ? (long long)(e1 + e) * p.dc + c : (long long)c * p.de + e1 + e];
-            }
-            for (int k = 0; k < it.segment; ++k) {
-                const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, k);
-                const float f = a.factors[slot];
-                const float4* from = reinterpret_cast<const float4*>(a.states + (slot * kDecayMaxWidth + c) * E + at);
-#pragma unroll
-                for (int e = 0; e < 64; e += 4) {
-                    const float4 x = from[e / 4];
-                    s[e] = fmaf(f, s[e], x.x);
-                    s[e + 1] = fmaf(f, s[e + 1], x.y);
-                    s[e + 2] = fmaf(f, s[e + 2], x.z);
-                    s[e + 3] = fmaf(f, s[e + 3], x.w);
-                }
-            }
-        }
-        auto to_shared = [&] {
-            if (rows) {
-                uint8_t* row = smem + C::offS + (at >> 6) * C::kSPanel + c * 128;
+        const uint32_t ts = tmem_addr(tb, (uint32_t)w * 32u, colO + E);
+        auto fade_of = [&](int i) -> float {
+            if (i >= count) return 1.f;
+            const uint32_t end = end_of(block_of(i));
+            return place_run(end) == 0 ? pw[place_count(end)] : 0.f;
+        };
+        // 32 columns of the state to shared memory in bf16, and back to TMEM faded by the next block (0: dropped, whatever it holds)
+        auto pass_on = [&](int e, uint32_t(&x)[32], float f) {
+            if (!STATES) {
+                uint8_t* row = smem + C::offS + (e >> 6) * C::kSPanel + c * 128;
                 const uint32_t sw = c & 7;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<uint4*>(row + (((uint32_t)j ^ sw) << 4)) =
-                        make_uint4(pack2(s[8 * j], s[8 * j + 1]), pack2(s[8 * j + 2], s[8 * j + 3]), pack2(s[8 * j + 4], s[8 * j + 5]),
-                                   pack2(s[8 * j + 6], s[8 * j + 7]));
-                fence_proxy_async_smem();
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(x[8 * j + 2 * k]), __uint_as_float(x[8 * j + 2 * k + 1]));
+                    *reinterpret_cast<uint4*>(row + (((uint32_t)((e & 32) / 8 + j) ^ sw) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                }
             }
+            if (f == 0.f) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) x[k] = 0u;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+            }
+            tmem_st32(ts + e, x);
+        };
+        auto passed_on = [&] {
+            tmem_wait_st();
+            fence_proxy_async_smem();
+            tc_fence_before();
             mbar_arrive(&bars[bS]);
         };
-        if (!STATES) to_shared();
+        const float* in = p.state_in ? p.state_in + it.head * p.dc * p.de : nullptr;
+        if (rows) {
+            const float f = fade_of(0);
+#pragma unroll 1
+            for (int e = 0; e < E; e += 32) {
+                uint32_t x[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) x[k] = 0u;
+                if (!STATES) {
+                    if (in && c < p.dc) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (e0 + e + k < p.de)
+                                x[k] = __float_as_uint(p.in_factor * in[p.turned ? (long long)(e0 + e + k) * p.dc + c : (long long)c * p.de + e0 + e + k]);
+                    }
+#pragma unroll 1
+                    for (int q = 0; q < it.segment; ++q) {
+                        const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, q);
+                        const float g = a.factors[slot];
+                        const float4* from = reinterpret_cast<const float4*>(a.states + (slot * kDecayMaxWidth + c) * E + e);
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) {
+                            const float4 y = from[k / 4];
+                            const float ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[k + j] = __float_as_uint(g == 0.f ? ys[j] : fmaf(g, __uint_as_float(x[k + j]), ys[j]));
+                        }
+                    }
+                }
+                pass_on(e, x, f);
+            }
+        }
+        passed_on();
         float whole = cut ? 0.f : 1.f;
         for (int i = 0; i < count; ++i) {
-            const uint32_t end = end_of(block_of(i));
-            const float f = place_run(end) == 0 ? pw[place_count(end)] : 0.f;
+            const float f = fade_of(i + 1);
+            whole *= fade_of(i);
             ok = wait(bDS, i);
             if (!ok) break;
             tc_fence_after();
-            if (rows) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t x[16];
-                    tmem_ld16(tmem_addr(tb, (uint32_t)w * 32u, colO + E + at + 16 * q), x);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[16 * q + e] = fmaf(f, s[16 * q + e], __uint_as_float(x[e]));
+            if (i + 1 < count) {                                     // (this product comes behind x S in order: the state ahead has been read)
+                if (rows) {
+#pragma unroll 1
+                    for (int e = 0; e < E; e += 32) {
+                        uint32_t x[32];
+                        tmem_ld32(ts + e, x);
+                        tmem_wait_ld();
+                        pass_on(e, x, f);
+                    }
                 }
+                passed_on();
             }
-            whole *= f;
-            tc_fence_before();
-            mbar_arrive(&bars[bDSread]);
-            if (!STATES && i + 1 < count) to_shared();               // (dS comes behind x S in order: the state before has been read)
         }
         if (ok && rows) {
-            if (STATES) {
-                const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, it.segment);
-                float4* to = reinterpret_cast<float4*>(a.states + (slot * kDecayMaxWidth + c) * E + at);
+            float* out = !STATES && p.state_out && it.segment == a.segments - 1 && c < p.dc ? p.state_out + it.head * p.dc * p.de : nullptr;
+            const long long slot = STATES ? decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, it.segment) : 0;
+            if (STATES || p.state_out) {
+#pragma unroll 1
+                for (int e = 0; e < E; e += 32) {
+                    uint32_t x[32];
+                    tmem_ld32(ts + e, x);
+                    tmem_wait_ld();
+                    if (STATES) {
+                        uint4* to = reinterpret_cast<uint4*>(a.states + (slot * kDecayMaxWidth + c) * E + e);
 #pragma unroll
-                for (int e = 0; e < 64; e += 4) to[e / 4] = make_float4(s[e], s[e + 1], s[e + 2], s[e + 3]);
-                if (c == 0 && at == 0) a.factors[slot] = whole;
-            } else if (p.state_out && it.segment == a.segments - 1 && c < p.dc) {
-                float* to = p.state_out + it.head * p.dc * p.de;
+                        for (int k = 0; k < 8; ++k) to[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                    } else if (out) {
 #pragma unroll
-                for (int e = 0; e < 64; ++e)
-                    if (e1 + e < p.de) to[p.turned ? (long long)(e1 + e) * p.dc + c : (long long)c * p.de + e1 + e] = p.out_factor * s[e];
+                        for (int k = 0; k < 32; ++k)
+                            if (e0 + e + k < p.de)
+                                out[p.turned ? (long long)(e0 + e + k) * p.dc + c : (long long)c * p.de + e0 + e + k] = p.out_factor * __uint_as_float(x[k]);
+                    }
+                }
+            }
+            if (STATES && c == 0) a.factors[slot] = whole;
+        }
+    } else if (warp >= 12 && warp < 16) {
+        // ---- results: thread = row of the block, TMEM lane
+        if constexpr (!STATES) {
+            const int w = warp & 3, r = 32 * w + lane;
+            const uint32_t to = tmem_addr(tb, (uint32_t)w * 32u, colO), sw = r & 7;
+            for (int i = 0; i < count; ++i) {
+                const int n = block_of(i), s = i % NS;
+                const uint32_t end = end_of(n);
+                float take;
+                if (plain(end, n)) {
+                    take = pw[back ? max(place_count(end) - 1 - r, 0) : r + 1];
+                } else {
+                    const uint32_t own = places_of(n)[r];
+                    take = own & kPadding ? 0.f
+                           : back         ? (place_run(own) == place_run(end) ? pw[place_count(end) - place_count(own)] : 0.f)
+                                          : (place_run(own) == 0 ? pw[place_count(own)] : 0.f);
+                }
+                const bool all = __all_sync(0xffffffffu, take != 0.f);
+                take *= a.c.factor;
+                ok = wait(bXS, i);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int e = 0; e < E; e += 32) {
+                    uint32_t x[32];
+                    tmem_ld32(to + e, x);
+                    tmem_wait_ld();
+                    if (all) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * take);
+                    } else {                                         // (no product with a weight of 0: there the state's share need not be finite)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = take == 0.f ? 0u : __float_as_uint(__uint_as_float(x[k]) * take);
+                    }
+                    tmem_st32(to + e, x);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&bars[bTake]);
+                ok = wait(bO, i);
+                if (!ok) break;
+                tc_fence_after();
+                uint8_t* row = smem + C::offZ + s * C::kZ * kPanel + r * 128;
+                // all of it out of tensor memory first: the next block's products wait for that
+                uint32_t v[E / 2];
+#pragma unroll
+                for (int e = 0; e < E; e += 16) {
+                    uint32_t x[16];
+                    tmem_ld16(to + e, x);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[e / 2 + k] = pack2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
+                }
+                tc_fence_before();
+                mbar_arrive(&bars[bOread]);
+#pragma unroll
+                for (int j = 0; j < E / 8; ++j)
+                    *reinterpret_cast<uint4*>(row + (j >> 3) * kPanel + (((uint32_t)(j & 7) ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                fence_proxy_async_smem();
+                mbar_arrive(&bars[bOut + s]);
             }
         }
     } else if (warp >= 4 && warp < 8) {
         // ---- feed: thread = dimension of y, TMEM lane; its tokens faded, in bf16 parts over themselves
         const int w = warp & 3, u = tid & 127;
         const bool rows = w * 32 < DC;                               // (the whole warp's)
-        const uint32_t ty = tmem_addr(tb, (uint32_t)w * 32u, colY), tx = tmem_addr(tb, (uint32_t)w * 32u, colX + 64);
+        const uint32_t tl = tmem_addr(tb, (uint32_t)w * 32u, 0);
         float* give = reinterpret_cast<float*>(smem + C::offGive);
         // rows of padding out of y and z
         auto clean = [&](int i) -> bool {
@@ -513,19 +675,26 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             mbar_arrive(&bars[bClean]);
             return true;
         };
-        if (DOCS) ok = clean(0);
-        int held = 0;                                                // what `give` holds: 1 a whole plain block's weights
+        if (DOCS && count > 0) ok = clean(0);
+        pairs::pair near[8];                                         // a^steps from token k of 16 to the end that is nearer to where the state goes
+#pragma unroll
+        for (int k = 0; k < 8; ++k) near[k] = pairs::make(faded(rate2, back ? 2 * k : 15 - 2 * k), faded(rate2, back ? 2 * k + 1 : 14 - 2 * k));
         for (int i = 0; i < count; ++i) {
             const int n = block_of(i);
             const uint32_t end = end_of(n);
             const int c1 = place_count(end);
             const bool simple = plain(end, n), whole = simple && c1 == kT;
             // (the third part goes where scores were that P does not need)
-            ok = ok && mbar_wait(&bars[bTurn], i & 1, abort_flag);
+            ok = ok && mbar_wait(&bars[bTurn + (kTwo ? i & 1 : 0)], (kTwo ? i >> 1 : i) & 1, abort_flag);
             if (!STATES && a.parts == 3) ok = ok && mbar_wait(&bars[bP], i & 1, abort_flag);
             ok = group_all(1, ok);
             if (!ok) break;
-            if (!whole || !held) {
+            // (the next block's, once the products are past the wait for this one's)
+            if (DOCS && i + 1 < count) {
+                ok = group_all(1, clean(i + 1));
+                if (!ok) break;
+            }
+            if (!whole) {
                 float x;
                 if (simple) {
                     x = u < c1 ? pw[back ? u + 1 : c1 - 1 - u] : 0.f;
@@ -536,43 +705,21 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                                      : (place_run(q) == place_run(end) ? pw[c1 - place_count(q)] : 0.f);
                 }
                 give[u] = x;
-                held = whole;
                 group_all(1, true);
             }
             tc_fence_after();
             if (rows) {
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {                        // 32 tokens a time
-                    uint32_t x[32], hi[16], lo[16];
-                    tmem_ld32(ty + 32 * c, x);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int k = 0; k < 32; k += 4) {
-                        const float4 q = *reinterpret_cast<const float4*>(give + 32 * c + k);
-                        const float x0 = __uint_as_float(x[k]) * q.x, x1 = __uint_as_float(x[k + 1]) * q.y, x2 = __uint_as_float(x[k + 2]) * q.z,
-                                    x3 = __uint_as_float(x[k + 3]) * q.w;
-                        hi[k / 2] = pack2(x0, x1);
-                        hi[k / 2 + 1] = pack2(x2, x3);
-                        const float y0 = x0 - lo_f32(hi[k / 2]), y1 = x1 - hi_f32(hi[k / 2]), y2 = x2 - lo_f32(hi[k / 2 + 1]), y3 = x3 - hi_f32(hi[k / 2 + 1]);
-                        lo[k / 2] = pack2(y0, y1);
-                        lo[k / 2 + 1] = pack2(y2, y3);
-                        x[k / 2] = pack2(y0 - lo_f32(lo[k / 2]), y1 - hi_f32(lo[k / 2]));
-                        x[k / 2 + 1] = pack2(y2 - lo_f32(lo[k / 2 + 1]), y3 - hi_f32(lo[k / 2 + 1]));
-                    }
-                    tmem_st16(ty + 32 * c, hi);
-                    tmem_st16(ty + 32 * c + 16, lo);
-                    if (a.parts == 3) {
-                        uint32_t third[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) third[k] = x[k];
-                        tmem_st16(tx + 16 * c, third);
-                    }
+                const uint32_t ty = tl + col_y<E, STATES>(i), tx = tl + col_third<STATES>(i);
+                if (a.parts == 2) {
+                    if (whole) feed_row<2, true>(ty, tx, near, rate2, back, give);
+                    else feed_row<2, false>(ty, tx, near, rate2, back, give);
+                } else {
+                    if (whole) feed_row<3, true>(ty, tx, near, rate2, back, give);
+                    else feed_row<3, false>(ty, tx, near, rate2, back, give);
                 }
-                tmem_wait_st();
             }
             tc_fence_before();
-            mbar_arrive(&bars[bFeed]);
-            if (DOCS && i + 1 < count) ok = clean(i + 1);
+            mbar_arrive(&bars[bFeed + (kTwo ? i & 1 : 0)]);
         }
     }
 
