@@ -728,9 +728,11 @@ static based_status decay_sizes_check(int B, int H, int L, int d_k, int d_v, bas
     return BASED_OK;
 }
 static DecayPlan decay_plan_of(const DecayCall& c, based_dtype io) { return io == BASED_F32 ? decay_plan_f32(c) : decay_plan_tc(c); }
-// the sizes of a call's passes, without its arrays
-static DecayCall decay_call(int passes, int B, int H, int L, int d_k, int d_v, bool documents) {
+// what a call of these sizes takes, whether it returns a state or not
+static size_t decay_bytes(int passes, int B, int H, int L, int d_k, int d_v, bool documents, based_dtype io) {
+    if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
     static const int given = 0;
+    static float wanted = 0.f;
     DecayCall c{};
     c.passes = passes;
     c.B = B; c.H = H; c.L = L;
@@ -740,7 +742,10 @@ static DecayCall decay_call(int passes, int B, int H, int L, int d_k, int d_v, b
         c.pass[i].dc = dc[passes == 3][i];
         c.pass[i].de = de[passes == 3][i];
     }
-    return c;
+    const size_t without = decay_plan_of(c, io).bytes();
+    c.pass[passes - 1].state_out = &wanted;
+    const size_t with = decay_plan_of(c, io).bytes();
+    return with > without ? with : without;
 }
 static based_status decay_run(const DecayCall& c, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     const DecayPlan plan = decay_plan_of(c, io);
@@ -752,12 +757,10 @@ static based_status decay_run(const DecayCall& c, based_dtype io, void* workspac
 }
 
 size_t based_decay_attention_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {
-    if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
-    return decay_plan_of(decay_call(1, B, H, L, d_k, d_v, with_documents != 0), io).bytes();
+    return decay_bytes(1, B, H, L, d_k, d_v, with_documents != 0, io);
 }
 size_t based_decay_attention_backward_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io) {
-    if (decay_sizes_check(B, H, L, d_k, d_v, io) != BASED_OK) return 0;
-    return decay_plan_of(decay_call(3, B, H, L, d_k, d_v, with_documents != 0), io).bytes();
+    return decay_bytes(3, B, H, L, d_k, d_v, with_documents != 0, io);
 }
 
 based_status based_decay_attention_forward(based_heads q, based_heads k, based_heads v, const float* rate, const int* documents,

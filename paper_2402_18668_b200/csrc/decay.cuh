@@ -63,8 +63,10 @@ struct DecayPlan {
     size_t places_bytes, states_bytes, factors_bytes;
     size_t bytes() const { return places_bytes + states_bytes + factors_bytes; }
 };
-// slots: CTAs that the device holds at a time; per_block: a block's time at this width, in blocks of width 64
-DecayPlan decay_plan(int passes, int max_de, int B, int H, int L, bool documents, int T, int width, int slots, double per_block);
+// Times in blocks of width 64: a block's at this width, the share of it that its state alone takes, a launch, adding up one segment
+struct DecayCosts { double block, states, launch, sum; };
+// slots: CTAs that the device holds at a time
+DecayPlan decay_plan(int passes, int max_de, int B, int H, int L, bool documents, int T, int width, int slots, DecayCosts costs);
 // the first block of a segment
 __host__ __device__ inline int decay_first(int blocks, int segments, int s) { return (int)((long long)blocks * s / segments); }
 
@@ -72,11 +74,11 @@ __host__ __device__ inline int decay_first(int blocks, int segments, int s) { re
 struct DecayItem {
     int pass, tile, segment;               // the segment as the pass goes through them: back passes begin with the last one
     long long head;                        // b H + h
-    __device__ __forceinline__ DecayItem(long long i, int passes, int tiles, int segments) {
-        pass = (int)(i % passes); i /= passes;
-        tile = (int)(i % tiles); i /= tiles;
-        segment = (int)(i % segments);
-        head = i / segments;
+    __device__ __forceinline__ DecayItem(unsigned i, int passes, int tiles, int segments) {
+        pass = (int)(i % (unsigned)passes); i /= (unsigned)passes;
+        tile = (int)(i % (unsigned)tiles); i /= (unsigned)tiles;
+        segment = (int)(i % (unsigned)segments);
+        head = i / (unsigned)segments;
     }
 };
 // the segments' states and factors in the workspace, of all but the last: states [128][width] each

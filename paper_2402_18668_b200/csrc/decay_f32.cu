@@ -80,6 +80,17 @@ __global__ void __launch_bounds__(kThreads, DC == 64 ? 2 : 1) decay_f32_kernel(c
                                          : (uint32_t)min(tid + 1, L - t0) | (tid < L - t0 ? 0u : kPadding);
         __syncthreads();
         const int c1 = place_count(pl[kT - 1]), r1 = place_run(pl[kT - 1]);
+        if (c1 == 0) {                               // nothing but padding: zeros, and the state as it is
+            if (!STATES)
+                for (int j = tid; j < kT * kTile / 4; j += kThreads) {
+                    const int t = t0 + j / (kTile / 4), e = e0 + j % (kTile / 4) * 4;
+                    if (t < L && e < p.de)
+                        *reinterpret_cast<float4*>(static_cast<float*>(const_cast<void*>(p.out.data)) + b * p.out.batch_stride + h * p.out.head_stride +
+                                                   (long long)t * p.out.token_stride + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            __syncthreads();
+            continue;
+        }
         const float f = r1 == 0 ? faded(rate2, c1) : 0.f;
         if (tid < kT) {
             const uint32_t w = pl[tid];
@@ -249,7 +260,7 @@ bool wide(const DecayCall& c) {
 DecayPlan decay_plan_f32(const DecayCall& c) {
     int de = 0;
     for (int i = 0; i < c.passes; ++i) de = c.pass[i].de > de ? c.pass[i].de : de;
-    return decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, kTile, wide(c) ? kSMs : 2 * kSMs, 1.0);
+    return decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, kTile, wide(c) ? kSMs : 2 * kSMs, {1.0, 0.4, 0.8, 0.1});
 }
 
 based_status launch_decay_f32(const DecayCall& c, const DecayPlan& plan, void* workspace, cudaStream_t stream) {

@@ -124,19 +124,20 @@ based_status launch_decay_places(const int* documents, uint32_t* places, int B, 
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
 }
 
-DecayPlan decay_plan(int passes, int max_de, int B, int H, int L, bool documents, int T, int width, int slots, double per_block) {
+DecayPlan decay_plan(int passes, int max_de, int B, int H, int L, bool documents, int T, int width, int slots, DecayCosts costs) {
     DecayPlan p{};
     p.T = T;
     p.width = width;
     p.blocks = (int)(((long long)L + T - 1) / T);
     p.tiles = (max_de + width - 1) / width;
     const long long items = (long long)passes * p.tiles * B * H;
-    // Time in blocks per CTA slot: all segments of all items in turns; ahead of them the states of all but the last segments, at
-    // some half a block each, a launch and the segments' states that each has to add up
+    // Time in blocks of a CTA: all segments of all items in turns; ahead of them the states of all but the last segments, a launch and the
+    // segments' states that each has to add up
     p.segments = 1;
     for (int n = 1; n <= p.blocks && n <= 64 && (n == 1 || items * n <= 4ll * slots); ++n) {
-        const double turns = (double)((items * n + slots - 1) / slots), each = (double)((p.blocks + n - 1) / n) * per_block;
-        const double time = n == 1 ? turns * each : turns * each + 0.5 * (double)((items * (n - 1) + slots - 1) / slots) * each + 3 + 0.1 * n;
+        auto turns = [&](long long ctas) { return (double)((ctas + slots - 1) / slots); };
+        const double each = (double)((p.blocks + n - 1) / n) * costs.block;
+        const double time = turns(items * n) * each + (n == 1 ? 0 : costs.states * turns(items * (n - 1)) * each + costs.launch + costs.sum * n);
         if (n == 1 || time < p.time) {
             p.time = time;
             p.segments = n;

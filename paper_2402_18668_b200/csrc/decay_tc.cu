@@ -50,12 +50,11 @@ template <int DC, int E, bool STATES> struct Cfg {
     static constexpr uint32_t kBytes = offPlaces + kStages * kT * 4;
     static_assert(kBytes <= 232448, "shared memory budget");
 };
-// TMEM columns: scores (P, and the third part of the faded y behind it), the turned y, O, S
+// TMEM columns: scores, then P; the turned y; O; S; E = 64: a second turned y, or the third part of a faded one
 constexpr uint32_t colX = 0, colY = 128, colO = 256;
-// Where there is room, two turned y in turn; where only states are wanted, two third parts too
-template <int E, bool STATES> constexpr bool kTwoY = STATES || E == 64;
-template <int E, bool STATES> __device__ __forceinline__ uint32_t col_y(int i) { return kTwoY<E, STATES> && (i & 1) ? (E == 128 ? colO : 384u) : colY; }
-template <bool STATES> __device__ __forceinline__ uint32_t col_third(int i) { return STATES ? colX + 64u * (i & 1) : colX + 64u; }
+// Where there is room, two turned y in turn (`two`); where only states are wanted, two third parts too
+template <int E> __device__ __forceinline__ uint32_t col_y(bool two, int i) { return two && (i & 1) ? (E == 128 ? colO : 384u) : colY; }
+template <bool STATES> __device__ __forceinline__ uint32_t col_third(int i) { return STATES ? colX + 64u * (i & 1) : 384u; }
 
 // Rings: full and empty places of x, y, z, and the output in z's place.  One phase a block (bTurn, bFeed: of two in turn where there are two
 // turned y): bTurn, bFeed y turned, faded; bX, bP scores there, P written; bClean padding out of y, z; bDS the state behind the
@@ -63,6 +62,7 @@ template <bool STATES> __device__ __forceinline__ uint32_t col_third(int i) { re
 enum Bar { bFullX = 0, bFullY = 4, bFullZ = 8, bEmptyX = 12, bEmptyY = 16, bEmptyZ = 20, bOut = 24, bTurn = 28, bFeed = 30, bX = 32, bP, bClean, bDS, bS, bXS, bTake, bO, bOread, bCount };
 static_assert(bCount * 8 + 8 <= 352, "barrier area");
 
+struct Words { uint32_t end, own; };
 struct alignas(64) Maps { CUtensorMap m[3][4]; };                    // [pass] x, y, z, out
 struct Args {
     DecayCall c;
@@ -123,6 +123,84 @@ __device__ __forceinline__ void feed_row(uint32_t ty, uint32_t tx, const pairs::
     }
     tmem_wait_st();
 }
+// A row of scores in TMEM, faded and masked, over itself in bf16; row r = 32 w + lane.  KIND 0: one document, no padding; 1: several, no padding
+// between their tokens (the row's own word tells where its document lies); 2: any (the words pl of all tokens, the powers pw).
+// near[k]: a^steps from column k of 16 to the end that is nearer to rows outside; among[k]: factor a^steps to a row among the 16 (0: it does not see it).
+// 32 columns a turn; a kind has a loop of its own, so that the one that runs stays in the instruction caches.
+template <int KIND>
+__device__ __forceinline__ void score_row(uint32_t tx, int w, int lane, bool back, float rate2, float factor, const pairs::pair (&near)[8],
+                                          const pairs::pair (&among)[8], uint32_t own, const uint32_t* pl, const float* pw) {
+    const int r = 32 * w + lane;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        uint32_t pk[16];
+        if (back ? c < w : c > w) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) pk[k] = 0u;
+        } else {
+            uint32_t v[32];
+            tmem_ld32(tx + 32 * c, v);
+            if constexpr (KIND < 2) {
+                const int steps = back ? 32 * c - r : r - 32 * c - 15;             // to the nearer end of the first 16 columns
+                pairs::pair f0 = pairs::both(factor * exp2f(-rate2 * (float)steps)), f1 = pairs::both(factor * exp2f(-rate2 * (float)(back ? steps + 16 : steps - 16)));
+                tmem_wait_ld();
+                if (c != w) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float2 y = pairs::split(pairs::mul2(as_pair(v[2 * k], v[2 * k + 1]), pairs::mul2(k < 8 ? f0 : f1, near[k & 7])));
+                        pk[k] = pack2(y.x, y.y);
+                    }
+                } else {                                             // of either 16 the row is one, or it sees them all, or none
+                    const bool high = lane >= 16;
+                    if (back ? high : !high) f0 = f1 = 0;
+                    if (back) f0 = 0;
+                    else f1 = 0;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const pairs::pair t = pairs::mul2(k < 8 ? f0 : f1, near[k & 7]);
+                        const float2 y = pairs::split(pairs::mul2(as_pair(v[2 * k], v[2 * k + 1]), high == (k >= 8) ? among[k & 7] : t));
+                        pk[k] = pack2(y.x, y.y);
+                    }
+                }
+                if constexpr (KIND == 1) {                           // the row's document alone: columns lo .. hi of these 32, two a register
+                    const int lo = own & kPadding ? 32 : (back ? 0 : max(place_from(own) - 32 * c, 0)), hi = back ? min(place_to(own) - 32 * c, 31) : 31;
+                    const uint32_t m = lo > hi ? 0u : (0xffffffffu >> (31 - hi)) & (0xffffffffu << lo);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        if (!((m >> (2 * k)) & 1u)) pk[k] &= 0xffff0000u;
+                        if (!((m >> (2 * k + 1)) & 1u)) pk[k] &= 0x0000ffffu;
+                    }
+                }
+            } else {
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    const uint32_t q = pl[32 * c + k];
+                    const int steps = back ? place_count(q) - place_count(own) : place_count(own) - place_count(q);
+                    const bool seen = ((q ^ own) & 0xff00u) == 0 && !((q | own) & kPadding) && (c != w || (back ? k >= lane : k <= lane));
+                    const float f = pw[max(steps, 0)] * factor;
+                    v[k] = seen ? __float_as_uint(__uint_as_float(v[k]) * f) : 0u;
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) pk[k] = pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
+            }
+        }
+        tmem_st16(tx + 16 * c, pk);                                  // (over columns that this row has read, or does not need)
+    }
+    tmem_wait_st();
+}
+// mbar_wait in few instructions: every one that a block's way leads through has to fit into the instruction caches with all the others (88 KB
+// of code, of which a block runs some 30; with the timed wait at each place a block with documents took 1.9 times as long).
+// Parked for up to 20 us a turn, given up after kTurns of them.
+constexpr int kTurns = 1 << 20;
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+#pragma unroll 1
+    for (int n = 0; !mbar_try_wait_hint(bar, parity, 20000u); ++n) {
+        if (n == kTurns) *abort_flag = 1;
+        if (*abort_flag) return false;
+    }
+    return true;
+}
 // barrier of a group of 128 threads that also tells whether all of them say yes
 __device__ __forceinline__ bool group_all(int id, bool pred) {
     uint32_t r;
@@ -143,14 +221,14 @@ template <int DC, int E, bool STATES, bool DOCS>
 __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
     using C = Cfg<DC, E, STATES>;
     constexpr int NS = C::kStages;
-    constexpr bool kTwo = kTwoY<E, STATES>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::offBars);
     uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(bars + bCount);
     volatile uint32_t* abort_flag = tmem_base_s + 1;
     float* pw = reinterpret_cast<float*>(smem + C::offPow);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const DecayItem it(blockIdx.x, a.c.passes, a.tiles, STATES ? a.segments - 1 : a.segments);
+    DecayItem it(blockIdx.x, a.c.passes, a.tiles, STATES ? a.segments - 1 : a.segments);
+    it.pass = __reduce_min_sync(0xffffffffu, it.pass);               // (uniform, as below)
     const DecayPass& p = a.c.pass[it.pass];
     const int e0 = it.tile * E, L = a.c.L;
     if (e0 >= p.de) return;
@@ -159,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         return;
     }
     const int b = (int)(it.head / a.c.H), h = (int)(it.head % a.c.H);
-    const bool back = p.back;
+    const bool back = p.back, two = STATES || (E == 64 && a.parts == 2);
 
     if (tid == 0) {
         for (int s = 0; s < bCount; ++s) {
@@ -243,28 +321,113 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             }
         }
     }
+    // (the same in every lane, and known to be: the products' addresses stay in uniform registers.  B8 H32 L4096 64/64 with documents
+    // took 185 us without, 159 with)
+    first = __reduce_min_sync(0xffffffffu, first);
+    count = __reduce_min_sync(0xffffffffu, count);
     auto block_of = [&](int i) { return back ? first + count - 1 - i : first + i; };
-    auto wait = [&](int bar, int phase) -> bool { return __all_sync(0xffffffffu, mbar_wait(&bars[bar], phase & 1, abort_flag)); };
+    auto wait = [&](int bar, int phase) -> bool { return __all_sync(0xffffffffu, wait_for(&bars[bar], phase & 1, abort_flag)); };
+    // what block i leaves of the state ahead of it, from its last token's place
+    auto fade_of = [&](uint32_t end) -> float { return place_run(end) == 0 ? pw[place_count(end)] : 0.f; };
+    // N columns from e on of row c of the state: to shared memory in bf16, and to TMEM faded by the next block (0: dropped, whatever it holds)
+    auto pass_on = [&](int c, int e, auto& x, float f) {
+        constexpr int N = sizeof(x) / 4;
+        if (!STATES) {
+            uint8_t* row = smem + C::offS + (e >> 6) * C::kSPanel + c * 128;
+            const uint32_t sw = c & 7;
+#pragma unroll
+            for (int j = 0; j < N / 8; ++j) {
+                uint32_t v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(x[8 * j + 2 * k]), __uint_as_float(x[8 * j + 2 * k + 1]));
+                *reinterpret_cast<uint4*>(row + (((uint32_t)((e & 63) / 8 + j) ^ sw) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+        }
+        if (f == 0.f) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = 0u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+        }
+        const uint32_t at = tmem_addr(tb, (uint32_t)(c & ~31), colO + E + e);
+        if constexpr (N == 32) tmem_st32(at, x);
+        else tmem_st16(at, x);
+    };
+    // A block's last place and a token's own, asked for a block ahead of their use
+    auto words_of = [&](int i, int r) -> Words {
+        if (i >= count) return {0u, 0u};
+        const int n = block_of(i);
+        return {end_of(n), DOCS ? places_of(n)[r] : 0u};
+    };
+    // The state ahead of the first block, by all four groups, a quarter of its columns each: what was given, and the segments before
+    // this one
+    if (warp < 16 && (warp & 3) * 32 < DC) {
+        constexpr int N = E / 4;
+        const int c = 32 * (warp & 3) + lane, e = (warp >> 2) * N;
+        uint32_t x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = 0u;
+        if (!STATES) {
+            if (p.state_in && c < p.dc) {
+                const float* in = p.state_in + it.head * p.dc * p.de;
+#pragma unroll
+                for (int k = 0; k < N; k += 4)
+                    if (e0 + e + k < p.de) {                         // (widths are multiples of 8)
+                        float4 y;
+                        if (p.turned) {
+                            const float* col = in + (long long)(e0 + e + k) * p.dc + c;
+                            y = make_float4(col[0], col[p.dc], col[2 * p.dc], col[3 * p.dc]);
+                        } else {
+                            y = *reinterpret_cast<const float4*>(in + (long long)c * p.de + e0 + e + k);
+                        }
+                        x[k] = __float_as_uint(p.in_factor * y.x);
+                        x[k + 1] = __float_as_uint(p.in_factor * y.y);
+                        x[k + 2] = __float_as_uint(p.in_factor * y.z);
+                        x[k + 3] = __float_as_uint(p.in_factor * y.w);
+                    }
+            }
+#pragma unroll 2
+            for (int q = 0; q < it.segment; ++q) {
+                const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, q);
+                const float g = a.factors[slot];
+                const float4* from = reinterpret_cast<const float4*>(a.states + (slot * kDecayMaxWidth + c) * E + e);
+#pragma unroll
+                for (int k = 0; k < N; k += 4) {
+                    const float4 y = from[k / 4];
+                    const float ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[k + j] = __float_as_uint(g == 0.f ? ys[j] : fmaf(g, __uint_as_float(x[k + j]), ys[j]));
+                }
+            }
+        }
+        pass_on(c, e, x, count > 0 ? fade_of(end_of(block_of(0))) : 1.f);
+        tmem_wait_st();
+        fence_proxy_async_smem();
+    }
+    tc_fence_before();
+    if (warp != kWarpTma && warp < kWarpStore) asm volatile("bar.sync 2, 544;" ::: "memory");      // (the loads are under way meanwhile)
+    tc_fence_after();
 
     if (warp == kWarpTma) {
         if (lane == 0) {
             for (int i = 0; i < count; ++i) {
                 const int s = i % NS, n = block_of(i), t0 = n * kT, turn = i / NS - 1;
-                if (i >= NS) ok = mbar_wait(&bars[bEmptyY + s], turn & 1, abort_flag);
+                if (i >= NS) ok = wait_for(&bars[bEmptyY + s], turn & 1, abort_flag);
                 if (!ok) break;
                 mbar_arrive_expect_tx(&bars[bFullY + s], C::kX * kPanel);
 #pragma unroll
                 for (int j = 0; j < C::kX; ++j)
                     tma_load_4d(smem + C::offY + (s * C::kX + j) * kPanel, &maps.m[it.pass][1], &bars[bFullY + s], 64 * j, t0, h, b);
                 if (!STATES) {
-                    if (i >= NS) ok = mbar_wait(&bars[bEmptyX + s], turn & 1, abort_flag);
+                    if (i >= NS) ok = wait_for(&bars[bEmptyX + s], turn & 1, abort_flag);
                     if (!ok) break;
                     mbar_arrive_expect_tx(&bars[bFullX + s], C::kX * kPanel);
 #pragma unroll
                     for (int j = 0; j < C::kX; ++j)
                         tma_load_4d(smem + (s * C::kX + j) * kPanel, &maps.m[it.pass][0], &bars[bFullX + s], 64 * j, t0, h, b);
                 }
-                if (i >= NS) ok = mbar_wait(&bars[bEmptyZ + s], turn & 1, abort_flag);
+                if (i >= NS) ok = wait_for(&bars[bEmptyZ + s], turn & 1, abort_flag);
                 if (!ok) break;
                 mbar_arrive_expect_tx(&bars[bFullZ + s], C::kZ * kPanel + (DOCS ? kT * 4 : 0));
                 if (DOCS) bulk_load_1d(smem + C::offPlaces + s * kT * 4, places_of(n), kT * 4, &bars[bFullZ + s]);
@@ -277,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         if (!STATES && lane == 0) {
             for (int i = 0; i < count; ++i) {
                 const int s = i % NS;
-                ok = mbar_wait(&bars[bOut + s], (i / NS) & 1, abort_flag);
+                ok = wait_for(&bars[bOut + s], (i / NS) & 1, abort_flag);
                 if (!ok) break;
 #pragma unroll
                 for (int j = 0; j < C::kZ; ++j)
@@ -300,6 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         constexpr uint32_t colS = colO + E;
         const uint32_t sm = smem_u32(smem);
         auto lo = [](uint64_t base, uint32_t addr) { return desc_lo(base) + (addr >> 4); };
+        // (rolled where the documents' code crowds the caches: B8 H16 L4096 128/128 119 -> 108 us there; B8 H32 64/64 without 124 -> 130)
         auto x_of = [&](int i) { return lo(dK, sm + (i % NS) * C::kX * kPanel); };
         auto y_of = [&](int i) { return sm + C::offY + (i % NS) * C::kX * kPanel; };
         auto z_of = [&](int i) { return lo(dZ, sm + C::offZ + (i % NS) * C::kZ * kPanel); };
@@ -307,18 +471,18 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         auto turn = [&](int i) -> bool {
             if (!wait(bFullY + i % NS, i / NS) || (DOCS && !wait(bClean, i))) return false;
             tc_fence_after();
-            const uint32_t lt = lo(dZ, y_of(i)), lu = lo(dU, sm + C::offUnit), d = tb + col_y<E, STATES>(i);
-#pragma unroll
+            const uint32_t lt = lo(dZ, y_of(i)), lu = lo(dU, sm + C::offUnit), d = tb + col_y<E>(two, i);
+#pragma unroll (DOCS ? 2 : 8)
             for (int k = 0; k < kT / 16; ++k) mma_ss_w<false>(lead, d + 16 * k, lt + k * 128, desc_hi(dZ), lu, desc_hi(dU), iT);
-            mma_commit_w(lead, &bars[bTurn + (kTwo ? i & 1 : 0)]);
+            mma_commit_w(lead, &bars[bTurn + (two ? i & 1 : 0)]);
             if (STATES) mma_commit_w(lead, &bars[bEmptyY + i % NS]);
             return true;
         };
         auto delta = [&](int i) -> bool {
-            if (!wait(bFullZ + i % NS, i / NS) || !wait(bFeed + (kTwo ? i & 1 : 0), kTwo ? i >> 1 : i) || !wait(bS, i)) return false;
+            if (!wait(bFullZ + i % NS, i / NS) || !wait(bFeed + (two ? i & 1 : 0), two ? i >> 1 : i) || (i > 0 && !wait(bS, i - 1))) return false;
             tc_fence_after();
-            const uint32_t lz = z_of(i), ty = tb + col_y<E, STATES>(i);
-#pragma unroll
+            const uint32_t lz = z_of(i), ty = tb + col_y<E>(two, i);
+#pragma unroll (DOCS ? 2 : 8)
             for (int k = 0; k < kT / 16; ++k) {
                 const uint32_t at = ty + 16 * k;
                 mma_ts_w<true>(lead, tb + colS, at, lz + k * 128, desc_hi(dZ), iO);
@@ -348,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             return true;
         };
         auto before = [&](int i) -> bool {
-            if (!wait(bS, i) || (i > 0 && !wait(bOread, i - 1))) return false;
+            if (i > 0 && (!wait(bS, i - 1) || !wait(bOread, i - 1))) return false;
             tc_fence_after();
             const uint32_t lx = x_of(i), ls = lo(dS, sm + C::offS);
 #pragma unroll
@@ -365,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             if (!wait(bP, i) || !wait(bTake, i)) return false;
             tc_fence_after();
             const uint32_t lz = z_of(i);
-#pragma unroll
+#pragma unroll (DOCS ? 2 : 8)
             for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, tb + colO, tb + colX + k * 8, lz + k * 128, desc_hi(dZ), iO);
             mma_commit_w(lead, &bars[bO]);
             return true;
@@ -381,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
 #pragma unroll 1
             for (int i = 0; i < count && ok; ++i) {
                 const bool more = i + 1 < count;
-                if (kTwo) ok = (!more || turn(i + 1)) && delta(i) && inside(i);
+                if (two) ok = (!more || turn(i + 1)) && delta(i) && inside(i);
                 else ok = delta(i) && (!more || turn(i + 1)) && inside(i);
                 if (more && ok) ok = scores(i + 1) && before(i + 1);
             }
@@ -401,73 +565,19 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                 near[k] = pairs::make(faded(rate2, back ? j : 15 - j), faded(rate2, back ? j + 1 : 14 - j));
                 among[k] = pairs::make(s0 >= 0 ? factor * faded(rate2, s0) : 0.f, s1 >= 0 ? factor * faded(rate2, s1) : 0.f);
             }
+            Words next = words_of(0, r);
             for (int i = 0; i < count; ++i) {
                 const int n = block_of(i), s = i % NS;
-                const uint32_t end = end_of(n);
+                const uint32_t end = next.end, own = next.own;
+                next = words_of(i + 1, r);
                 const bool simple = plain(end, n);
-                const uint32_t own = DOCS && !simple ? places_of(n)[r] : 0u;
                 const uint32_t* pl = reinterpret_cast<const uint32_t*>(smem + C::offPlaces + s * kT * 4);
                 ok = wait(bX, i) && (simple || (end & kCompact) || wait(bFullZ + s, i / NS));      // (the places come with z)
                 if (!ok) break;
                 tc_fence_after();
-                // 32 columns a time; P goes over columns that this row has read, or does not need
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t pk[16];
-                    if (back ? c < w : c > w) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) pk[k] = 0u;
-                    } else {
-                        uint32_t v[32];
-                        tmem_ld32(tl + colX + 32 * c, v);
-                        if (!DOCS || simple || (end & kCompact)) {
-                            const int steps = back ? 32 * c - r : r - 32 * c - 15;             // to the nearer end of the first 16 columns
-                            pairs::pair f0 = pairs::both(factor * exp2f(-rate2 * (float)steps)), f1 = pairs::both(factor * exp2f(-rate2 * (float)(back ? steps + 16 : steps - 16)));
-                            tmem_wait_ld();
-                            if (c != w) {
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    const float2 y = pairs::split(pairs::mul2(as_pair(v[2 * k], v[2 * k + 1]), pairs::mul2(k < 8 ? f0 : f1, near[k & 7])));
-                                    pk[k] = pack2(y.x, y.y);
-                                }
-                            } else {                                 // of either 16 the row is one, or it sees them all, or none
-                                const bool high = lane >= 16;
-                                if (back ? high : !high) f0 = f1 = 0;
-                                if (back) f0 = 0;
-                                else f1 = 0;
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    const pairs::pair t = pairs::mul2(k < 8 ? f0 : f1, near[k & 7]);
-                                    const float2 y = pairs::split(pairs::mul2(as_pair(v[2 * k], v[2 * k + 1]), high == (k >= 8) ? among[k & 7] : t));
-                                    pk[k] = pack2(y.x, y.y);
-                                }
-                            }
-                            if (DOCS && !simple) {                   // the row's document alone: columns lo .. hi of these 32, two a register
-                                const int lo = own & kPadding ? 32 : (back ? 0 : max(place_from(own) - 32 * c, 0)), hi = back ? min(place_to(own) - 32 * c, 31) : 31;
-                                const uint32_t m = lo > hi ? 0u : (0xffffffffu >> (31 - hi)) & (0xffffffffu << lo);
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    if (!((m >> (2 * k)) & 1u)) pk[k] &= 0xffff0000u;
-                                    if (!((m >> (2 * k + 1)) & 1u)) pk[k] &= 0x0000ffffu;
-                                }
-                            }
-                        } else {
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) {
-                                const uint32_t q = pl[32 * c + k];
-                                const int steps = back ? place_count(q) - place_count(own) : place_count(own) - place_count(q);
-                                const bool seen = ((q ^ own) & (kPadding | 0xff00u)) == 0 && !(own & kPadding) && (c != w || (back ? k >= lane : k <= lane));
-                                const float f = pw[max(steps, 0)] * factor;
-                                v[k] = seen ? __float_as_uint(__uint_as_float(v[k]) * f) : 0u;
-                            }
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) pk[k] = pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
-                        }
-                    }
-                    tmem_st16(tl + colX + 16 * c, pk);
-                }
-                tmem_wait_st();
+                if (!DOCS || simple) score_row<0>(tl + colX, w, lane, back, rate2, factor, near, among, own, pl, pw);
+                else if (end & kCompact) score_row<1>(tl + colX, w, lane, back, rate2, factor, near, among, own, pl, pw);
+                else score_row<2>(tl + colX, w, lane, back, rate2, factor, near, among, own, pl, pw);
                 tc_fence_before();
                 mbar_arrive(&bars[bP]);
             }
@@ -477,76 +587,10 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         const int w = warp & 3, c = 32 * w + lane;
         const bool rows = w * 32 < DC;                               // (the whole warp's)
         const uint32_t ts = tmem_addr(tb, (uint32_t)w * 32u, colO + E);
-        auto fade_of = [&](int i) -> float {
-            if (i >= count) return 1.f;
-            const uint32_t end = end_of(block_of(i));
-            return place_run(end) == 0 ? pw[place_count(end)] : 0.f;
-        };
-        // 32 columns of the state to shared memory in bf16, and back to TMEM faded by the next block (0: dropped, whatever it holds)
-        auto pass_on = [&](int e, uint32_t(&x)[32], float f) {
-            if (!STATES) {
-                uint8_t* row = smem + C::offS + (e >> 6) * C::kSPanel + c * 128;
-                const uint32_t sw = c & 7;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t v[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = pack2(__uint_as_float(x[8 * j + 2 * k]), __uint_as_float(x[8 * j + 2 * k + 1]));
-                    *reinterpret_cast<uint4*>(row + (((uint32_t)((e & 32) / 8 + j) ^ sw) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                }
-            }
-            if (f == 0.f) {
-#pragma unroll
-                for (int k = 0; k < 32; ++k) x[k] = 0u;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-            }
-            tmem_st32(ts + e, x);
-        };
-        auto passed_on = [&] {
-            tmem_wait_st();
-            fence_proxy_async_smem();
-            tc_fence_before();
-            mbar_arrive(&bars[bS]);
-        };
-        const float* in = p.state_in ? p.state_in + it.head * p.dc * p.de : nullptr;
-        if (rows) {
-            const float f = fade_of(0);
-#pragma unroll 1
-            for (int e = 0; e < E; e += 32) {
-                uint32_t x[32];
-#pragma unroll
-                for (int k = 0; k < 32; ++k) x[k] = 0u;
-                if (!STATES) {
-                    if (in && c < p.dc) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (e0 + e + k < p.de)
-                                x[k] = __float_as_uint(p.in_factor * in[p.turned ? (long long)(e0 + e + k) * p.dc + c : (long long)c * p.de + e0 + e + k]);
-                    }
-#pragma unroll 1
-                    for (int q = 0; q < it.segment; ++q) {
-                        const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, q);
-                        const float g = a.factors[slot];
-                        const float4* from = reinterpret_cast<const float4*>(a.states + (slot * kDecayMaxWidth + c) * E + e);
-#pragma unroll
-                        for (int k = 0; k < 32; k += 4) {
-                            const float4 y = from[k / 4];
-                            const float ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) x[k + j] = __float_as_uint(g == 0.f ? ys[j] : fmaf(g, __uint_as_float(x[k + j]), ys[j]));
-                        }
-                    }
-                }
-                pass_on(e, x, f);
-            }
-        }
-        passed_on();
-        float whole = cut ? 0.f : 1.f;
+        float whole = cut ? 0.f : 1.f, f = count > 0 ? fade_of(end_of(block_of(0))) : 1.f;
         for (int i = 0; i < count; ++i) {
-            const float f = fade_of(i + 1);
-            whole *= fade_of(i);
+            whole *= f;
+            if (i + 1 < count) f = fade_of(end_of(block_of(i + 1)));
             ok = wait(bDS, i);
             if (!ok) break;
             tc_fence_after();
@@ -557,31 +601,40 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                         uint32_t x[32];
                         tmem_ld32(ts + e, x);
                         tmem_wait_ld();
-                        pass_on(e, x, f);
+                        pass_on(c, e, x, f);
                     }
+                    tmem_wait_st();
+                    fence_proxy_async_smem();
                 }
-                passed_on();
+                tc_fence_before();
+                mbar_arrive(&bars[bS]);
             }
         }
-        if (ok && rows) {
-            float* out = !STATES && p.state_out && it.segment == a.segments - 1 && c < p.dc ? p.state_out + it.head * p.dc * p.de : nullptr;
+        if (ok && rows && (STATES || (p.state_out && it.segment == a.segments - 1))) {
             const long long slot = STATES ? decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, it.segment) : 0;
-            if (STATES || p.state_out) {
 #pragma unroll 1
-                for (int e = 0; e < E; e += 32) {
-                    uint32_t x[32];
-                    tmem_ld32(ts + e, x);
-                    tmem_wait_ld();
-                    if (STATES) {
-                        uint4* to = reinterpret_cast<uint4*>(a.states + (slot * kDecayMaxWidth + c) * E + e);
+            for (int e = 0; e < E; e += 32) {
+                uint32_t x[32];
+                tmem_ld32(ts + e, x);
+                tmem_wait_ld();
+                if (STATES) {
+                    uint4* to = reinterpret_cast<uint4*>(a.states + (slot * kDecayMaxWidth + c) * E + e);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) to[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
-                    } else if (out) {
+                    for (int k = 0; k < 8; ++k) to[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                } else if (c < p.dc) {
+                    float* out = p.state_out + it.head * p.dc * p.de;
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (e0 + e + k < p.de)
-                                out[p.turned ? (long long)(e0 + e + k) * p.dc + c : (long long)c * p.de + e0 + e + k] = p.out_factor * __uint_as_float(x[k]);
-                    }
+                    for (int k = 0; k < 32; k += 4)
+                        if (e0 + e + k < p.de) {
+                            float4 y = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                            y = make_float4(p.out_factor * y.x, p.out_factor * y.y, p.out_factor * y.z, p.out_factor * y.w);
+                            if (p.turned) {
+                                float* col = out + (long long)(e0 + e + k) * p.dc + c;
+                                col[0] = y.x; col[p.dc] = y.y; col[2 * p.dc] = y.z; col[3 * p.dc] = y.w;
+                            } else {
+                                *reinterpret_cast<float4*>(out + (long long)c * p.de + e0 + e + k) = y;
+                            }
+                        }
                 }
             }
             if (STATES && c == 0) a.factors[slot] = whole;
@@ -591,14 +644,15 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         if constexpr (!STATES) {
             const int w = warp & 3, r = 32 * w + lane;
             const uint32_t to = tmem_addr(tb, (uint32_t)w * 32u, colO), sw = r & 7;
+            Words next = words_of(0, r);
             for (int i = 0; i < count; ++i) {
                 const int n = block_of(i), s = i % NS;
-                const uint32_t end = end_of(n);
+                const uint32_t end = next.end, own = next.own;
+                next = words_of(i + 1, r);
                 float take;
                 if (plain(end, n)) {
                     take = pw[back ? max(place_count(end) - 1 - r, 0) : r + 1];
                 } else {
-                    const uint32_t own = places_of(n)[r];
                     take = own & kPadding ? 0.f
                            : back         ? (place_run(own) == place_run(end) ? pw[place_count(end) - place_count(own)] : 0.f)
                                           : (place_run(own) == 0 ? pw[place_count(own)] : 0.f);
@@ -655,9 +709,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         const uint32_t tl = tmem_addr(tb, (uint32_t)w * 32u, 0);
         float* give = reinterpret_cast<float*>(smem + C::offGive);
         // rows of padding out of y and z
-        auto clean = [&](int i) -> bool {
+        auto clean = [&](int i, uint32_t end) -> bool {
             const int n = block_of(i), s = i % NS;
-            if (place_count(end_of(n)) < min(kT, L - n * kT)) {
+            if (place_count(end) < min(kT, L - n * kT)) {
                 if (!wait(bFullY + s, i / NS) || !wait(bFullZ + s, i / NS)) return false;
                 const uint32_t* pl = reinterpret_cast<const uint32_t*>(smem + C::offPlaces + s * kT * 4);
                 const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -675,41 +729,42 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             mbar_arrive(&bars[bClean]);
             return true;
         };
-        if (DOCS && count > 0) ok = clean(0);
+        Words next = words_of(0, u);
         pairs::pair near[8];                                         // a^steps from token k of 16 to the end that is nearer to where the state goes
 #pragma unroll
         for (int k = 0; k < 8; ++k) near[k] = pairs::make(faded(rate2, back ? 2 * k : 15 - 2 * k), faded(rate2, back ? 2 * k + 1 : 14 - 2 * k));
-        for (int i = 0; i < count; ++i) {
-            const int n = block_of(i);
-            const uint32_t end = end_of(n);
-            const int c1 = place_count(end);
-            const bool simple = plain(end, n), whole = simple && c1 == kT;
-            // (the third part goes where scores were that P does not need)
-            ok = ok && mbar_wait(&bars[bTurn + (kTwo ? i & 1 : 0)], (kTwo ? i >> 1 : i) & 1, abort_flag);
-            if (!STATES && a.parts == 3) ok = ok && mbar_wait(&bars[bP], i & 1, abort_flag);
-            ok = group_all(1, ok);
-            if (!ok) break;
-            // (the next block's, once the products are past the wait for this one's)
-            if (DOCS && i + 1 < count) {
-                ok = group_all(1, clean(i + 1));
+        Words here{0u, 0u};
+        for (int i = DOCS ? -1 : 0; i < count; ++i) {
+            if (i >= 0) {
+                here = next;
+                next = words_of(i + 1, u);
+                ok = group_all(1, ok && wait_for(&bars[bTurn + (two ? i & 1 : 0)], (two ? i >> 1 : i) & 1, abort_flag));
                 if (!ok) break;
             }
+            // (the next block's, once the products are past the wait for this one's)
+            if (DOCS && i + 1 < count) {
+                ok = group_all(1, clean(i + 1, next.end));
+                if (!ok) break;
+            }
+            if (DOCS && i < 0) continue;
+            const uint32_t end = here.end, own = here.own;
+            const int c1 = place_count(end);
+            const bool simple = plain(end, block_of(i)), whole = simple && c1 == kT;
             if (!whole) {
                 float x;
                 if (simple) {
                     x = u < c1 ? pw[back ? u + 1 : c1 - 1 - u] : 0.f;
                 } else {
-                    const uint32_t q = places_of(n)[u];
-                    x = q & kPadding ? 0.f
-                        : back       ? (place_run(q) == 0 ? pw[place_count(q)] : 0.f)
-                                     : (place_run(q) == place_run(end) ? pw[c1 - place_count(q)] : 0.f);
+                    x = own & kPadding ? 0.f
+                        : back         ? (place_run(own) == 0 ? pw[place_count(own)] : 0.f)
+                                       : (place_run(own) == place_run(end) ? pw[c1 - place_count(own)] : 0.f);
                 }
                 give[u] = x;
                 group_all(1, true);
             }
             tc_fence_after();
             if (rows) {
-                const uint32_t ty = tl + col_y<E, STATES>(i), tx = tl + col_third<STATES>(i);
+                const uint32_t ty = tl + col_y<E>(two, i), tx = tl + col_third<STATES>(i);
                 if (a.parts == 2) {
                     if (whole) feed_row<2, true>(ty, tx, near, rate2, back, give);
                     else feed_row<2, false>(ty, tx, near, rate2, back, give);
@@ -719,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                 }
             }
             tc_fence_before();
-            mbar_arrive(&bars[bFeed + (kTwo ? i & 1 : 0)]);
+            mbar_arrive(&bars[bFeed + (two ? i & 1 : 0)]);
         }
     }
 
@@ -763,13 +818,19 @@ template <int DC, int E> based_status launch_docs(const Maps& maps, const Args& 
 
 }  // namespace
 
+static bool state_wanted(const DecayCall& c) {
+    for (int i = 0; i < c.passes; ++i)
+        if (c.pass[i].state_out) return true;
+    return false;
+}
 DecayPlan decay_plan_tc(const DecayCall& c) {
     int de = 0;
     for (int i = 0; i < c.passes; ++i) de = c.pass[i].de > de ? c.pass[i].de : de;
-    const DecayPlan narrow = decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, 64, kSMs, 1.0);
-    if (de <= 64) return narrow;
+    const DecayPlan narrow = decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, 64, kSMs, {1.0, 0.7, 2.5, 0.15});
+    // (three parts of the faded y have no place beside tiles of 128)
+    if (de <= 64 || state_wanted(c)) return narrow;
     // tiles of 128 columns read x and y once: worth it unless there are so few heads that half as many CTAs leave SMs idle
-    const DecayPlan wide = decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, 128, kSMs, 1.5);
+    const DecayPlan wide = decay_plan(c.passes, de, c.B, c.H, c.L, c.documents != nullptr, kT, 128, kSMs, {1.5, 0.7, 2.5, 0.15});
     return wide.time <= narrow.time ? wide : narrow;
 }
 
@@ -777,17 +838,16 @@ based_status launch_decay_tc(const DecayCall& c, const DecayPlan& plan, void* wo
     char* ws = static_cast<char*>(workspace);
     uint32_t* places = c.documents ? reinterpret_cast<uint32_t*>(ws) : nullptr;
     Maps maps;
-    bool wide = false, wanted = false;
+    bool wide = false;
     for (int i = 0; i < c.passes; ++i) {
         const DecayPass& p = c.pass[i];
         if (!make_heads_map_bf16(&maps.m[i][0], p.x, c.B, c.H, c.L, p.dc, kT) || !make_heads_map_bf16(&maps.m[i][1], p.y, c.B, c.H, c.L, p.dc, kT) ||
             !make_heads_map_bf16(&maps.m[i][2], p.z, c.B, c.H, c.L, p.de, kT) || !make_heads_map_bf16(&maps.m[i][3], p.out, c.B, c.H, c.L, p.de, kT))
             return BASED_ERR_CUDA;
         wide = wide || p.dc > 64;
-        wanted = wanted || p.state_out;
     }
     Args a{c, places, reinterpret_cast<float*>(ws + plan.places_bytes), reinterpret_cast<float*>(ws + plan.places_bytes + plan.states_bytes),
-           nullptr, plan.blocks, plan.segments, plan.tiles, wanted ? 3 : 2};
+           nullptr, plan.blocks, plan.segments, plan.tiles, state_wanted(c) ? 3 : 2};
     if (error_word_ptr(&a.err) != BASED_OK) return BASED_ERR_CUDA;
     if (places) {
         const based_status st = launch_decay_places(c.documents, places, c.B, c.L, kT, stream);
