@@ -594,9 +594,47 @@ based_status based_decay_attention_backward(based_heads q, based_heads k, based_
 size_t based_decay_attention_backward_workspace_bytes(int B, int H, int L, int d_k, int d_v, int with_documents, based_dtype io);
 
 /*
+ * A paged key-value cache: two pools of `pages` pages of page_size tokens.  Key (value) element c of head h in slot s of page p is at
+ * k (v) + p * page_stride + h * head_stride + s * token_stride + c, strides in elements, multiples of 16 bytes: [pages,H_k,page_size,d] and
+ * [pages,page_size,H_k,d] are both taken as they lie.  Token j of sequence b lies in slot j % page_size of page page_table[b, j / page_size]
+ * (int32 [B,max_pages] on the device; entries past a sequence's last token are not read).
+ * The numbers are checked on the device: a page that is not in the pool is not touched (its tokens read as zeros), and the next
+ * based_poll_error of the device returns BASED_ERR_INVALID_ARG.
+ */
+typedef struct { void *k, *v; long long page_stride, head_stride, token_stride; int pages, page_size; } based_pages;
+
+/*
+ * Softmax attention of one new token per sequence over such a cache (the exact-recall layers of a hybrid stack at generation): the key and
+ * value of sequence b are written to position pos[b], and its queries attend to the keys j = max(0, pos[b] - window + 1) .. pos[b]
+ * (window 0: all), query head h to key head h / (H_q / H_k):
+ *
+ *   s_j = softcap tanh(softmax_scale q . k_j / softcap) - slopes[h] (pos[b] - j),     out = sum_j softmax(s)_j v_j
+ *
+ * q, out [B,H_q,d], k, v [B,H_k,d] contiguous, in the io dtype, which is the cache's too; pos int32 [B] on the device, pos[b] < 0: the
+ * sequence has no token (its output is 0, nothing is written); one beyond max_pages * page_size counts as a bad page and has output 0.
+ * softcap 0: no cap; slopes [H_q] fp32 (NULL: no bias).  softmax_scale <= 0: 1 / sqrt(d).  The work is divided evenly over the tokens that there
+ * are, in whichever sequences; scores, sums and outputs are fp32, in bf16 io the softmax weights are rounded to bf16 once, as operands.  No
+ * result depends on the order in which the parts end.
+ * Supported: d a multiple of 8 up to 128; H_q a multiple of H_k; any page_size, max_pages * page_size < 2^31; io in {F32, BF16}.
+ * workspace: paged_decode_step_workspace_bytes.  out must not alias an input; two sequences must not write to one slot.
+ */
+based_status paged_decode_step(const void* q, const void* k, const void* v, based_pages cache, const int* page_table, const int* pos,
+                               const float* slopes, void* out, int B, int H_q, int H_k, int d, int max_pages, int window, float softmax_scale,
+                               float softcap, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t paged_decode_step_workspace_bytes(int B, int H_q, int H_k, int d, int page_size, int max_pages, based_dtype io);
+
+/*
+ * Copies the keys and values of prompts into their pages: token t < counts[b] (NULL: L) of k, v [B,H,L,d] to position pos[b] + t of sequence
+ * b (pos[b] < 0: none of them).  Everything else in the pools stays as it is.  Supported: as above.
+ */
+based_status paged_cache_write(based_heads k, based_heads v, based_pages cache, const int* page_table, const int* pos, const int* counts, int B,
+                               int H, int L, int d, int max_pages, based_dtype io, void* cuda_stream);
+
+/*
  * Synchronises the stream and returns the sticky device-side status: BASED_OK, or
  * BASED_ERR_DEVICE_TIMEOUT if a kernel abandoned a bounded wait (its outputs are then
- * undefined), or BASED_ERR_CUDA if the stream reported a CUDA error.  Clears the flag.
+ * undefined), or BASED_ERR_INVALID_ARG if one met a page number that is not in the pool (based_pages),
+ * or BASED_ERR_CUDA if the stream reported a CUDA error.  Clears the flag.
  */
 based_status based_poll_error(void* cuda_stream);
 

@@ -7,5 +7,5 @@ from .binding import (  # noqa: F401
     based_static_scratch_bytes, based_selftest_bounded_wait, launch_count, lib,
     based_gated_recurrence_backward, based_gated_recurrence_forward, based_gated_recurrence_step, based_qk_norm_rotate, based_qk_norm_rotate_backward,
     based_decay_attention_backward, based_decay_attention_forward, based_decay_attention_step,
-    new_state, status_string, swa_backward, swa_decode_step, swa_decode_step_ragged, swa_forward, version,
+    new_state, paged_cache_write, paged_decode_step, status_string, swa_backward, swa_decode_step, swa_decode_step_ragged, swa_forward, version,
 )

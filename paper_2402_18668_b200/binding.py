@@ -39,7 +39,7 @@ EXPORTS = (
     "based_gated_recurrence_backward", "based_gated_recurrence_backward_workspace_bytes", "based_qk_norm_rotate",
     "based_qk_norm_rotate_backward", "based_qk_norm_rotate_backward_workspace_bytes", "swa_backward", "swa_backward_workspace_bytes",
     "based_decay_attention_forward", "based_decay_attention_workspace_bytes", "based_decay_attention_step", "based_decay_attention_backward",
-    "based_decay_attention_backward_workspace_bytes",
+    "based_decay_attention_backward_workspace_bytes", "paged_decode_step", "paged_decode_step_workspace_bytes", "paged_cache_write",
 )
 
 _lib = None
@@ -55,6 +55,12 @@ class Heads(ctypes.Structure):
     """based_heads: [B,H,L,d] values with strides, in elements."""
     _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
                 ("token_stride", ctypes.c_longlong)]
+
+
+class Pages(ctypes.Structure):
+    """based_pages: the pools of a paged key-value cache, strides in elements."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
+                ("token_stride", ctypes.c_longlong), ("pages", ctypes.c_int), ("page_size", ctypes.c_int)]
 
 
 class BasedError(RuntimeError):
@@ -159,6 +165,12 @@ def lib() -> ctypes.CDLL:
         for name in ("based_decay_attention_workspace_bytes", "based_decay_attention_backward_workspace_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [i] * 7
+        L.paged_decode_step.restype = i
+        L.paged_decode_step.argtypes = [vp, vp, vp, Pages, vp, vp, vp, vp, i, i, i, i, i, i, f, f, i, vp, sz, vp]
+        L.paged_decode_step_workspace_bytes.restype = sz
+        L.paged_decode_step_workspace_bytes.argtypes = [i] * 7
+        L.paged_cache_write.restype = i
+        L.paged_cache_write.argtypes = [Heads, Heads, Pages, vp, vp, vp, i, i, i, i, i, i, vp]
         L.based_poll_error.restype = i
         L.based_poll_error.argtypes = [vp]
         L.based_status_string.restype = ctypes.c_char_p
@@ -490,6 +502,23 @@ def based_decay_attention_backward(q, k, v, rate, dout, documents=None, state_in
     state_out.  dstate_in is None without state_in; the rates are constants."""
     return (_native_module or native()).decay_backward(q, k, v, rate, documents, state_in, dout, dstate_out, float(scale), workspace,
                                                        _handle(stream))
+
+
+def paged_decode_step(q, k, v, k_pages, v_pages, page_table, pos, out=None, softmax_scale: float = 0.0, softcap: float = 0.0, slopes=None,
+                      window: int = 0, workspace=None, stream=None):
+    """Softmax attention of one new token per sequence over a paged cache: q [B,H_q,d], k, v [B,H_k,d]; k_pages, v_pages
+    [pages,H_k,page_size,d] (of any one layout, such as [pages,page_size,H_k,d] transposed), page_table int32 [B,max_pages], pos int32
+    [B], all on the device.  k, v are written to position pos[b]; the queries attend to it and what lies before it (the last `window` keys,
+    0: all).  softcap: scores become softcap tanh(s / softcap); slopes [H_q] fp32: less slope * distance.  pos[b] < 0: no token,
+    output 0.  Page numbers are checked on the device (based_poll_error: 1).  Returns out [B,H_q,d]."""
+    return (_native_module or native()).paged_decode(q, k, v, k_pages, v_pages, page_table, pos, out, float(softmax_scale), float(softcap),
+                                                     slopes, int(window), workspace, _handle(stream))
+
+
+def paged_cache_write(k, v, k_pages, v_pages, page_table, pos, counts=None, stream=None):
+    """Copies keys and values [B,H,L,d] into their pages: token t < counts[b] (None: all L) to position pos[b] + t of sequence b; counts,
+    pos int32 [B].  pos[b] < 0: none of them."""
+    return (_native_module or native()).paged_write(k, v, k_pages, v_pages, page_table, pos, counts, _handle(stream))
 
 
 def based_selftest_bounded_wait(limit_ms: int = 20, stream=None) -> None:

@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "decay.cuh"
+#include "paged.cuh"
 
 namespace based {
 
@@ -835,6 +836,72 @@ based_status based_decay_attention_backward(based_heads q, based_heads k, based_
     return decay_run(c, io, workspace, workspace_bytes, cuda_stream);
 }
 
+static based_status pages_check(const based_pages& c, const int* page_table, const int* pos, int B, int H, int d, int max_pages, based_dtype io) {
+    if (!c.k || !c.v || c.k == c.v || !page_table || !pos || B <= 0 || H <= 0 || d <= 0 || c.pages <= 0 || c.page_size <= 0 || max_pages <= 0 ||
+        (io != BASED_F32 && io != BASED_BF16))
+        return BASED_ERR_INVALID_ARG;
+    if (d % 8 || d > 128 || (long long)max_pages * c.page_size > 0x7fffffffLL || (long long)B * H > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    const long long per16 = 16 / (long long)esize(io);
+    struct { long long stride; int size; } dim[3] = {{c.page_stride, c.pages}, {c.head_stride, H}, {c.token_stride, c.page_size}};
+    for (const auto& x : dim)
+        if (x.size > 1 && x.stride < d) return BASED_ERR_INVALID_ARG;
+    for (const auto& x : dim)
+        if (x.size > 1 && (x.stride % per16 != 0 || x.stride >= 1ll << 40)) return BASED_ERR_UNSUPPORTED;
+    long long extent = d;                  // no slot lies in another, as with outputs given by strides
+    for (int turn = 0; turn < 3; ++turn) {
+        int least = -1;
+        for (int i = 0; i < 3; ++i)
+            if (dim[i].size > 1 && (least < 0 || dim[i].stride < dim[least].stride)) least = i;
+        if (least < 0) break;
+        if (dim[least].stride < extent) return BASED_ERR_INVALID_ARG;
+        extent += dim[least].stride * (dim[least].size - 1);
+        dim[least].size = 0;
+    }
+    if (!aligned16(c.k) || !aligned16(c.v) || (reinterpret_cast<uintptr_t>(page_table) & 3) || (reinterpret_cast<uintptr_t>(pos) & 3)) return BASED_ERR_ALIGNMENT;
+    return BASED_OK;
+}
+
+size_t paged_decode_step_workspace_bytes(int B, int H_q, int H_k, int d, int page_size, int max_pages, based_dtype io) {
+    if (B <= 0 || H_q <= 0 || H_k <= 0 || H_q % H_k || d <= 0 || d % 8 || d > 128 || page_size <= 0 || max_pages <= 0 ||
+        (long long)max_pages * page_size > 0x7fffffffLL || (io != BASED_F32 && io != BASED_BF16))
+        return 0;
+    return paged_decode_bytes(B, H_q, H_k, d, page_size, max_pages, io);
+}
+
+based_status paged_decode_step(const void* q, const void* k, const void* v, based_pages cache, const int* page_table, const int* pos,
+                               const float* slopes, void* out, int B, int H_q, int H_k, int d, int max_pages, int window, float softmax_scale,
+                               float softcap, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!q || !k || !v || !out || H_q <= 0 || H_k <= 0 || H_q % H_k || window < 0 || !(softcap >= 0.f)) return BASED_ERR_INVALID_ARG;
+    const based_status st = pages_check(cache, page_table, pos, B, H_k, d, max_pages, io);
+    if (st != BASED_OK) return st;
+    if (is_one_of(out, {q, k, v, cache.k, cache.v, page_table, pos, slopes, workspace}) || is_one_of(workspace, {q, k, v, cache.k, cache.v, page_table, pos, slopes}))
+        return BASED_ERR_INVALID_ARG;
+    if ((long long)B * H_q > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    for (const void* p : {q, k, v, (const void*)out, (const void*)workspace})
+        if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
+    if (reinterpret_cast<uintptr_t>(slopes) & 3) return BASED_ERR_ALIGNMENT;
+    const size_t need = paged_decode_bytes(B, H_q, H_k, d, cache.page_size, max_pages, io);
+    if (!workspace || workspace_bytes < need) return BASED_ERR_WORKSPACE;
+    const PagedCall c{q, k, v, cache.k, cache.v, cache.page_stride, cache.head_stride, cache.token_stride, page_table, pos, slopes, out, B, H_q, H_k, d,
+                      cache.pages, cache.page_size, max_pages, window, softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf((float)d), softcap};
+    return launch_paged_decode(c, workspace, io, static_cast<cudaStream_t>(cuda_stream));
+}
+
+based_status paged_cache_write(based_heads k, based_heads v, based_pages cache, const int* page_table, const int* pos, const int* counts, int B,
+                               int H, int L, int d, int max_pages, based_dtype io, void* cuda_stream) {
+    if (!k.data || !v.data || L <= 0) return BASED_ERR_INVALID_ARG;
+    based_status st = pages_check(cache, page_table, pos, B, H, d, max_pages, io);
+    if (st == BASED_OK) st = heads_check(k, B, H, L, d, io, false);
+    if (st == BASED_OK) st = heads_check(v, B, H, L, d, io, false);
+    if (st != BASED_OK) return st;
+    if (is_one_of(cache.k, {k.data, v.data}) || is_one_of(cache.v, {k.data, v.data})) return BASED_ERR_INVALID_ARG;
+    if (L > 0x7fff0000 || (long long)B * H * (((long long)L + 63) / 64) > 0x7fffffffLL) return BASED_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(counts) & 3) return BASED_ERR_ALIGNMENT;
+    const PagedWrite c{k, v, cache.k, cache.v, cache.page_stride, cache.head_stride, cache.token_stride, page_table, pos, counts, B, H, L, d, cache.pages,
+                       cache.page_size, max_pages};
+    return launch_paged_write(c, io, static_cast<cudaStream_t>(cuda_stream));
+}
+
 size_t based_prefill_backward_workspace_bytes(int B, int H, int L, int d_v, based_dtype io) {
     if (B <= 0 || H <= 0 || L <= 0 || !dv_ok(d_v)) return 0;
     const int heads = (long long)B * H > kHeadSlab ? (int)kHeadSlab : B * H;       // the largest slab of heads
@@ -972,7 +1039,7 @@ based_status based_poll_error(void* cuda_stream) {
     if (word != 0) {
         const unsigned int zero = 0;
         if (cudaMemcpyToSymbol(g_error_word, &zero, sizeof(zero)) != cudaSuccess) return BASED_ERR_CUDA;
-        return BASED_ERR_DEVICE_TIMEOUT;
+        return word & 1u ? BASED_ERR_DEVICE_TIMEOUT : BASED_ERR_INVALID_ARG;
     }
     return BASED_OK;
 }

@@ -885,6 +885,69 @@ PyObject* decay_backward(PyObject* const* a) {
     return wrap({g.dq, g.dk, g.dv, g.dstate});
 }
 
+// ---------------------------------------------------------------------------------------------- paged cache
+// two pools [pages,H,page_size,d] of one shape and layout (any order of the dimensions ahead of d)
+struct Pages {
+    const Tensor &k, &v, &table, &pos;
+    int pages, H, page_size, d, max_pages;
+    Pages(PyObject* k_, PyObject* v_, PyObject* table_, PyObject* pos_, int B, const Tensor& like)
+        : k(heads(k_, "k_pages")), v(heads(v_, "v_pages")), table(need(table_, "page_table")), pos(need(pos_, "pos")) {
+        if (v.sizes() != k.sizes() || v.strides() != k.strides() || k.scalar_type() != like.scalar_type() || v.scalar_type() != like.scalar_type())
+            value_error("k_pages and v_pages must be [pages,H_k,page_size,d] of one layout, in the dtype of k");
+        pages = dim(k, 0); H = dim(k, 1); page_size = dim(k, 2); d = dim(k, 3);
+        if (table.scalar_type() != at::kInt || table.dim() != 2 || table.size(0) != B) value_error("page_table is an int32 tensor [B,max_pages]");
+        check_int32(pos, {B}, "pos");
+        max_pages = dim(table, 1);
+    }
+    based_pages cache() const { return {k.mutable_data_ptr(), v.mutable_data_ptr(), k.stride(0), k.stride(1), k.stride(2), pages, page_size}; }
+    const int* t() const { return static_cast<const int*>(cptr(table)); }
+    const int* p() const { return static_cast<const int*>(cptr(pos)); }
+};
+// q, k, v, k_pages, v_pages, page_table, pos, out, softmax_scale, softcap, slopes, window, workspace, stream
+PyObject* paged_decode(PyObject* const* a) {
+    const Tensor &q = need(a[0], "q"), &k = need(a[1], "k"), &v = need(a[2], "v"), &slopes = dev(a[10]), &workspace = dev(a[12]);
+    Tensor out = dev(a[7]);
+    dims(q, 3, "q");
+    dims(k, 3, "k");
+    if (v.sizes() != k.sizes() || k.size(0) != q.size(0) || k.size(2) != q.size(2) || k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type())
+        value_error("q, k, v shapes/dtypes disagree");
+    const int B = dim(q, 0), Hq = dim(q, 1), Hk = dim(k, 1), d = dim(q, 2);
+    const Pages c(a[3], a[4], a[5], a[6], B, q);
+    if (c.H != Hk || c.d != d) value_error("k_pages and v_pages must have the heads and the width of k");
+    check_like(out, q, "out", "q");
+    check_f32(slopes, {Hq}, "slopes");
+    check_places({&q, &k, &v, &c.table, &c.pos, &slopes}, {&out, &c.k, &c.v, &workspace});
+    const float scale = number(a[8]), cap = number(a[9]);
+    const int window = integer(a[11]);
+    const based_dtype io = dtype_code(q);
+    void* stream = stream_on(a[13], q);
+    away(q, [&] {
+        if (!out.defined()) out = blank(q.sizes(), q.scalar_type());
+        const Workspace ws(workspace, paged_decode_step_workspace_bytes(B, Hq, Hk, d, c.page_size, c.max_pages, io), q, stream);
+        check(paged_decode_step(cptr(q), cptr(k), cptr(v), c.cache(), c.t(), c.p(), f32(slopes), ptr(out), B, Hq, Hk, d, c.max_pages, window, scale, cap,
+                                io, ws.data, ws.bytes, stream),
+              "paged_decode_step");
+    });
+    return wrap(out);
+}
+// k, v, k_pages, v_pages, page_table, pos, counts, stream
+PyObject* paged_write(PyObject* const* a) {
+    const Tensor &k = heads(a[0], "k"), &v = heads(a[1], "v"), &counts = dev(a[6]);
+    check_like(v, k, "v", "k");
+    const int B = dim(k, 0), H = dim(k, 1), L = dim(k, 2), d = dim(k, 3);
+    const Pages c(a[2], a[3], a[4], a[5], B, k);
+    if (c.H != H || c.d != d) value_error("k_pages and v_pages must have the heads and the width of k");
+    check_int32(counts, {B}, "counts");
+    check_places({&k, &v, &c.table, &c.pos, &counts}, {&c.k, &c.v});
+    const based_dtype io = dtype_code(k);
+    void* stream = stream_on(a[7], k);
+    away(k, [&] {
+        check(paged_cache_write(as_heads(k), as_heads(v), c.cache(), c.t(), c.p(), static_cast<const int*>(cptr(counts)), B, H, L, d, c.max_pages, io, stream),
+              "paged_cache_write");
+    });
+    Py_RETURN_NONE;
+}
+
 // Python's exception for a status of the library
 void set_status_error(const StatusFault& e) {
     PyObject* mod = PyImport_ImportModule("paper_2402_18668_b200.binding");
@@ -1280,7 +1343,8 @@ PyMethodDef methods[] = {method<prefill, 9>("prefill"), method<prefill_backward,
                          method<swa_grad, 8>("swa_grad"), method<gated_recurrence, 5>("gated_recurrence"),
                          method<qk_norm_rotate, 9>("qk_norm_rotate"), method<sliding_window, 5>("sliding_window"),
                          method<decay_forward, 11>("decay_forward"), method<decay_step, 9>("decay_step"), method<decay_backward, 11>("decay_backward"),
-                         method<decay_attention, 7>("decay_attention"), {nullptr, nullptr, 0, nullptr}};
+                         method<decay_attention, 7>("decay_attention"), method<paged_decode, 14>("paged_decode"), method<paged_write, 8>("paged_write"),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 
