@@ -24,9 +24,10 @@ constexpr int kUnit = 64, kWarps = 4, kThreads = 128, kSub = 16;         // toke
 constexpr unsigned kBadPage = 2u;                                        // in the error word
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <typename T, int DP> struct Cfg {
+// R: query heads at a time, 16 on tensor cores, else as many as share a key head (8 at most)
+template <typename T, int DP, int R> struct Cfg {
     static constexpr bool kTc = sizeof(T) == 2;
-    static constexpr int kRows = kTc ? 16 : 8;                           // query heads at a time
+    static constexpr int kRows = R;
     static constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16;
     static constexpr int kStage = 2 * kSub * kRowBytes;                  // a warp's keys and values of a unit
     static constexpr int kStages = kStage >= 16384 ? 3 : kStage >= 8192 ? 3 : 4;
@@ -73,19 +74,26 @@ struct Span {
     }
 };
 
-// sum over the sequences before b0 .. (all threads of the CTA; buf: 33 long longs): units of sequences 0 .. n - 1
-__device__ __forceinline__ long long units_before(const PagedCall& c, int n, long long* buf) {
-    long long mine = 0;
-    for (int b = threadIdx.x; b < n; b += blockDim.x) mine += Span(c, b).count;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = mine;
-    __syncthreads();
-    long long all = 0;
-    for (int w = 0; w < (int)(blockDim.x + 31) / 32; ++w) all += buf[w];
-    return all;
-}
+// The units of all sequences in one row, cut into G shares that differ by one at most
+struct Shares {
+    long long total, base, more;                                         // the first `more` shares have base + 1 units
+    int G;
+    __device__ __forceinline__ Shares(long long total_, int G_) : total(total_), G(G_) {
+        if (total >> 31 == 0) {
+            base = (unsigned)total / (unsigned)G;
+            more = (unsigned)total % (unsigned)G;
+        } else {
+            base = total / G;
+            more = total % G;
+        }
+    }
+    __device__ __forceinline__ long long begin(long long i) const { return i * base + (i < more ? i : more); }
+    __device__ __forceinline__ long long of(long long x) const {
+        const long long wide = more * (base + 1);
+        if (total >> 31 == 0) return x < wide ? (unsigned)x / (unsigned)(base + 1) : more + (unsigned)(x - wide) / (unsigned)base;
+        return x < wide ? x / (base + 1) : more + (x - wide) / base;
+    }
+};
 
 struct Args {
     PagedCall c;
@@ -93,11 +101,12 @@ struct Args {
     unsigned int* err;
     int blocks;                                                          // row blocks of a key head's queries
     int shift;                                                           // page_size = 1 << shift, or -1
+    bool whole;                                                          // 16 tokens from a multiple of 16 on lie in one page
 };
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_kernel(const __grid_constant__ Args a) {
-    using C = Cfg<T, DP>;
+template <typename T, int DP, int R>
+__global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_kernel(const __grid_constant__ Args a) {
+    using C = Cfg<T, DP, R>;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long s_sum[4], s_from[2];
     const PagedCall& c = a.c;
@@ -107,16 +116,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
     const int group = c.Hq / c.Hk, heads = c.Hk * a.blocks;              // "heads": key heads and row blocks of their queries
     enter_dependent();
 
-    // This CTA's units, and the sequence that they begin in
-    const long long total = units_before(c, c.B, s_sum) * heads;
-    long long u = total * blockIdx.x / gridDim.x;
-    const long long end = total * (blockIdx.x + 1) / gridDim.x;
-    if (u >= end) return;
+    // This CTA's units, and the sequence that they begin in: inclusive sums of the sequences' units, 128 a turn, by shuffles.  Twice where there are
+    // more sequences than that (the first time for the total alone)
+    long long total = 0, u = 0, end = 0, base = 0;                       // base: the units of the sequences before b
     int b = 0;
-    long long base = 0;                                                  // the units of the sequences before b
-    {
+    for (int pass = c.B > kThreads ? 0 : 1; pass < 2; ++pass) {
         long long before = 0;
-        for (int b0 = 0; b0 < c.B; b0 += kThreads) {                     // 128 sequences a turn: inclusive sums by shuffles
+        for (int b0 = 0; b0 < c.B; b0 += kThreads) {
             const long long n = b0 + tid < c.B ? (long long)Span(c, b0 + tid).count * heads : 0;
             long long sum = n;
 #pragma unroll
@@ -130,17 +136,27 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
             long long off = before;
             for (int w = 0; w < warp; ++w) off += s_sum[w];
             sum += off;
-            if (sum - n <= u && u < sum) {
-                s_from[0] = b0 + tid;
-                s_from[1] = sum - n;
-            }
             before += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-            if (before > u) break;
+            if (pass == 1) {
+                if (c.B <= kThreads) total = before;
+                if (b0 == 0) {
+                    const Shares sh(total, (int)gridDim.x);
+                    u = sh.begin(blockIdx.x);
+                    end = sh.begin(blockIdx.x + 1);
+                    if (u >= end) return;
+                }
+                if (sum - n <= u && u < sum) {
+                    s_from[0] = b0 + tid;
+                    s_from[1] = sum - n;
+                }
+                if (before > u) break;
+            }
         }
-        __syncthreads();
-        b = (int)s_from[0];
-        base = s_from[1];
+        if (pass == 0) total = before;
     }
+    __syncthreads();
+    b = (int)s_from[0];
+    base = s_from[1];
     const long long range = u;
 
     for (; u < end; ) {
@@ -161,33 +177,55 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
         T* vp = static_cast<T*>(c.v_pages) + hk * c.head_stride;
         const int* table = c.table + (long long)b * c.max_pages;
 
-        // tokens j0 .. j0 + 15 of unit n are this warp's; lane < 16 (and its double) finds where token j0 + lane lies: -1 nowhere
+        // tokens j0 .. j0 + 15 of unit n are this warp's; lane < 16 (and its double) looks up the page of token j0 + lane a turn before it is needed:
+        // what is checked is checked then, so that nothing waits for the table
         auto tokens = [&](int n) { return (sp.first + unit0 + n) * kUnit + warp * kSub; };
-        auto place = [&](int n) -> long long {
+        auto page_of = [&](int j) { return a.shift >= 0 ? j >> a.shift : (int)((unsigned)j / (unsigned)c.page_size); };
+        auto here = [&](int n, int j) { return n < units && j <= sp.pos && j >= sp.lo; };
+        auto look = [&](int n) -> int {
             const int j = tokens(n) + (lane & 15);
-            if (n >= units || j > sp.pos || j < sp.lo) return -1;
-            const int page = a.shift >= 0 ? j >> a.shift : j / c.page_size, slot = j - page * c.page_size;
-            const int id = table[page];
-            if ((unsigned)id >= (unsigned)c.pages) {
-                atomicOr(a.err, kBadPage);
-                return -1;
-            }
-            return id * c.page_stride + slot * c.token_stride;
+            return here(n, j) ? table[page_of(j)] : 0;
         };
-        auto load = [&](int n, long long at) {
+        // tokens strictly inside, whose page is one: nothing to check but that
+        auto inside = [&](int n) { const int j0 = tokens(n); return n < units && j0 >= sp.lo && j0 + kSub <= sp.pos; };
+        constexpr int V = 16 / (int)sizeof(T), kStep = 32 / C::kChunks > 0 ? 32 / C::kChunks : 1;          // values of a chunk, rows of a turn
+        const int lrow = lane / C::kChunks, lch = lane % C::kChunks;     // (fp32, 128 wide: a row a turn)
+        const bool lin = lch * V < c.d;
+        const long long lane_at = lrow * c.token_stride + (lin ? lch * V : 0);
+        auto load = [&](int n, int id) {
             uint8_t* st = ring + n % C::kStages * C::kStage;
-            const int j0 = tokens(n);
+            const int j0 = tokens(n), j = j0 + (lane & 15);
+            if (a.whole && inside(n) && (unsigned)id < (unsigned)c.pages) {
+                const long long at = id * c.page_stride + (long long)(j0 - page_of(j0) * c.page_size) * c.token_stride + lane_at;
+                const T *ks = kp + at, *vs = vp + at;
+                const long long step = kStep * c.token_stride;
 #pragma unroll
-            for (int i = 0; i < kSub * C::kChunks / 32; ++i) {
-                const int row = (i * 32 + lane) / C::kChunks, ch = (i * 32 + lane) % C::kChunks;
+                for (int i = 0; i < kSub / kStep; ++i) {
+                    const int row = i * kStep + lrow;
+                    uint8_t* to = st + row * C::kRowBytes + ((lch ^ (row & 7)) << 4);
+                    pairs::copy_async16(to, ks, lin);
+                    pairs::copy_async16(to + kSub * C::kRowBytes, vs, lin);
+                    ks += step;
+                    vs += step;
+                }
+                pairs::copy_async_commit();
+                return;
+            }
+            long long at = -1;
+            if (here(n, j)) {
+                if ((unsigned)id < (unsigned)c.pages) at = id * c.page_stride + (long long)(j - page_of(j) * c.page_size) * c.token_stride;
+                else atomicOr(a.err, kBadPage);
+            }
+#pragma unroll 1
+            for (int i = 0; i < kSub / kStep; ++i) {
+                const int row = i * kStep + lrow;
                 const long long off = __shfl_sync(0xffffffffu, at, row);
                 const bool fresh = j0 + row == sp.pos && n < units;      // the new token's, which may not be in its page yet
-                const bool in = (off >= 0 || fresh) && ch * (16 / (int)sizeof(T)) < c.d;
-                const int e = ch * (16 / (int)sizeof(T));
+                const bool in = (off >= 0 || fresh) && lin;
                 const T *ks = fresh ? knew : kp + (off >= 0 ? off : 0), *vs = fresh ? vnew : vp + (off >= 0 ? off : 0);
-                uint8_t* to = st + row * C::kRowBytes + ((ch ^ (row & 7)) << 4);
-                pairs::copy_async16(to, in ? ks + e : c.q, in);
-                pairs::copy_async16(to + kSub * C::kRowBytes, in ? vs + e : c.q, in);
+                uint8_t* to = st + row * C::kRowBytes + ((lch ^ (row & 7)) << 4);
+                pairs::copy_async16(to, in ? ks + lch * V : c.q, in);
+                pairs::copy_async16(to + kSub * C::kRowBytes, in ? vs + lch * V : c.q, in);
             }
             pairs::copy_async_commit();
         };
@@ -197,12 +235,12 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
             const int r = i / DP, e = i % DP;
             sq[i] = r < rows && e < c.d ? to_f32(q[(long long)r * c.d + e]) : 0.f;
         }
-        long long next = place(0);
+        int next = look(0);
 #pragma unroll
         for (int n = 0; n < C::kStages - 1; ++n) {
-            const long long at = next;
-            next = place(n + 1);
-            load(n, at);
+            const int id = next;
+            next = look(n + 1);
+            load(n, id);
         }
         __syncthreads();
 
@@ -234,6 +272,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
                 slope[1] = r + 8 < rows ? c.slopes[h0 + r + 8] : 0.f;
             }
         }
+        const bool modified = c.cap > 0.f || c.slopes;
         // a score as the softmax takes it, in base 2
         auto weigh = [&](float s, float sl, int j) -> float {
             if (j > sp.pos || j < sp.lo) return -INFINITY;
@@ -245,9 +284,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
 
         for (int n = 0; n < units; ++n) {
             {
-                const long long at = next;
-                next = place(n + C::kStages);
-                load(n + C::kStages - 1, at);
+                const int id = next;
+                next = look(n + C::kStages);
+                load(n + C::kStages - 1, id);
             }
             pairs::copy_async_wait<C::kStages - 1>();
             __syncwarp();
@@ -266,20 +305,20 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
                         mma16816(s[1], qf[k], f[2], f[3]);
                     }
                     float fade[2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {                        // rows lane / 4 and lane / 4 + 8
-                        float top = -INFINITY;
+                    const bool plain = !modified && inside(n);           // the scores as they are, all of them
+                    const float sc = plain ? c.scale * kLog2e : 1.f;
+                    if (!plain) {
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                float& y = s[t][2 * h + x];
-                                y = weigh(y, slope[h], j0 + 8 * t + (lane & 3) * 2 + x);
-                                top = fmaxf(top, y);
-                            }
+                            for (int x = 0; x < 4; ++x) s[t][x] = weigh(s[t][x], slope[x >> 1], j0 + 8 * t + (lane & 3) * 2 + (x & 1));
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {                        // rows lane / 4 and lane / 4 + 8
+                        float top = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                        const float to = fmaxf(m[h], top), z = to == -INFINITY ? 0.f : to;
+                        const float to = fmaxf(m[h], top * sc), z = to == -INFINITY ? 0.f : to;
                         fade[h] = ex2(m[h] - z);
                         m[h] = to;
                         float sum = 0.f;
@@ -287,10 +326,19 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                s[t][2 * h + x] = ex2(s[t][2 * h + x] - z);
+                                s[t][2 * h + x] = ex2(fmaf(s[t][2 * h + x], sc, -z));
                                 sum += s[t][2 * h + x];
                             }
                         l[h] = fmaf(l[h], fade[h], sum);
+                    }
+                    if (__any_sync(0xffffffffu, fade[0] != 1.f || fade[1] != 1.f)) {      // (seldom, once the largest score has come)
+#pragma unroll
+                        for (int k = 0; k < DP / 8; ++k) {
+                            acc[k][0] *= fade[0];
+                            acc[k][1] *= fade[0];
+                            acc[k][2] *= fade[1];
+                            acc[k][3] *= fade[1];
+                        }
                     }
                     const uint32_t p[4] = {pack2(s[0][0], s[0][1]), pack2(s[0][2], s[0][3]), pack2(s[1][0], s[1][1]), pack2(s[1][2], s[1][3])};
                     const int vr = lane & 15, vc = lane >> 4;
@@ -300,12 +348,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
                         ldmatrix4t(f, vs + vr * C::kRowBytes + (((2 * k + vc) ^ (vr & 7)) << 4));
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
-                            float(&o)[4] = acc[2 * k + x];
-                            o[0] *= fade[0];
-                            o[1] *= fade[0];
-                            o[2] *= fade[1];
-                            o[3] *= fade[1];
-                            mma16816(o, p, f[2 * x], f[2 * x + 1]);
+                            mma16816(acc[2 * k + x], p, f[2 * x], f[2 * x + 1]);
                         }
                     }
                 } else {
@@ -317,30 +360,26 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
                         const int ch = half * (C::kChunks / 2) + k;
                         const float4 x = *reinterpret_cast<const float4*>(st + tok * C::kRowBytes + ((ch ^ (tok & 7)) << 4));
 #pragma unroll
-                        for (int r = 0; r < C::kRows; ++r)
-                            if (r < rows) {
-                                const float4 y = *reinterpret_cast<const float4*>(sq + r * DP + 4 * ch);
-                                s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
-                            }
-                    }
-#pragma unroll
-                    for (int r = 0; r < C::kRows; ++r)
-                        if (r < rows) {
-                            s[r] += __shfl_xor_sync(0xffffffffu, s[r], 16);
-                            s[r] = weigh(s[r], c.slopes ? c.slopes[h0 + r] : 0.f, j0 + tok);
-                            float top = s[r];
-#pragma unroll
-                            for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                            const float to = fmaxf(m[r], top), z = to == -INFINITY ? 0.f : to, fade = exp2f(m[r] - z);
-                            m[r] = to;
-                            s[r] = exp2f(s[r] - z);
-                            float sum = s[r];
-#pragma unroll
-                            for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                            l[r] = fmaf(l[r], fade, sum);
-#pragma unroll
-                            for (int x = 0; x < DP / 32; ++x) acc[r][x] *= fade;
+                        for (int r = 0; r < C::kRows; ++r) {             // (rows past the last: queries of zeros)
+                            const float4 y = *reinterpret_cast<const float4*>(sq + r * DP + 4 * ch);
+                            s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
                         }
+                    }
+                    const bool plain = !modified && inside(n);
+#pragma unroll
+                    for (int r = 0; r < C::kRows; ++r) {
+                        s[r] += __shfl_xor_sync(0xffffffffu, s[r], 16);
+                        s[r] = plain ? s[r] * (c.scale * kLog2e) : weigh(s[r], c.slopes && r < rows ? c.slopes[h0 + r] : 0.f, j0 + tok);
+                        float top = s[r];
+#pragma unroll
+                        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const float to = fmaxf(m[r], top), z = to == -INFINITY ? 0.f : to, fade = exp2f(m[r] - z);
+                        m[r] = to;
+                        s[r] = exp2f(s[r] - z);
+                        l[r] = fmaf(l[r], fade, s[r]);                   // a lane's own tokens: joined at the end
+#pragma unroll
+                        for (int x = 0; x < DP / 32; ++x) acc[r][x] *= fade;
+                    }
                     // output: lane = DP / 32 columns
 #pragma unroll 4
                     for (int t = 0; t < kSub; ++t) {
@@ -354,17 +393,16 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
                             x[0] = y.x; x[1] = y.y;
                         }
 #pragma unroll
-                        for (int r = 0; r < C::kRows; ++r)
-                            if (r < rows) {
-                                const float w = __shfl_sync(0xffffffffu, s[r], t);
+                        for (int r = 0; r < C::kRows; ++r) {
+                            const float w = __shfl_sync(0xffffffffu, s[r], t);
 #pragma unroll
-                                for (int k = 0; k < DP / 32; ++k) acc[r][k] = fmaf(w, x[k], acc[r][k]);
-                            }
+                            for (int k = 0; k < DP / 32; ++k) acc[r][k] = fmaf(w, x[k], acc[r][k]);
+                        }
                     }
                 }
                 // the new token into its page, once for a key head
                 if (row0 == 0 && j0 <= sp.pos && sp.pos < j0 + kSub) {
-                    const int page = a.shift >= 0 ? sp.pos >> a.shift : sp.pos / c.page_size, id = table[page];
+                    const int page = a.shift >= 0 ? sp.pos >> a.shift : (int)((unsigned)sp.pos / (unsigned)c.page_size), id = table[page];
                     if ((unsigned)id < (unsigned)c.pages) {
                         const long long at = id * c.page_stride + (long long)(sp.pos - page * c.page_size) * c.token_stride;
                         constexpr int V = 16 / sizeof(T);
@@ -402,6 +440,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
         } else {
 #pragma unroll
             for (int r = 0; r < C::kRows; ++r) {
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
 #pragma unroll
                 for (int k = 0; k < DP / 32; ++k) piece[r * (DP + 2) + 2 + lane * (DP / 32) + k] = acc[r][k];
                 if (lane == 0) {
@@ -441,9 +481,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP>::kPerSm) paged_decode_ker
 }
 
 // the outputs that were cut, from their pieces, and zeros where a sequence has no token; a CTA per sequence and "head"
-template <typename T, int DP> __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ Args a, int G) {
-    using C = Cfg<T, DP>;
-    __shared__ long long s_sum[4];
+template <typename T, int DP, int R> __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ Args a, int G) {
+    using C = Cfg<T, DP, R>;
+    __shared__ long long s_sum[8];
     const PagedCall& c = a.c;
     const int heads = c.Hk * a.blocks, group = c.Hq / c.Hk, b = blockIdx.x / heads, hm = blockIdx.x % heads;
     const int row0 = (hm % a.blocks) * C::kRows, rows = min(C::kRows, group - row0), h0 = (hm / a.blocks) * group + row0;
@@ -455,66 +495,98 @@ template <typename T, int DP> __global__ void __launch_bounds__(kThreads) paged_
         if (threadIdx.x == 0 && sp.pos >= 0) atomicOr(a.err, kBadPage);
         return;
     }
-    const long long before = units_before(c, b, s_sum) * heads, total = units_before(c, c.B, s_sum) * heads;
-    const long long first = before + (long long)hm * sp.count, last = first + sp.count - 1;
-    // CTA i took units total i / G .. total (i + 1) / G - 1: unit x is in the one of the largest i with total i / G <= x
-    auto cta_of = [&](long long x) {
-        long long i = x * G / total;
-        while (i + 1 < G && total * (i + 1) / G <= x) ++i;
-        return i;
-    };
-    const long long i0 = cta_of(first), i1 = cta_of(last);
+    long long mine[2] = {0, 0};                                          // the units before this sequence, and of all
+    for (int k = threadIdx.x; k < c.B; k += kThreads) {
+        const int n = Span(c, k).count;
+        mine[0] += k < b ? n : 0;
+        mine[1] += n;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        mine[0] += __shfl_xor_sync(0xffffffffu, mine[0], o);
+        mine[1] += __shfl_xor_sync(0xffffffffu, mine[1], o);
+    }
+    if ((threadIdx.x & 31) == 0) {
+        s_sum[threadIdx.x >> 5] = mine[0];
+        s_sum[4 + (threadIdx.x >> 5)] = mine[1];
+    }
+    __syncthreads();
+    const long long first = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * heads + (long long)hm * sp.count, last = first + sp.count - 1;
+    const Shares sh((s_sum[4] + s_sum[5] + s_sum[6] + s_sum[7]) * heads, G);
+    const long long i0 = sh.of(first), i1 = sh.of(last);
     if (i0 == i1) return;
-    auto piece = [&](long long i) { return a.pieces + (2 * i + (i == i0 && total * i / G != first)) * C::kPiece; };
-    // (every CTA in between has units: total >= G, or each unit is a CTA's own)
+    const bool begun = sh.begin(i0) != first;                            // the first CTA had something else before it
+    const int count = (int)(i1 - i0) + 1;
+    const float* from = a.pieces + 2 * i0 * C::kPiece;
     for (int k = threadIdx.x; k < rows * DP; k += kThreads) {
         const int r = k / DP, e = k % DP;
         if (e >= c.d) continue;
         float top = -INFINITY, sum = 0.f, o = 0.f;
-        for (long long i = i0; i <= i1; ++i)
-            if (total * i / G != total * (i + 1) / G) top = fmaxf(top, piece(i)[r * (DP + 2)]);
-        const float z = top == -INFINITY ? 0.f : top;
-        for (long long i = i0; i <= i1; ++i)
-            if (total * i / G != total * (i + 1) / G) {
-                const float* x = piece(i) + r * (DP + 2);
-                const float f = exp2f(x[0] - z);
-                sum = fmaf(x[1], f, sum);
-                o = fmaf(x[2 + e], f, o);
+        for (int i = 0; i < count; i += 8) {                             // eight pieces' values asked for at once
+            float x[8][3];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const float* p = from + (2 * (long long)(i + s) + (i + s == 0 && begun)) * C::kPiece + r * (DP + 2);
+                x[s][0] = i + s < count ? p[0] : -INFINITY;
+                x[s][1] = i + s < count ? p[1] : 0.f;
+                x[s][2] = i + s < count ? p[2 + e] : 0.f;
             }
+            float to = top;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) to = fmaxf(to, x[s][0]);
+            const float z = to == -INFINITY ? 0.f : to, f = exp2f(top - z);
+            sum *= f;
+            o *= f;
+            top = to;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const float g = exp2f(x[s][0] - z);
+                sum = fmaf(x[s][1], g, sum);
+                o = fmaf(x[s][2], g, o);
+            }
+        }
         out[r * c.d + e] = from_f32<T>(o / sum);
     }
 }
 
-template <typename T> int row_blocks(int Hq, int Hk) { return (Hq / Hk + Cfg<T, 128>::kRows - 1) / Cfg<T, 128>::kRows; }
+template <int R> int row_blocks(int Hq, int Hk) { return (Hq / Hk + R - 1) / R; }
 // CTAs of a launch: what the device holds at a time, or one per unit where there cannot be as many
-template <typename T, int DP> int grid_of(int B, int Hq, int Hk, int page_size, int max_pages) {
-    const long long units = (long long)B * Hk * row_blocks<T>(Hq, Hk) * (((long long)max_pages * page_size + kUnit - 1) / kUnit);
-    const int most = kSMs * Cfg<T, DP>::kPerSm;
+template <typename T, int DP, int R> int grid_of(int B, int Hq, int Hk, int page_size, int max_pages) {
+    const long long units = (long long)B * Hk * row_blocks<R>(Hq, Hk) * (((long long)max_pages * page_size + kUnit - 1) / kUnit);
+    const int most = kSMs * Cfg<T, DP, R>::kPerSm;
     return units < most ? (int)units : most;
 }
 
-template <typename T, int DP> based_status launch(const PagedCall& c, void* workspace, cudaStream_t stream) {
-    using C = Cfg<T, DP>;
+template <typename T, int DP, int R> based_status launch(const PagedCall& c, void* workspace, cudaStream_t stream) {
+    using C = Cfg<T, DP, R>;
     static std::atomic<bool> ready[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return BASED_ERR_CUDA;
     if (!ready[dev].load(std::memory_order_acquire)) {
-        if (cudaFuncSetAttribute(paged_decode_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes) != cudaSuccess) return BASED_ERR_CUDA;
+        if (cudaFuncSetAttribute(paged_decode_kernel<T, DP, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes) != cudaSuccess) return BASED_ERR_CUDA;
         ready[dev].store(true, std::memory_order_release);
     }
-    Args a{c, static_cast<float*>(workspace), nullptr, row_blocks<T>(c.Hq, c.Hk), -1};
+    Args a{c, static_cast<float*>(workspace), nullptr, row_blocks<R>(c.Hq, c.Hk), -1, c.page_size % kSub == 0};
     if (error_word_ptr(&a.err) != BASED_OK) return BASED_ERR_CUDA;
     for (int s = 0; s < 31; ++s)
         if (c.page_size == 1 << s) a.shift = s;
-    const int G = grid_of<T, DP>(c.B, c.Hq, c.Hk, c.page_size, c.max_pages);
-    cudaError_t e = launch_ex(paged_decode_kernel<T, DP>, dim3(G), dim3(kThreads), C::kBytes, 1, true, stream, a);
+    const int G = grid_of<T, DP, R>(c.B, c.Hq, c.Hk, c.page_size, c.max_pages);
+    cudaError_t e = launch_ex(paged_decode_kernel<T, DP, R>, dim3(G), dim3(kThreads), C::kBytes, 1, true, stream, a);
     note_launch();
     based_status st = check_launch("paged_decode_kernel");
     if (e != cudaSuccess || st != BASED_OK) return e != cudaSuccess ? BASED_ERR_CUDA : st;
-    e = launch_ex(paged_join_kernel<T, DP>, dim3((unsigned)((long long)c.B * c.Hk * a.blocks)), dim3(kThreads), 0, 1, true, stream, a, G);
+    e = launch_ex(paged_join_kernel<T, DP, R>, dim3((unsigned)((long long)c.B * c.Hk * a.blocks)), dim3(kThreads), 0, 1, true, stream, a, G);
     note_launch();
     st = check_launch("paged_join_kernel");
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
+}
+// f with the kernel's type, width and rows for a call: f(T{}, width, rows) as types
+template <int N> struct Num { static constexpr int value = N; };
+template <typename F> auto for_call(based_dtype io, int d, int group, F f) {
+    if (io == BASED_BF16) return d > 64 ? f(__nv_bfloat16(), Num<128>(), Num<16>()) : f(__nv_bfloat16(), Num<64>(), Num<16>());
+    if (group == 1) return d > 64 ? f(0.f, Num<128>(), Num<1>()) : f(0.f, Num<64>(), Num<1>());
+    if (group <= 4) return d > 64 ? f(0.f, Num<128>(), Num<4>()) : f(0.f, Num<64>(), Num<4>());
+    return d > 64 ? f(0.f, Num<128>(), Num<8>()) : f(0.f, Num<64>(), Num<8>());
 }
 
 // ------------------------------------------------------------------------------------------------ a prompt into its pages
@@ -563,17 +635,17 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const __grid_constant_
 }  // namespace
 
 size_t paged_decode_bytes(int B, int Hq, int Hk, int d, int page_size, int max_pages, based_dtype io) {
-    auto bytes = [&](int G, int piece) { return (size_t)G * 2 * piece * sizeof(float); };
-    if (io == BASED_BF16)
-        return d > 64 ? bytes(grid_of<__nv_bfloat16, 128>(B, Hq, Hk, page_size, max_pages), Cfg<__nv_bfloat16, 128>::kPiece)
-                      : bytes(grid_of<__nv_bfloat16, 64>(B, Hq, Hk, page_size, max_pages), Cfg<__nv_bfloat16, 64>::kPiece);
-    return d > 64 ? bytes(grid_of<float, 128>(B, Hq, Hk, page_size, max_pages), Cfg<float, 128>::kPiece)
-                  : bytes(grid_of<float, 64>(B, Hq, Hk, page_size, max_pages), Cfg<float, 64>::kPiece);
+    return for_call(io, d, Hq / Hk, [&](auto t, auto width, auto rows) {
+        using T = decltype(t);
+        constexpr int W = decltype(width)::value, R = decltype(rows)::value;
+        return (size_t)grid_of<T, W, R>(B, Hq, Hk, page_size, max_pages) * 2 * Cfg<T, W, R>::kPiece * sizeof(float);
+    });
 }
 
 based_status launch_paged_decode(const PagedCall& c, void* workspace, based_dtype io, cudaStream_t stream) {
-    if (io == BASED_BF16) return c.d > 64 ? launch<__nv_bfloat16, 128>(c, workspace, stream) : launch<__nv_bfloat16, 64>(c, workspace, stream);
-    return c.d > 64 ? launch<float, 128>(c, workspace, stream) : launch<float, 64>(c, workspace, stream);
+    return for_call(io, c.d, c.Hq / c.Hk, [&](auto t, auto width, auto rows) {
+        return launch<decltype(t), decltype(width)::value, decltype(rows)::value>(c, workspace, stream);
+    });
 }
 
 based_status launch_paged_write(const PagedWrite& c, based_dtype io, cudaStream_t stream) {
