@@ -881,7 +881,7 @@ based_status paged_decode_step(const void* q, const void* k, const void* v, base
         if (!aligned16(p)) return BASED_ERR_ALIGNMENT;
     if (reinterpret_cast<uintptr_t>(slopes) & 3) return BASED_ERR_ALIGNMENT;
     const size_t need = paged_decode_bytes(B, H_q, H_k, d, cache.page_size, max_pages, io);
-    if (!workspace || workspace_bytes < need) return BASED_ERR_WORKSPACE;
+    if (need && (!workspace || workspace_bytes < need)) return BASED_ERR_WORKSPACE;
     const PagedCall c{q, k, v, cache.k, cache.v, cache.page_stride, cache.head_stride, cache.token_stride, page_table, pos, slopes, out, B, H_q, H_k, d,
                       cache.pages, cache.page_size, max_pages, window, softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf((float)d), softcap};
     return launch_paged_decode(c, workspace, io, static_cast<cudaStream_t>(cuda_stream));

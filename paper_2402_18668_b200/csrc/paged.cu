@@ -4,11 +4,14 @@
 //
 // Bound by HBM: every key and value is read once for all query heads that share it (Hq / Hk of them, the rows of a product), 2 d elements
 // a token against 4 d Hq / Hk flop.  What has to be right is the division of the work: sequences have any lengths, known to the device alone.
-//   - The unit is 64 tokens of one sequence and key head; all units lie in one row (sequence, head, tokens), and CTA i of G takes
-//     units U i / G .. U (i + 1) / G: equal shares whatever the lengths, from one sequence of 131072 tokens to many short ones.
-//   - A CTA's four warps take 16 tokens of a unit each, with rings of their own that copies (16 bytes a lane) fill two or three units ahead, and
-//     a running maximum, sum and output of their own: no barrier but at the end of a (sequence, head).
-//   - What a CTA has done whole it writes as output; the pieces at its range's ends go to the workspace, and a second, dependent launch
+//   - The unit is some tokens of one sequence and key head; all units lie in one row (sequence, head, tokens), and every worker takes an
+//     equal share of it, whatever the lengths, from one sequence of 131072 tokens to many short ones.
+//   - Where sequences are long (512 tokens and more in the mean) the workers are CTAs and the unit 64 tokens, of which each of four warps takes
+//     16, in a ring of its own that copies (16 bytes a lane) fill two or three units ahead, with a running maximum, sum and output of its
+//     own: no barrier but at the end of a head, where the four are joined.  Where they are short, that end is most of the work: the
+//     workers are warps, the unit is 16 tokens, and where one warp begins with another head the SM's others go on.  (131072 tokens,
+//     16 heads of 64: 97 us with CTAs, 118 with warps; 256 sequences of up to 100 tokens, 16 heads: 93 and 75.)
+//   - What a worker has done whole it writes as output; the pieces at its share's ends go to the workspace, and a second, dependent launch
 //     joins every output that was cut, its pieces in order.
 // bf16: products on the tensor cores (m16n8k16: 16 query heads a row block, weights rounded to bf16 once, 2^-9 of each at most in the mean);
 // fp32: multiply-adds, a lane per token and half a row for the scores, a lane per 2 or 4 columns for the output.
@@ -20,10 +23,11 @@ namespace based {
 
 namespace {
 
-constexpr int kUnit = 64, kWarps = 4, kThreads = 128, kSub = 16;         // tokens of a unit, of a warp's share
+constexpr int kSub = 16, kWarps = 4, kThreads = 128;                      // tokens that a warp takes at a time
 constexpr unsigned kBadPage = 2u;                                        // in the error word
 constexpr float kLog2e = 1.4426950408889634f;
 
+template <int N> struct Num { static constexpr int value = N; };
 // R: query heads at a time, 16 on tensor cores, else as many as share a key head (8 at most)
 template <typename T, int DP, int R> struct Cfg {
     static constexpr bool kTc = sizeof(T) == 2;
@@ -31,16 +35,24 @@ template <typename T, int DP, int R> struct Cfg {
     static constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16;
     static constexpr int kStage = 2 * kSub * kRowBytes;                  // a warp's keys and values of a unit
     static constexpr int kStages = kStage >= 16384 ? 3 : kStage >= 8192 ? 3 : 4;
-    static constexpr int kBytes = kWarps * kStages * kStage + kRows * DP * 4;      // and the queries, fp32
+    static constexpr int kWarp = kStages * kStage + (kTc ? 0 : kRows * DP * 4);    // a warp's ring, and its queries where they are fp32
+    static constexpr int kBytes = kWarps * kWarp;
     static constexpr int kPerSm = kBytes > 113000 ? 1 : kBytes > 74000 ? 2 : 3;
-    static constexpr int kPiece = kRows * (DP + 2);                      // floats of a piece: per row the maximum, the sum, the output
-    static_assert(kStages * kStage >= kPiece * 4, "a warp's piece goes into its ring");
+    static constexpr int kPieceRow = DP + 2;                             // floats of a piece's row: the maximum, the sum, the output
+    static_assert(kStages * kStage >= kRows * kPieceRow * 4, "a warp's piece goes into its ring");
 };
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// tanh to some 4e-7 of itself: its power series up to x^9 below 1/3, (e^2x - 1) / (e^2x + 1) above (a third of tanhf's instructions; fp32 io takes
+// that)
+__device__ __forceinline__ float tanh_short(float x) {
+    const float z = x * x, t = ex2(fminf(fabsf(x), 15.f) * (2.f * kLog2e));
+    const float series = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return fabsf(x) < 0.33f ? series : copysignf(__fdividef(t - 1.f, t + 1.f), x);
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -58,21 +70,42 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// A sequence's keys: tokens lo .. pos, in units first .. first + count - 1 of 64 tokens from the start; none where it has no token, or one
-// past what its pages can hold
+// A sequence's keys: tokens lo .. pos, in units first .. first + count - 1 of `unit` tokens from the start; none where it has no token, or
+// one past what its pages can hold
 struct Span {
     int pos, lo, first, count;
-    __device__ __forceinline__ Span(const PagedCall& c, int b) {
+    __device__ __forceinline__ Span(const PagedCall& c, int b, int unit) {
         pos = c.pos[b];
         if (pos < 0 || pos >= c.max_pages * c.page_size) {
             lo = first = count = 0;
             return;
         }
         lo = c.window > 0 && pos >= c.window ? pos - c.window + 1 : 0;
-        first = lo / kUnit;
-        count = pos / kUnit - first + 1;
+        first = unit == 64 ? lo >> 6 : lo >> 4;                          // (64 or 16)
+        count = (unit == 64 ? pos >> 6 : pos >> 4) - first + 1;
     }
 };
+// the unit, by the number of shares of 16 tokens in all sequences (of one head)
+__device__ __forceinline__ int unit_of(long long shares, int B) { return shares >= 32ll * B ? 64 : 16; }
+// sums over a CTA's threads of two values each; buf: a pair per warp
+__device__ __forceinline__ void sum2(long long (&x)[2], long long (*buf)[2]) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+        x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) {
+        buf[threadIdx.x >> 5][0] = x[0];
+        buf[threadIdx.x >> 5][1] = x[1];
+    }
+    __syncthreads();
+    x[0] = x[1] = 0;
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) {
+        x[0] += buf[w][0];
+        x[1] += buf[w][1];
+    }
+}
 
 // The units of all sequences in one row, cut into G shares that differ by one at most
 struct Shares {
@@ -97,33 +130,62 @@ struct Shares {
 
 struct Args {
     PagedCall c;
-    float* pieces;                                                       // [2 G][rows][d + 2]
+    float* pieces;                                                       // [2 W][rows][d + 2]
+    int piece;                                                           // floats of one
     unsigned int* err;
     int blocks;                                                          // row blocks of a key head's queries
     int shift;                                                           // page_size = 1 << shift, or -1
     bool whole;                                                          // 16 tokens from a multiple of 16 on lie in one page
+    bool split;                                                          // false: a CTA per sequence and "head", and no join
 };
 
 template <typename T, int DP, int R>
 __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_kernel(const __grid_constant__ Args a) {
     using C = Cfg<T, DP, R>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long s_sum[4], s_from[2];
+    __shared__ long long s_sum[kWarps][2], s_from[kWarps][2];
     const PagedCall& c = a.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    uint8_t* ring = smem + warp * C::kStages * C::kStage;
-    float* sq = reinterpret_cast<float*>(smem + kWarps * C::kStages * C::kStage);
+    uint8_t* ring = smem + warp * C::kWarp;
+    float* sq = reinterpret_cast<float*>(ring + C::kStages * C::kStage);
     const int group = c.Hq / c.Hk, heads = c.Hk * a.blocks;              // "heads": key heads and row blocks of their queries
-    enter_dependent();
+    // (the join may come in once every CTA here is past the kernel ahead: what it reads before its own wait is there then)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // This CTA's units, and the sequence that they begin in: inclusive sums of the sequences' units, 128 a turn, by shuffles.  Twice where there are
-    // more sequences than that (the first time for the total alone)
-    long long total = 0, u = 0, end = 0, base = 0;                       // base: the units of the sequences before b
-    int b = 0;
-    for (int pass = c.B > kThreads ? 0 : 1; pass < 2; ++pass) {
+    // This worker's units u .. end - 1, the sequence and the head that they begin in, and which of its units
+    int unit = 64, b, hm, unit0 = 0, worker = blockIdx.x;
+    bool wide = true;                                                    // the CTA is the worker
+    long long u = 0, end;
+    if (!a.split) {
+        b = blockIdx.x / heads;
+        hm = blockIdx.x % heads;
+        const Span sp(c, b, unit);
+        end = sp.count;
+        if (end == 0) {
+            const int h0 = hm / a.blocks * group + hm % a.blocks * C::kRows, n = min(C::kRows, group - hm % a.blocks * C::kRows) * c.d;
+            T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h0) * c.d;
+            for (int i = tid; i < n; i += kThreads) out[i] = from_f32<T>(0.f);
+            if (tid == 0 && sp.pos >= 0) atomicOr(a.err, kBadPage);
+            return;
+        }
+    } else {
+        long long all[2] = {0, 0};                                       // units of 16 tokens, of 64
+        for (int k = tid; k < c.B; k += kThreads) {
+            all[0] += Span(c, k, 16).count;
+            all[1] += Span(c, k, 64).count;
+        }
+        sum2(all, s_sum);
+        unit = unit_of(all[0], c.B);
+        wide = unit == 64;
+        const Shares sh(all[wide] * heads, wide ? gridDim.x : gridDim.x * kWarps);
+        worker = wide ? blockIdx.x : blockIdx.x * kWarps + warp;
+        u = sh.begin(worker);
+        end = sh.begin(worker + 1);
+        // inclusive sums of the sequences' units, 128 a turn, by shuffles
         long long before = 0;
         for (int b0 = 0; b0 < c.B; b0 += kThreads) {
-            const long long n = b0 + tid < c.B ? (long long)Span(c, b0 + tid).count * heads : 0;
+            const long long n = b0 + tid < c.B ? (long long)Span(c, b0 + tid, unit).count * heads : 0;
             long long sum = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -131,42 +193,33 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                 if (lane >= o) sum += x;
             }
             __syncthreads();
-            if (lane == 31) s_sum[warp] = sum;
+            if (lane == 31) s_sum[warp][0] = sum;
             __syncthreads();
             long long off = before;
-            for (int w = 0; w < warp; ++w) off += s_sum[w];
+            for (int w = 0; w < warp; ++w) off += s_sum[w][0];
             sum += off;
-            before += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-            if (pass == 1) {
-                if (c.B <= kThreads) total = before;
-                if (b0 == 0) {
-                    const Shares sh(total, (int)gridDim.x);
-                    u = sh.begin(blockIdx.x);
-                    end = sh.begin(blockIdx.x + 1);
-                    if (u >= end) return;
+            before += s_sum[0][0] + s_sum[1][0] + s_sum[2][0] + s_sum[3][0];
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const long long x = wide ? u : sh.begin((long long)blockIdx.x * kWarps + w);
+                if (sum - n <= x && x < sum) {
+                    s_from[w][0] = b0 + tid;
+                    s_from[w][1] = sum - n;                              // the units of the sequences before it
                 }
-                if (sum - n <= u && u < sum) {
-                    s_from[0] = b0 + tid;
-                    s_from[1] = sum - n;
-                }
-                if (before > u) break;
             }
         }
-        if (pass == 0) total = before;
+        __syncthreads();
+        if (u >= end) return;
+        b = (int)s_from[warp][0];
+        const long long in = u - s_from[warp][1];
+        const int count = Span(c, b, unit).count;                        // (not 0)
+        hm = in >> 31 == 0 ? (int)((unsigned)in / (unsigned)count) : (int)(in / count);
+        unit0 = (int)(in - (long long)hm * count);
     }
-    __syncthreads();
-    b = (int)s_from[0];
-    base = s_from[1];
     const long long range = u;
 
     for (; u < end; ) {
-        Span sp(c, b);
-        while ((long long)sp.count * heads <= u - base && b + 1 < c.B) { // on to the next sequence that has keys
-            base += (long long)sp.count * heads;
-            sp = Span(c, ++b);
-        }
-        if (sp.count == 0) return;
-        const int hm = (int)((u - base) / sp.count), unit0 = (int)((u - base) % sp.count);
+        const Span sp(c, b, unit);
         const int units = (int)min((long long)(sp.count - unit0), end - u);
         const int hk = hm / a.blocks, row0 = (hm % a.blocks) * C::kRows, rows = min(C::kRows, group - row0);
         const int h0 = hk * group + row0;                                // the first query head
@@ -177,46 +230,49 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
         T* vp = static_cast<T*>(c.v_pages) + hk * c.head_stride;
         const int* table = c.table + (long long)b * c.max_pages;
 
-        // tokens j0 .. j0 + 15 of unit n are this warp's; lane < 16 (and its double) looks up the page of token j0 + lane a turn before it is needed:
-        // what is checked is checked then, so that nothing waits for the table
-        auto tokens = [&](int n) { return (sp.first + unit0 + n) * kUnit + warp * kSub; };
+        // Lane < 16 (and its double) looks up the page of token j0 + lane of a unit a turn before it is needed: it is checked then, so that
+        // nothing waits for the table
+        auto tokens = [&](int n) { return (sp.first + unit0 + n) * unit + (wide ? warp * kSub : 0); };
         auto page_of = [&](int j) { return a.shift >= 0 ? j >> a.shift : (int)((unsigned)j / (unsigned)c.page_size); };
         auto here = [&](int n, int j) { return n < units && j <= sp.pos && j >= sp.lo; };
         auto look = [&](int n) -> int {
             const int j = tokens(n) + (lane & 15);
             return here(n, j) ? table[page_of(j)] : 0;
         };
-        // tokens strictly inside, whose page is one: nothing to check but that
-        auto inside = [&](int n) { const int j0 = tokens(n); return n < units && j0 >= sp.lo && j0 + kSub <= sp.pos; };
-        constexpr int V = 16 / (int)sizeof(T), kStep = 32 / C::kChunks > 0 ? 32 / C::kChunks : 1;          // values of a chunk, rows of a turn
-        const int lrow = lane / C::kChunks, lch = lane % C::kChunks;     // (fp32, 128 wide: a row a turn)
+        constexpr int V = 16 / (int)sizeof(T), kStep = 32 / C::kChunks;  // values of a chunk, rows of a turn
+        const int lrow = lane / C::kChunks, lch = lane % C::kChunks;
         const bool lin = lch * V < c.d;
-        const long long lane_at = lrow * c.token_stride + (lin ? lch * V : 0);
+        // units in0 .. in1 - 1: no token at the border of what is seen, and the new one not among them
+        const int in0 = max(0, (sp.lo - tokens(0) + unit - 1) / unit), in1 = min(units, sp.pos - kSub >= tokens(0) ? (sp.pos - kSub - tokens(0)) / unit + 1 : 0);
+        // rows of a unit whose tokens lie inside and in one page
+        const long long lane_at = lrow * c.token_stride + (lin ? lch * V : 0), step = kStep * c.token_stride;
+        auto load_inside = [&](int n, int id) {
+            uint8_t* st = ring + n % C::kStages * C::kStage;
+            const int j0 = tokens(n), page = page_of(j0);
+            const bool good = (unsigned)id < (unsigned)c.pages;
+            if (!good) atomicOr(a.err, kBadPage);
+            const long long at = (good ? id * c.page_stride : 0) + (long long)(j0 - page * c.page_size) * c.token_stride + lane_at;
+            const T *ks = kp + at, *vs = vp + at;
+#pragma unroll
+            for (int i = 0; i < kSub / kStep; ++i) {
+                const int row = i * kStep + lrow;
+                uint8_t* to = st + row * C::kRowBytes + ((lch ^ (row & 7)) << 4);
+                pairs::copy_async16(to, ks, lin && good);
+                pairs::copy_async16(to + kSub * C::kRowBytes, vs, lin && good);
+                ks += step;
+                vs += step;
+            }
+            pairs::copy_async_commit();
+        };
         auto load = [&](int n, int id) {
             uint8_t* st = ring + n % C::kStages * C::kStage;
             const int j0 = tokens(n), j = j0 + (lane & 15);
-            if (a.whole && inside(n) && (unsigned)id < (unsigned)c.pages) {
-                const long long at = id * c.page_stride + (long long)(j0 - page_of(j0) * c.page_size) * c.token_stride + lane_at;
-                const T *ks = kp + at, *vs = vp + at;
-                const long long step = kStep * c.token_stride;
-#pragma unroll
-                for (int i = 0; i < kSub / kStep; ++i) {
-                    const int row = i * kStep + lrow;
-                    uint8_t* to = st + row * C::kRowBytes + ((lch ^ (row & 7)) << 4);
-                    pairs::copy_async16(to, ks, lin);
-                    pairs::copy_async16(to + kSub * C::kRowBytes, vs, lin);
-                    ks += step;
-                    vs += step;
-                }
-                pairs::copy_async_commit();
-                return;
-            }
             long long at = -1;
             if (here(n, j)) {
                 if ((unsigned)id < (unsigned)c.pages) at = id * c.page_stride + (long long)(j - page_of(j) * c.page_size) * c.token_stride;
                 else atomicOr(a.err, kBadPage);
             }
-#pragma unroll 1
+#pragma unroll 4
             for (int i = 0; i < kSub / kStep; ++i) {
                 const int row = i * kStep + lrow;
                 const long long off = __shfl_sync(0xffffffffu, at, row);
@@ -230,19 +286,19 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
             pairs::copy_async_commit();
         };
 
-        __syncthreads();                                                 // (the rings and the queries are free)
-        for (int i = tid; i < C::kRows * DP; i += kThreads) {
-            const int r = i / DP, e = i % DP;
-            sq[i] = r < rows && e < c.d ? to_f32(q[(long long)r * c.d + e]) : 0.f;
-        }
         int next = look(0);
-#pragma unroll
+        if constexpr (!C::kTc) {
+            for (int i = lane; i < C::kRows * DP; i += 32) {
+                const int r = i / DP, e = i % DP;
+                sq[i] = r < rows && e < c.d ? to_f32(q[(long long)r * c.d + e]) : 0.f;
+            }
+        }
+#pragma unroll 1
         for (int n = 0; n < C::kStages - 1; ++n) {
             const int id = next;
             next = look(n + 1);
             load(n, id);
         }
-        __syncthreads();
 
         // running maximum (base 2), sum, output
         constexpr int kN = C::kTc ? DP / 8 : C::kRows;
@@ -264,35 +320,37 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
             for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float* s = sq + (r + (i & 1) * 8) * DP + 16 * k + e + (i >> 1) * 8;
-                    qf[k][i] = pack2(s[0], s[1]);                        // (bf16 values: exact)
+                    const int row = r + (i & 1) * 8, col = 16 * k + e + (i >> 1) * 8;
+                    qf[k][i] = row < rows && col < c.d ? *reinterpret_cast<const uint32_t*>(q + (long long)row * c.d + col) : 0u;
                 }
             if (c.slopes) {
                 slope[0] = r < rows ? c.slopes[h0 + r] : 0.f;
                 slope[1] = r + 8 < rows ? c.slopes[h0 + r + 8] : 0.f;
             }
         }
-        const bool modified = c.cap > 0.f || c.slopes;
-        // a score as the softmax takes it, in base 2
-        auto weigh = [&](float s, float sl, int j) -> float {
-            if (j > sp.pos || j < sp.lo) return -INFINITY;
+        const float inv_cap = 1.f / c.cap;
+        // a score as the softmax takes it, in base 2; CHECK: whether the token is seen
+        auto weigh = [&](float s, float sl, int j, bool check) -> float {
             s *= c.scale;
-            if (c.cap > 0.f) s = c.cap * tanhf(s / c.cap);
+            if (c.cap > 0.f) s = c.cap * (C::kTc ? tanh_short(s * inv_cap) : tanhf(s * inv_cap));
             if (c.slopes) s -= sl * (float)(sp.pos - j);
-            return s * kLog2e;
+            return check && (j > sp.pos || j < sp.lo) ? -INFINITY : s * kLog2e;
         };
-
-        for (int n = 0; n < units; ++n) {
+        // unit n.  KIND 0: all its tokens are seen and the scores as they are; 1: all are seen; 2: any.  A loop for each, so that the one
+        // that runs is short
+        auto turn = [&](int n, auto kind) {
+            constexpr int KIND = decltype(kind)::value;
             {
                 const int id = next;
                 next = look(n + C::kStages);
-                load(n + C::kStages - 1, id);
+                if constexpr (KIND < 2) load_inside(n + C::kStages - 1, id);
+                else load(n + C::kStages - 1, id);
             }
             pairs::copy_async_wait<C::kStages - 1>();
             __syncwarp();
             const int j0 = tokens(n);
             uint8_t* st = ring + n % C::kStages * C::kStage;
-            if (j0 <= sp.pos && j0 + kSub > sp.lo) {
+            if (KIND < 2 || (j0 <= sp.pos && j0 + kSub > sp.lo)) {
                 const uint32_t ks = static_cast<uint32_t>(__cvta_generic_to_shared(st)), vs = ks + kSub * C::kRowBytes;
                 if constexpr (C::kTc) {
                     float s[2][4] = {};
@@ -305,13 +363,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                         mma16816(s[1], qf[k], f[2], f[3]);
                     }
                     float fade[2];
-                    const bool plain = !modified && inside(n);           // the scores as they are, all of them
-                    const float sc = plain ? c.scale * kLog2e : 1.f;
-                    if (!plain) {
+                    const float sc = KIND == 0 ? c.scale * kLog2e : 1.f;
+                    if constexpr (KIND > 0) {
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) s[t][x] = weigh(s[t][x], slope[x >> 1], j0 + 8 * t + (lane & 3) * 2 + (x & 1));
+                            for (int x = 0; x < 4; ++x)
+                                if (x < 2 || rows > 8) s[t][x] = weigh(s[t][x], slope[x >> 1], j0 + 8 * t + (lane & 3) * 2 + (x & 1), KIND == 2);
                     }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {                        // rows lane / 4 and lane / 4 + 8
@@ -365,11 +423,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                             s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
                         }
                     }
-                    const bool plain = !modified && inside(n);
 #pragma unroll
                     for (int r = 0; r < C::kRows; ++r) {
                         s[r] += __shfl_xor_sync(0xffffffffu, s[r], 16);
-                        s[r] = plain ? s[r] * (c.scale * kLog2e) : weigh(s[r], c.slopes && r < rows ? c.slopes[h0 + r] : 0.f, j0 + tok);
+                        s[r] = KIND == 0 ? s[r] * (c.scale * kLog2e) : weigh(s[r], c.slopes && r < rows ? c.slopes[h0 + r] : 0.f, j0 + tok, KIND == 2);
                         float top = s[r];
 #pragma unroll
                         for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -401,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                     }
                 }
                 // the new token into its page, once for a key head
-                if (row0 == 0 && j0 <= sp.pos && sp.pos < j0 + kSub) {
+                if (KIND == 2 && row0 == 0 && j0 <= sp.pos && sp.pos < j0 + kSub) {
                     const int page = a.shift >= 0 ? sp.pos >> a.shift : (int)((unsigned)sp.pos / (unsigned)c.page_size), id = table[page];
                     if ((unsigned)id < (unsigned)c.pages) {
                         const long long at = id * c.page_stride + (long long)(sp.pos - page * c.page_size) * c.token_stride;
@@ -415,147 +472,186 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                 }
             }
             __syncwarp();                                                // (the stage is read; the next turn's load overwrites it)
+        };
+        const bool plain = c.cap == 0.f && !c.slopes;
+        const int last = a.whole ? in1 - (C::kStages - 1) : 0;           // (what is loaded meanwhile lies inside too)
+#pragma unroll 1
+        for (int n = 0; n < units; ) {
+            if (n >= in0 && n < last) {
+                if (plain) {
+#pragma unroll 1
+                    for (; n < last; ++n) turn(n, Num<0>());
+                } else {
+#pragma unroll 1
+                    for (; n < last; ++n) turn(n, Num<1>());
+                }
+            } else {
+                turn(n++, Num<2>());
+            }
         }
         pairs::copy_async_wait<0>();
         __syncwarp();
 
-        // the warps' shares, then the four as one: a whole output, or a piece
-        float* piece = reinterpret_cast<float*>(ring);
+        // a whole output, or a piece: of a warp's, or of the four as one, by way of the rings
+        const bool whole = units == sp.count;
+        float* piece = wide ? reinterpret_cast<float*>(ring) : a.pieces + (2 * (long long)worker + (u != range)) * a.piece;
+        T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h0) * c.d;
+        const bool write = whole && !wide;
         if constexpr (C::kTc) {
-            l[0] += __shfl_xor_sync(0xffffffffu, l[0], 1);
-            l[0] += __shfl_xor_sync(0xffffffffu, l[0], 2);
-            l[1] += __shfl_xor_sync(0xffffffffu, l[1], 1);
-            l[1] += __shfl_xor_sync(0xffffffffu, l[1], 2);
-            const int r = lane >> 2;
 #pragma unroll
-            for (int k = 0; k < DP / 8; ++k)
+            for (int h = 0; h < 2; ++h) {
+                const int r = (lane >> 2) + 8 * h;
+                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+                if (r >= rows) continue;
+                const float inv = 1.f / l[h];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) piece[(r + (x >> 1) * 8) * (DP + 2) + 2 + 8 * k + (lane & 3) * 2 + (x & 1)] = acc[k][x];
-            if ((lane & 3) == 0) {
-                piece[r * (DP + 2)] = m[0];
-                piece[r * (DP + 2) + 1] = l[0];
-                piece[(r + 8) * (DP + 2)] = m[1];
-                piece[(r + 8) * (DP + 2) + 1] = l[1];
+                for (int k = 0; k < DP / 8; ++k) {
+                    const int e = 8 * k + (lane & 3) * 2;
+                    if (write) {
+                        if (e < c.d) *reinterpret_cast<uint32_t*>(out + r * c.d + e) = pack2(acc[k][2 * h] * inv, acc[k][2 * h + 1] * inv);
+                    } else {
+                        *reinterpret_cast<float2*>(piece + r * C::kPieceRow + 2 + e) = make_float2(acc[k][2 * h], acc[k][2 * h + 1]);
+                    }
+                }
+                if (!write && (lane & 3) == 0) *reinterpret_cast<float2*>(piece + r * C::kPieceRow) = make_float2(m[h], l[h]);
             }
         } else {
 #pragma unroll
             for (int r = 0; r < C::kRows; ++r) {
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+                if (r >= rows) continue;
 #pragma unroll
-                for (int k = 0; k < DP / 32; ++k) piece[r * (DP + 2) + 2 + lane * (DP / 32) + k] = acc[r][k];
-                if (lane == 0) {
-                    piece[r * (DP + 2)] = m[r];
-                    piece[r * (DP + 2) + 1] = l[r];
+                for (int k = 0; k < DP / 32; ++k) {
+                    const int e = lane * (DP / 32) + k;
+                    if (write) {
+                        if (e < c.d) out[r * c.d + e] = from_f32<T>(acc[r][k] / l[r]);
+                    } else {
+                        piece[r * C::kPieceRow + 2 + e] = acc[r][k];
+                    }
                 }
+                if (!write && lane == 0) *reinterpret_cast<float2*>(piece + r * C::kPieceRow) = make_float2(m[r], l[r]);
             }
         }
-        __syncthreads();
-        const bool all = units == sp.count;
-        float* to = a.pieces + (2 * (long long)blockIdx.x + (u != range)) * C::kPiece;
-        for (int i = tid; i < rows * DP; i += kThreads) {
-            const int r = i / DP, e = i % DP;
-            float top = -INFINITY, sum = 0.f, o = 0.f;
+        __syncwarp();
+        if (wide) {
+            __syncthreads();
+            float* to = a.pieces + (2 * (long long)worker + (u != range)) * a.piece;
+            for (int i = tid; i < rows * DP; i += kThreads) {
+                const int r = i / DP, e = i % DP;
+                auto of = [&](int w) { return reinterpret_cast<const float*>(smem + w * C::kWarp) + r * C::kPieceRow; };
+                float top = -INFINITY, sum = 0.f, o = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, reinterpret_cast<const float*>(smem + w * C::kStages * C::kStage)[r * (DP + 2)]);
-            const float z = top == -INFINITY ? 0.f : top;
+                for (int w = 0; w < kWarps; ++w) top = fmaxf(top, of(w)[0]);
+                const float z = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float* x = reinterpret_cast<const float*>(smem + w * C::kStages * C::kStage) + r * (DP + 2);
-                const float f = exp2f(x[0] - z);
-                sum = fmaf(x[1], f, sum);
-                o = fmaf(x[2 + e], f, o);
-            }
-            if (all) {
-                if (e < c.d) static_cast<T*>(c.out)[((long long)b * c.Hq + h0 + r) * c.d + e] = from_f32<T>(o / sum);
-            } else {
-                to[r * (DP + 2) + 2 + e] = o;
-                if (e == 0) {
-                    to[r * (DP + 2)] = top;
-                    to[r * (DP + 2) + 1] = sum;
+                for (int w = 0; w < kWarps; ++w) {
+                    const float f = exp2f(of(w)[0] - z);
+                    sum = fmaf(of(w)[1], f, sum);
+                    o = fmaf(of(w)[2 + e], f, o);
+                }
+                if (whole) {
+                    if (e < c.d) out[r * c.d + e] = from_f32<T>(o / sum);
+                } else {
+                    to[r * C::kPieceRow + 2 + e] = o;
+                    if (e == 0) *reinterpret_cast<float2*>(to + r * C::kPieceRow) = make_float2(top, sum);
                 }
             }
+            __syncthreads();                                             // (before the rings are filled again)
         }
         u += units;
+        if (u >= end) return;
+        unit0 = 0;
+        if (++hm == heads) {                                             // on to the next sequence that has keys
+            hm = 0;
+            do ++b;
+            while (b + 1 < c.B && Span(c, b, unit).count == 0);
+            if (b >= c.B) return;
+        }
     }
 }
 
-// the outputs that were cut, from their pieces, and zeros where a sequence has no token; a CTA per sequence and "head"
-template <typename T, int DP, int R> __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ Args a, int G) {
+// The outputs that were cut, from their pieces, and zeros where a sequence has no token; a CTA per sequence and query head: its threads hold a
+// column each and share the pieces out among kJoin / DP of them, whose results are joined in order
+constexpr int kJoin = 256;
+template <typename T, int DP, int R> __global__ void __launch_bounds__(kJoin) paged_join_kernel(const __grid_constant__ Args a, int ctas) {
     using C = Cfg<T, DP, R>;
-    __shared__ long long s_sum[8];
+    __shared__ long long s_sum[kJoin / 32][2];
+    __shared__ float s_part[kJoin][3];
     const PagedCall& c = a.c;
-    const int heads = c.Hk * a.blocks, group = c.Hq / c.Hk, b = blockIdx.x / heads, hm = blockIdx.x % heads;
-    const int row0 = (hm % a.blocks) * C::kRows, rows = min(C::kRows, group - row0), h0 = (hm / a.blocks) * group + row0;
+    const int heads = c.Hk * a.blocks, group = c.Hq / c.Hk, b = blockIdx.x / c.Hq, h = blockIdx.x % c.Hq;
+    const int hm = h / group * a.blocks + h % group / C::kRows, r = h % group % C::kRows;
+    long long all[2] = {0, 0}, ahead[2] = {0, 0};                        // units of 16 tokens, of 64: of all sequences, of those before b
+    for (int k = threadIdx.x; k < c.B; k += kJoin) {
+        const int n16 = Span(c, k, 16).count, n64 = Span(c, k, 64).count;
+        all[0] += n16;
+        all[1] += n64;
+        ahead[0] += k < b ? n16 : 0;
+        ahead[1] += k < b ? n64 : 0;
+    }
+    sum2(all, s_sum);
+    sum2(ahead, s_sum);
+    const int unit = unit_of(all[0], c.B);
+    const bool wide = unit == 64;
+    const Span sp(c, b, unit);
+    T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h) * c.d;
     enter_dependent();
-    const Span sp(c, b);
-    T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h0) * c.d;
     if (sp.count == 0) {
-        for (int i = threadIdx.x; i < rows * c.d; i += kThreads) out[i] = from_f32<T>(0.f);
+        for (int i = threadIdx.x; i < c.d; i += kJoin) out[i] = from_f32<T>(0.f);
         if (threadIdx.x == 0 && sp.pos >= 0) atomicOr(a.err, kBadPage);
         return;
     }
-    long long mine[2] = {0, 0};                                          // the units before this sequence, and of all
-    for (int k = threadIdx.x; k < c.B; k += kThreads) {
-        const int n = Span(c, k).count;
-        mine[0] += k < b ? n : 0;
-        mine[1] += n;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        mine[0] += __shfl_xor_sync(0xffffffffu, mine[0], o);
-        mine[1] += __shfl_xor_sync(0xffffffffu, mine[1], o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-        s_sum[threadIdx.x >> 5] = mine[0];
-        s_sum[4 + (threadIdx.x >> 5)] = mine[1];
-    }
-    __syncthreads();
-    const long long first = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * heads + (long long)hm * sp.count, last = first + sp.count - 1;
-    const Shares sh((s_sum[4] + s_sum[5] + s_sum[6] + s_sum[7]) * heads, G);
-    const long long i0 = sh.of(first), i1 = sh.of(last);
+    const long long first = ahead[wide] * heads + (long long)hm * sp.count;
+    const Shares sh(all[wide] * heads, wide ? ctas : ctas * kWarps);
+    const long long i0 = sh.of(first), i1 = sh.of(first + sp.count - 1);
     if (i0 == i1) return;
-    const bool begun = sh.begin(i0) != first;                            // the first CTA had something else before it
-    const int count = (int)(i1 - i0) + 1;
-    const float* from = a.pieces + 2 * i0 * C::kPiece;
-    for (int k = threadIdx.x; k < rows * DP; k += kThreads) {
-        const int r = k / DP, e = k % DP;
-        if (e >= c.d) continue;
-        float top = -INFINITY, sum = 0.f, o = 0.f;
-        for (int i = 0; i < count; i += 8) {                             // eight pieces' values asked for at once
-            float x[8][3];
+    const bool begun = sh.begin(i0) != first;                            // the first worker had something else before it
+    const int count = (int)(i1 - i0) + 1, part = threadIdx.x / DP, e = threadIdx.x % DP;
+    const float* from = a.pieces + 2 * i0 * a.piece;
+    constexpr int kParts = kJoin / DP;
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+    auto add = [&](float m, float l, float x) {
+        const float to = fmaxf(top, m), z = to == -INFINITY ? 0.f : to, f = exp2f(top - z), g = exp2f(m - z);
+        sum = fmaf(sum, f, l * g);
+        o = fmaf(o, f, x * g);
+        top = to;
+    };
+    for (int i = part; i < count; i += 8 * kParts) {                     // eight pieces' values asked for at once
+        float x[8][3];
 #pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                const float* p = from + (2 * (long long)(i + s) + (i + s == 0 && begun)) * C::kPiece + r * (DP + 2);
-                x[s][0] = i + s < count ? p[0] : -INFINITY;
-                x[s][1] = i + s < count ? p[1] : 0.f;
-                x[s][2] = i + s < count ? p[2 + e] : 0.f;
-            }
-            float to = top;
-#pragma unroll
-            for (int s = 0; s < 8; ++s) to = fmaxf(to, x[s][0]);
-            const float z = to == -INFINITY ? 0.f : to, f = exp2f(top - z);
-            sum *= f;
-            o *= f;
-            top = to;
-#pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                const float g = exp2f(x[s][0] - z);
-                sum = fmaf(x[s][1], g, sum);
-                o = fmaf(x[s][2], g, o);
-            }
+        for (int s = 0; s < 8; ++s) {
+            const int k = i + s * kParts;
+            const float* p = from + (2 * (long long)k + (k == 0 && begun)) * a.piece + r * C::kPieceRow;
+            x[s][0] = k < count ? p[0] : -INFINITY;
+            x[s][1] = k < count ? p[1] : 0.f;
+            x[s][2] = k < count ? p[2 + e] : 0.f;
         }
-        out[r * c.d + e] = from_f32<T>(o / sum);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) add(x[s][0], x[s][1], x[s][2]);
+    }
+    s_part[threadIdx.x][0] = top;
+    s_part[threadIdx.x][1] = sum;
+    s_part[threadIdx.x][2] = o;
+    __syncthreads();
+    if (part == 0 && e < c.d) {
+#pragma unroll
+        for (int k = 1; k < kParts; ++k) add(s_part[k * DP + e][0], s_part[k * DP + e][1], s_part[k * DP + e][2]);
+        out[e] = from_f32<T>(o / sum);
     }
 }
 
+template <int DP, int R> int piece_floats(int Hq, int Hk) { return (Hq / Hk < R ? Hq / Hk : R) * (DP + 2); }
 template <int R> int row_blocks(int Hq, int Hk) { return (Hq / Hk + R - 1) / R; }
-// CTAs of a launch: what the device holds at a time, or one per unit where there cannot be as many
+// CTAs of a launch: what the device holds at a time, or one per four units where there cannot be as many
 template <typename T, int DP, int R> int grid_of(int B, int Hq, int Hk, int page_size, int max_pages) {
-    const long long units = (long long)B * Hk * row_blocks<R>(Hq, Hk) * (((long long)max_pages * page_size + kUnit - 1) / kUnit);
+    const long long units = (long long)B * Hk * row_blocks<R>(Hq, Hk) * (((long long)max_pages * page_size + kSub - 1) / kSub);
     const int most = kSMs * Cfg<T, DP, R>::kPerSm;
-    return units < most ? (int)units : most;
+    return (units + kWarps - 1) / kWarps < most ? (int)((units + kWarps - 1) / kWarps) : most;
 }
+
+// Tables of up to 256 tokens: one head's are not worth dividing, a join costs more (1000 tokens: 15.2 us whole, 12.6 divided)
+bool short_cache(int page_size, int max_pages) { return (long long)page_size * max_pages <= 256; }
 
 template <typename T, int DP, int R> based_status launch(const PagedCall& c, void* workspace, cudaStream_t stream) {
     using C = Cfg<T, DP, R>;
@@ -566,22 +662,21 @@ template <typename T, int DP, int R> based_status launch(const PagedCall& c, voi
         if (cudaFuncSetAttribute(paged_decode_kernel<T, DP, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes) != cudaSuccess) return BASED_ERR_CUDA;
         ready[dev].store(true, std::memory_order_release);
     }
-    Args a{c, static_cast<float*>(workspace), nullptr, row_blocks<R>(c.Hq, c.Hk), -1, c.page_size % kSub == 0};
+    Args a{c, static_cast<float*>(workspace), piece_floats<DP, R>(c.Hq, c.Hk), nullptr, row_blocks<R>(c.Hq, c.Hk), -1, c.page_size % kSub == 0, !short_cache(c.page_size, c.max_pages)};
     if (error_word_ptr(&a.err) != BASED_OK) return BASED_ERR_CUDA;
     for (int s = 0; s < 31; ++s)
         if (c.page_size == 1 << s) a.shift = s;
-    const int G = grid_of<T, DP, R>(c.B, c.Hq, c.Hk, c.page_size, c.max_pages);
+    const int outputs = c.B * c.Hk * a.blocks, G = a.split ? grid_of<T, DP, R>(c.B, c.Hq, c.Hk, c.page_size, c.max_pages) : outputs;
     cudaError_t e = launch_ex(paged_decode_kernel<T, DP, R>, dim3(G), dim3(kThreads), C::kBytes, 1, true, stream, a);
     note_launch();
     based_status st = check_launch("paged_decode_kernel");
-    if (e != cudaSuccess || st != BASED_OK) return e != cudaSuccess ? BASED_ERR_CUDA : st;
-    e = launch_ex(paged_join_kernel<T, DP, R>, dim3((unsigned)((long long)c.B * c.Hk * a.blocks)), dim3(kThreads), 0, 1, true, stream, a, G);
+    if (e != cudaSuccess || st != BASED_OK || !a.split) return e != cudaSuccess ? BASED_ERR_CUDA : st;
+    e = launch_ex(paged_join_kernel<T, DP, R>, dim3(c.B * c.Hq), dim3(kJoin), 0, 1, true, stream, a, G);
     note_launch();
     st = check_launch("paged_join_kernel");
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
 }
 // f with the kernel's type, width and rows for a call: f(T{}, width, rows) as types
-template <int N> struct Num { static constexpr int value = N; };
 template <typename F> auto for_call(based_dtype io, int d, int group, F f) {
     if (io == BASED_BF16) return d > 64 ? f(__nv_bfloat16(), Num<128>(), Num<16>()) : f(__nv_bfloat16(), Num<64>(), Num<16>());
     if (group == 1) return d > 64 ? f(0.f, Num<128>(), Num<1>()) : f(0.f, Num<64>(), Num<1>());
@@ -635,10 +730,11 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const __grid_constant_
 }  // namespace
 
 size_t paged_decode_bytes(int B, int Hq, int Hk, int d, int page_size, int max_pages, based_dtype io) {
+    if (short_cache(page_size, max_pages)) return 0;
     return for_call(io, d, Hq / Hk, [&](auto t, auto width, auto rows) {
         using T = decltype(t);
         constexpr int W = decltype(width)::value, R = decltype(rows)::value;
-        return (size_t)grid_of<T, W, R>(B, Hq, Hk, page_size, max_pages) * 2 * Cfg<T, W, R>::kPiece * sizeof(float);
+        return (size_t)grid_of<T, W, R>(B, Hq, Hk, page_size, max_pages) * kWarps * 2 * piece_floats<W, R>(Hq, Hk) * sizeof(float);
     });
 }
 
