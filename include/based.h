@@ -616,18 +616,18 @@ typedef struct { void *k, *v; long long page_stride, head_stride, token_stride; 
  * are, in whichever sequences; scores, sums and outputs are fp32, in bf16 io the softmax weights are rounded to bf16 once, as operands.  No
  * result depends on the order in which the parts end.
  * Supported: d a multiple of 8 up to 128; H_q a multiple of H_k; any page_size, max_pages * page_size < 2^31; io in {F32, BF16}.
- * workspace: paged_decode_step_workspace_bytes (0 is possible).  out must not alias an input; two sequences must not write to one slot.
+ * workspace: based_paged_decode_step_workspace_bytes (0 is possible).  out must not alias an input; two sequences must not write to one slot.
  */
-based_status paged_decode_step(const void* q, const void* k, const void* v, based_pages cache, const int* page_table, const int* pos,
+based_status based_paged_decode_step(const void* q, const void* k, const void* v, based_pages cache, const int* page_table, const int* pos,
                                const float* slopes, void* out, int B, int H_q, int H_k, int d, int max_pages, int window, float softmax_scale,
                                float softcap, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream);
-size_t paged_decode_step_workspace_bytes(int B, int H_q, int H_k, int d, int page_size, int max_pages, based_dtype io);
+size_t based_paged_decode_step_workspace_bytes(int B, int H_q, int H_k, int d, int page_size, int max_pages, based_dtype io);
 
 /*
  * Copies the keys and values of prompts into their pages: token t < counts[b] (NULL: L) of k, v [B,H,L,d] to position pos[b] + t of sequence
  * b (pos[b] < 0: none of them).  Everything else in the pools stays as it is.  Supported: as above.
  */
-based_status paged_cache_write(based_heads k, based_heads v, based_pages cache, const int* page_table, const int* pos, const int* counts, int B,
+based_status based_paged_cache_write(based_heads k, based_heads v, based_pages cache, const int* page_table, const int* pos, const int* counts, int B,
                                int H, int L, int d, int max_pages, based_dtype io, void* cuda_stream);
 
 /*

@@ -39,7 +39,7 @@ EXPORTS = (
     "based_gated_recurrence_backward", "based_gated_recurrence_backward_workspace_bytes", "based_qk_norm_rotate",
     "based_qk_norm_rotate_backward", "based_qk_norm_rotate_backward_workspace_bytes", "swa_backward", "swa_backward_workspace_bytes",
     "based_decay_attention_forward", "based_decay_attention_workspace_bytes", "based_decay_attention_step", "based_decay_attention_backward",
-    "based_decay_attention_backward_workspace_bytes", "paged_decode_step", "paged_decode_step_workspace_bytes", "paged_cache_write",
+    "based_decay_attention_backward_workspace_bytes", "based_paged_decode_step", "based_paged_decode_step_workspace_bytes", "based_paged_cache_write",
 )
 
 _lib = None
@@ -165,12 +165,12 @@ def lib() -> ctypes.CDLL:
         for name in ("based_decay_attention_workspace_bytes", "based_decay_attention_backward_workspace_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [i] * 7
-        L.paged_decode_step.restype = i
-        L.paged_decode_step.argtypes = [vp, vp, vp, Pages, vp, vp, vp, vp, i, i, i, i, i, i, f, f, i, vp, sz, vp]
-        L.paged_decode_step_workspace_bytes.restype = sz
-        L.paged_decode_step_workspace_bytes.argtypes = [i] * 7
-        L.paged_cache_write.restype = i
-        L.paged_cache_write.argtypes = [Heads, Heads, Pages, vp, vp, vp, i, i, i, i, i, i, vp]
+        L.based_paged_decode_step.restype = i
+        L.based_paged_decode_step.argtypes = [vp, vp, vp, Pages, vp, vp, vp, vp, i, i, i, i, i, i, f, f, i, vp, sz, vp]
+        L.based_paged_decode_step_workspace_bytes.restype = sz
+        L.based_paged_decode_step_workspace_bytes.argtypes = [i] * 7
+        L.based_paged_cache_write.restype = i
+        L.based_paged_cache_write.argtypes = [Heads, Heads, Pages, vp, vp, vp, i, i, i, i, i, i, vp]
         L.based_poll_error.restype = i
         L.based_poll_error.argtypes = [vp]
         L.based_status_string.restype = ctypes.c_char_p
@@ -506,7 +506,7 @@ def based_decay_attention_backward(q, k, v, rate, dout, documents=None, state_in
 
 def paged_decode_step(q, k, v, k_pages, v_pages, page_table, pos, out=None, softmax_scale: float = 0.0, softcap: float = 0.0, slopes=None,
                       window: int = 0, workspace=None, stream=None):
-    """Softmax attention of one new token per sequence over a paged cache: q [B,H_q,d], k, v [B,H_k,d]; k_pages, v_pages
+    """based_paged_decode_step: softmax attention of one new token per sequence over a paged cache: q [B,H_q,d], k, v [B,H_k,d]; k_pages, v_pages
     [pages,H_k,page_size,d] (of any one layout, such as [pages,page_size,H_k,d] transposed), page_table int32 [B,max_pages], pos int32
     [B], all on the device.  k, v are written to position pos[b]; the queries attend to it and what lies before it (the last `window` keys,
     0: all).  softcap: scores become softcap tanh(s / softcap); slopes [H_q] fp32: less slope * distance.  pos[b] < 0: no token,
@@ -516,7 +516,7 @@ def paged_decode_step(q, k, v, k_pages, v_pages, page_table, pos, out=None, soft
 
 
 def paged_cache_write(k, v, k_pages, v_pages, page_table, pos, counts=None, stream=None):
-    """Copies keys and values [B,H,L,d] into their pages: token t < counts[b] (None: all L) to position pos[b] + t of sequence b; counts,
+    """based_paged_cache_write: copies keys and values [B,H,L,d] into their pages: token t < counts[b] (None: all L) to position pos[b] + t of sequence b; counts,
     pos int32 [B].  pos[b] < 0: none of them."""
     return (_native_module or native()).paged_write(k, v, k_pages, v_pages, page_table, pos, counts, _handle(stream))
 

@@ -861,14 +861,14 @@ static based_status pages_check(const based_pages& c, const int* page_table, con
     return BASED_OK;
 }
 
-size_t paged_decode_step_workspace_bytes(int B, int H_q, int H_k, int d, int page_size, int max_pages, based_dtype io) {
+size_t based_paged_decode_step_workspace_bytes(int B, int H_q, int H_k, int d, int page_size, int max_pages, based_dtype io) {
     if (B <= 0 || H_q <= 0 || H_k <= 0 || H_q % H_k || d <= 0 || d % 8 || d > 128 || page_size <= 0 || max_pages <= 0 ||
         (long long)max_pages * page_size > 0x7fffffffLL || (io != BASED_F32 && io != BASED_BF16))
         return 0;
     return paged_decode_bytes(B, H_q, H_k, d, page_size, max_pages, io);
 }
 
-based_status paged_decode_step(const void* q, const void* k, const void* v, based_pages cache, const int* page_table, const int* pos,
+based_status based_paged_decode_step(const void* q, const void* k, const void* v, based_pages cache, const int* page_table, const int* pos,
                                const float* slopes, void* out, int B, int H_q, int H_k, int d, int max_pages, int window, float softmax_scale,
                                float softcap, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (!q || !k || !v || !out || H_q <= 0 || H_k <= 0 || H_q % H_k || window < 0 || !(softcap >= 0.f)) return BASED_ERR_INVALID_ARG;
@@ -887,7 +887,7 @@ based_status paged_decode_step(const void* q, const void* k, const void* v, base
     return launch_paged_decode(c, workspace, io, static_cast<cudaStream_t>(cuda_stream));
 }
 
-based_status paged_cache_write(based_heads k, based_heads v, based_pages cache, const int* page_table, const int* pos, const int* counts, int B,
+based_status based_paged_cache_write(based_heads k, based_heads v, based_pages cache, const int* page_table, const int* pos, const int* counts, int B,
                                int H, int L, int d, int max_pages, based_dtype io, void* cuda_stream) {
     if (!k.data || !v.data || L <= 0) return BASED_ERR_INVALID_ARG;
     based_status st = pages_check(cache, page_table, pos, B, H, d, max_pages, io);

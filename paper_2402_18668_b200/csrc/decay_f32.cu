@@ -66,7 +66,9 @@ __global__ void __launch_bounds__(kThreads, DC == 64 ? 2 : 1) decay_f32_kernel(c
                 s = p.in_factor * p.state_in[it.head * p.dc * p.de + (p.turned ? (long long)(e0 + e) * p.dc + c : (long long)c * p.de + e0 + e)];
             for (int g = 0; g < it.segment; ++g) {
                 const long long slot = decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, g);
-                s = fmaf(a.factors[slot], s, a.states[slot * kDecayMaxWidth * kTile + i]);
+                // (a factor of 0 drops what was before, whatever it holds)
+                const float f = a.factors[slot], x = a.states[slot * kDecayMaxWidth * kTile + i];
+                s = f == 0.f ? x : fmaf(f, s, x);
             }
         }
         sS[c * C::kZ + e] = s;
@@ -210,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, DC == 64 ? 2 : 1) decay_f32_kernel(c
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float4* s = reinterpret_cast<float4*>(sS + (ty * R + r) * C::kZ + 4 * tx);
-                const float4 o = *s;
+                const float4 o = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : *s;              // (0 drops it, whatever it holds)
                 *s = make_float4(fmaf(f, o.x, acc[r][0].x), fmaf(f, o.y, acc[r][0].y), fmaf(f, o.z, acc[r][1].x), fmaf(f, o.w, acc[r][1].y));
             }
         }

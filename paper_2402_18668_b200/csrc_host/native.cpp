@@ -923,10 +923,10 @@ PyObject* paged_decode(PyObject* const* a) {
     void* stream = stream_on(a[13], q);
     away(q, [&] {
         if (!out.defined()) out = blank(q.sizes(), q.scalar_type());
-        const Workspace ws(workspace, paged_decode_step_workspace_bytes(B, Hq, Hk, d, c.page_size, c.max_pages, io), q, stream);
-        check(paged_decode_step(cptr(q), cptr(k), cptr(v), c.cache(), c.t(), c.p(), f32(slopes), ptr(out), B, Hq, Hk, d, c.max_pages, window, scale, cap,
+        const Workspace ws(workspace, based_paged_decode_step_workspace_bytes(B, Hq, Hk, d, c.page_size, c.max_pages, io), q, stream);
+        check(based_paged_decode_step(cptr(q), cptr(k), cptr(v), c.cache(), c.t(), c.p(), f32(slopes), ptr(out), B, Hq, Hk, d, c.max_pages, window, scale, cap,
                                 io, ws.data, ws.bytes, stream),
-              "paged_decode_step");
+              "based_paged_decode_step");
     });
     return wrap(out);
 }
@@ -942,8 +942,8 @@ PyObject* paged_write(PyObject* const* a) {
     const based_dtype io = dtype_code(k);
     void* stream = stream_on(a[7], k);
     away(k, [&] {
-        check(paged_cache_write(as_heads(k), as_heads(v), c.cache(), c.t(), c.p(), static_cast<const int*>(cptr(counts)), B, H, L, d, c.max_pages, io, stream),
-              "paged_cache_write");
+        check(based_paged_cache_write(as_heads(k), as_heads(v), c.cache(), c.t(), c.p(), static_cast<const int*>(cptr(counts)), B, H, L, d, c.max_pages, io, stream),
+              "based_paged_cache_write");
     });
     Py_RETURN_NONE;
 }
