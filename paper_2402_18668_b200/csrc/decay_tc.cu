@@ -54,6 +54,10 @@ template <int DC, int E, bool STATES> struct Cfg {
 constexpr uint32_t colX = 0, colY = 128, colO = 256;
 // Where there is room, two turned y in turn (`two`); where only states are wanted, two third parts too
 template <int E> __device__ __forceinline__ uint32_t col_y(bool two, int i) { return two && (i & 1) ? (E == 128 ? colO : 384u) : colY; }
+// With three parts a block's own share of the state is summed apart and added by the state's group: the products' sums are cut off, not
+// rounded (24 of them a block, 8 that count in a sum begun with the small parts; a state over 32768 tokens with 0.4 % decay 1e-6 off for
+// 2e-7)
+template <bool STATES> constexpr uint32_t colD = STATES ? colO : 448;
 template <bool STATES> __device__ __forceinline__ uint32_t col_third(int i) { return STATES ? colX + 64u * (i & 1) : 384u; }
 
 // Rings: full and empty places of x, y, z, and the output in z's place.  One phase a block (bTurn, bFeed: of two in turn where there are two
@@ -401,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                 }
             }
         }
-        pass_on(c, e, x, count > 0 ? fade_of(end_of(block_of(0))) : 1.f);
+        pass_on(c, e, x, count > 0 && a.parts == 2 ? fade_of(end_of(block_of(0))) : 1.f);
         tmem_wait_st();
         fence_proxy_async_smem();
     }
@@ -482,16 +486,24 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             if (!wait(bFullZ + i % NS, i / NS) || !wait(bFeed + (two ? i & 1 : 0), two ? i >> 1 : i) || (i > 0 && !wait(bS, i - 1))) return false;
             tc_fence_after();
             const uint32_t lz = z_of(i), ty = tb + col_y<E>(two, i);
+            if (a.parts == 3) {                                      // the small parts first, into a sum of their own (see colD)
+                const uint32_t t3 = tb + col_third<STATES>(i), d = tb + colD<STATES>;
+#pragma unroll 2
+                for (int k = 0; k < kT / 16; ++k) {
+                    if (k == 0) mma_ts_w<false>(lead, d, t3, lz, desc_hi(dZ), iO);
+                    else mma_ts_w<true>(lead, d, t3 + 8 * k, lz + k * 128, desc_hi(dZ), iO);
+                }
+#pragma unroll 2
+                for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, d, ty + 16 * k + 8, lz + k * 128, desc_hi(dZ), iO);
+#pragma unroll 2
+                for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, d, ty + 16 * k, lz + k * 128, desc_hi(dZ), iO);
+            } else {
 #pragma unroll (DOCS ? 2 : 8)
-            for (int k = 0; k < kT / 16; ++k) {
-                const uint32_t at = ty + 16 * k;
-                mma_ts_w<true>(lead, tb + colS, at, lz + k * 128, desc_hi(dZ), iO);
-                mma_ts_w<true>(lead, tb + colS, at + 8, lz + k * 128, desc_hi(dZ), iO);
-            }
-            if (a.parts == 3) {
-                const uint32_t t3 = tb + col_third<STATES>(i);
-#pragma unroll
-                for (int k = 0; k < kT / 16; ++k) mma_ts_w<true>(lead, tb + colS, t3 + 8 * k, lz + k * 128, desc_hi(dZ), iO);
+                for (int k = 0; k < kT / 16; ++k) {
+                    const uint32_t at = ty + 16 * k;
+                    mma_ts_w<true>(lead, tb + colS, at, lz + k * 128, desc_hi(dZ), iO);
+                    mma_ts_w<true>(lead, tb + colS, at + 8, lz + k * 128, desc_hi(dZ), iO);
+                }
             }
             mma_commit_w(lead, &bars[bDS]);
             if (STATES) mma_commit_w(lead, &bars[bEmptyZ + i % NS]);
@@ -590,10 +602,31 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         float whole = cut ? 0.f : 1.f, f = count > 0 ? fade_of(end_of(block_of(0))) : 1.f;
         for (int i = 0; i < count; ++i) {
             whole *= f;
+            const float here = f;
             if (i + 1 < count) f = fade_of(end_of(block_of(i + 1)));
             ok = wait(bDS, i);
             if (!ok) break;
             tc_fence_after();
+            if (a.parts == 3) {
+                if (rows) {
+#pragma unroll 1
+                    for (int e = 0; e < E; e += 16) {
+                        uint32_t x[16], y[16];
+                        tmem_ld16(ts + e, x);
+                        tmem_ld16(ts - (colO + E) + colD<STATES> + e, y);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            x[k] = here == 0.f ? y[k] : __float_as_uint(fmaf(here, __uint_as_float(x[k]), __uint_as_float(y[k])));
+                        pass_on(c, e, x, 1.f);
+                    }
+                    tmem_wait_st();
+                    fence_proxy_async_smem();
+                }
+                tc_fence_before();
+                if (i + 1 < count) mbar_arrive(&bars[bS]);
+                continue;
+            }
             if (i + 1 < count) {                                     // (this product comes behind x S in order: the state ahead has been read)
                 if (rows) {
 #pragma unroll 1
