@@ -205,6 +205,20 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
     }
     return true;
 }
+// Two at once: asked for side by side, since one answer takes some 150 cycles (five pairs a block in the products' warp)
+__device__ __forceinline__ bool wait_for_both(uint64_t* x, uint32_t px, uint64_t* y, uint32_t py, volatile uint32_t* abort_flag) {
+    uint32_t there;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+        "and.pred p, p, q;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(there)
+        : "r"(smem_u32(x)), "r"(px), "r"(smem_u32(y)), "r"(py)
+        : "memory");
+    return there || (wait_for(x, px, abort_flag) && wait_for(y, py, abort_flag));
+}
 // barrier of a group of 128 threads that also tells whether all of them say yes
 __device__ __forceinline__ bool group_all(int id, bool pred) {
     uint32_t r;
@@ -331,6 +345,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
     count = __reduce_min_sync(0xffffffffu, count);
     auto block_of = [&](int i) { return back ? first + count - 1 - i : first + i; };
     auto wait = [&](int bar, int phase) -> bool { return __all_sync(0xffffffffu, wait_for(&bars[bar], phase & 1, abort_flag)); };
+    auto wait2 = [&](int x, int px, int y, int py) -> bool {
+        return __all_sync(0xffffffffu, wait_for_both(&bars[x], px & 1, &bars[y], py & 1, abort_flag));
+    };
     // what block i leaves of the state ahead of it, from its last token's place
     auto fade_of = [&](uint32_t end) -> float { return place_run(end) == 0 ? pw[place_count(end)] : 0.f; };
     // N columns from e on of row c of the state: to shared memory in bf16, and to TMEM faded by the next block (0: dropped, whatever it holds)
@@ -473,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         auto z_of = [&](int i) { return lo(dZ, sm + C::offZ + (i % NS) * C::kZ * kPanel); };
         // y^T; products have 128 rows: those past the dimensions of a narrow y hold what lies behind it, and nobody reads them
         auto turn = [&](int i) -> bool {
-            if (!wait(bFullY + i % NS, i / NS) || (DOCS && !wait(bClean, i))) return false;
+            if (!(DOCS ? wait2(bFullY + i % NS, i / NS, bClean, i) : wait(bFullY + i % NS, i / NS))) return false;
             tc_fence_after();
             const uint32_t lt = lo(dZ, y_of(i)), lu = lo(dU, sm + C::offUnit), d = tb + col_y<E>(two, i);
 #pragma unroll (DOCS ? 2 : 8)
@@ -483,7 +500,8 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             return true;
         };
         auto delta = [&](int i) -> bool {
-            if (!wait(bFullZ + i % NS, i / NS) || !wait(bFeed + (two ? i & 1 : 0), two ? i >> 1 : i) || (i > 0 && !wait(bS, i - 1))) return false;
+            // (x S has waited for the state ahead)
+            if (!wait2(bFullZ + i % NS, i / NS, bFeed + (two ? i & 1 : 0), two ? i >> 1 : i) || (STATES && i > 0 && !wait(bS, i - 1))) return false;
             tc_fence_after();
             const uint32_t lz = z_of(i), ty = tb + col_y<E>(two, i);
             if (a.parts == 3) {                                      // the small parts first, into a sum of their own (see colD)
@@ -524,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             return true;
         };
         auto before = [&](int i) -> bool {
-            if (i > 0 && (!wait(bS, i - 1) || !wait(bOread, i - 1))) return false;
+            if (i > 0 && !wait2(bS, i - 1, bOread, i - 1)) return false;
             tc_fence_after();
             const uint32_t lx = x_of(i), ls = lo(dS, sm + C::offS);
 #pragma unroll
@@ -538,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             return true;
         };
         auto inside = [&](int i) -> bool {
-            if (!wait(bP, i) || !wait(bTake, i)) return false;
+            if (!wait2(bP, i, bTake, i)) return false;
             tc_fence_after();
             const uint32_t lz = z_of(i);
 #pragma unroll (DOCS ? 2 : 8)
