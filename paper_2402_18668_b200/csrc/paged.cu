@@ -4,15 +4,14 @@
 //
 // Bound by HBM: every key and value is read once for all query heads that share it (Hq / Hk of them, the rows of a product), 2 d elements
 // a token against 4 d Hq / Hk flop.  What has to be right is the division of the work: sequences have any lengths, known to the device alone.
-//   - The unit is some tokens of one sequence and key head; all units lie in one row (sequence, head, tokens), and every worker takes an
-//     equal share of it, whatever the lengths, from one sequence of 131072 tokens to many short ones.
-//   - Where sequences are long (512 tokens and more in the mean) the workers are CTAs and the unit 64 tokens, of which each of four warps takes
-//     16, in a ring of its own that copies (16 bytes a lane) fill two or three units ahead, with a running maximum, sum and output of its
-//     own: no barrier but at the end of a head, where the four are joined.  Where they are short, that end is most of the work: the
-//     workers are warps, the unit is 16 tokens, and where one warp begins with another head the SM's others go on.  (131072 tokens,
-//     16 heads of 64: 97 us with CTAs, 118 with warps; 256 sequences of up to 100 tokens, 16 heads: 93 and 75.)
-//   - What a worker has done whole it writes as output; the pieces at its share's ends go to the workspace, and a second, dependent launch
-//     joins every output that was cut, its pieces in order.
+//   - The unit is 64 tokens of one sequence and key head; all units lie in one row (sequence, head, tokens), and every CTA takes an equal
+//     share of it, whatever the lengths, from one sequence of 131072 tokens to many short ones.
+//   - Each of a CTA's four warps takes 16 tokens of a unit, in a ring of its own that copies (16 bytes a lane) fill two or three units
+//     ahead, with a running maximum, sum and output of its own: no barrier but at the end of a head, where the four are joined.
+//     (Single warps as the workers of units of 16 tokens: 116.6 -> 118.9 us for 131072 tokens, 16 heads of 64; 53.5 -> 56.1 for 256
+//     sequences of up to 100.)
+//   - What a CTA has done whole it writes as output; the pieces at its share's ends go to the workspace, and a second, dependent launch
+//     joins every output that was cut, its pieces in order.  Where no sequence can be long and there are heads enough, nothing is cut (uncut).
 // bf16: products on the tensor cores (m16n8k16: 16 query heads a row block, weights rounded to bf16 once, 2^-9 of each at most in the mean);
 // fp32: multiply-adds, a lane per token and half a row for the scores, a lane per 2 or 4 columns for the output.
 #include "paged.cuh"
@@ -23,7 +22,10 @@ namespace based {
 
 namespace {
 
-constexpr int kSub = 16, kWarps = 4, kThreads = 128;                      // tokens that a warp takes at a time
+constexpr int kSub = 16, kWarps = 4, kThreads = 128, kUnit = kSub * kWarps;  // tokens that a warp, a CTA takes at a time
+// To begin with a head's tokens of a sequence and to join its warps takes about as long as 8 units do where HBM is shared by all CTAs: 256
+// sequences of up to 1000 tokens (16 heads of 64, tables for 8192) took 196 us with shares of units alone, 171, 131, 121, 148 with 4, 6, 8, 12
+constexpr int kBegin = 8;
 constexpr unsigned kBadPage = 2u;                                        // in the error word
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -70,42 +72,67 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// A sequence's keys: tokens lo .. pos, in units first .. first + count - 1 of `unit` tokens from the start; none where it has no token, or
+// A sequence's keys: tokens lo .. pos, in units first .. first + count - 1 from the start; none where it has no token, or
 // one past what its pages can hold
 struct Span {
     int pos, lo, first, count;
-    __device__ __forceinline__ Span(const PagedCall& c, int b, int unit) {
+    __device__ __forceinline__ Span(const PagedCall& c, int b) {
         pos = c.pos[b];
         if (pos < 0 || pos >= c.max_pages * c.page_size) {
             lo = first = count = 0;
             return;
         }
         lo = c.window > 0 && pos >= c.window ? pos - c.window + 1 : 0;
-        first = unit == 64 ? lo >> 6 : lo >> 4;                          // (64 or 16)
-        count = (unit == 64 ? pos >> 6 : pos >> 4) - first + 1;
+        first = lo / kUnit;
+        count = pos / kUnit - first + 1;
     }
+    // what it takes for one head, in units: to begin with it and to join its warps takes as long as some units
+    __device__ __forceinline__ int cost() const { return count > 0 ? count + kBegin : 0; }
 };
-// the unit, by the number of shares of 16 tokens in all sequences (of one head)
-__device__ __forceinline__ int unit_of(long long shares, int B) { return shares >= 32ll * B ? 64 : 16; }
-// sums over a CTA's threads of two values each; buf: a pair per warp
-__device__ __forceinline__ void sum2(long long (&x)[2], long long (*buf)[2]) {
+// the sum of a value over a CTA's threads; buf: a word per warp
+__device__ __forceinline__ long long sum_all(long long x, long long* buf) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
-        x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
-    }
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) {
-        buf[threadIdx.x >> 5][0] = x[0];
-        buf[threadIdx.x >> 5][1] = x[1];
-    }
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = x;
     __syncthreads();
-    x[0] = x[1] = 0;
-    for (int w = 0; w < (int)blockDim.x / 32; ++w) {
-        x[0] += buf[w][0];
-        x[1] += buf[w][1];
-    }
+    x = 0;
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) x += buf[w];
+    return x;
 }
+// The sequence in which unit x of all sequences' (`heads` times over) lies, and the units ahead of that sequence: inclusive sums, one turn of
+// the CTA's threads after the other.  buf: a word per warp and two more; for all threads
+struct Found { int b; long long ahead; };
+__device__ __forceinline__ Found find_unit(const PagedCall& c, int heads, long long x, long long* buf) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    long long before = 0;
+    for (int b0 = 0; b0 < c.B && before <= x; b0 += blockDim.x) {
+        const int b = b0 + (int)threadIdx.x;
+        const long long n = b < c.B ? (long long)Span(c, b).cost() * heads : 0;
+        long long sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += y;
+        }
+        __syncthreads();
+        if (lane == 31) buf[warp] = sum;
+        __syncthreads();
+        sum += before;
+        for (int w = 0; w < warps; ++w) {
+            if (w < warp) sum += buf[w];
+            before += buf[w];
+        }
+        if (sum - n <= x && x < sum) {
+            buf[warps] = b;
+            buf[warps + 1] = sum - n;
+        }
+    }
+    __syncthreads();
+    return {(int)buf[warps], buf[warps + 1]};
+}
+// x / y, whose quotient is an int; in 32 bits where that does
+__device__ __forceinline__ int quotient(long long x, int y) { return x >> 31 == 0 ? (int)((unsigned)x / (unsigned)y) : (int)(x / y); }
 
 // The units of all sequences in one row, cut into G shares that differ by one at most
 struct Shares {
@@ -130,7 +157,7 @@ struct Shares {
 
 struct Args {
     PagedCall c;
-    float* pieces;                                                       // [2 W][rows][d + 2]
+    float* pieces;                                                       // [2 G][rows][d + 2]
     int piece;                                                           // floats of one
     unsigned int* err;
     int blocks;                                                          // row blocks of a key head's queries
@@ -143,7 +170,7 @@ template <typename T, int DP, int R>
 __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_kernel(const __grid_constant__ Args a) {
     using C = Cfg<T, DP, R>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long s_sum[kWarps][2], s_from[kWarps][2];
+    __shared__ long long s_buf[kWarps + 2];
     const PagedCall& c = a.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t* ring = smem + warp * C::kWarp;
@@ -153,14 +180,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // This worker's units u .. end - 1, the sequence and the head that they begin in, and which of its units
-    int unit = 64, b, hm, unit0 = 0, worker = blockIdx.x;
-    bool wide = true;                                                    // the CTA is the worker
+    // This CTA's units u .. end - 1, the sequence and the head that they begin in, and which of its units
+    int b, hm, unit0 = 0;
     long long u = 0, end;
     if (!a.split) {
         b = blockIdx.x / heads;
         hm = blockIdx.x % heads;
-        const Span sp(c, b, unit);
+        const Span sp(c, b);
         end = sp.count;
         if (end == 0) {
             const int h0 = hm / a.blocks * group + hm % a.blocks * C::kRows, n = min(C::kRows, group - hm % a.blocks * C::kRows) * c.d;
@@ -170,57 +196,34 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
             return;
         }
     } else {
-        long long all[2] = {0, 0};                                       // units of 16 tokens, of 64
-        for (int k = tid; k < c.B; k += kThreads) {
-            all[0] += Span(c, k, 16).count;
-            all[1] += Span(c, k, 64).count;
+        for (int k = blockIdx.x; k < c.B; k += gridDim.x) {              // sequences without a token
+            const Span sp(c, k);
+            if (sp.count > 0) continue;
+            T* out = static_cast<T*>(c.out) + (long long)k * c.Hq * c.d;
+            for (int i = tid; i < c.Hq * c.d; i += kThreads) out[i] = from_f32<T>(0.f);
+            if (tid == 0 && sp.pos >= 0) atomicOr(a.err, kBadPage);
         }
-        sum2(all, s_sum);
-        unit = unit_of(all[0], c.B);
-        wide = unit == 64;
-        const Shares sh(all[wide] * heads, wide ? gridDim.x : gridDim.x * kWarps);
-        worker = wide ? blockIdx.x : blockIdx.x * kWarps + warp;
-        u = sh.begin(worker);
-        end = sh.begin(worker + 1);
-        // inclusive sums of the sequences' units, 128 a turn, by shuffles
-        long long before = 0;
-        for (int b0 = 0; b0 < c.B; b0 += kThreads) {
-            const long long n = b0 + tid < c.B ? (long long)Span(c, b0 + tid, unit).count * heads : 0;
-            long long sum = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += x;
-            }
-            __syncthreads();
-            if (lane == 31) s_sum[warp][0] = sum;
-            __syncthreads();
-            long long off = before;
-            for (int w = 0; w < warp; ++w) off += s_sum[w][0];
-            sum += off;
-            before += s_sum[0][0] + s_sum[1][0] + s_sum[2][0] + s_sum[3][0];
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const long long x = wide ? u : sh.begin((long long)blockIdx.x * kWarps + w);
-                if (sum - n <= x && x < sum) {
-                    s_from[w][0] = b0 + tid;
-                    s_from[w][1] = sum - n;                              // the units of the sequences before it
-                }
-            }
-        }
-        __syncthreads();
+        long long all = 0;
+        for (int k = tid; k < c.B; k += kThreads) all += Span(c, k).cost();
+        const Shares sh(sum_all(all, s_buf) * heads, gridDim.x);
+        u = sh.begin(blockIdx.x);
+        end = sh.begin(blockIdx.x + 1);
         if (u >= end) return;
-        b = (int)s_from[warp][0];
-        const long long in = u - s_from[warp][1];
-        const int count = Span(c, b, unit).count;                        // (not 0)
-        hm = in >> 31 == 0 ? (int)((unsigned)in / (unsigned)count) : (int)(in / count);
-        unit0 = (int)(in - (long long)hm * count);
+        const Found at = find_unit(c, heads, u, s_buf);
+        b = at.b;
+        const int cost = Span(c, b).cost();                              // (not 0)
+        hm = quotient(u - at.ahead, cost);
+        unit0 = (int)(u - at.ahead - (long long)hm * cost) - kBegin;
     }
-    const long long range = u;
+    int later = 0;                                                       // (a share has pieces at its beginning and at its end)
 
     for (; u < end; ) {
-        const Span sp(c, b, unit);
-        const int units = (int)min((long long)(sp.count - unit0), end - u);
+        const Span sp(c, b);
+        const int left = (int)min((long long)(sp.count - unit0), end - u);      // this share's part, from unit0 (below 0: its beginning) on
+        const int units = left + min(unit0, 0);
+        u += left;
+        unit0 = max(unit0, 0);
+        if (units <= 0) return;                                          // (the share ends with its beginning)
         const int hk = hm / a.blocks, row0 = (hm % a.blocks) * C::kRows, rows = min(C::kRows, group - row0);
         const int h0 = hk * group + row0;                                // the first query head
         const T* q = static_cast<const T*>(c.q) + ((long long)b * c.Hq + h0) * c.d;
@@ -232,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
 
         // Lane < 16 (and its double) looks up the page of token j0 + lane of a unit a turn before it is needed: it is checked then, so that
         // nothing waits for the table
-        auto tokens = [&](int n) { return (sp.first + unit0 + n) * unit + (wide ? warp * kSub : 0); };
+        auto tokens = [&](int n) { return (sp.first + unit0 + n) * kUnit + warp * kSub; };
         auto page_of = [&](int j) { return a.shift >= 0 ? j >> a.shift : (int)((unsigned)j / (unsigned)c.page_size); };
         auto here = [&](int n, int j) { return n < units && j <= sp.pos && j >= sp.lo; };
         auto look = [&](int n) -> int {
@@ -243,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
         const int lrow = lane / C::kChunks, lch = lane % C::kChunks;
         const bool lin = lch * V < c.d;
         // units in0 .. in1 - 1: no token at the border of what is seen, and the new one not among them
-        const int in0 = max(0, (sp.lo - tokens(0) + unit - 1) / unit), in1 = min(units, sp.pos - kSub >= tokens(0) ? (sp.pos - kSub - tokens(0)) / unit + 1 : 0);
+        const int in0 = max(0, (sp.lo - tokens(0) + kUnit - 1) / kUnit), in1 = min(units, sp.pos - kSub >= tokens(0) ? (sp.pos - kSub - tokens(0)) / kUnit + 1 : 0);
         // rows of a unit whose tokens lie inside and in one page
         const long long lane_at = lrow * c.token_stride + (lin ? lch * V : 0), step = kStep * c.token_stride;
         auto load_inside = [&](int n, int id) {
@@ -492,11 +495,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
         pairs::copy_async_wait<0>();
         __syncwarp();
 
-        // a whole output, or a piece: of a warp's, or of the four as one, by way of the rings
+        // the four warps' shares joined, by way of the rings: a whole output, or a piece
         const bool whole = units == sp.count;
-        float* piece = wide ? reinterpret_cast<float*>(ring) : a.pieces + (2 * (long long)worker + (u != range)) * a.piece;
-        T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h0) * c.d;
-        const bool write = whole && !wide;
+        float* mine = reinterpret_cast<float*>(ring);
         if constexpr (C::kTc) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -504,17 +505,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
                 if (r >= rows) continue;
-                const float inv = 1.f / l[h];
 #pragma unroll
-                for (int k = 0; k < DP / 8; ++k) {
-                    const int e = 8 * k + (lane & 3) * 2;
-                    if (write) {
-                        if (e < c.d) *reinterpret_cast<uint32_t*>(out + r * c.d + e) = pack2(acc[k][2 * h] * inv, acc[k][2 * h + 1] * inv);
-                    } else {
-                        *reinterpret_cast<float2*>(piece + r * C::kPieceRow + 2 + e) = make_float2(acc[k][2 * h], acc[k][2 * h + 1]);
-                    }
-                }
-                if (!write && (lane & 3) == 0) *reinterpret_cast<float2*>(piece + r * C::kPieceRow) = make_float2(m[h], l[h]);
+                for (int k = 0; k < DP / 8; ++k)
+                    *reinterpret_cast<float2*>(mine + r * C::kPieceRow + 2 + 8 * k + (lane & 3) * 2) = make_float2(acc[k][2 * h], acc[k][2 * h + 1]);
+                if ((lane & 3) == 0) *reinterpret_cast<float2*>(mine + r * C::kPieceRow) = make_float2(m[h], l[h]);
             }
         } else {
 #pragma unroll
@@ -523,135 +517,150 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                 for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
                 if (r >= rows) continue;
 #pragma unroll
-                for (int k = 0; k < DP / 32; ++k) {
-                    const int e = lane * (DP / 32) + k;
-                    if (write) {
-                        if (e < c.d) out[r * c.d + e] = from_f32<T>(acc[r][k] / l[r]);
-                    } else {
-                        piece[r * C::kPieceRow + 2 + e] = acc[r][k];
-                    }
-                }
-                if (!write && lane == 0) *reinterpret_cast<float2*>(piece + r * C::kPieceRow) = make_float2(m[r], l[r]);
+                for (int k = 0; k < DP / 32; ++k) mine[r * C::kPieceRow + 2 + lane * (DP / 32) + k] = acc[r][k];
+                if (lane == 0) *reinterpret_cast<float2*>(mine + r * C::kPieceRow) = make_float2(m[r], l[r]);
             }
         }
-        __syncwarp();
-        if (wide) {
-            __syncthreads();
-            float* to = a.pieces + (2 * (long long)worker + (u != range)) * a.piece;
-            for (int i = tid; i < rows * DP; i += kThreads) {
-                const int r = i / DP, e = i % DP;
-                auto of = [&](int w) { return reinterpret_cast<const float*>(smem + w * C::kWarp) + r * C::kPieceRow; };
-                float top = -INFINITY, sum = 0.f, o = 0.f;
+        __syncthreads();
+        T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h0) * c.d;
+        float* to = a.pieces + (2 * (long long)blockIdx.x + later) * a.piece;
+        for (int i = tid; i < rows * DP; i += kThreads) {
+            const int r = i / DP, e = i % DP;
+            auto of = [&](int w) { return reinterpret_cast<const float*>(smem + w * C::kWarp) + r * C::kPieceRow; };
+            float top = -INFINITY, sum = 0.f, o = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) top = fmaxf(top, of(w)[0]);
-                const float z = top == -INFINITY ? 0.f : top;
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, of(w)[0]);
+            const float z = top == -INFINITY ? 0.f : top;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float f = exp2f(of(w)[0] - z);
-                    sum = fmaf(of(w)[1], f, sum);
-                    o = fmaf(of(w)[2 + e], f, o);
-                }
-                if (whole) {
-                    if (e < c.d) out[r * c.d + e] = from_f32<T>(o / sum);
-                } else {
-                    to[r * C::kPieceRow + 2 + e] = o;
-                    if (e == 0) *reinterpret_cast<float2*>(to + r * C::kPieceRow) = make_float2(top, sum);
-                }
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = exp2f(of(w)[0] - z);
+                sum = fmaf(of(w)[1], f, sum);
+                o = fmaf(of(w)[2 + e], f, o);
             }
-            __syncthreads();                                             // (before the rings are filled again)
+            if (whole) {
+                if (e < c.d) out[r * c.d + e] = from_f32<T>(o / sum);
+            } else {
+                to[r * C::kPieceRow + 2 + e] = o;
+                if (e == 0) *reinterpret_cast<float2*>(to + r * C::kPieceRow) = make_float2(top, sum);
+            }
         }
-        u += units;
         if (u >= end) return;
-        unit0 = 0;
-        if (++hm == heads) {                                             // on to the next sequence that has keys
+        unit0 = -kBegin;
+        later = 1;
+        __syncthreads();                                                 // (before the rings are filled again)
+        if (++hm == heads) {                                             // on to the next sequence that has keys, 32 looked at a turn
             hm = 0;
-            do ++b;
-            while (b + 1 < c.B && Span(c, b, unit).count == 0);
-            if (b >= c.B) return;
+            for (++b; ; b += 32) {
+                const uint32_t some = __ballot_sync(0xffffffffu, b + lane < c.B && Span(c, b + lane).count > 0);
+                if (some) {
+                    b += __ffs(some) - 1;
+                    break;
+                }
+                if (b + 32 >= c.B) return;
+            }
         }
     }
 }
 
-// The outputs that were cut, from their pieces, and zeros where a sequence has no token; a CTA per sequence and query head: its threads hold a
-// column each and share the pieces out among kJoin / DP of them, whose results are joined in order
+// The outputs that were cut, from their pieces.  BY_CUT: a CTA per border of the shares, which sees to the output that is cut there first (with all its
+// rows); else a CTA per sequence and query head.  Threads hold a column each and share the pieces out among kJoin / DP of them, whose
+// results are joined in order.
 constexpr int kJoin = 256;
-template <typename T, int DP, int R> __global__ void __launch_bounds__(kJoin) paged_join_kernel(const __grid_constant__ Args a, int ctas) {
+template <typename T, int DP, int R, bool BY_CUT> __global__ void __launch_bounds__(kJoin) paged_join_kernel(const __grid_constant__ Args a, int ctas) {
     using C = Cfg<T, DP, R>;
-    __shared__ long long s_sum[kJoin / 32][2];
+    __shared__ long long s_buf[kJoin / 32 + 2];
     __shared__ float s_part[kJoin][3];
     const PagedCall& c = a.c;
-    const int heads = c.Hk * a.blocks, group = c.Hq / c.Hk, b = blockIdx.x / c.Hq, h = blockIdx.x % c.Hq;
-    const int hm = h / group * a.blocks + h % group / C::kRows, r = h % group % C::kRows;
-    long long all[2] = {0, 0}, ahead[2] = {0, 0};                        // units of 16 tokens, of 64: of all sequences, of those before b
+    const int heads = c.Hk * a.blocks, group = c.Hq / c.Hk;
+    int b = blockIdx.x / c.Hq, h = blockIdx.x % c.Hq, hm = h / group * a.blocks + h % group / C::kRows, r = h % group % C::kRows, rows = 1;
+    long long all = 0, ahead = 0;
     for (int k = threadIdx.x; k < c.B; k += kJoin) {
-        const int n16 = Span(c, k, 16).count, n64 = Span(c, k, 64).count;
-        all[0] += n16;
-        all[1] += n64;
-        ahead[0] += k < b ? n16 : 0;
-        ahead[1] += k < b ? n64 : 0;
+        const int n = Span(c, k).cost();
+        all += n;
+        ahead += !BY_CUT && k < b ? n : 0;
     }
-    sum2(all, s_sum);
-    sum2(ahead, s_sum);
-    const int unit = unit_of(all[0], c.B);
-    const bool wide = unit == 64;
-    const Span sp(c, b, unit);
-    T* out = static_cast<T*>(c.out) + ((long long)b * c.Hq + h) * c.d;
-    enter_dependent();
-    if (sp.count == 0) {
-        for (int i = threadIdx.x; i < c.d; i += kJoin) out[i] = from_f32<T>(0.f);
-        if (threadIdx.x == 0 && sp.pos >= 0) atomicOr(a.err, kBadPage);
-        return;
-    }
-    const long long first = ahead[wide] * heads + (long long)hm * sp.count;
-    const Shares sh(all[wide] * heads, wide ? ctas : ctas * kWarps);
-    const long long i0 = sh.of(first), i1 = sh.of(first + sp.count - 1);
-    if (i0 == i1) return;
-    const bool begun = sh.begin(i0) != first;                            // the first worker had something else before it
-    const int count = (int)(i1 - i0) + 1, part = threadIdx.x / DP, e = threadIdx.x % DP;
-    const float* from = a.pieces + 2 * i0 * a.piece;
-    constexpr int kParts = kJoin / DP;
-    float top = -INFINITY, sum = 0.f, o = 0.f;
-    auto add = [&](float m, float l, float x) {
-        const float to = fmaxf(top, m), z = to == -INFINITY ? 0.f : to, f = exp2f(top - z), g = exp2f(m - z);
-        sum = fmaf(sum, f, l * g);
-        o = fmaf(o, f, x * g);
-        top = to;
-    };
-    for (int i = part; i < count; i += 8 * kParts) {                     // eight pieces' values asked for at once
-        float x[8][3];
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            const int k = i + s * kParts;
-            const float* p = from + (2 * (long long)k + (k == 0 && begun)) * a.piece + r * C::kPieceRow;
-            x[s][0] = k < count ? p[0] : -INFINITY;
-            x[s][1] = k < count ? p[1] : 0.f;
-            x[s][2] = k < count ? p[2 + e] : 0.f;
+    const Shares sh(sum_all(all, s_buf) * heads, ctas);
+    if constexpr (BY_CUT) {
+        const long long x = sh.begin(blockIdx.x + 1);
+        if (x >= sh.total) {
+            enter_dependent();                                           // (what comes behind this launch relies on its wait)
+            return;
         }
-#pragma unroll
-        for (int s = 0; s < 8; ++s) add(x[s][0], x[s][1], x[s][2]);
+        const Found at = find_unit(c, heads, x, s_buf);
+        b = at.b;
+        ahead = at.ahead;
+        hm = quotient(x - ahead, Span(c, b).cost());
+        r = 0;
+        rows = min(C::kRows, group - hm % a.blocks * C::kRows);
+        h = hm / a.blocks * group + hm % a.blocks * C::kRows;
+    } else {
+        ahead = sum_all(ahead, s_buf) * heads;
     }
-    s_part[threadIdx.x][0] = top;
-    s_part[threadIdx.x][1] = sum;
-    s_part[threadIdx.x][2] = o;
-    __syncthreads();
-    if (part == 0 && e < c.d) {
+    const Span sp(c, b);
+    enter_dependent();
+    if (sp.count == 0) return;
+    const long long first = ahead + (long long)hm * sp.cost() + kBegin;    // its first unit
+    const long long i0 = sh.of(first), i1 = sh.of(first + sp.count - 1);
+    if (i0 == i1 || (BY_CUT && i0 != blockIdx.x)) return;
+    const bool begun = sh.begin(i0) < first - kBegin;                        // the first CTA had something else before it
+    const int count = (int)(i1 - i0) + 1, part = threadIdx.x / DP, e = threadIdx.x % DP;
+    constexpr int kParts = kJoin / DP;
+#pragma unroll 1
+    for (; rows > 0; --rows, ++r, ++h) {
+        const float* from = a.pieces + 2 * i0 * a.piece + r * C::kPieceRow;
+        float top = -INFINITY, sum = 0.f, o = 0.f;
+        auto add = [&](float m, float l, float x) {
+            const float to = fmaxf(top, m), z = to == -INFINITY ? 0.f : to, f = exp2f(top - z), g = exp2f(m - z);
+            sum = fmaf(sum, f, l * g);
+            o = fmaf(o, f, x * g);
+            top = to;
+        };
+        for (int i = part; i < count; i += 8 * kParts) {                 // eight pieces' values asked for at once
+            float x[8][3];
 #pragma unroll
-        for (int k = 1; k < kParts; ++k) add(s_part[k * DP + e][0], s_part[k * DP + e][1], s_part[k * DP + e][2]);
-        out[e] = from_f32<T>(o / sum);
+            for (int s = 0; s < 8; ++s) {
+                const int k = i + s * kParts;
+                const float* p = from + (2 * (long long)k + (k == 0 && begun)) * a.piece;
+                x[s][0] = k < count ? p[0] : -INFINITY;
+                x[s][1] = k < count ? p[1] : 0.f;
+                x[s][2] = k < count ? p[2 + e] : 0.f;
+            }
+#pragma unroll
+            for (int s = 0; s < 8; ++s) add(x[s][0], x[s][1], x[s][2]);
+        }
+        s_part[threadIdx.x][0] = top;
+        s_part[threadIdx.x][1] = sum;
+        s_part[threadIdx.x][2] = o;
+        __syncthreads();
+        if (part == 0 && e < c.d) {
+#pragma unroll
+            for (int k = 1; k < kParts; ++k) add(s_part[k * DP + e][0], s_part[k * DP + e][1], s_part[k * DP + e][2]);
+            static_cast<T*>(c.out)[((long long)b * c.Hq + h) * c.d + e] = from_f32<T>(o / sum);
+        }
+        __syncthreads();
     }
 }
 
 template <int DP, int R> int piece_floats(int Hq, int Hk) { return (Hq / Hk < R ? Hq / Hk : R) * (DP + 2); }
 template <int R> int row_blocks(int Hq, int Hk) { return (Hq / Hk + R - 1) / R; }
-// CTAs of a launch: what the device holds at a time, or one per four units where there cannot be as many
+// CTAs of a launch: what the device holds at a time, or one per unit where there cannot be as many
 template <typename T, int DP, int R> int grid_of(int B, int Hq, int Hk, int page_size, int max_pages) {
-    const long long units = (long long)B * Hk * row_blocks<R>(Hq, Hk) * (((long long)max_pages * page_size + kSub - 1) / kSub);
+    const long long units = (long long)B * Hk * row_blocks<R>(Hq, Hk) * (((long long)max_pages * page_size + kUnit - 1) / kUnit);
     const int most = kSMs * Cfg<T, DP, R>::kPerSm;
-    return (units + kWarps - 1) / kWarps < most ? (int)((units + kWarps - 1) / kWarps) : most;
+    return units < most ? (int)units : most;
 }
 
-// Tables of up to 256 tokens: one head's are not worth dividing, a join costs more (1000 tokens: 15.2 us whole, 12.6 divided)
-bool short_cache(int page_size, int max_pages) { return (long long)page_size * max_pages <= 256; }
+// Whether no output is cut: where the tables hold up to 256 tokens (250 tokens, 16 heads: 7.7 us for 13.2 cut), or up to 1024 and there are
+// outputs (of a key head) for a quarter of the SMs (256 sequences of up to 1000 tokens: 110 us for 167; but 1000 tokens, 32 outputs: 18.2 for
+// 15.1)
+bool uncut(long long outputs, int page_size, int max_pages) {
+    const long long most = (long long)page_size * max_pages;
+    return most <= 256 || (most <= 1024 && 4 * outputs >= kSMs);
+}
+
+// More outputs than this: a join per cut (1024 sequences of up to 300 tokens, 16 query heads: 57 us for 120); fewer: one per output, whose
+// query heads then need not wait for one another (20000 tokens, 32 query heads on 8: 27 us for 32)
+constexpr int kManyOutputs = 1024;
 
 template <typename T, int DP, int R> based_status launch(const PagedCall& c, void* workspace, cudaStream_t stream) {
     using C = Cfg<T, DP, R>;
@@ -662,16 +671,21 @@ template <typename T, int DP, int R> based_status launch(const PagedCall& c, voi
         if (cudaFuncSetAttribute(paged_decode_kernel<T, DP, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes) != cudaSuccess) return BASED_ERR_CUDA;
         ready[dev].store(true, std::memory_order_release);
     }
-    Args a{c, static_cast<float*>(workspace), piece_floats<DP, R>(c.Hq, c.Hk), nullptr, row_blocks<R>(c.Hq, c.Hk), -1, c.page_size % kSub == 0, !short_cache(c.page_size, c.max_pages)};
+    Args a{c, static_cast<float*>(workspace), piece_floats<DP, R>(c.Hq, c.Hk), nullptr, row_blocks<R>(c.Hq, c.Hk), -1, c.page_size % kSub == 0, true};
+    const int outputs = c.B * c.Hk * a.blocks;
+    a.split = !uncut(outputs, c.page_size, c.max_pages);
     if (error_word_ptr(&a.err) != BASED_OK) return BASED_ERR_CUDA;
     for (int s = 0; s < 31; ++s)
         if (c.page_size == 1 << s) a.shift = s;
-    const int outputs = c.B * c.Hk * a.blocks, G = a.split ? grid_of<T, DP, R>(c.B, c.Hq, c.Hk, c.page_size, c.max_pages) : outputs;
+    const int G = a.split ? grid_of<T, DP, R>(c.B, c.Hq, c.Hk, c.page_size, c.max_pages) : outputs;
     cudaError_t e = launch_ex(paged_decode_kernel<T, DP, R>, dim3(G), dim3(kThreads), C::kBytes, 1, true, stream, a);
     note_launch();
     based_status st = check_launch("paged_decode_kernel");
     if (e != cudaSuccess || st != BASED_OK || !a.split) return e != cudaSuccess ? BASED_ERR_CUDA : st;
-    e = launch_ex(paged_join_kernel<T, DP, R>, dim3(c.B * c.Hq), dim3(kJoin), 0, 1, true, stream, a, G);
+    if (G == 1) return BASED_OK;
+    const bool by_cut = (long long)c.B * c.Hq > kManyOutputs;
+    e = by_cut ? launch_ex(paged_join_kernel<T, DP, R, true>, dim3(G - 1), dim3(kJoin), 0, 1, true, stream, a, G)
+               : launch_ex(paged_join_kernel<T, DP, R, false>, dim3(c.B * c.Hq), dim3(kJoin), 0, 1, true, stream, a, G);
     note_launch();
     st = check_launch("paged_join_kernel");
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
@@ -730,11 +744,11 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const __grid_constant_
 }  // namespace
 
 size_t paged_decode_bytes(int B, int Hq, int Hk, int d, int page_size, int max_pages, based_dtype io) {
-    if (short_cache(page_size, max_pages)) return 0;
     return for_call(io, d, Hq / Hk, [&](auto t, auto width, auto rows) {
         using T = decltype(t);
         constexpr int W = decltype(width)::value, R = decltype(rows)::value;
-        return (size_t)grid_of<T, W, R>(B, Hq, Hk, page_size, max_pages) * kWarps * 2 * piece_floats<W, R>(Hq, Hk) * sizeof(float);
+        if (uncut((long long)B * Hk * row_blocks<R>(Hq, Hk), page_size, max_pages)) return (size_t)0;
+        return (size_t)grid_of<T, W, R>(B, Hq, Hk, page_size, max_pages) * 2 * piece_floats<W, R>(Hq, Hk) * sizeof(float);
     });
 }
 

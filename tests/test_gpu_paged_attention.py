@@ -108,6 +108,35 @@ def test_one_long_sequence(based, dtype):
     check(based, gen, DTYPES[dtype], [12345], 16, 2, 128, 16, cap=30.0, slopes=True)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_tables_longer_than_the_sequences(based, dtype):
+    """How the work is cut goes by the tables' length as well: with more outputs than joins, hardly any tokens, none at all, one token for all CTAs."""
+    gen = torch.Generator(device="cuda").manual_seed(25)
+    check(based, gen, DTYPES[dtype], [(37 * i) % 330 - 30 for i in range(300)], 4, 2, 64, 16, wide=120)
+    check(based, gen, DTYPES[dtype], [70 if i % 401 == 5 else -1 for i in range(1300)], 1, 1, 64, 16, wide=120)
+    check(based, gen, DTYPES[dtype], [-1] * 3, 4, 2, 64, 16, wide=120)
+    check(based, gen, DTYPES[dtype], [-1] * 600, 2, 1, 64, 16, wide=120)
+    check(based, gen, DTYPES[dtype], [0], 2, 1, 128, 16, wide=500)
+    check(based, gen, DTYPES[dtype], [65, 0, 4000], 6, 2, 64, 16, wide=500, window=64)
+    check(based, gen, DTYPES[dtype], [(61 * i) % 900 for i in range(40)], 2, 1, 64, 16)                # 900 tokens at most: nothing is cut
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_sequences_that_share_pages(based, dtype):
+    """Two sequences with one prompt, whose whole pages they share; each has a last page of its own."""
+    gen = torch.Generator(device="cuda").manual_seed(26)
+    kp, vp, table = cache(gen, [1500], 2, 16, 64, DTYPES[dtype])
+    kp, vp = torch.cat([kp, kp]), torch.cat([vp, vp])
+    both = table.expand(2, -1).clone()
+    both[1, 1500 // 16] += kp.shape[0] // 2
+    q, k, v = normal(gen, 2, 4, 64, dtype=DTYPES[dtype]), normal(gen, 2, 2, 64, dtype=DTYPES[dtype]), normal(gen, 2, 2, 64, dtype=DTYPES[dtype])
+    pos = torch.tensor([1500, 1500], dtype=torch.int32, device="cuda")
+    want, bound, kw, vw = ref.paged(q, k, v, kp, vp, both, pos, None, 0.0, None, 0)
+    out = based.paged_decode_step(q, k, v, kp, vp, both, pos)
+    assert ((out.double() - want).abs() <= bound).all()
+    assert torch.equal(kp.nan_to_num(7.0), kw.nan_to_num(7.0)) and torch.equal(vp.nan_to_num(7.0), vw.nan_to_num(7.0))
+
+
 def test_offsets_past_32_bits(based):
     """A pool of more than 2^32 elements, of which the pages at its end are used."""
     free, _ = torch.cuda.mem_get_info()
