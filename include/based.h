@@ -554,12 +554,12 @@ typedef struct { const void* data; long long batch_stride, head_stride, token_st
  *
  * q, k [B,H,L,d_k], v, out [B,H,L,d_v] in the io dtype; rate [H] fp32, >= 0 (not checked; 0: no decay); state_in, state_out
  * [B,H,d_k,d_v] fp32: the states before token 0 and behind token L-1 (NULL: not wanted), which must not be one array.  scale <= 0:
- * 1 / sqrt(d_k).
+ * 1 / sqrt(d_k); else from 2^-60 to 2^60.
  * documents [B,L] int32, or NULL: a token whose document is negative is padding, and passed over as if it were not there (its
  * inputs are not used, its output is 0); one whose document is not that of the last token before it that counts starts from an
  * empty state.  A sequence's first document continues state_in, whatever its number.
  * fp32 io: fp32 multiply-adds.  bf16 io: the faded scores and the state as operands of products with q are rounded to bf16 once; sums, the
- * state itself and what goes into it are fp32 (16 bits of every faded v).  Where a value that counts is not finite, the outputs of its
+ * state itself and what goes into it are fp32 (of every faded k 16 bits, 24 where a state is returned).  Where a value that counts is not finite, the outputs of its
  * sequence and head from up to 127 tokens ahead of it on may not be either, in other documents too.
  * Supported: d_k, d_v multiples of 8 up to 128; io in {F32, BF16}; 1 <= L <= 2^31 - 2^16.
  * workspace: based_decay_attention_workspace_bytes (with_documents: whether documents is given; 0 bytes are possible).  Outputs must not
@@ -612,9 +612,9 @@ typedef struct { void *k, *v; long long page_stride, head_stride, token_stride; 
  *
  * q, out [B,H_q,d], k, v [B,H_k,d] contiguous, in the io dtype, which is the cache's too; pos int32 [B] on the device, pos[b] < 0: the
  * sequence has no token (its output is 0, nothing is written); one beyond max_pages * page_size counts as a bad page and has output 0.
- * softcap 0: no cap; slopes [H_q] fp32 (NULL: no bias).  softmax_scale <= 0: 1 / sqrt(d).  The work is divided evenly over the tokens that there
- * are, in whichever sequences; scores, sums and outputs are fp32, in bf16 io the softmax weights are rounded to bf16 once, as operands.  No
- * result depends on the order in which the parts end.
+ * softcap 0: no cap; slopes [H_q] fp32 (NULL: no bias).  softmax_scale <= 0: 1 / sqrt(d); else it, and softcap,
+ * from 2^-60 to 2^60.  The work is divided evenly over the tokens that there are, in whichever sequences; scores, sums and outputs are fp32,
+ * in bf16 io the softmax weights are rounded to bf16 once, as operands.  No result depends on the order in which the parts end.
  * Supported: d a multiple of 8 up to 128; H_q a multiple of H_k; any page_size, max_pages * page_size < 2^31; io in {F32, BF16}.
  * workspace: based_paged_decode_step_workspace_bytes (0 is possible).  out must not alias an input; two sequences must not write to one slot.
  */

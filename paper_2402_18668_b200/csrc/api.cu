@@ -699,6 +699,8 @@ based_status swa_backward(const void* q, const void* k, const void* v, const voi
     return BASED_OK;
 }
 
+// a factor of scores: chosen here if not above 0; its reciprocal, and products with it, are to be in the range of fp32
+static bool factor_ok(float x) { return !(x > 0.f) || (x >= 0x1p-60f && x <= 0x1p60f); }
 static based_status heads_check(const based_heads& t, int B, int H, int L, int d, based_dtype io, bool written) {
     if (!t.data) return BASED_ERR_INVALID_ARG;
     const long long per16 = 16 / (long long)esize(io);
@@ -769,6 +771,7 @@ based_status based_decay_attention_forward(based_heads q, based_heads k, based_h
                                            float scale, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (!q.data || !k.data || !v.data || !out.data || !rate) return BASED_ERR_INVALID_ARG;
     based_status st = decay_sizes_check(B, H, L, d_k, d_v, io);
+    if (st == BASED_OK && !factor_ok(scale)) st = BASED_ERR_UNSUPPORTED;
     if (st != BASED_OK) return st;
     if (is_one_of(out.data, {q.data, k.data, v.data, rate, documents, state_in, state_out, workspace}) ||
         is_one_of(state_out, {q.data, k.data, v.data, rate, documents, state_in, workspace}))
@@ -792,7 +795,8 @@ based_status based_decay_attention_forward(based_heads q, based_heads k, based_h
 based_status based_decay_attention_step(const void* q, const void* k, const void* v, const float* rate, const float* state_in, void* out,
                                         float* state_out, int B, int H, int d_k, int d_v, float scale, based_dtype io, void* cuda_stream) {
     if (!q || !k || !v || !rate || !state_in || !out || !state_out) return BASED_ERR_INVALID_ARG;
-    const based_status st = decay_sizes_check(B, H, 1, d_k, d_v, io);
+    based_status st = decay_sizes_check(B, H, 1, d_k, d_v, io);
+    if (st == BASED_OK && !factor_ok(scale)) st = BASED_ERR_UNSUPPORTED;
     if (st != BASED_OK) return st;
     if (is_one_of(out, {q, k, v, rate, state_in, state_out}) || is_one_of(state_out, {q, k, v, rate})) return BASED_ERR_INVALID_ARG;
     for (const void* p : {q, k, v, (const void*)rate, (const void*)state_in, (const void*)out, (const void*)state_out})
@@ -807,6 +811,7 @@ based_status based_decay_attention_backward(based_heads q, based_heads k, based_
                                             based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (!q.data || !k.data || !v.data || !dout.data || !dq.data || !dk.data || !dv.data || !rate) return BASED_ERR_INVALID_ARG;
     based_status st = decay_sizes_check(B, H, L, d_k, d_v, io);
+    if (st == BASED_OK && !factor_ok(scale)) st = BASED_ERR_UNSUPPORTED;
     if (st != BASED_OK) return st;
     const void* outs[] = {dq.data, dk.data, dv.data, dstate_in};
     for (int i = 0; i < 4; ++i) {
@@ -872,7 +877,8 @@ based_status based_paged_decode_step(const void* q, const void* k, const void* v
                                const float* slopes, void* out, int B, int H_q, int H_k, int d, int max_pages, int window, float softmax_scale,
                                float softcap, based_dtype io, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (!q || !k || !v || !out || H_q <= 0 || H_k <= 0 || H_q % H_k || window < 0 || !(softcap >= 0.f)) return BASED_ERR_INVALID_ARG;
-    const based_status st = pages_check(cache, page_table, pos, B, H_k, d, max_pages, io);
+    based_status st = pages_check(cache, page_table, pos, B, H_k, d, max_pages, io);
+    if (st == BASED_OK && !(factor_ok(softmax_scale) && factor_ok(softcap))) st = BASED_ERR_UNSUPPORTED;
     if (st != BASED_OK) return st;
     if (is_one_of(out, {q, k, v, cache.k, cache.v, page_table, pos, slopes, workspace}) || is_one_of(workspace, {q, k, v, cache.k, cache.v, page_table, pos, slopes}))
         return BASED_ERR_INVALID_ARG;

@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(Cfg<DC, STATES>::kThreads, STATES && DC == 64 
     enter_dependent();
     if (e0 >= p.de) return;
     const int b = (int)(it.head / a.c.H), h = (int)(it.head % a.c.H);
-    const float rate2 = a.c.rate[h] * kLog2e;
+    const float rate2 = rate_of(a.c.rate[h]);
     const int g = back ? a.segments - 1 - it.segment : it.segment;
     const int first = decay_first(a.blocks, a.segments, g), count = decay_first(a.blocks, a.segments, g + 1) - first;
     auto block_of = [&](int i) { return back ? first + count - 1 - i : first + i; };

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kThreads) decay_step_kernel(const T* __restric
         sq[tid] = to_f32(q[head * dk + tid]) * scale;
         sk[tid] = to_f32(k[head * dk + tid]);
     }
-    const float a = faded(rate[head % H] * kLog2e, 1);
+    const float a = faded(rate_of(rate[head % H]), 1);
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f), acc = x;
     if (mine) x = make_float4(to_f32(v[head * dv + 4 * c]), to_f32(v[head * dv + 4 * c + 1]), to_f32(v[head * dv + 4 * c + 2]), to_f32(v[head * dv + 4 * c + 3]));
     __syncthreads();

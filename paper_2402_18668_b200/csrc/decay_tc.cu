@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
     fence_proxy_async_smem();
     if (warp == kWarpMma) { tmem_alloc(tmem_base_s, 512); tmem_relinquish(); }
     enter_dependent();
-    const float rate2 = a.c.rate[h] * kLog2e;
+    const float rate2 = rate_of(a.c.rate[h]);
     if (tid <= kT) pw[tid] = faded(rate2, tid);
     tc_fence_before();
     __syncthreads();

@@ -1226,7 +1226,7 @@ Tensor as_rows(const Tensor& t) {
 struct DecayAttention : torch::autograd::Function<DecayAttention> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& q_, const Tensor& k_, const Tensor& v_,
                                                   const Tensor& rate_, const std::optional<Tensor>& documents,
-                                                  const std::optional<Tensor>& in, double scale) {
+                                                  const std::optional<Tensor>& in, double scale, bool with_last) {
         ctx->set_materialize_grads(false);
         on_gpu(q_);
         on_gpu(k_);
@@ -1236,20 +1236,22 @@ struct DecayAttention : torch::autograd::Function<DecayAttention> {
         const Decay o(as_rows(q_), as_rows(k_), as_rows(v_), packed(rate_), packed(documents), packed(in), static_cast<float>(scale));
         check_places({&o.q, &o.k, &o.v, &o.rate, &o.documents, &o.in}, {});
         const c10::cuda::CUDAGuard device(o.q.device());
-        const Tensor last = blank({o.B, o.H, o.dk, o.dv}, at::kFloat);
+        const Tensor last = with_last ? blank({o.B, o.H, o.dk, o.dv}, at::kFloat) : Tensor();
         const Tensor out = o.forward(Tensor(), last, kNone, c10::cuda::getCurrentCUDAStream(o.q.get_device()).stream());
         ctx->save_for_backward({o.q, o.k, o.v, o.rate, o.documents, o.in});
         ctx->saved_data["scale"] = scale;
+        if (!with_last) return {out};
         return {out, last};
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
         const auto s = ctx->get_saved_variables();
-        if (!grads[0].defined() && !grads[1].defined()) return {Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        const Tensor dlast = grads.size() > 1 ? grads[1] : Tensor();
+        if (!grads[0].defined() && !dlast.defined()) return {Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
         const Decay o(s[0], s[1], s[2], s[3], s[4], s[5], static_cast<float>(ctx->saved_data["scale"].toDouble()));
         return node_backward(o.q, [&](void* stream) -> torch::autograd::variable_list {
             const Tensor dout = grads[0].defined() ? as_rows(grads[0].to(o.v.scalar_type())) : at::zeros(o.v.sizes(), o.v.options());
-            const Decay::Grads g = o.backward(dout, as_input(grads[1], o.rate), kNone, stream);
-            return {g.dq, g.dk, g.dv, Tensor(), Tensor(), g.dstate, Tensor()};
+            const Decay::Grads g = o.backward(dout, as_input(dlast, o.rate), kNone, stream);
+            return {g.dq, g.dk, g.dv, Tensor(), Tensor(), g.dstate, Tensor(), Tensor()};
         });
     }
 };
@@ -1296,13 +1298,14 @@ PyObject* sliding_window(PyObject* const* a) {
     return wrap(applied([&] { return SlidingWindow::apply(q, k, v, window, scale); }));
 }
 
-// q, k, v, rate, documents, state, scale
+// q, k, v, rate, documents, state, scale, whether the last state is wanted
 PyObject* decay_attention(PyObject* const* a) {
     const Tensor q = given(a[0], "q"), k = given(a[1], "k"), v = given(a[2], "v"), rate = given(a[3], "rate");
     const auto documents = maybe(tensor(a[4])), in = maybe(tensor(a[5]));
     const double scale = number(a[6]);
-    const auto y = applied([&] { return DecayAttention::apply(q, k, v, rate, documents, in, scale); });
-    return wrap({y[0], y[1]});
+    const bool with_last = integer(a[7]) != 0;
+    const auto y = applied([&] { return DecayAttention::apply(q, k, v, rate, documents, in, scale, with_last); });
+    return wrap({y[0], with_last ? y[1] : Tensor()});
 }
 
 // ---------------------------------------------------------------------------------------------- module
@@ -1343,7 +1346,7 @@ PyMethodDef methods[] = {method<prefill, 9>("prefill"), method<prefill_backward,
                          method<swa_grad, 8>("swa_grad"), method<gated_recurrence, 5>("gated_recurrence"),
                          method<qk_norm_rotate, 9>("qk_norm_rotate"), method<sliding_window, 5>("sliding_window"),
                          method<decay_forward, 11>("decay_forward"), method<decay_step, 9>("decay_step"), method<decay_backward, 11>("decay_backward"),
-                         method<decay_attention, 7>("decay_attention"), method<paged_decode, 14>("paged_decode"), method<paged_write, 8>("paged_write"),
+                         method<decay_attention, 8>("decay_attention"), method<paged_decode, 14>("paged_decode"), method<paged_write, 8>("paged_write"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace

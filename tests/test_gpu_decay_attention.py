@@ -156,6 +156,26 @@ def test_rates(based, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
+def test_rates_that_leave_nothing(based, dtype):
+    """A rate without bound: every token is on its own."""
+    gen = torch.Generator(device="cuda").manual_seed(30)
+    q, k, v = (normal(gen, 1, 2, 300, 64, dtype=DTYPES[dtype]) for _ in range(3))
+    rate = torch.tensor([float("inf"), 3e38], device="cuda")
+    last = torch.empty(1, 2, 64, 64, device="cuda")
+    out = based.based_decay_attention_forward(q, k, v, rate, state_in=torch.ones(1, 2, 64, 64, device="cuda"), state_out=last)
+    score = (q.double() * k.double()).sum(-1, keepdim=True) / 8
+    eps = torch.finfo(DTYPES[dtype]).eps
+    # the score's sum of 64 products, its rounding and the output's; nothing of another token
+    bound = (q.double() * k.double()).abs().sum(-1, keepdim=True) / 8 * v.double().abs() * 64 * 2.0**-24 + 1.01 * eps * (score * v.double()).abs() + 1e-30
+    assert ((out.double() - score * v.double()).abs() <= bound).all()
+    want = k[:, :, -1, :, None].double() * v[:, :, -1, None, :].double()
+    assert ((last.double() - want).abs() <= want.abs() * 2.0**-20 + 1e-30).all()
+    state = torch.ones(1, 2, 64, 64, device="cuda")
+    based.based_decay_attention_step(q[:, :, -1].contiguous(), k[:, :, -1].contiguous(), v[:, :, -1].contiguous(), rate, state)
+    assert ((state.double() - want).abs() <= want.abs() * 2.0**-20 + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
 def test_padding_may_hold_anything(based, dtype):
     gen = torch.Generator(device="cuda").manual_seed(4)
     B, H, L, d = 2, 2, 300, 64
@@ -271,6 +291,12 @@ def test_autograd_forms(based):
     assert torch.equal(dq, want[0]) and torch.equal(v.grad, want[2])
     out, last = decay_attention(q, k, v, rate)
     last.sum().backward()                                      # and the other way round
+    want, none = decay_attention(q, k, v, rate, return_state=False)
+    assert none is None and ((want - out).abs() <= 2**-6 * out.abs() + 2**-6 * out.abs().max()).all()     # (their roundings differ)
+    for x in (q, k, v):
+        x.grad = None
+    want.float().sum().backward()
+    assert torch.equal(q.grad, dq)
     odd = torch.randn(2, 2, 70, 65, device="cuda")[..., 1:].bfloat16()
     assert odd[..., 1:9].data_ptr() % 16                       # rows that the kernels cannot read as they lie are copied
     decay_attention(odd[..., 1:9], odd[..., 2:10], odd[..., :64], rate)

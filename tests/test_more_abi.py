@@ -44,16 +44,17 @@ def test_decay_forward(lib):
     assert f(q_=V(P(0), token=68)) == f(q_=V(P(0), token=1 << 38)) == UNSUPPORTED
     assert f(out_=V(P(6), head=64, token=64)) == f(out_=V(P(6), batch=64)) == INVALID         # rows over each other
     assert f(n=need - 1) == f(ws=None) == WORKSPACE
+    assert f(scale=1e-30) == f(scale=1e30) == f(scale=float("inf")) == UNSUPPORTED
 
 
 def test_decay_step(lib):
-    def f(q=P(0), k=P(1), v=P(2), rate=P(3), si=P(4), out=P(5), so=P(6), B=2, H=2, dk=64, dv=64, io=1):
-        return lib.based_decay_attention_step(q, k, v, rate, si, out, so, B, H, dk, dv, 0.0, io, None)
+    def f(q=P(0), k=P(1), v=P(2), rate=P(3), si=P(4), out=P(5), so=P(6), B=2, H=2, dk=64, dv=64, io=1, scale=0.0):
+        return lib.based_decay_attention_step(q, k, v, rate, si, out, so, B, H, dk, dv, scale, io, None)
     for x in ("q", "k", "v", "rate", "si", "out", "so"):
         assert f(**{x: None}) == INVALID
         assert f(**{x: U}) == ALIGNMENT
     assert f(B=0) == f(H=0) == f(dk=0) == f(io=7) == f(out=P(0)) == f(out=P(4)) == f(out=P(6)) == f(so=P(0)) == f(so=P(3)) == INVALID
-    assert f(dk=12) == f(dv=136) == f(B=2**16, H=2**16) == UNSUPPORTED
+    assert f(dk=12) == f(dv=136) == f(B=2**16, H=2**16) == f(scale=1e-30) == f(scale=float("inf")) == UNSUPPORTED
 
 
 def test_decay_backward(lib):
@@ -62,16 +63,16 @@ def test_decay_backward(lib):
     names = ("q", "k", "v", "rate", "docs", "si", "do", "dso", "dq", "dk", "dv", "dsi")
     views = {"q", "k", "v", "do", "dq", "dk", "dv"}
 
-    def f(n=need, ws=P(20), B=2, io=1, d_k=64, **kw):
+    def f(n=need, ws=P(20), B=2, io=1, d_k=64, scale=0.0, **kw):
         a = {x: P(i) for i, x in enumerate(names)} | kw
         a |= {x: V(a[x]) for x in views}
-        return lib.based_decay_attention_backward(*(a[x] for x in names), B, 2, 300, d_k, 64, 0.0, io, ws, n, None)
+        return lib.based_decay_attention_backward(*(a[x] for x in names), B, 2, 300, d_k, 64, scale, io, ws, n, None)
     for x in ("q", "k", "v", "rate", "do", "dq", "dk", "dv"):
         assert f(**{x: None}) == INVALID
         assert f(**{x: U}) == ALIGNMENT
     assert f(si=U) == f(dso=U) == f(dsi=U) == f(ws=U) == ALIGNMENT
     assert f(dq=P(0)) == f(dk=P(9 - 1)) == f(dv=P(6)) == f(dsi=P(5)) == f(dsi=P(7)) == f(dv=P(20)) == f(B=0) == f(io=3) == INVALID
-    assert f(d_k=60) == UNSUPPORTED
+    assert f(d_k=60) == f(scale=1e-30) == f(scale=1e30) == UNSUPPORTED
     assert f(ws=None) == f(n=need - 1) == WORKSPACE
 
 
@@ -84,8 +85,8 @@ def test_paged(lib):
     def C(k=P(10), v=P(11), page=2 * 16 * 64, head=16 * 64, token=64, pages=50, size=16):
         return Pages(k, v, page, head, token, pages, size)
 
-    def f(q=P(0), k=P(1), v=P(2), c=None, table=P(3), pos=P(4), slopes=P(5), out=P(6), B=2, Hq=4, Hk=2, d=64, mp=100, window=0, cap=0.0, io=1, ws=P(7), n=need):
-        return lib.based_paged_decode_step(q, k, v, c or C(), table, pos, slopes, out, B, Hq, Hk, d, mp, window, 0.0, cap, io, ws, n, None)
+    def f(q=P(0), k=P(1), v=P(2), c=None, table=P(3), pos=P(4), slopes=P(5), out=P(6), B=2, Hq=4, Hk=2, d=64, mp=100, window=0, cap=0.0, io=1, ws=P(7), n=need, scale=0.0):
+        return lib.based_paged_decode_step(q, k, v, c or C(), table, pos, slopes, out, B, Hq, Hk, d, mp, window, scale, cap, io, ws, n, None)
 
     def w(k=P(0), v=P(1), c=None, table=P(3), pos=P(4), counts=P(5), B=2, H=2, L=300, d=64, mp=100, io=1):
         return lib.based_paged_cache_write(V(k), V(v), c or C(), table, pos, counts, B, H, L, d, mp, io, None)
@@ -104,6 +105,7 @@ def test_paged(lib):
         assert g(c=C(k=U)) == ALIGNMENT
     assert f(Hq=3) == f(Hk=0) == f(window=-1) == f(cap=-1.0) == f(cap=float("nan")) == f(out=P(0)) == f(out=P(10)) == f(out=P(7)) == f(ws=P(10)) == INVALID
     assert f(n=need - 1) == f(ws=None) == WORKSPACE
+    assert f(cap=float("inf")) == f(cap=1e-30) == f(scale=1e-30) == f(scale=float("inf")) == UNSUPPORTED
     assert w(L=0) == w(k=P(10)) == w(v=P(11)) == INVALID
     assert w(L=2**31 - 1) == w(B=2**18, H=2**13) == UNSUPPORTED
 
