@@ -14,7 +14,9 @@
 // that loads are always under way.  x, y and z have rings of their own whose places are free as soon as the products have read
 // them (y after the first third of a block), the output leaves through z's place, and nothing else of a block lies in shared memory but S.
 // With give z written to shared memory in two parts (the first form of this kernel) there was room for two stages that a
-// block held to its end: 224 us for B8 H16 L4096 128/128.
+// block held to its end: 224 us for B8 H16 L4096 128/128, which takes 97 now (5.5 TB/s; with documents 108, with a state returned 174, in twice
+// as many tiles); B8 H32 L4096 64/64 117 and 146.  There, with blocks of 64 KB, the chain of a block's steps bounds it: 3300 cycles, 4100 with
+// documents.
 //
 // Warps: 0-3 scores, 4-7 feed (fades Y), 8-11 state, 12-15 results, then one each for loads, products and stores.  The groups' work
 // is counted in instructions and ways to tensor memory and back, 32 columns a time: with the state in registers, loads ahead of
@@ -55,8 +57,8 @@ constexpr uint32_t colX = 0, colY = 128, colO = 256;
 // Where there is room, two turned y in turn (`two`); where only states are wanted, two third parts too
 template <int E> __device__ __forceinline__ uint32_t col_y(bool two, int i) { return two && (i & 1) ? (E == 128 ? colO : 384u) : colY; }
 // With three parts a block's own share of the state is summed apart and added by the state's group: the products' sums are cut off, not
-// rounded (24 of them a block, 8 that count in a sum begun with the small parts; a state over 32768 tokens with 0.4 % decay 1e-6 off for
-// 2e-7)
+// rounded (24 of them a block, 8 that count in a sum begun with the small parts: a state over 12000 tokens without decay 5e-7 off, over 1e-6
+// with all of them in one sum)
 template <bool STATES> constexpr uint32_t colD = STATES ? colO : 448;
 template <bool STATES> __device__ __forceinline__ uint32_t col_third(int i) { return STATES ? colX + 64u * (i & 1) : 384u; }
 
@@ -194,7 +196,7 @@ __device__ __forceinline__ void score_row(uint32_t tx, int w, int lane, bool bac
     tmem_wait_st();
 }
 // mbar_wait in few instructions: every one that a block's way leads through has to fit into the instruction caches with all the others (88 KB
-// of code, of which a block runs some 30; with the timed wait at each place a block with documents took 1.9 times as long).
+// of code, of which a block runs some 30; B8 H32 L4096 64/64 with documents took 220 us with the timed wait at each place, 195 with this).
 // Parked for up to 20 us a turn, given up after kTurns of them.
 constexpr int kTurns = 1 << 20;
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
@@ -205,7 +207,7 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
     }
     return true;
 }
-// Two at once: asked for side by side, since one answer takes some 150 cycles (five pairs a block in the products' warp)
+// Two at once: asked for side by side, since one answer takes some 150 cycles (in the products' warp: B2 H16 L32768 64/64 187 -> 178 us)
 __device__ __forceinline__ bool wait_for_both(uint64_t* x, uint32_t px, uint64_t* y, uint32_t py, volatile uint32_t* abort_flag) {
     uint32_t there;
     asm volatile(
