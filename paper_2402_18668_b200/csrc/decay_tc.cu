@@ -76,7 +76,6 @@ struct Args {
     float *states, *factors;
     unsigned int* err;
     int blocks, segments, tiles;
-    int parts;                                                       // of the faded y: 2 or 3
 };
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -237,7 +236,9 @@ __device__ __forceinline__ bool group_all(int id, bool pred) {
 
 }  // namespace
 
-template <int DC, int E, bool STATES, bool DOCS>
+// PARTS: of the faded y.  (A kernel for each number, though tiles of 128 columns have two only: with code for both, which the instruction caches
+// hold beside what runs, B8 H32 L4096 64/64 with documents took 148 us for 137, B2 H16 L32768 218 for 195)
+template <int DC, int E, bool STATES, bool DOCS, int PARTS>
 __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
     using C = Cfg<DC, E, STATES>;
     constexpr int NS = C::kStages;
@@ -257,7 +258,8 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         return;
     }
     const int b = (int)(it.head / a.c.H), h = (int)(it.head % a.c.H);
-    const bool back = p.back, two = STATES || (E == 64 && a.parts == 2);
+    const bool back = p.back;
+    constexpr bool two = STATES || (E == 64 && PARTS == 2);
 
     if (tid == 0) {
         for (int s = 0; s < bCount; ++s) {
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                 }
             }
         }
-        pass_on(c, e, x, count > 0 && a.parts == 2 ? fade_of(end_of(block_of(0))) : 1.f);
+        pass_on(c, e, x, count > 0 && PARTS == 2 ? fade_of(end_of(block_of(0))) : 1.f);
         tmem_wait_st();
         fence_proxy_async_smem();
     }
@@ -506,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             if (!wait2(bFullZ + i % NS, i / NS, bFeed + (two ? i & 1 : 0), two ? i >> 1 : i) || (STATES && i > 0 && !wait(bS, i - 1))) return false;
             tc_fence_after();
             const uint32_t lz = z_of(i), ty = tb + col_y<E>(two, i);
-            if (a.parts == 3) {                                      // the small parts first, into a sum of their own (see colD)
+            if constexpr (PARTS == 3) {                              // the small parts first, into a sum of their own (see colD)
                 const uint32_t t3 = tb + col_third<STATES>(i), d = tb + colD<STATES>;
 #pragma unroll 2
                 for (int k = 0; k < kT / 16; ++k) {
@@ -627,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             ok = wait(bDS, i);
             if (!ok) break;
             tc_fence_after();
-            if (a.parts == 3) {
+            if constexpr (PARTS == 3) {
                 if (rows) {
 #pragma unroll 1
                     for (int e = 0; e < E; e += 16) {
@@ -818,13 +820,8 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
             tc_fence_after();
             if (rows) {
                 const uint32_t ty = tl + col_y<E>(two, i), tx = tl + col_third<STATES>(i);
-                if (a.parts == 2) {
-                    if (whole) feed_row<2, true>(ty, tx, near, rate2, back, give);
-                    else feed_row<2, false>(ty, tx, near, rate2, back, give);
-                } else {
-                    if (whole) feed_row<3, true>(ty, tx, near, rate2, back, give);
-                    else feed_row<3, false>(ty, tx, near, rate2, back, give);
-                }
+                if (whole) feed_row<PARTS, true>(ty, tx, near, rate2, back, give);
+                else feed_row<PARTS, false>(ty, tx, near, rate2, back, give);
             }
             tc_fence_before();
             mbar_arrive(&bars[bFeed + (two ? i & 1 : 0)]);
@@ -843,9 +840,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
 
 namespace {
 
-template <int DC, int E, bool STATES, bool DOCS> based_status launch(const Maps& maps, const Args& a, long long ctas, cudaStream_t stream) {
+template <int DC, int E, bool STATES, bool DOCS, int PARTS> based_status launch(const Maps& maps, const Args& a, long long ctas, cudaStream_t stream) {
     using C = Cfg<DC, E, STATES>;
-    auto kern = decay_tc_kernel<DC, E, STATES, DOCS>;
+    auto kern = decay_tc_kernel<DC, E, STATES, DOCS, PARTS>;
     static std::atomic<bool> ready[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return BASED_ERR_CUDA;
@@ -858,15 +855,15 @@ template <int DC, int E, bool STATES, bool DOCS> based_status launch(const Maps&
     const based_status st = check_launch("decay_tc_kernel");
     return e == cudaSuccess ? st : BASED_ERR_CUDA;
 }
-template <int DC, int E, bool DOCS> based_status launch_both(const Maps& maps, const Args& a, const DecayPlan& plan, cudaStream_t stream) {
+template <int DC, int E, bool DOCS, int PARTS> based_status launch_both(const Maps& maps, const Args& a, const DecayPlan& plan, cudaStream_t stream) {
     if (plan.segments > 1) {
-        const based_status st = launch<DC, E, true, DOCS>(maps, a, plan.ctas / plan.segments * (plan.segments - 1), stream);
+        const based_status st = launch<DC, E, true, DOCS, PARTS>(maps, a, plan.ctas / plan.segments * (plan.segments - 1), stream);
         if (st != BASED_OK) return st;
     }
-    return launch<DC, E, false, DOCS>(maps, a, plan.ctas, stream);
+    return launch<DC, E, false, DOCS, PARTS>(maps, a, plan.ctas, stream);
 }
-template <int DC, int E> based_status launch_docs(const Maps& maps, const Args& a, const DecayPlan& plan, cudaStream_t stream) {
-    return a.places ? launch_both<DC, E, true>(maps, a, plan, stream) : launch_both<DC, E, false>(maps, a, plan, stream);
+template <int DC, int E, int PARTS> based_status launch_docs(const Maps& maps, const Args& a, const DecayPlan& plan, cudaStream_t stream) {
+    return a.places ? launch_both<DC, E, true, PARTS>(maps, a, plan, stream) : launch_both<DC, E, false, PARTS>(maps, a, plan, stream);
 }
 
 }  // namespace
@@ -900,14 +897,15 @@ based_status launch_decay_tc(const DecayCall& c, const DecayPlan& plan, void* wo
         wide = wide || p.dc > 64;
     }
     Args a{c, places, reinterpret_cast<float*>(ws + plan.places_bytes), reinterpret_cast<float*>(ws + plan.places_bytes + plan.states_bytes),
-           nullptr, plan.blocks, plan.segments, plan.tiles, state_wanted(c) ? 3 : 2};
+           nullptr, plan.blocks, plan.segments, plan.tiles};
     if (error_word_ptr(&a.err) != BASED_OK) return BASED_ERR_CUDA;
     if (places) {
         const based_status st = launch_decay_places(c.documents, places, c.B, c.L, kT, stream);
         if (st != BASED_OK) return st;
     }
-    if (plan.width == 64) return wide ? launch_docs<128, 64>(maps, a, plan, stream) : launch_docs<64, 64>(maps, a, plan, stream);
-    return wide ? launch_docs<128, 128>(maps, a, plan, stream) : launch_docs<64, 128>(maps, a, plan, stream);
+    if (state_wanted(c)) return wide ? launch_docs<128, 64, 3>(maps, a, plan, stream) : launch_docs<64, 64, 3>(maps, a, plan, stream);
+    if (plan.width == 64) return wide ? launch_docs<128, 64, 2>(maps, a, plan, stream) : launch_docs<64, 64, 2>(maps, a, plan, stream);
+    return wide ? launch_docs<128, 128, 2>(maps, a, plan, stream) : launch_docs<64, 128, 2>(maps, a, plan, stream);
 }
 
 }  // namespace based
