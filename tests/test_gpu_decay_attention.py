@@ -125,6 +125,16 @@ def test_layouts(based, dtype, layout):
     check_backward(based, gen, DTYPES[dtype], 2, 3, 200, 64, 96, layout=layout)
 
 
+@pytest.mark.parametrize("docs", ["none", "packed", "holes"])
+def test_many_heads(based, docs):
+    """More heads than SMs: tiles of all columns where no state is returned, and a backward pass of its own for the one that returns one."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    for with_state in (True, False):
+        check_forward(based, gen, torch.bfloat16, 16, 16, 300, 128, 128, docs=docs, with_state=with_state)
+        check_backward(based, gen, torch.bfloat16, 16, 16, 512, 128, 128, docs=docs, with_state=with_state)
+        check_backward(based, gen, torch.bfloat16, 16, 16, 257, 64, 120, docs=docs, with_state=with_state, layout="tokens")
+
+
 @pytest.mark.parametrize("dtype", list(DTYPES))
 @pytest.mark.parametrize("docs", ["none", "packed", "holes"])
 def test_long_in_segments(based, dtype, docs):
