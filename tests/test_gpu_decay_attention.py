@@ -385,3 +385,35 @@ def test_same_results_again(based):
     first = based.based_decay_attention_backward(q, k, v, rate, v)
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(first[:3], based.based_decay_attention_backward(q, k, v, rate, v)[:3]))
+
+
+def test_captured_training_step(based):
+    """Forward and backward pass in one graph, replayed on other inputs."""
+    from paper_2402_18668_b200.autograd import decay_attention
+
+    def leaves(seed):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        t = [normal(gen, 2, 300, 2, 64, dtype=torch.bfloat16).transpose(1, 2) for _ in range(3)] + [normal(gen, 2, 2, 64, 64)]
+        return [x.requires_grad_() for x in t], rates(gen, 2), documents(gen, 2, 300, "holes")
+
+    def step(t, rate, ids):
+        out, last = decay_attention(*t[:3], rate, documents=ids, state=t[3])
+        return torch.autograd.grad(out.float().square().sum() + last.square().sum(), t)
+
+    t, rate, ids = leaves(1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(t, rate, ids)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(t, rate, ids)
+    for seed in (1, 2):
+        with torch.no_grad():
+            new, r, d = leaves(seed)
+            for x, y in zip(t + [rate, ids], new + [r, d]):
+                x.copy_(y)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, step(t, rate, ids)))
+    assert based.based_poll_error() == 0
