@@ -665,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
                 mbar_arrive(&bars[bS]);
             }
         }
-        if (ok && rows && (STATES || (p.state_out && it.segment == a.segments - 1))) {
+        if ((STATES || PARTS == 3) && ok && rows && (STATES || (p.state_out && it.segment == a.segments - 1))) {
             const long long slot = STATES ? decay_slot(it.pass, a.c.passes, it.head, a.tiles, it.tile, a.segments, it.segment) : 0;
 #pragma unroll 1
             for (int e = 0; e < E; e += 32) {
