@@ -14,8 +14,8 @@
 // that loads are always under way.  x, y and z have rings of their own whose places are free as soon as the products have read
 // them (y after the first third of a block), the output leaves through z's place, and nothing else of a block lies in shared memory but S.
 // With give z written to shared memory in two parts (the first form of this kernel) there was room for two stages that a
-// block held to its end: 224 us for B8 H16 L4096 128/128, which takes 97 now (5.5 TB/s; with documents 108, with a state returned 174, in twice
-// as many tiles); B8 H32 L4096 64/64 117 and 146.  There, with blocks of 64 KB, the chain of a block's steps bounds it: 3300 cycles, 4100 with
+// block held to its end: 224 us for B8 H16 L4096 128/128, which takes 96 now (5.6 TB/s; with documents 105, with a state returned 163, in twice
+// as many tiles); B8 H32 L4096 64/64 110 and 134.  There, with blocks of 64 KB, the chain of a block's steps bounds it: 3200 cycles, 3900 with
 // documents.
 //
 // Warps: 0-3 scores, 4-7 feed (fades Y), 8-11 state, 12-15 results, then one each for loads, products and stores.  The groups' work
