@@ -417,3 +417,43 @@ def test_captured_training_step(based):
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(got, step(t, rate, ids)))
     assert based.based_poll_error() == 0
+
+
+@pytest.fixture
+def room():
+    torch.cuda.empty_cache()
+    yield torch.cuda.mem_get_info()[0]
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+def test_offsets_past_32_bits(based, room, dtype, layout):
+    """Inputs of more than 2^31 elements: the last head's outputs and gradients are those of the head alone."""
+    H, L, d = 33, 1 << 20, 64
+    if room < 8 * H * L * d * torch.finfo(DTYPES[dtype]).bits // 8:
+        pytest.skip("no room for seven tensors of 2.2e9 elements")
+    gen = torch.Generator(device="cuda").manual_seed(33)
+    rate = torch.full((H,), 0.01, device="cuda")
+
+    def tensor():
+        x = torch.zeros((1, H, L, d) if layout == "heads" else (1, L, H, d), device="cuda", dtype=DTYPES[dtype])
+        x = x if layout == "heads" else x.transpose(1, 2)
+        x[:, -1] = normal(gen, 1, L, d, dtype=DTYPES[dtype])
+        return x
+    q, k, v = tensor(), tensor(), tensor()
+    one = [x[:, -1:].contiguous() for x in (q, k, v)]
+    eps = torch.finfo(DTYPES[dtype]).eps
+
+    def same(a, b):
+        # two divisions into segments: the roundings of a state to bf16 (of its sums in fp32), some ten that count, each at most eps / 2 of outputs of this size
+        return (a[:, -1:].float() - b.float()).abs().max() <= 10 * max(eps, 2.0**-20) * b.float().abs().max()
+    out = based.based_decay_attention_forward(q, k, v, rate)
+    assert same(out, based.based_decay_attention_forward(*one, rate[:1]))
+    assert not out[:, :-1].any()
+    del out
+    if layout == "heads":
+        grads = based.based_decay_attention_backward(q, k, v, rate, v)
+        for a, b in zip(grads[:3], based.based_decay_attention_backward(*one, rate[:1], one[2])[:3]):
+            assert same(a, b)
+    assert based.based_poll_error() == 0

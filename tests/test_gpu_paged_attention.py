@@ -302,7 +302,9 @@ def test_refusals(based):
                        (dict(v_pages=vp[:5]), ValueError), (dict(page_table=table.long()), ValueError), (dict(page_table=table[:1]), ValueError),
                        (dict(pos=pos.long()), TypeError), (dict(pos=pos[:1]), ValueError), (dict(slopes=torch.zeros(3, device="cuda")), ValueError),
                        (dict(window=-1), RuntimeError), (dict(softcap=-1.0), RuntimeError), (dict(softcap=float("nan")), RuntimeError),
-                       (dict(out=q), ValueError), (dict(k_pages=kp, v_pages=kp), ValueError), (dict(q=q.cpu()), ValueError)):
+                       (dict(out=q), ValueError), (dict(k_pages=kp, v_pages=kp), ValueError), (dict(q=q.cpu()), ValueError),
+                       (dict(page_table=torch.zeros(2, 8, dtype=torch.int32, device="cuda")[:, :4]), ValueError),
+                       (dict(pos=torch.zeros(4, dtype=torch.int32, device="cuda")[::2]), ValueError)):
         with pytest.raises(error):
             f(**{**dict(q=q, k=k, v=k.clone(), k_pages=kp, v_pages=vp, page_table=table, pos=pos), **bad})
     rows = torch.zeros(2, 2, 8, 64, device="cuda")
