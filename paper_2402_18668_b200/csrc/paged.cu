@@ -50,11 +50,11 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 // tanh to some 4e-7 of itself: its power series up to x^9 below 1/3, (e^2x - 1) / (e^2x + 1) above (a third of tanhf's instructions; fp32 io takes
-// that)
+// that).  NaN takes the series, which keeps it (fminf does not)
 __device__ __forceinline__ float tanh_short(float x) {
     const float z = x * x, t = ex2(fminf(fabsf(x), 15.f) * (2.f * kLog2e));
     const float series = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-    return fabsf(x) < 0.33f ? series : copysignf(__fdividef(t - 1.f, t + 1.f), x);
+    return fabsf(x) >= 0.33f ? copysignf(__fdividef(t - 1.f, t + 1.f), x) : series;
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
