@@ -235,7 +235,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
 
         // Lane < 16 (and its double) looks up the page of token j0 + lane of a unit a turn before it is needed: it is checked then, so that
         // nothing waits for the table
-        auto tokens = [&](int n) { return (sp.first + unit0 + n) * kUnit + warp * kSub; };
+        // (units behind the last may begin past 2^31: their numbers wrap, and `here` goes by n first)
+        auto tokens = [&](int n) { return (int)((unsigned)(sp.first + unit0 + n) * kUnit + warp * kSub); };
         auto page_of = [&](int j) { return a.shift >= 0 ? j >> a.shift : (int)((unsigned)j / (unsigned)c.page_size); };
         auto here = [&](int n, int j) { return n < units && j <= sp.pos && j >= sp.lo; };
         auto look = [&](int n) -> int {
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
             __syncwarp();
             const int j0 = tokens(n);
             uint8_t* st = ring + n % C::kStages * C::kStage;
-            if (KIND < 2 || (j0 <= sp.pos && j0 + kSub > sp.lo)) {
+            if (KIND < 2 || (j0 <= sp.pos && sp.lo - j0 < kSub)) {        // (j0 + kSub may be 2^31)
                 const uint32_t ks = static_cast<uint32_t>(__cvta_generic_to_shared(st)), vs = ks + kSub * C::kRowBytes;
                 if constexpr (C::kTc) {
                     float s[2][4] = {};
@@ -461,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<T, DP, R>::kPerSm) paged_decode_
                     }
                 }
                 // the new token into its page, once for a key head
-                if (KIND == 2 && row0 == 0 && j0 <= sp.pos && sp.pos < j0 + kSub) {
+                if (KIND == 2 && row0 == 0 && j0 <= sp.pos && sp.pos - j0 < kSub) {
                     const int page = a.shift >= 0 ? sp.pos >> a.shift : (int)((unsigned)sp.pos / (unsigned)c.page_size), id = table[page];
                     if ((unsigned)id < (unsigned)c.pages) {
                         const long long at = id * c.page_stride + (long long)(sp.pos - page * c.page_size) * c.token_stride;
