@@ -508,6 +508,47 @@ bool stretches_overlap(const Tensor& a, const Tensor& b) {
     };
     return static_cast<const char*>(a.const_data_ptr()) < end(b) && static_cast<const char*>(b.const_data_ptr()) < end(a);
 }
+// Whether some byte belongs to both: tensors may lie in each other's gaps, as the halves of one pool [pages,2,H,page_size,d] do.  A byte of a
+// and one of b are the same if the distance of the two beginnings is a sum of steps along the dimensions, forth in one and back in the other,
+// up to what lies inside an element.
+struct Step { int64_t stride, least, most; };
+bool reaches(const Step* s, const Step* end, int64_t distance, int64_t a, int64_t b) {
+    if (s == end) return -b < distance && distance < a;
+    int64_t lo = 1 - b, hi = a - 1;                                  // what the smaller steps and an element's bytes come to
+    for (const Step* t = s + 1; t != end; ++t) {
+        lo += t->stride * t->least;
+        hi += t->stride * t->most;
+    }
+    auto down = [&](int64_t x) { return x >= 0 ? x / s->stride : -((-x + s->stride - 1) / s->stride); };
+    const int64_t from = std::max(s->least, -down(hi - distance)), to = std::min(s->most, down(distance - lo));
+    if (to - from > 3) return true;                                  // (steps that do not nest: taken to meet)
+    for (int64_t n = from; n <= to; ++n)
+        if (reaches(s + 1, end, distance - n * s->stride, a, b)) return true;
+    return false;
+}
+bool elements_overlap(const Tensor& a, const Tensor& b) {
+    constexpr int kDims = 16;
+    if (!stretches_overlap(a, b)) return false;
+    if (a.dim() + b.dim() > kDims) return true;
+    Step s[kDims];
+    int n = 0;
+    auto add = [&](const Tensor& t, int sign) {
+        for (int64_t i = 0; i < t.dim(); ++i) {
+            const int64_t stride = t.stride(i) * static_cast<int64_t>(t.element_size()), last = t.size(i) - 1;
+            if (last == 0 || stride == 0) continue;
+            int k = 0;
+            while (k < n && s[k].stride != stride) ++k;
+            if (k == n) s[n++] = {stride, 0, 0};
+            if (sign > 0) s[k].most += last;
+            else s[k].least -= last;
+        }
+    };
+    add(a, 1);                                                       // a + steps in a = b + steps in b
+    add(b, -1);
+    std::sort(s, s + n, [](const Step& x, const Step& y) { return x.stride > y.stride; });
+    const int64_t distance = static_cast<const char*>(b.const_data_ptr()) - static_cast<const char*>(a.const_data_ptr());
+    return reaches(s, s + n, distance, static_cast<int64_t>(a.element_size()), static_cast<int64_t>(b.element_size()));
+}
 // Every tensor of a call lies on one device, and what it writes overlaps nothing else of the call.  An undefined tensor is
 // passed over.
 void check_places(std::initializer_list<const Tensor*> in, std::initializer_list<const Tensor*> out) {
@@ -520,9 +561,9 @@ void check_places(std::initializer_list<const Tensor*> in, std::initializer_list
         if (!(*o)->defined()) continue;
         same(**o);
         for (const Tensor* t : in)
-            if (t->defined() && stretches_overlap(**o, *t)) value_error("an output overlaps an input");
+            if (t->defined() && elements_overlap(**o, *t)) value_error("an output overlaps an input");
         for (auto p = out.begin(); p != o; ++p)
-            if ((*p)->defined() && stretches_overlap(**o, **p)) value_error("two outputs overlap");
+            if ((*p)->defined() && elements_overlap(**o, **p)) value_error("two outputs overlap");
     }
 }
 // None: the current stream of the tensors' device
