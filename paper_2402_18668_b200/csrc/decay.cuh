@@ -50,8 +50,11 @@ __device__ __forceinline__ int place_to(uint32_t w) { return (int)(w >> 23 & 127
 
 // exp(-rate n) for a rate held as rate log2(e); n = 0 gives 1 whatever the rate
 __device__ __forceinline__ float faded(float rate2, int n) { return n == 0 ? 1.f : exp2f(-rate2 * (float)n); }
-// (finite: an infinite rate, or one that is after the product, fades all within a token either way)
-__device__ __forceinline__ float rate_of(float rate) { return fminf(rate * 1.4426950408889634f, 1e30f); }
+// (finite: an infinite rate, or one that is after the product, fades all within a token either way.  NaN stays NaN, and shows in all that it fades)
+__device__ __forceinline__ float rate_of(float rate) {
+    const float rate2 = rate * 1.4426950408889634f;
+    return rate2 > 1e30f ? 1e30f : rate2;
+}
 
 // How a call is cut: every pass and head into tiles of `width` output columns, every one of those into segments of whole blocks of tokens.
 // More than one segment: a launch ahead writes every segment's own state.
