@@ -552,9 +552,10 @@ typedef struct { const void* data; long long batch_stride, head_stride, token_st
  *
  *   S_t = a S_{t-1} + k_t v_t^T,     out_t = scale q_t S_t
  *
- * q, k [B,H,L,d_k], v, out [B,H,L,d_v] in the io dtype; rate [H] fp32, >= 0 (not checked; 0: no decay); state_in, state_out
- * [B,H,d_k,d_v] fp32: the states before token 0 and behind token L-1 (NULL: not wanted), which must not be one array.  scale <= 0:
- * 1 / sqrt(d_k); else from 2^-60 to 2^60.
+ * q, k [B,H,L,d_k], v, out [B,H,L,d_v] in the io dtype; rate [H] fp32, >= 0 (not checked; 0: no decay; NaN shows in all that it fades);
+ * state_in, state_out [B,H,d_k,d_v] fp32: the states before token 0 and behind token L-1 (NULL: not wanted), which must not be one array.
+ * Where the decay up to a token is 0 in fp32, nothing is left of the state ahead, whatever it holds.  scale <= 0: 1 / sqrt(d_k); else from
+ * 2^-60 to 2^60.
  * documents [B,L] int32, or NULL: a token whose document is negative is padding, and passed over as if it were not there (its
  * inputs are not used, its output is 0); one whose document is not that of the last token before it that counts starts from an
  * empty state.  A sequence's first document continues state_in, whatever its number.

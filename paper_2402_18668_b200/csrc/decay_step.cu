@@ -42,6 +42,7 @@ __global__ void __launch_bounds__(kThreads) decay_step_kernel(const T* __restric
         if (i < rows) {
             const int r = g + i * groups;
             const float kr = sk[r], qr = sq[r];
+            if (a == 0.f) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);        // dropped, whatever it holds, as in the prompt's kernels
             s[i] = make_float4(fmaf(a, s[i].x, kr * x.x), fmaf(a, s[i].y, kr * x.y), fmaf(a, s[i].z, kr * x.z), fmaf(a, s[i].w, kr * x.w));
             acc = make_float4(fmaf(qr, s[i].x, acc.x), fmaf(qr, s[i].y, acc.y), fmaf(qr, s[i].z, acc.z), fmaf(qr, s[i].w, acc.w));
             to[(long long)r * cols] = s[i];
