@@ -243,6 +243,14 @@ def _check(status: int, where: str):
         raise BasedError(status, where)
 
 
+def _written(*tensors):
+    """What a call has written in the caller's tensors counts as changed in place: a graph that saved one of them refuses to go on.
+    (Tensors of inference mode have no count.)"""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 # The C ABI takes bare pointers and cannot know how large the caller's buffers are; a state of the wrong
 # format or an output that is too short would make the kernels write past the allocation.  The binding is
 # the one place that sees the tensors, so it checks them before the call.
@@ -304,6 +312,7 @@ def based_prefill_state(k, v, kv_state=None, z_state=None, flags: int = BASED_ST
                                    0 if workspace is None else workspace.numel() * workspace.element_size(),
                                    _stream(stream))
     _check(st, "based_prefill_state")
+    _written(kv_state, z_state)
     return kv_state, z_state
 
 
@@ -341,6 +350,7 @@ def based_prefill_static_scratch(q, k, v, out, kv_state=None, z_state=None, flag
     st = lib().based_prefill_static_scratch(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(kv_state), _ptr(z_state), B, H,
                                             L, d_feat, v.shape[-1], _dtype_code(q), flags, _stream(stream))
     _check(st, "based_prefill_static_scratch")
+    _written(out, kv_state, z_state)
     return out
 
 
@@ -373,6 +383,7 @@ def based_state_to_sym(kv_state, z_state, kv_sym=None, z_sym=None, stream=None):
     st = lib().based_state_to_sym(_ptr(kv_state), _ptr(z_state), _ptr(kv_sym), _ptr(z_sym), B, H, D_FEAT, d_v,
                                   _stream(stream))
     _check(st, "based_state_to_sym")
+    _written(kv_sym, z_sym)
     return kv_sym, z_sym
 
 
@@ -388,6 +399,7 @@ def based_state_from_sym(kv_sym, z_sym, kv_state=None, z_state=None, stream=None
     st = lib().based_state_from_sym(_ptr(kv_sym), _ptr(z_sym), _ptr(kv_state), _ptr(z_state), B, H, D_FEAT, d_v,
                                     _stream(stream))
     _check(st, "based_state_from_sym")
+    _written(kv_state, z_state)
     return kv_state, z_state
 
 

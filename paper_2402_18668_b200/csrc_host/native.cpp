@@ -133,6 +133,12 @@ void check_caches(const Tensor& kc, const Tensor& vc, const Tensor& q, const cha
 void check(based_status st, const char* where) {
     if (st != BASED_OK) throw StatusFault(st, where);
 }
+// What a call has written in tensors of the caller's counts as changed in place: a graph that saved one of them refuses to go on.  (Tensors of
+// inference mode have no count.)
+void written(std::initializer_list<const Tensor*> ts) {
+    for (const Tensor* t : ts)
+        if (t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 // a tensor like t, which is contiguous (at::empty_like takes 0.85 us, 0.1 of it to look at the strides)
 Tensor fresh(const Tensor& t) { return at::empty(t.sizes(), t.options()); }
 // a workspace of at least `need` bytes: the caller's, or a fresh one that lives as long as this object (memory of torch's
@@ -236,6 +242,7 @@ PyObject* prefill(PyObject* const* a) {
     }
     Py_END_ALLOW_THREADS
     if (fault) std::rethrow_exception(fault);
+    written({&out, &kv, &z});
     return wrap(r);
 }
 
@@ -277,6 +284,7 @@ PyObject* decode_step(PyObject* const* a) {
         return based_decode_step_flags(cptr(q), cptr(k), cptr(v), fptr(kv), fptr(z), ptr(out), B, H, d_feat, d_v, io, flags, stream);
     });
     check(st, PyUnicode_AsUTF8(a[8]));
+    written({&out, &kv, &z});
     return wrap(out);
 }
 
@@ -296,6 +304,7 @@ PyObject* swa(PyObject* const* a) {
         return swa_forward(cptr(q), cptr(k), cptr(v), ptr(out), size(q, 0), size(q, 1), size(q, 2), size(q, 3), window, scale, io, stream);
     });
     check(st, "swa_forward");
+    written({&out});
     return wrap(out);
 }
 
@@ -328,6 +337,7 @@ PyObject* swa_decode(PyObject* const* a) {
                       : swa_decode_step(cptr(q), cptr(k), cptr(v), ptr(kc), ptr(vc), ptr(out), B, H, d, window, pos, scale, io, stream);
     });
     check(st, ragged ? "swa_decode_step_ragged" : "swa_decode_step");
+    written({&out, &kc, &vc});
     return wrap(out);
 }
 
@@ -363,6 +373,7 @@ PyObject* generation_step(PyObject* const* a) {
                                      flags, stream);
     });
     check(st, "based_generation_step");
+    written({&out, &out_w, &kv, &z, &kc, &vc, &pos});
     return wrap({out, out_w});
 }
 
@@ -370,6 +381,9 @@ struct GenerationGraph {
     based_generation_graph* graph;
     Tensor in[6];                              // q, k, v, qw, kw, vw: the buffers of the last token's inputs
     Tensor written[7];                         // state, caches, position and outputs
+    void mark() const {                        // (a step has written them)
+        for (const Tensor& t : written) ::written({&t});
+    }
     c10::Device device() const { return in[0].device(); }
     // the steps belong on the current stream of the graph's own device, whichever device is current
     void* stream() const { return c10::cuda::getCurrentCUDAStream(in[0].get_device()).stream(); }
@@ -443,6 +457,7 @@ PyObject* generation_graph_step(PyObject* const* a) {
     void* stream = g.stream();
     const based_status st = unlocked([&] { return based_generation_graph_step(g.graph, p[0], p[1], p[2], p[3], p[4], p[5], stream); });
     check(st, "based_generation_graph_step");
+    g.mark();
     Py_RETURN_TRUE;
 }
 // graph: the step on what the buffers hold
@@ -454,6 +469,7 @@ PyObject* generation_graph_replay(PyObject* const* a) {
         return based_generation_graph_step(g.graph, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, stream);
     });
     check(st, "based_generation_graph_step");
+    g.mark();
     Py_RETURN_NONE;
 }
 
@@ -482,6 +498,7 @@ PyObject* baseconv(PyObject* const* p) {
                     : baseconv_gate_forward(cptr(a), cptr(g), filter, bias, ptr(out), B, N, C, width, io, stream);
     });
     check(st, step ? "baseconv_gate_step" : "baseconv_gate_forward");
+    written({&out, &state});
     return wrap(out);
 }
 
@@ -650,6 +667,7 @@ PyObject* recurrence(PyObject* const* a) {
     void* stream = stream_on(a[7], x);
     Tensor y;
     away(x, [&] { y = recurrence_call(x, r, g, rate, in, out, last, stream); });
+    written({&out, &last});
     return wrap(y);
 }
 // x, r, g, rate, out, dout, state_in, dstate_out, workspace, stream -> dx, dr, dg, drate, dstate_in (None without state_in)
@@ -762,6 +780,7 @@ PyObject* rotate(PyObject* const* a) {
     o.own(ok, {&oq});
     void* stream = stream_on(a[11], o.q);
     away(o.q, [&] { o.forward(oq, ok, stream); });
+    written({&oq, &ok});
     return wrap({oq, ok});
 }
 // q, k, dout_q, dout_k, q_weight, k_weight, freqs, positions, eps, flags, start, dq, dk, workspace, stream
@@ -791,6 +810,7 @@ PyObject* rotate_backward(PyObject* const* a) {
     void* stream = stream_on(a[14], o.q);
     Tensor dwq, dwk;
     away(o.q, [&] { o.backward(gq, gk, dq, dk, o.wq.defined() || o.wk.defined(), dwq, dwk, ws, stream); });
+    written({&dq, &dk});
     return wrap({dq, dk, dwq, dwk});
 }
 
@@ -887,6 +907,7 @@ PyObject* decay_forward(PyObject* const* a) {
     void* stream = stream_on(a[10], o.q);
     Tensor y;
     away(o.q, [&] { y = o.forward(out, last, ws, stream); });
+    written({&out, &last});
     return wrap(y);
 }
 // q, k, v, rate, state_in, out, state_out, scale, stream; one token: q, k [B,H,d_k], v [B,H,d_v]
@@ -911,6 +932,7 @@ PyObject* decay_step(PyObject* const* a) {
         check(based_decay_attention_step(cptr(q), cptr(k), cptr(v), f32(rate), f32(in), ptr(out), fptr(last), B, H, dk, dv, scale, io, stream),
               "based_decay_attention_step");
     });
+    written({&out, &last});
     return wrap(out);
 }
 // q, k, v, rate, documents, state_in, dout, dstate_out, scale, workspace, stream -> dq, dk, dv, dstate_in (None without state_in)
@@ -969,6 +991,7 @@ PyObject* paged_decode(PyObject* const* a) {
                                 io, ws.data, ws.bytes, stream),
               "based_paged_decode_step");
     });
+    written({&out, &c.k, &c.v});
     return wrap(out);
 }
 // k, v, k_pages, v_pages, page_table, pos, counts, stream
@@ -986,6 +1009,7 @@ PyObject* paged_write(PyObject* const* a) {
         check(based_paged_cache_write(as_heads(k), as_heads(v), c.cache(), c.t(), c.p(), static_cast<const int*>(cptr(counts)), B, H, L, d, c.max_pages, io, stream),
               "based_paged_cache_write");
     });
+    written({&c.k, &c.v});
     Py_RETURN_NONE;
 }
 
