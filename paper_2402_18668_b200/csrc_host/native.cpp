@@ -955,7 +955,9 @@ struct Pages {
     int pages, H, page_size, d, max_pages;
     Pages(PyObject* k_, PyObject* v_, PyObject* table_, PyObject* pos_, int B, const Tensor& like)
         : k(heads(k_, "k_pages")), v(heads(v_, "v_pages")), table(need(table_, "page_table")), pos(need(pos_, "pos")) {
-        if (v.sizes() != k.sizes() || v.strides() != k.strides() || k.scalar_type() != like.scalar_type() || v.scalar_type() != like.scalar_type())
+        bool alike = v.sizes() == k.sizes() && k.scalar_type() == like.scalar_type() && v.scalar_type() == like.scalar_type();
+        for (int i = 0; i < 3 && alike; ++i) alike = k.size(i) == 1 || v.stride(i) == k.stride(i);     // (the step along one is never taken)
+        if (!alike)
             value_error("k_pages and v_pages must be [pages,H_k,page_size,d] of one layout, in the dtype of k");
         pages = dim(k, 0); H = dim(k, 1); page_size = dim(k, 2); d = dim(k, 3);
         if (table.scalar_type() != at::kInt || table.dim() != 2 || table.size(0) != B) value_error("page_table is an int32 tensor [B,max_pages]");
