@@ -560,8 +560,9 @@ typedef struct { const void* data; long long batch_stride, head_stride, token_st
  * inputs are not used, its output is 0); one whose document is not that of the last token before it that counts starts from an
  * empty state.  A sequence's first document continues state_in, whatever its number.
  * fp32 io: fp32 multiply-adds.  bf16 io: the faded scores and the state as operands of products with q are rounded to bf16 once; sums, the
- * state itself and what goes into it are fp32 (of every faded k 16 bits, 24 where a state is returned).  Where a value that counts is not finite, the outputs of its
- * sequence and head from up to 127 tokens ahead of it on may not be either, in other documents too.
+ * state itself and what goes into it are fp32 (of every faded k 16 bits, 24 where a state is returned: with state_out the
+ * outputs may differ in their last bits from those without).  Where a value that counts is not finite, the outputs of its sequence and head from
+ * up to 127 tokens ahead of it on may not be either, in other documents too.
  * Supported: d_k, d_v multiples of 8 up to 128; io in {F32, BF16}; 1 <= L <= 2^31 - 2^16.
  * workspace: based_decay_attention_workspace_bytes (with_documents: whether documents is given; 0 bytes are possible).  Outputs must not
  * alias inputs.

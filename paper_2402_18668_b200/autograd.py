@@ -45,5 +45,5 @@ def gated_recurrence(x, r, g, rate, state=None):
 def decay_attention(q, k, v, rate, documents=None, state=None, scale: float = 0.0, return_state: bool = True):
     """based_decay_attention_forward, differentiable with respect to q, k [B,H,L,d_k], v [B,H,L,d_v] and state [B,H,d_k,d_v]; the
     rates [H] are constants (one that requires a gradient is refused).  Returns (out, the state behind the last token), both
-    differentiable; with return_state=False (out, None), which in bf16 takes up to half the time."""
+    differentiable; with return_state=False (out, None), which in bf16 takes up to half the time and may differ in the last bits of out."""
     return _b.native().decay_attention(q, k, v, rate, documents, state, float(scale), int(return_state))

@@ -496,7 +496,8 @@ def based_decay_attention_forward(q, k, v, rate, documents=None, state_in=None, 
     """S_t = exp(-rate) S_{t-1} + k_t v_t^T, out_t = scale q_t S_t per head: q, k [B,H,L,d_k], v [B,H,L,d_v] (the heads of a projection,
     [B,L,H,d] transposed, and slices of a fused one are taken as they lie), rate [H] fp32; scale <= 0: 1/sqrt(d_k).  documents int32
     [B,L]: a negative one marks padding, which is passed over; where it changes the state starts anew.  state_in, state_out
-    [B,H,d_k,d_v] fp32 (state_out is written).  Returns out [B,H,L,d_v]."""
+    [B,H,d_k,d_v] fp32 (state_out is written; in bf16 that takes longer, and the last bits of out may differ).  out may lie in the gaps of a
+    fused buffer.  Returns out [B,H,L,d_v]."""
     return (_native_module or native()).decay_forward(q, k, v, rate, documents, state_in, out, state_out, float(scale), workspace,
                                                       _handle(stream))
 
@@ -519,7 +520,7 @@ def based_decay_attention_backward(q, k, v, rate, dout, documents=None, state_in
 def paged_decode_step(q, k, v, k_pages, v_pages, page_table, pos, out=None, softmax_scale: float = 0.0, softcap: float = 0.0, slopes=None,
                       window: int = 0, workspace=None, stream=None):
     """based_paged_decode_step: softmax attention of one new token per sequence over a paged cache: q [B,H_q,d], k, v [B,H_k,d]; k_pages, v_pages
-    [pages,H_k,page_size,d] (of any one layout, such as [pages,page_size,H_k,d] transposed), page_table int32 [B,max_pages], pos int32
+    [pages,H_k,page_size,d] (of any one layout, such as [pages,page_size,H_k,d] transposed, or the halves of one pool [pages,2,H_k,page_size,d]), page_table int32 [B,max_pages], pos int32
     [B], all on the device.  k, v are written to position pos[b]; the queries attend to it and what lies before it (the last `window` keys,
     0: all).  softcap: scores become softcap tanh(s / softcap); slopes [H_q] fp32: less slope * distance.  pos[b] < 0: no token,
     output 0.  Page numbers are checked on the device (based_poll_error: 1).  Returns out [B,H_q,d]."""

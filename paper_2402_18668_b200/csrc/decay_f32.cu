@@ -11,7 +11,7 @@
 // Rows lie in shared memory in the order in which the pass goes through them, so that back passes are the same from there on.
 // What bounds it: multiply-adds, 3.25 (wide heads 5.9) times 64^3 of them a block, at 4 cycles a pair where registers and shared memory are
 // read for them too (2.5 without): a block takes 8 us.  256 threads that did all of it one after another on 4 x 4 tiles, two CTAs
-// on an SM and the loads in between, took 1007 us for B8 H16 L4096 64/64 where this takes 499.
+// on an SM and the loads in between, took 1007 us for B8 H16 L4096 64/64 where this takes 501.
 #include "decay.cuh"
 #include "f32_tiles.cuh"
 #include "pairs.cuh"

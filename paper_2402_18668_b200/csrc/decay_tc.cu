@@ -14,9 +14,9 @@
 // that loads are always under way.  x, y and z have rings of their own whose places are free as soon as the products have read
 // them (y after the first third of a block), the output leaves through z's place, and nothing else of a block lies in shared memory but S.
 // With give z written to shared memory in two parts (the first form of this kernel) there was room for two stages that a
-// block held to its end: 224 us for B8 H16 L4096 128/128, which takes 96 now (5.6 TB/s; with documents 105, with a state returned 163, in twice
-// as many tiles); B8 H32 L4096 64/64 110 and 134.  There, with blocks of 64 KB, the chain of a block's steps bounds it: 3200 cycles, 3900 with
-// documents.
+// block held to its end: 224 us for B8 H16 L4096 128/128, which takes 97 now (5.5 TB/s; with documents 108, with a state returned 169, in twice
+// as many tiles; in loops of seconds, under the power limit, up to 117); B8 H32 L4096 64/64 114 and 134.  There, with blocks of 64 KB, the chain of
+// a block's steps bounds it: some 3300 cycles, 4000 with documents.
 //
 // Warps: 0-3 scores, 4-7 feed (fades Y), 8-11 state, 12-15 results, then one each for loads, products and stores.  The groups' work
 // is counted in instructions and ways to tensor memory and back, 32 columns a time: with the state in registers, loads ahead of
@@ -571,7 +571,8 @@ __global__ void __launch_bounds__(kThreads, 1) decay_tc_kernel(const __grid_cons
         // Products of one accumulator and shape run in the order of their issue; of others PTX promises no order.  So one that overwrites what
         // another reads waits for that one's end: the scores for P z (bO), the turned y for the product that reads the one ahead (bDS; of
         // two in turn the one before, whose end lies behind the wait for S: but where only states are wanted there is none).  B2 H16
-        // L32768 64/64: 171 -> 173 us, with documents 184 -> 189; 128 columns and 128 dimensions: no difference.
+        // L32768 64/64: 171 -> 175 us, with documents 184 -> 189, its backward pass 493 -> 518; B8 H16 L4096 128/128 with a state returned 165 -> 169,
+        // without 97 either way.
         if (count == 0) {
         } else if constexpr (STATES) {
             ok = turn(0);

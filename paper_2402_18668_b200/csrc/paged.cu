@@ -2,8 +2,8 @@
 //
 //   s_j = cap tanh(scale q . k_j / cap) - slope (pos - j),   o = sum_j exp(s_j) v_j / sum_j exp(s_j),   j = max(0, pos - window + 1) .. pos
 //
-// Bound by HBM (131072 tokens, 16 heads of 64: 102 us, 5.3 TB/s): every key and value is read once for all query heads that share it (Hq / Hk of them, the rows of a product), 2 d elements
-// a token against 4 d Hq / Hk flop.  What has to be right is the division of the work: sequences have any lengths, known to the device alone.
+// Bound by HBM (131072 tokens, 16 heads of 64: 104 us, 5.2 TB/s): every key and value is read once for up to 16 (fp32 8) query heads that share it, the
+// rows of a product (more are cut into blocks of so many, each of which reads it), 2 d elements a token against 4 d Hq / Hk flop.  What has to be right is the division of the work: sequences have any lengths, known to the device alone.
 //   - The unit is 64 tokens of one sequence and key head; all units lie in one row (sequence, head, tokens), and every CTA takes an equal
 //     share of it, whatever the lengths, from one sequence of 131072 tokens to many short ones.
 //   - Each of a CTA's four warps takes 16 tokens of a unit, in a ring of its own that copies (16 bytes a lane) fill two or three units
@@ -36,7 +36,7 @@ template <typename T, int DP, int R> struct Cfg {
     static constexpr int kRows = R;
     static constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16;
     static constexpr int kStage = 2 * kSub * kRowBytes;                  // a warp's keys and values of a unit
-    static constexpr int kStages = kStage >= 16384 ? 3 : kStage >= 8192 ? 3 : 4;
+    static constexpr int kStages = kStage >= 8192 ? 3 : 4;
     static constexpr int kWarp = kStages * kStage + (kTc ? 0 : kRows * DP * 4);    // a warp's ring, and its queries where they are fp32
     static constexpr int kBytes = kWarps * kWarp;
     static constexpr int kPerSm = kBytes > 113000 ? 1 : kBytes > 74000 ? 2 : 3;
